@@ -77,7 +77,12 @@ enum {
                             TMPS_FLAG_RELU */
     TMPS_AVGPOOL = 10    /* dims = {H, W, C}; mean over the H*W positions: [H, W, C] -> [C] */
 };
-enum { TMPS_FLAG_RELU = 1, TMPS_FLAG_GELU = 2 /* exact: z * Phi(z) */ };
+enum {
+    TMPS_FLAG_RELU = 1,
+    TMPS_FLAG_GELU = 2, /* exact: z * Phi(z) */
+    TMPS_FLAG_RMS = 4,  /* a norm without a mean: v / sqrt(mean(v^2) + 1e-5) */
+    TMPS_FLAG_GATE = 8  /* rows [f | a]: f under the gate 1 / (1 + exp(-a)) */
+};
 /* A convolution normally reads the result of the layer before it.  TMPS_FLAG_SRC(k), k = 2..255, in its flags
  * makes it read the result of the layer k positions before it instead (one position before the first layer of a
  * stage = the stage input): the branch of a residual connection. */
@@ -253,6 +258,60 @@ int tmps_schedule_run_1f1b(tmps_stage** stages, int K, int n_batches, const void
 /* In-place update (the update rule for TiMePReSt, with momentum): buf <- mu*buf + g,
  * w <- w - lr*buf on the fp32 master values, refreshes the bf16 working copy, version += 1. */
 int tmps_update(tmps_stage* stage, void* hip_stream);
+
+/* ---- operators on their own ----
+ *
+ * What stands between the contractions of a transformer's stage, for programs that call it over arrays of their own: rotary positions, the norms around a
+ * block, a distillation loss.  Activations and their gradients are of `dtype` (fp32, or bf16 with TMPS_BF16_F32MASTER), parameters, their gradients, statistics and
+ * losses fp32; sums are fp32.  Rows are contiguous unless a stride (in elements) is given.  All pointers are device memory of the stream's device, on whole elements (on
+ * 16 bytes and with widths of whole 8 elements the calls are faster); workspaces belong to one call at a time.  Zero rows are nothing to do (arrays of rows may then be
+ * NULL; gradients of parameters, where given, are zeros).  Errors: TMPS_EINVAL, TMPS_ESHAPE, TMPS_EUNSUPPORTED, TMPS_ECAP (workspace too small), TMPS_EHIP. */
+
+/* Rotary positions with several axes (time, height, width).  Each of the `heads` heads of dh features that begin a row has pairs[0] + pairs[1] + pairs[2] pairs of
+ * features (u, v): feature i and i + all pairs, or neighbours 2i and 2i + 1 with TMPS_ROTARY_INTERLEAVED.  The first pairs[0] turn with the row's time, the next pairs[1]
+ * with its height, the rest with its width: u' = u cos - v sin, v' = v cos + u sin at the angle position * base^(-i / all pairs) or, with TMPS_ROTARY_OWN_LADDERS,
+ * base^(-j / the axis's pairs), j counted on the axis.  Features behind the pairs are copied; what follows the heads in a row of x is not read, in a row of y not written.
+ * Angles are formed in 64 bits.  positions: int32 [n_positions, 3]; row r has those of r % n_positions.  inverse != 0 turns back, which is also the gradient's way.
+ * y may be x, or other columns of x's rows. */
+enum { TMPS_ROTARY_INTERLEAVED = 1, TMPS_ROTARY_OWN_LADDERS = 2 };
+typedef struct {
+    int32_t heads, dh;
+    int32_t pairs[3];
+    int32_t flags;
+    float base;
+} tmps_rotary_desc;
+int tmps_rotary(int dtype, const tmps_rotary_desc* desc, const void* x, int64_t x_stride, void* y, int64_t y_stride, const int32_t* positions,
+                int64_t n_positions, int64_t rows, int inverse, void* hip_stream);
+
+/* The norm behind a block, its gate, the scaled residual connection around it, and the norm in front of the next block, in one pass over memory:
+ *   y = scale * r + g * gain * n(f),   u = n(y) * pre_gain + pre_shift
+ * per row of D <= 16384 features.  n: layer normalisation, or its form without a mean with TMPS_FLAG_RMS (then without pre_shift); g = 1 / (1 + exp(-a)) with
+ * TMPS_FLAG_GATE, where x holds rows [f | a] of 2 D features, else 1 and x holds f.  u (NULL with pre_gain and pre_shift: y alone) is formed from y as it is stored.
+ * stats: float [rows, 4], mean (0 with TMPS_FLAG_RMS) and 1/std of f and of y, for the backward pass.  y may be r. */
+int tmps_norm_join_forward(int dtype, int flags, int64_t rows, int D, const void* x, const void* r, const float* gain, const float* scale, void* y,
+                           const float* pre_gain, const float* pre_shift, void* u, float* stats, void* hip_stream);
+/* Its gradients from dy (w.r.t. y as others read it) and du (w.r.t. u), of which one may be NULL; with du also y and pre_gain are needed.  dx (the layout of x) and
+ * dr may be NULL; dgain_dscale: D gradients of gain, then D of scale; dpre (with du): D of pre_gain and, without TMPS_FLAG_RMS, D of pre_shift.  dr may be dy.  Sums
+ * over rows are in a fixed order.  workspace: tmps_norm_join_workspace bytes. */
+size_t tmps_norm_join_workspace(int64_t rows, int D);
+int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D, const void* dy, const void* du, const void* x, const void* r, const void* y,
+                            const float* stats, const float* gain, const float* scale, const float* pre_gain, void* dx, void* dr, float* dgain_dscale,
+                            float* dpre, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's k <= 1024 largest logits: with q = softmax(z / T), T = temperature, and p the softmax of the row's teacher entries over T,
+ *   loss = alpha T^2 sum_j p_j (log p_j - log q[id_j]) + (1 - alpha) (-log softmax(z)[label])
+ * row_loss receives each row's, dlogits (may be NULL; gradient dtype) grad_scale times its gradient w.r.t. the row's fp32 logits z.  ids and teacher hold k entries a row,
+ * entry_stride elements apart from row to row, labels (NULL: none) one a row, label_stride apart.  An id of -1 is no entry (its logit is not looked at), a label
+ * of -1 no label: a row without entries lacks the first term, one without a label the second, one without both has loss and gradient 0 whatever its logits are.  Entries
+ * of the same class add up.  Any other id or label outside the classes gives a NaN loss, and no part in the gradient.  0 <= alpha <= 1; at 0 the teacher, at 1
+ * the labels are not looked at.  workspace: tmps_distill_workspace bytes (may be 0). */
+typedef struct {
+    int32_t classes, k;
+    float temperature, alpha, grad_scale;
+} tmps_distill_desc;
+size_t tmps_distill_workspace(int64_t rows, int classes);
+int tmps_distill(int dtype, const tmps_distill_desc* desc, int64_t rows, const float* logits, const int32_t* labels, int64_t label_stride, const int32_t* ids,
+                 const float* teacher, int64_t entry_stride, void* dlogits, float* row_loss, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---- nF1B schedule (sections "Work Scheduling" and "Multiple Sequence Problem") ----
  *

@@ -180,6 +180,56 @@ hipError_t attention_backward(int dtype, const void* qkv, const void* o, const v
                               float* delta, void* dqkv, int B, int S, int D, int H, hipStream_t s);
 size_t attention_workspace_elems(int B, int S, int H);
 
+// Rotary positions: every head's pairs of features turned by an angle of the row's positions on up to three axes (inverse: back).  `heads` heads of dh features
+// begin each row of x and y, whose rows are x_stride and y_stride elements apart; pairs[a] pairs turn with axis a, features behind them are copied.  Row r has the
+// positions pos[r % pos_rows][0..2] or, without pos, those of a grid: row r % grid_rows is (time, height, width) in row-major order.  y may be x.
+enum { kRotaryInterleaved = 1, kRotaryOwnLadders = 2 };   // pairs are neighbours (else i and i + all pairs); frequencies begin anew on each axis
+struct Rotary {
+    const void* x;
+    void* y;
+    int64_t x_stride, y_stride, rows;
+    int heads, dh, pairs[3], flags;
+    float base;
+    bool inverse;
+    const int32_t* pos;
+    int64_t pos_rows;
+    int grid_rows, grid_h, grid_w;
+};
+hipError_t rotary(int dtype, const Rotary& r, hipStream_t s);
+
+// A block's result behind its norm and under its gate, joined with the scaled residual, and the norm in front of the next block:
+//   y = scale r + g gain n(f),  u = n(y) pre_gain + pre_shift,  n(v) = (v - mean) / sqrt(var + 1e-5), with rms v / sqrt(mean(v^2) + 1e-5)
+// x holds rows [f], with gate rows [f | a], g = 1 / (1 + exp(-a)).  Without x, y is given and its norm alone is formed; without u the join alone.
+// stats, pre_stats: (mean or 0, 1/std) of each row of f and of y, stats_stride floats from row to row.
+constexpr int kJoinMaxFeatures = 16384;
+struct NormJoin {
+    const void *x, *r;
+    const float *gain, *scale;
+    void* y;
+    float* stats;
+    const float *pre_gain, *pre_shift;
+    void* u;
+    float* pre_stats;
+    int64_t stats_stride, rows;
+    int D;
+    bool rms, gate;
+};
+hipError_t norm_join_forward(int dtype, const NormJoin& j, hipStream_t s);
+// Its backward pass: dh = dy + gradient through the norm of y (either may be missing); dr = scale dh, dx = the gradient of the rows of x (both may be null; without
+// x, dr receives dh itself), dgain_dscale: D gain gradients and D scale gradients, dpre: D pre_gain gradients and, without rms, D pre_shift gradients.  Results may
+// be operands of the same layout.  part, part_pre: norm_join_part_elems(rows, D) fp32 elements each; their sums may wait.
+struct NormJoinBackward {
+    const void *dy, *du, *x, *r, *y;
+    const float *stats, *pre_stats, *gain, *scale, *pre_gain;
+    void *dx, *dr;
+    float *dgain_dscale, *dpre;
+    int64_t stats_stride, rows;
+    int D;
+    bool rms, gate;
+};
+hipError_t norm_join_backward(int dtype, const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s);
+size_t norm_join_part_elems(int64_t rows, int D);
+
 // y[row] = wte[tok[row]] + wpe[row % S] (tables in the contraction dtype), and the table gradients
 // (fp32; dwte cleared, then every occurring token's rows of dy added in row order, no atomic adds; dwpe summed over the batch).
 hipError_t embedding_forward(int dtype, const int32_t* tok, const void* wte, const void* wpe, void* y,
@@ -197,6 +247,24 @@ hipError_t softmax_ce(int dtype, const float* logits, const int32_t* labels, voi
 bool softmax_ce_small_takes(int64_t rows, int C);
 hipError_t softmax_ce_small(int dtype, const float* logits, const int32_t* labels, void* dlogits, float* y, float* row_loss, int rows,
                             int C, int before, float inv_M, float scale, float* loss_out, hipStream_t s);
+// Distillation: a row's loss alpha T^2 KL(p | softmax(z / T)) + (1 - alpha) (-log softmax(z)[label]), p the softmax of the teacher's k logits over T, and
+// dlogits (may be null) = grad_scale times its gradient.  ids, teacher, labels: entry_stride and label_stride elements from row to row; an id or label of -1 is none
+// (a row without entries or label lacks that term, without both its loss and gradient are 0 whatever its logits), any other outside the classes a NaN loss.
+// Repeated ids add up.  labels may be null where alpha is 1.  ws: distill_workspace_elems.
+constexpr int kDistillMaxEntries = 1024;
+struct Distill {
+    const float* logits;
+    const int32_t *labels, *ids;
+    const float* teacher;
+    int64_t label_stride, entry_stride, rows;
+    int classes, k;
+    float temperature, alpha, grad_scale;
+    void* dlogits;
+    float* row_loss;
+};
+hipError_t distill(int dtype, const Distill& d, float* ws, hipStream_t s);
+size_t distill_workspace_elems(int64_t rows, int classes);
+int check_distill(int64_t classes, int64_t k, float temperature, float alpha);   // TMPS_OK, or the refusal
 // out[0] = scale * sum(in[0..n))   (deterministic single-block tree)
 hipError_t reduce_scaled_sum(const float* in, int n, float scale, float* out, hipStream_t s);
 

@@ -1,0 +1,246 @@
+"""Distillation loss and gradient against 64 bits.
+
+Bounds, in steps of 2^-24: an exponential of (z - m) / T is off by |z - m| / T + 4 of its own size; a sum of C of them in threads' chains and trees by at most C / 64 + 32 (terms are
+positive); so probabilities are off by c = C / 64 + 64 + 2 max|z - m| / T, and the loss, a sum of p (log p - log q), by c times sum p (1 + |log p| + |log q|).  A gradient is off by c of
+the sizes of what it adds and subtracts, a bf16 one by 2^-8 of itself more."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2410_14312_amd as tmps
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+STEP = 2.0 ** -24
+
+
+def problem(rows, C, k, seed=0, spread=2.0, repeated=False):
+    gen = torch.Generator().manual_seed(seed)
+    z = spread * torch.randn(rows, C, generator=gen)
+    if repeated:
+        ids = torch.randint(0, min(C, max(1, k // 2)), (rows, k), generator=gen).to(torch.int32)
+    else:
+        ids = torch.stack([torch.randperm(C, generator=gen)[:k] for _ in range(rows)]).to(torch.int32)
+    teacher = spread * torch.randn(rows, k, generator=gen)
+    labels = torch.randint(0, C, (rows,), generator=gen).to(torch.int32)
+    return z, labels, ids, teacher
+
+
+def reference(z, labels, ids, teacher, T, alpha, scale):
+    """Row by row in 64 bits: loss, gradient, and the sizes that the bounds are counted in."""
+    z, teacher = z.double().numpy(), teacher.double().numpy()
+    rows, C = z.shape
+    loss, size, grad, gsize, c = np.zeros(rows), np.zeros(rows), np.zeros((rows, C)), np.zeros((rows, C)), np.zeros(rows)
+    for r in range(rows):
+        on = [(int(i), t) for i, t in zip(ids[r], teacher[r]) if i >= 0 and t != -np.inf] if alpha > 0 else []
+        label = -1 if labels is None or alpha >= 1 else int(labels[r])
+        if not on and label < 0:
+            continue
+        v = z[r] - z[r].max()
+        finite = np.abs(v[np.isfinite(v)]).max()
+        c[r] = C / 64 + 64 + 2 * finite * max(1.0, 1.0 / T)
+        if on:
+            lq = v / T - np.log(np.exp(v / T).sum())
+            t = np.array([b for _, b in on]) / T
+            at = np.array([a for a, _ in on])
+            lp = t - t.max() - np.log(np.exp(t - t.max()).sum())
+            p = np.exp(lp)
+            c[r] += 2 * np.abs(t - t.max()).max()
+            loss[r] += alpha * T * T * (p * (lp - lq[at])).sum()
+            size[r] += alpha * T * T * (p * (1 + np.abs(lp) + np.abs(lq[at]) + np.abs(v[at]) / T)).sum()
+            grad[r] += alpha * T * np.exp(lq)
+            gsize[r] += alpha * T * np.exp(lq)
+            np.add.at(grad[r], at, -alpha * T * p)
+            np.add.at(gsize[r], at, alpha * T * p)
+        if label >= 0:
+            ls = v - np.log(np.exp(v).sum())
+            loss[r] += (1 - alpha) * -ls[label]
+            size[r] += (1 - alpha) * (1 + np.abs(ls[label]) + np.abs(v[label]))
+            grad[r] += (1 - alpha) * np.exp(ls)
+            gsize[r] += (1 - alpha) * np.exp(ls)
+            grad[r, label] -= 1 - alpha
+            gsize[r, label] += 1 - alpha
+    return loss, size * c, grad * scale, gsize * abs(scale) * c[:, None]
+
+
+def check(z, labels, ids, teacher, T, alpha, dtype, scale=None):
+    rows = len(z)
+    dev = lambda v: None if v is None else v.to(DEV)   # noqa: E731
+    loss, g = tmps.distill(dev(z), dev(labels), dev(ids), dev(teacher), temperature=T, alpha=alpha, dtype=dtype, grad_scale=scale)
+    T, alpha = float(np.float32(T)), float(np.float32(alpha))
+    want, size, grad, gsize = reference(z, labels, ids, teacher, T, alpha, 1.0 / rows if scale is None else scale)
+    err = np.abs(loss.double().cpu().numpy() - want)
+    assert np.all(err <= STEP * size), float(np.max(err - STEP * size))
+    err = np.abs(g.double().cpu().numpy() - grad)
+    bound = STEP * gsize + (2.0 ** -8 * np.abs(grad) if dtype == "bf16" else 0.0) + 1e-30
+    assert np.all(err <= bound), (float(np.max(err - bound)), np.unravel_index(np.argmax(err - bound), err.shape))
+    alone, none = tmps.distill(dev(z), dev(labels), dev(ids), dev(teacher), temperature=T, alpha=alpha, gradient=False)
+    assert none is None and torch.equal(alone, loss)
+    return loss, g
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C,k", [(1, 1, 1), (3, 2, 2), (5, 10, 3), (64, 100, 10), (9, 255, 64), (7, 256, 256), (4, 1000, 100), (33, 2048, 64), (6, 2052, 33), (5, 4099, 5),
+                                      (3, 8192, 300), (9, 16384, 64), (3, 16388, 64), (300, 5000, 20), (2, 32000, 1024), (270, 32000, 8), (2, 32771, 50), (1, 65536, 64), (5, 70001, 100), (3, 131072, 7),
+                                      (1, 200000, 64)])
+def test_sizes(dtype, rows, C, k):
+    z, labels, ids, teacher = problem(rows, C, k, seed=C + k)
+    check(z, labels, ids, teacher, 2.0, 0.7, dtype)
+    check(z, labels, ids, teacher, 1.0, 0.25, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("alpha", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("C", [37, 3000, 9001, 66000])
+def test_weights_and_temperatures(dtype, T, alpha, C):
+    z, labels, ids, teacher = problem(3, C, 12, seed=C)
+    check(z, labels, ids, teacher, T, alpha, dtype, scale=0.37)
+    if alpha == 1.0:
+        check(z, None, ids, teacher, T, alpha, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C", [(16, 40), (16, 5003), (16, 20000), (12, 50000), (300, 40004)])
+def test_masks(dtype, rows, C):
+    """Rows without teacher, without label, without both (their logits NaN or infinite), entries masked here and there with NaN behind the mask, one entry left; a teacher's entry
+    of minus infinity takes no part, and a row of those alone has no teacher; repeated classes and the label's class among them; masked classes of the student."""
+    z, labels, ids, teacher = problem(rows, C, 24, seed=C, repeated=True)
+    ids[::3, 1::2] = -1
+    teacher[::3, 1::2] = float("nan")
+    ids[1, 1:] = -1
+    ids[2] = -1
+    teacher[2] = float("nan")
+    labels[4] = -1
+    ids[5] = -1
+    labels[5] = -1
+    z[5] = float("nan")
+    ids[6] = -1
+    labels[6] = -1
+    z[6] = -float("inf")
+    ids[7], labels[7] = 9, 9
+    labels[8] = int(ids[8, 0])
+    teacher[9, :5] = -float("inf")
+    ids[10, :] = 3
+    teacher[10] = -float("inf")
+    ids[11], labels[11] = torch.arange(C - 24, C), C - 1
+    z[11, :7] = -float("inf")
+    z[0, 39], labels[0] = -float("inf"), 0
+    for alpha in (0.6, 1.0, 0.0):
+        loss, g = check(z, labels, ids, teacher, 1.5, alpha, dtype)
+        for r in (5, 6):
+            assert loss[r] == 0 and bool((g[r] == 0).all())
+
+
+@pytest.mark.parametrize("C", [30, 6001, 50001])
+def test_wrong_ids_and_what_cannot_be_learned(C):
+    """An id or label that is no class gives its row a NaN loss, no wild access and no part in the gradient; a class that the student cannot have (logit minus infinity) an
+    infinite one.  Other rows stay as they are."""
+    z, labels, ids, teacher = problem(6, C, 8, seed=1)
+    want, g0 = tmps.distill(z.to(DEV), labels.to(DEV), ids.to(DEV), teacher.to(DEV), alpha=0.5)
+    ids[1, 3], ids[2, 0], labels[3] = C, -2, C + 5
+    z[4, int(ids[4, 2])] = -float("inf")
+    loss, g = tmps.distill(z.to(DEV), labels.to(DEV), ids.to(DEV), teacher.to(DEV), alpha=0.5)
+    assert bool(torch.isnan(loss[1:4]).all()) and loss[4] == float("inf")
+    assert torch.equal(loss[[0, 5]], want[[0, 5]]) and torch.equal(g[[0, 5]], g0[[0, 5]])
+    assert bool(torch.isfinite(g).all())
+    ids[1, 3] = ids[2, 0] = labels[3] = -1
+    _, g1 = tmps.distill(z.to(DEV), labels.to(DEV), ids.to(DEV), teacher.to(DEV), alpha=0.5)
+    assert torch.equal(g, g1)
+
+
+@pytest.mark.parametrize("C", [50, 7000, 40001])
+def test_large_logits(C):
+    """Spread of hundreds: the smallest probabilities vanish, nothing overflows."""
+    z, labels, ids, teacher = problem(4, C, 16, seed=2, spread=150.0)
+    check(z, labels, ids, teacher, 1.0, 0.5, "f32")
+    check(z + 3e4, labels, ids, teacher, 2.0, 1.0, "bf16")
+
+
+@pytest.mark.parametrize("C", [64, 3001, 66002])
+def test_gradient_is_that_of_differences(C):
+    """Central differences of the fp32 losses along a direction: the third derivative along a unit direction is below 1 / T; a loss of size l is off by some 2^-22 l."""
+    z, labels, ids, teacher = problem(2, C, 10, seed=5)
+    T, alpha, h = 1.5, 0.6, 2.0 ** -5
+    run = lambda v: tmps.distill(v.to(DEV), labels.to(DEV), ids.to(DEV), teacher.to(DEV), temperature=T, alpha=alpha, grad_scale=1.0)   # noqa: E731
+    loss, g = run(z)
+    gen = torch.Generator().manual_seed(6)
+    d = torch.randn(z.shape, generator=gen)
+    d[:, :] += 3.0 * torch.nn.functional.one_hot(ids[:, 0].long(), C)
+    d /= d.norm(dim=1, keepdim=True)
+    up, down = run(z + h * d)[0], run(z - h * d)[0]
+    slope = (up.double() - down.double()) / (2 * h)
+    along = (g.double().cpu() * d.double()).sum(1).to(slope)
+    assert bool(((slope - along).abs() <= h * h + 2.0 ** -22 * (C / 64 + 64) / 16 * loss.abs() / h).all()), (slope, along)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,C", [(40, 90), (20, 4096), (300, 5001), (4, 90000)])
+def test_graph_replays_and_another_stream(dtype, rows, C):
+    z, labels, ids, teacher = (v.to(DEV) for v in problem(rows, C, 16))
+    kw = dict(temperature=2.0, alpha=0.5, dtype=dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = tmps.distill(z, labels, ids, teacher, **kw)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, tmps.distill(z, labels, ids, teacher, **kw)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = tmps.distill(z, labels, ids, teacher, **kw)
+    for seed in range(1, 5):
+        for a, b in zip((z, labels, ids, teacher), problem(rows, C, 16, seed=seed)):
+            a.copy_(b)
+        graph.replay()
+        eager = tmps.distill(z, labels, ids, teacher, **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager))
+
+
+def test_packed_records_and_memory_around():
+    """Labels, ids and teacher logits as one record a row, through strides; a gradient off 16 bytes; the memory around the results stays."""
+    import ctypes as C_
+    from paper_2410_14312_amd import binding
+    rows, C, k = 11, 3000, 9
+    z, labels, ids, teacher = problem(rows, C, k)
+    rec = torch.cat([labels[:, None], ids, teacher.view(torch.int32)], 1).to(DEV)
+    want = tmps.distill(z.to(DEV), labels.to(DEV), ids.to(DEV), teacher.to(DEV), alpha=0.5, dtype="bf16")
+    g = torch.full((rows * C + 9,), 7.0, dtype=torch.bfloat16, device=DEV)
+    loss = torch.full((rows + 2,), 7.0, device=DEV)
+    zd = z.to(DEV)
+    need = binding.lib().tmps_distill_workspace(rows, C)
+    ws = torch.empty(max(need, 4), dtype=torch.uint8, device=DEV)
+    d = binding.DistillDesc(C, k, 1.0, 0.5, 1.0 / rows)
+    at, step = rec.data_ptr(), 1 + 2 * k
+    binding._call(binding.lib().tmps_distill, zd.device, None, binding.TMPS_BF16_F32MASTER, C_.byref(d), rows, zd.data_ptr(), at, step, at + 4, at + 4 + 4 * k, step,
+                  g.data_ptr() + 2, loss.data_ptr() + 4, ws.data_ptr(), need)
+    torch.cuda.synchronize()
+    assert loss[0] == 7 and loss[-1] == 7 and g[0] == 7 and bool((g[1 + rows * C:] == 7).all())
+    assert (loss[1:-1] - want[0]).abs().max() < 1e-5
+    assert (g[1:1 + rows * C].view(rows, C).float() - want[1].float()).abs().max() <= 2.0 ** -7 * want[1].float().abs().max()
+
+
+def test_no_rows_and_many_rows():
+    z, labels, ids, teacher = problem(0 + 1, 12, 3)
+    loss, g = tmps.distill(z[:0].to(DEV), labels[:0].to(DEV), ids[:0].to(DEV), teacher[:0].to(DEV))
+    assert loss.shape == (0,) and g.shape == (0, 12)
+    gen = torch.Generator().manual_seed(0)
+    rows = 20001
+    z, ids = torch.randn(rows, 12, generator=gen), torch.randint(-1, 12, (rows, 3), generator=gen).to(torch.int32)
+    check(z, torch.randint(-1, 12, (rows,), generator=gen).to(torch.int32), ids, torch.randn(rows, 3, generator=gen), 2.0, 0.5, "bf16")
+
+
+def test_rows_beyond_32_bit_offsets():
+    """The last row of more than 2^31 logits."""
+    rows, C = 17000, 131072
+    z, labels, ids, teacher = problem(1, C, 8)
+    big = torch.zeros(rows, C, device=DEV)
+    big[-1] = z[0].to(DEV)
+    all_ids = torch.full((rows, 8), -1, dtype=torch.int32, device=DEV)
+    all_ids[-1] = ids[0].to(DEV)
+    t = torch.zeros(rows, 8, device=DEV)
+    t[-1] = teacher[0].to(DEV)
+    loss, g = tmps.distill(big, None, all_ids, t, grad_scale=1.0, dtype="bf16")
+    want, size, grad, gsize = reference(z, None, ids, teacher, 1.0, 1.0, 1.0)
+    assert abs(loss[-1].item() - want[0]) <= STEP * size[0] and float(loss[:-1].abs().max()) == 0
+    assert np.all(np.abs(g[-1].double().cpu().numpy() - grad[0]) <= STEP * gsize[0] + 2.0 ** -8 * np.abs(grad[0]))

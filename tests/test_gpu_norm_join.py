@@ -1,0 +1,288 @@
+"""Norm joins, forward and backward, against 64 bits.
+
+Bounds.  fp32 sums over a row are a chain of at most 16 a thread and trees, those over rows a chain of a team's rows and what the partial results' sum adds: a value that is
+a sum of terms of sizes a, b, .. is off by at most c 2^-24 (a + b + ..), c = 64 for rows (statistics, their use and the products included) and 64 + rows / 500 for sums over
+rows, the sizes taken with absolute values throughout.  The normalised value (v - mean) / std loses |mean| / std more steps.  A bf16 result is rounded on top: 2^-8 of
+its size.  The norm of y reads y as it is stored, and so do the references."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2410_14312_amd as tmps
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+STEP = 2.0 ** -24
+WIDTHS = [1, 2, 7, 8, 63, 64, 65, 200, 256, 511, 512, 520, 768, 1000, 1024, 1025, 1032, 2040, 2048, 2049, 4096, 4100, 5003, 8192, 8200, 16384]
+
+
+def norm_parts(v, rms):
+    m = np.zeros((len(v), 1)) if rms else v.mean(1, keepdims=True)
+    i = 1.0 / np.sqrt(((v - m) ** 2).mean(1, keepdims=True) + 1e-5)
+    return m, i, (v - m) * i
+
+
+def problem(rows, D, dtype, rms, gate, pre, seed=0, offset=0.0):
+    gen = torch.Generator().manual_seed(seed)
+    n = lambda *s: torch.randn(*s, generator=gen)   # noqa: E731
+    t = TYPES[dtype]
+    p = {"x": (n(rows, D * (2 if gate else 1)) + offset).to(t), "r": n(rows, D).to(t), "gain": 1 + 0.3 * n(D), "scale": 1 + 0.3 * n(D),
+         "pre_gain": 1 + 0.3 * n(D) if pre else None, "pre_shift": 0.3 * n(D) if pre and not rms else None, "dy": n(rows, D).to(t), "du": n(rows, D).to(t) if pre else None}
+    return {k: None if v is None else v.to(DEV) for k, v in p.items()}
+
+
+def f64(v):
+    return v.double().cpu().numpy()
+
+
+def near(name, got, want, size, c, dtype="f32"):
+    got = f64(got)
+    err = np.abs(got - want)
+    bound = c * STEP * size + (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0.0)
+    assert got.shape == want.shape and np.all(err <= bound + 1e-30), (name, float(np.max(err - bound)), float(np.max(err / (bound + 1e-300))))
+
+
+def sides(p, D, gate):
+    x = f64(p["x"])
+    f = x[:, :D]
+    g = 1.0 / (1.0 + np.exp(-x[:, D:])) if gate else np.ones_like(f)
+    return f, g
+
+
+def slope(p, D):
+    """g (1 - g), with 1 - g = 1 / (1 + exp(a)): the difference of two 64-bit numbers would keep 1e-16 of one, 1e-3 of it at a = 30."""
+    a = f64(p["x"])[:, D:]
+    return 1.0 / ((1.0 + np.exp(-a)) * (1.0 + np.exp(a)))
+
+
+def check_forward(p, D, dtype, rms, gate, pre):
+    y, u, stats = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], pre_gain=p["pre_gain"], pre_shift=p["pre_shift"], rms=rms, gate=gate)
+    f, g = sides(p, D, gate)
+    m, i, fh = norm_parts(f, rms)
+    a, b = f64(p["scale"]) * f64(p["r"]), g * f64(p["gain"]) * fh
+    lost = 1.0 + np.abs(m) * i
+    near("y", y, a + b, np.abs(a) + g * np.abs(f64(p["gain"])) * (np.abs(fh) + 1) * lost, 64, dtype)
+    near("mean", stats[:, 0:1], m, np.abs(f).mean(1, keepdims=True), 64)
+    near("1/std", stats[:, 1:2], i, i * lost, 64)
+    if pre:
+        m, i, yh = norm_parts(f64(y), rms)
+        lost = 1.0 + np.abs(m) * i
+        want = yh * f64(p["pre_gain"]) + (0.0 if rms else f64(p["pre_shift"]))
+        size = (np.abs(yh) + 1) * lost * np.abs(f64(p["pre_gain"])) + (0.0 if rms else np.abs(f64(p["pre_shift"])))
+        near("u", u, want, size, 64, dtype)
+        near("1/std of y", stats[:, 3:4], i, i * lost, 64)
+    else:
+        assert u is None
+    return y, u, stats
+
+
+def check_backward(p, y, stats, D, dtype, rms, gate, pre, dy=True):
+    rows = len(p["r"])
+    got = tmps.norm_join_backward(p["dy"] if dy else None, p["du"], p["x"], p["r"], y, stats, p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=rms, gate=gate)
+    dx, dr, dgain, dscale, dpg, dps = got
+    f, g = sides(p, D, gate)
+    m1, i1, fh = norm_parts(f, rms)
+    lost1 = 1.0 + np.abs(m1) * i1
+    dh = f64(p["dy"]) if dy else np.zeros((rows, D))
+    size = np.abs(dh)
+    cr = 64 + rows / 500
+    if pre:
+        m2, i2, yh = norm_parts(f64(y), rms)
+        lost2 = 1.0 + np.abs(m2) * i2
+        du, t = f64(p["du"]), f64(p["du"]) * f64(p["pre_gain"])
+        mean_t = 0.0 if rms else t.mean(1, keepdims=True)
+        dh = dh + i2 * (t - mean_t - yh * (t * yh).mean(1, keepdims=True))
+        ah = np.abs(yh) + 1
+        size = size + i2 * lost2 * (np.abs(t) + np.abs(t).mean(1, keepdims=True) + ah * (np.abs(t) * ah).mean(1, keepdims=True))
+        near("dpre_gain", dpg, (du * yh).sum(0), (np.abs(du) * ah * lost2).sum(0), cr)
+        if rms:
+            assert dps is None
+        else:
+            near("dpre_shift", dps, du.sum(0), np.abs(du).sum(0), cr)
+    else:
+        assert dpg is None and dps is None
+    sc, gn, r = f64(p["scale"]), f64(p["gain"]), f64(p["r"])
+    near("dr", dr, dh * sc, size * np.abs(sc), 128, dtype)
+    near("dscale", dscale, (dh * r).sum(0), (size * np.abs(r)).sum(0), 64 + cr)
+    af = (np.abs(fh) + 1) * lost1
+    near("dgain", dgain, (dh * g * fh).sum(0), (size * g * af).sum(0), 64 + cr)
+    v, av = dh * g * gn, size * g * np.abs(gn)
+    want = i1 * (v - (0.0 if rms else v.mean(1, keepdims=True)) - fh * (v * fh).mean(1, keepdims=True))
+    size_x = i1 * lost1 * (av + av.mean(1, keepdims=True) + af * (av * af).mean(1, keepdims=True))
+    if gate:
+        want = np.concatenate([want, dh * gn * fh * slope(p, D)], 1)
+        size_x = np.concatenate([size_x, size * np.abs(gn) * af * slope(p, D)], 1)
+    near("dx", dx, want, size_x, 256, dtype)
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", WIDTHS)
+def test_widths(dtype, D):
+    """Every width class, with every form taken in turn."""
+    k = WIDTHS.index(D)
+    for rms, gate, pre in [(k % 2 == 0, False, True), (k % 2 == 1, True, True), (k % 3 == 0, k % 2 == 0, False)]:
+        p = problem(5, D, dtype, rms, gate, pre, seed=D)
+        y, _, stats = check_forward(p, D, dtype, rms, gate, pre)
+        check_backward(p, y, stats, D, dtype, rms, gate, pre)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("pre,dy", [(False, True), (True, True), (True, False)])
+@pytest.mark.parametrize("rows,D", [(1, 72), (2051, 72), (37, 1100), (1030, 768), (700, 136)])
+def test_forms(dtype, rms, gate, pre, dy, rows, D):
+    p = problem(rows, D, dtype, rms, gate, pre, seed=rows)
+    y, _, stats = check_forward(p, D, dtype, rms, gate, pre)
+    check_backward(p, y, stats, D, dtype, rms, gate, pre, dy)
+
+
+@pytest.mark.parametrize("rms", [False, True])
+def test_large_means_and_tiny_rows(rms):
+    """Rows far from zero (the variance is that of differences), rows of zeros, rows of one value: finite results, the bounds as they are."""
+    p = problem(40, 264, "f32", rms, True, True, offset=30.0)
+    p["x"][3] = 0.0
+    p["x"][4] = 2.0
+    p["r"][3] = 0.0
+    y, u, stats = check_forward(p, 264, "f32", rms, True, True)
+    got = check_backward(p, y, stats, 264, "f32", rms, True, True)
+    assert all(bool(torch.isfinite(v).all()) for v in (y, u, stats) + tuple(g for g in got if g is not None))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_at_their_ends(dtype):
+    """Arguments of a gate up to the type's largest and both infinities: the gate is 0 or 1, its gradient 0, nothing is NaN."""
+    D = 48
+    p = problem(6, D, dtype, True, True, True)
+    ends = torch.tensor([-float("inf"), -3e38, -200.0, -88.0, -20.0, 20.0, 88.0, 200.0, 3e38, float("inf"), 0.0, -0.0], device=DEV)
+    p["x"][:, D:] = ends.repeat(4).to(TYPES[dtype])
+    with np.errstate(over="ignore", invalid="ignore"):
+        y, _, stats = check_forward(p, D, dtype, True, True, True)
+        got = check_backward(p, y, stats, D, dtype, True, True, True)
+    assert all(bool(torch.isfinite(v).all()) for v in got if v is not None)
+
+
+@pytest.mark.parametrize("D", [40, 1048])
+def test_a_row_of_nan_stays_alone(D):
+    """A row that is not finite leaves every other row's results as they are."""
+    p = problem(9, D, "bf16", True, False, True)
+    y0, u0, st0 = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=True)
+    args = lambda y, st: (p["dy"], p["du"], p["x"], p["r"], y, st, p["gain"], p["scale"], p["pre_gain"])   # noqa: E731
+    b0 = tmps.norm_join_backward(*args(y0, st0), rms=True)
+    p["x"][4, 3] = float("nan")
+    p["x"][6, 1] = float("inf")
+    y1, u1, st1 = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=True)
+    b1 = tmps.norm_join_backward(*args(y1, st1), rms=True)
+    others = [0, 1, 2, 3, 5, 7, 8]
+    for a, b in ((y0, y1), (u0, u1), (b0[0], b1[0]), (b0[1], b1[1])):
+        assert torch.equal(a[others], b[others])
+    assert bool(torch.isnan(u1[4]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 768, 4096])
+def test_addresses_off_16_bytes_and_in_place(dtype, D):
+    """Operands that begin one element later give what aligned ones give, up to the order of sums; y over r and dr over dy, and the memory around results stays."""
+    rows, t = 21, TYPES[dtype]
+    p = problem(rows, D, dtype, False, False, True, seed=1)
+
+    def moved(v):
+        flat = torch.full((v.numel() + 9,), 7.0, dtype=v.dtype, device=DEV)
+        at = flat[1:1 + v.numel()].view(v.shape)
+        at.copy_(v)
+        return at, flat
+    q = {k: moved(v)[0] for k, v in p.items() if v is not None}
+    y, _, stats = check_forward(q, D, dtype, False, False, True)
+    check_backward(q, y, stats, D, dtype, False, False, True)
+    r, flat = moved(p["r"])
+    y2, u2, st2 = tmps.norm_join(q["x"], r, q["gain"], q["scale"], pre_gain=q["pre_gain"], pre_shift=q["pre_shift"], y=r)
+    assert y2 is r and torch.equal(y2, y) and flat[0] == 7 and bool((flat[1 + rows * D:] == 7).all())
+    dy, flat = moved(p["dy"])
+    want = tmps.norm_join_backward(q["dy"], q["du"], q["x"], q["r"], y, stats, q["gain"], q["scale"], pre_gain=q["pre_gain"])
+    got = tmps.norm_join_backward(dy, q["du"], q["x"], q["r"], y, stats, q["gain"], q["scale"], pre_gain=q["pre_gain"], dr=dy)
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and flat[0] == 7 and bool((flat[1 + rows * D:] == 7).all())
+    assert y.dtype == t
+
+
+@pytest.mark.parametrize("D", [64, 1100])
+def test_gradients_are_those_of_differences(D):
+    """fp32 forward values of a loss sum(w y) + sum(v u) along a direction against the gradient: central differences of a smooth function, error h^2 and 2^-24 / h."""
+    rows = 4
+    p = problem(rows, D, "f32", False, True, True, seed=7)
+    w, v = p["dy"], p["du"]
+    names = ["x", "r", "gain", "scale", "pre_gain", "pre_shift"]
+
+    def loss(q):
+        y, u, _ = tmps.norm_join(q["x"], q["r"], q["gain"], q["scale"], pre_gain=q["pre_gain"], pre_shift=q["pre_shift"], gate=True)
+        return ((w.double() * y.double()).sum() + (v.double() * u.double()).sum()).item(), (w.double() * y.double()).norm().item() + (v.double() * u.double()).norm().item()
+    y, u, stats = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], pre_gain=p["pre_gain"], pre_shift=p["pre_shift"], gate=True)
+    grads = dict(zip(names, tmps.norm_join_backward(w, v, p["x"], p["r"], y, stats, p["gain"], p["scale"], pre_gain=p["pre_gain"], gate=True)))
+    gen = torch.Generator().manual_seed(11)
+    for name in names:
+        d = torch.randn(p[name].shape, generator=gen).to(DEV)
+        d /= d.norm()
+        h = 2.0 ** -5
+        up, size = loss(dict(p, **{name: p[name] + h * d}))
+        down, _ = loss(dict(p, **{name: p[name] - h * d}))
+        slope = (up - down) / (2 * h)
+        along = (grads[name].double() * d.double()).sum().item()
+        # the third derivative along a unit direction is at most a few tens here; values are off by some steps of 2^-24 each, independently
+        assert abs(slope - along) <= 30 * h * h + 16 * STEP * size / h, (name, slope, along)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [96, 1536])
+def test_graph_replays_and_another_stream(dtype, D):
+    """Both passes captured; several replays on new values between eager calls; sums over rows bit for bit the same each time."""
+    rows = 600
+    p = problem(rows, D, dtype, True, True, True, seed=0)
+
+    def both():
+        y, u, st = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=True, gate=True)
+        return (y, u, st) + tmps.norm_join_backward(p["dy"], p["du"], p["x"], p["r"], y, st, p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=True, gate=True)[:5]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = both()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, both()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    for seed in range(1, 5):
+        for k, v in problem(rows, D, dtype, True, True, True, seed=seed).items():
+            if v is not None:
+                p[k].copy_(v)
+        graph.replay()
+        eager = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager))
+
+
+def test_no_rows_and_many_rows():
+    p = problem(0, 40, "bf16", True, False, True)
+    y, u, st = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=True)
+    got = tmps.norm_join_backward(p["dy"], p["du"], p["x"], p["r"], y, st, p["gain"], p["scale"], pre_gain=p["pre_gain"], rms=True)
+    assert y.shape == u.shape == (0, 40) and all(bool((g == 0).all()) for g in got[2:5])
+    p = problem(60001, 16, "bf16", False, False, True)
+    y, _, st = check_forward(p, 16, "bf16", False, False, True)
+    check_backward(p, y, st, 16, "bf16", False, False, True)
+
+
+def test_rows_beyond_32_bit_offsets():
+    """The last row of an array of more than 2^31 elements, forward and backward."""
+    rows, D = 140000, 16384
+    x = torch.zeros(rows, D, dtype=torch.bfloat16, device=DEV)
+    r = torch.zeros(rows, D, dtype=torch.bfloat16, device=DEV)
+    p = problem(1, D, "bf16", True, False, False)
+    x[-1], r[-1] = p["x"][0], p["r"][0]
+    y, _, st = tmps.norm_join(x, r, p["gain"], p["scale"], rms=True)
+    one, _, st1 = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], rms=True)
+    assert torch.equal(y[-1], one[0]) and torch.equal(st[-1, :2], st1[0, :2])
+    r.zero_()
+    r[-1] = p["dy"][0]   # the upstream gradient from here on
+    dx, dr, dgain, _, _, _ = tmps.norm_join_backward(r, None, x, y, None, st, p["gain"], p["scale"], rms=True, dr=r)
+    want = tmps.norm_join_backward(p["dy"], None, p["x"], one, None, st1, p["gain"], p["scale"], rms=True)
+    assert torch.equal(dx[-1], want[0][0]) and torch.equal(dr[-1], want[1][0]) and torch.equal(dgain, want[2])
