@@ -63,7 +63,8 @@ enum {
     TMPS_SOFTMAX_CE = 4, /* dims = {classes, rows}; only as the last layer of the last stage, after a plain
                             TMPS_LINEAR with the same rows; labels are int32 [samples, rows]; the loss is the
                             mean over all rows */
-    TMPS_LAYERNORM = 5,  /* dims = {D, rows}; per row of D features, eps 1e-5; parameters gain (w) and shift (b) */
+    TMPS_LAYERNORM = 5,  /* dims = {D, rows}; per row of D features, eps 1e-5; parameters gain (w) and shift (b); with
+                            TMPS_FLAG_RMS no mean is subtracted and there is no shift */
     TMPS_ATTENTION = 6,  /* dims = {S, D, heads}; causal multi-head self-attention; input rows [q | k | v] of 3*D
                             features, output [S, D]; scores scaled by 1/sqrt(D/heads) */
     TMPS_EMBEDDING = 7,  /* dims = {vocab, S, D}; first layer of a stage only; the stage input is int32 tokens
@@ -75,13 +76,30 @@ enum {
     TMPS_RESADD = 9,     /* dims = {H, W, C, k}; y = act(a + b): a = the result of the layer before, b = the result of
                             the layer k positions before (one before the first layer = the stage input);
                             TMPS_FLAG_RELU */
-    TMPS_AVGPOOL = 10    /* dims = {H, W, C}; mean over the H*W positions: [H, W, C] -> [C] */
+    TMPS_AVGPOOL = 10,   /* dims = {H, W, C}; mean over the H*W positions: [H, W, C] -> [C] */
+    TMPS_ROTARY = 11,    /* dims = {S, D, heads, height, width, pairs_h, pairs_w, base}; rows [q | k | v] of 3*D features as
+                            TMPS_ATTENTION reads them; every head's q and k turn by the row's position (tmps_rotary): row
+                            (t * height + h) * width + w has time t, height h, width w (0 = 1: text, time is the row);
+                            pairs_h and pairs_w of a head's D/heads/2 pairs turn with height and width, the others, which
+                            come first, with time; base 0 = 10000; TMPS_FLAG_INTERLEAVED, TMPS_FLAG_OWN_LADDERS; must follow
+                            a layer without activation */
+    TMPS_NORMJOIN = 12,  /* dims = {D, rows, k}; a block's result behind its norm, joined with the scaled residual
+                            (tmps_norm_join_forward): y = scale * r + g * gain * n(f); f = the result of the layer before (with
+                            TMPS_FLAG_GATE rows [f | a] of 2*D features), r = the result of the layer k >= 2 positions before
+                            (one before the first layer = the stage input); TMPS_FLAG_RMS; parameters gain (w, [D]) and scale (b,
+                            [D]); both sources without activation.  A TMPS_LAYERNORM of the same kind behind it is part of
+                            its launches */
+    TMPS_DISTILL = 13    /* dims = {classes, rows, k, temperature, alpha}, the last two the bits of a float; in the place
+                            of TMPS_SOFTMAX_CE: loss and gradient of tmps_distill, averaged over all rows; labels are int32
+                            [samples, rows, 1 + 2 k]: the label, k ids, then the bits of the k teacher logits */
 };
 enum {
     TMPS_FLAG_RELU = 1,
     TMPS_FLAG_GELU = 2, /* exact: z * Phi(z) */
     TMPS_FLAG_RMS = 4,  /* a norm without a mean: v / sqrt(mean(v^2) + 1e-5) */
-    TMPS_FLAG_GATE = 8  /* rows [f | a]: f under the gate 1 / (1 + exp(-a)) */
+    TMPS_FLAG_GATE = 8, /* rows [f | a]: f under the gate 1 / (1 + exp(-a)) */
+    TMPS_FLAG_INTERLEAVED = 16, /* rotary positions: pairs of neighbours 2i and 2i + 1 (else i and i + all pairs) */
+    TMPS_FLAG_OWN_LADDERS = 32  /* rotary positions: frequencies begin anew on each axis (else one ladder over all pairs) */
 };
 /* A convolution normally reads the result of the layer before it.  TMPS_FLAG_SRC(k), k = 2..255, in its flags
  * makes it read the result of the layer k positions before it instead (one position before the first layer of a
@@ -268,16 +286,15 @@ int tmps_update(tmps_stage* stage, void* hip_stream);
  * NULL; gradients of parameters, where given, are zeros).  Errors: TMPS_EINVAL, TMPS_ESHAPE, TMPS_EUNSUPPORTED, TMPS_ECAP (workspace too small), TMPS_EHIP. */
 
 /* Rotary positions with several axes (time, height, width).  Each of the `heads` heads of dh features that begin a row has pairs[0] + pairs[1] + pairs[2] pairs of
- * features (u, v): feature i and i + all pairs, or neighbours 2i and 2i + 1 with TMPS_ROTARY_INTERLEAVED.  The first pairs[0] turn with the row's time, the next pairs[1]
- * with its height, the rest with its width: u' = u cos - v sin, v' = v cos + u sin at the angle position * base^(-i / all pairs) or, with TMPS_ROTARY_OWN_LADDERS,
+ * features (u, v): feature i and i + all pairs, or neighbours 2i and 2i + 1 with TMPS_FLAG_INTERLEAVED.  The first pairs[0] turn with the row's time, the next pairs[1]
+ * with its height, the rest with its width: u' = u cos - v sin, v' = v cos + u sin at the angle position * base^(-i / all pairs) or, with TMPS_FLAG_OWN_LADDERS,
  * base^(-j / the axis's pairs), j counted on the axis.  Features behind the pairs are copied; what follows the heads in a row of x is not read, in a row of y not written.
  * Angles are formed in 64 bits.  positions: int32 [n_positions, 3]; row r has those of r % n_positions.  inverse != 0 turns back, which is also the gradient's way.
  * y may be x, or other columns of x's rows. */
-enum { TMPS_ROTARY_INTERLEAVED = 1, TMPS_ROTARY_OWN_LADDERS = 2 };
 typedef struct {
     int32_t heads, dh;
     int32_t pairs[3];
-    int32_t flags;
+    int32_t flags;    /* TMPS_FLAG_INTERLEAVED, TMPS_FLAG_OWN_LADDERS */
     float base;
 } tmps_rotary_desc;
 int tmps_rotary(int dtype, const tmps_rotary_desc* desc, const void* x, int64_t x_stride, void* y, int64_t y_stride, const int32_t* positions,

@@ -85,6 +85,78 @@ def layernorm_backward(dy, cache, gamma_now):
     return dx.reshape(cache["x_shape"]), (dy2 * xhat).sum(axis=0), dy2.sum(axis=0)
 
 
+# ----------------------------------------------------------------------------- norms around a block
+def norm_rows(x2, rms, eps=1e-5):
+    """Normalised rows and 1/std; rms: no mean is subtracted."""
+    c = x2 if rms else x2 - x2.mean(axis=1, keepdims=True)
+    rstd = 1.0 / np.sqrt((c * c).mean(axis=1, keepdims=True) + eps)
+    return c * rstd, rstd
+
+
+def norm_rows_backward(t, xhat, rstd, rms):
+    """Gradient w.r.t. the rows from t, that w.r.t. the normalised rows."""
+    m = 0.0 if rms else t.mean(axis=1, keepdims=True)
+    return rstd * (t - m - xhat * (t * xhat).mean(axis=1, keepdims=True))
+
+
+def rmsnorm_forward(x, gain, d, eps=1e-5):
+    xhat, rstd = norm_rows(x.reshape(-1, d), True, eps)
+    return (xhat * gain).reshape(x.shape), {"xhat": xhat, "rstd": rstd, "x_shape": x.shape}
+
+
+def rmsnorm_backward(dy, cache, gain_now):
+    """Returns (dx, dgain)."""
+    dy2 = dy.reshape(cache["xhat"].shape)
+    dx = norm_rows_backward(dy2 * gain_now, cache["xhat"], cache["rstd"], True)
+    return dx.reshape(cache["x_shape"]), (dy2 * cache["xhat"]).sum(axis=0)
+
+
+def norm_join_forward(x, r, gain, scale, d, rms, gate):
+    """y = scale * r + g * gain * norm(f) on rows of d features; x holds f or, with gate, [f | a] with g = 1 / (1 + exp(-a))."""
+    B = x.shape[0]
+    x2, r2 = x.reshape(-1, 2 * d if gate else d), r.reshape(-1, d)
+    fhat, rstd = norm_rows(x2[:, :d], rms)
+    g = 1.0 / (1.0 + np.exp(-x2[:, d:])) if gate else 1.0
+    y = scale * r2 + g * gain * fhat
+    return y.reshape(B, -1), {"fhat": fhat, "rstd": rstd, "g": g, "r": r2, "x_shape": x.shape}
+
+
+def norm_join_backward(dy, cache, gain_now, scale_now, rms, gate):
+    """Returns (dx, dr, dgain, dscale)."""
+    fhat, g, r2 = cache["fhat"], cache["g"], cache["r"]
+    dy2 = dy.reshape(fhat.shape)
+    df = norm_rows_backward(dy2 * g * gain_now, fhat, cache["rstd"], rms)
+    dx = np.concatenate([df, dy2 * gain_now * fhat * g * (1.0 - g)], axis=1) if gate else df
+    return dx.reshape(cache["x_shape"]), (dy2 * scale_now).reshape(dy.shape[0], -1), (dy2 * g * fhat).sum(axis=0), (dy2 * r2).sum(axis=0)
+
+
+# ----------------------------------------------------------------------------- rotary positions
+def rotary_turns(spec):
+    """exp(i angle) of every row and pair: [s, d / heads / 2] complex numbers."""
+    s, pairs = spec["s"], spec["d"] // spec["heads"] // 2
+    row = np.arange(s)
+    pos = [row // (spec["width"] * spec["height"]), row // spec["width"] % spec["height"], row % spec["width"]]
+    counts = [pairs - spec["pairs_h"] - spec["pairs_w"], spec["pairs_h"], spec["pairs_w"]]
+    angle, first = [], 0
+    for p, n in zip(pos, counts):
+        for j in range(n):
+            angle.append(p * float(spec["base"] or 10000) ** -(j / n if spec["own_ladders"] else (first + j) / pairs))
+        first += n
+    return np.exp(1j * np.stack(angle, axis=1))
+
+
+def rotary_apply(qkv, spec, inverse=False):
+    """Packed [B, s, 3d] rows with the pairs of q and k turned (inverse: back, which is also the gradient's way)."""
+    B, s, heads = qkv.shape[0], spec["s"], spec["heads"]
+    dh = spec["d"] // heads
+    t = qkv.reshape(B, s, 3, heads, dh).copy()
+    e = rotary_turns(spec)[None, :, None, None, :]
+    a, b = (slice(0, dh, 2), slice(1, dh, 2)) if spec["interleaved"] else (slice(0, dh // 2), slice(dh // 2, dh))
+    z = (t[:, :, :2, :, a] + 1j * t[:, :, :2, :, b]) * (e.conj() if inverse else e)
+    t[:, :, :2, :, a], t[:, :, :2, :, b] = z.real, z.imag
+    return t.reshape(B, -1)
+
+
 # ----------------------------------------------------------------------------- attention
 def attention_forward(qkv, s, d, heads):
     """Causal multi-head self-attention on packed [B, s, 3d] = (q | k | v), heads of d/heads features:
@@ -271,3 +343,31 @@ def softmax_ce_backward(cache, M):
     g = p.copy()
     g[np.arange(p.shape[0]), cache["labels"]] -= 1.0
     return g / M
+
+
+# ----------------------------------------------------------------------------- distillation
+def distill_forward(logits, records, k, temperature, alpha):
+    """Mean over the rows of alpha T^2 KL(p | softmax(z / T)) + (1 - alpha) (-log softmax(z)[label]), p the softmax over T of the teacher's logits of its k
+    classes; records: int32 [rows, 1 + 2k] of label, classes and the bits of the logits.  -1: no label, no entry; a row without either has loss 0."""
+    records = np.ascontiguousarray(records, dtype=np.int32).reshape(logits.shape[0], -1)
+    T, losses, grads = temperature, np.zeros(logits.shape[0]), np.zeros(logits.shape)
+    for r, rec in enumerate(records):
+        ids, teacher = rec[1:1 + k], rec[1 + k:].view(np.float32).astype(np.float64)
+        on = (ids >= 0) & (teacher > -np.inf)
+        if alpha > 0 and on.any():
+            lq = logits[r] / T - np.logaddexp.reduce(logits[r] / T)
+            lp = teacher[on] / T - np.logaddexp.reduce(teacher[on] / T)
+            losses[r] += alpha * T * T * (np.exp(lp) * (lp - lq[ids[on]])).sum()
+            grads[r] += alpha * T * np.exp(lq)
+            np.add.at(grads[r], ids[on], -alpha * T * np.exp(lp))
+        if alpha < 1 and rec[0] >= 0:
+            ls = logits[r] - np.logaddexp.reduce(logits[r])
+            losses[r] -= (1 - alpha) * ls[rec[0]]
+            grads[r] += (1 - alpha) * np.exp(ls)
+            grads[r, rec[0]] -= 1 - alpha
+    return float(losses.mean()), {"g": grads}
+
+
+def distill_backward(cache, M):
+    """Gradient of (1/M) times the sum of the mini-batch's row losses."""
+    return cache["g"] / M

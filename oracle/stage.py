@@ -29,7 +29,7 @@ class Stage:
         self.bufs = [{k: np.zeros_like(v) for k, v in p.items()} for p in self.params]
         self.grads = [None] * len(layer_specs)
         self.lr, self.mu, self.M, self.N = float(lr), float(momentum), M, N
-        self.is_last = layer_specs[-1]["kind"] == "softmax_ce"
+        self.is_last = layer_specs[-1]["kind"] in ("softmax_ce", "distill")
         self.stash = {}
         self.version = 0
         self.keep_versions = 0   # older weight versions kept for vertical weight stashing
@@ -61,7 +61,7 @@ class Stage:
             if k == "conv" and spec.get("src", 1) != 1:
                 a = earlier(li, spec["src"])
             inputs.append(a)
-            feeds_loss = li + 1 < len(self.specs) and self.specs[li + 1]["kind"] == "softmax_ce"
+            feeds_loss = li + 1 < len(self.specs) and self.specs[li + 1]["kind"] in ("softmax_ce", "distill")
             if k == "linear":
                 skip = inputs[li - spec["skip"]] if spec.get("skip") else None
                 a, c = L.linear_forward(a, q(p["w"]), p["b"], spec["relu"], spec.get("act"), spec.get("rows", 1),
@@ -83,6 +83,14 @@ class Stage:
             elif k == "avgpool":
                 a, c = L.avgpool_forward(a.reshape(a.shape[0], spec["h"], spec["w"], spec["c"]))
                 a = q(a)
+            elif k == "layernorm" and spec.get("rms"):
+                a, c = L.rmsnorm_forward(a, p["w"], spec["d"], spec["eps"])
+                a = q(a)
+            elif k == "norm_join":
+                a, c = L.norm_join_forward(a, earlier(li, spec["src"]), p["w"], p["b"], spec["d"], spec["rms"], spec["gate"])
+                a = q(a)
+            elif k == "rotary":
+                a, c = q(L.rotary_apply(a, spec)), None
             elif k == "layernorm":
                 a, c = L.layernorm_forward(a, p["w"], p["b"], spec["d"], spec["eps"])
                 a = q(a)
@@ -92,6 +100,8 @@ class Stage:
             elif k == "embedding":
                 a, c = L.embedding_forward(a, q(p["w"]), q(p["b"]))
                 a = q(a)
+            elif k == "distill":
+                loss, c = L.distill_forward(a.reshape(a.shape[0] * spec["rows"], -1), labels, spec["k"], spec["temperature"], spec["alpha"])
             elif k == "softmax_ce":
                 rows = spec.get("rows", 1)
                 loss, c = L.softmax_ce_forward(a.reshape(a.shape[0] * rows, -1), np.asarray(labels).reshape(-1))
@@ -158,6 +168,15 @@ class Stage:
                     give(max(li - spec["src_b"], -1), g)
                 elif k == "avgpool":
                     g = L.avgpool_backward(g, c)
+                elif k == "distill":
+                    g = L.distill_backward(c, self.M * spec["rows"])
+                elif k == "layernorm" and spec.get("rms"):
+                    g, dw = L.rmsnorm_backward(g, c, p["w"])
+                elif k == "norm_join":
+                    g, dr, dw, db = L.norm_join_backward(g, c, p["w"], p["b"], spec["rms"], spec["gate"])
+                    give(max(li - spec["src"], -1), dr)
+                elif k == "rotary":
+                    g = L.rotary_apply(g, spec, inverse=True)
                 elif k == "layernorm":
                     g, dw, db = L.layernorm_backward(g, c, p["w"])
                 elif k == "attention":
@@ -171,11 +190,8 @@ class Stage:
                     give(max(src, -1), g)
                 if dw is None:
                     continue
-                if acc[li] is None:
-                    acc[li] = {"w": dw, "b": db}
-                else:
-                    acc[li]["w"] = acc[li]["w"] + dw
-                    acc[li]["b"] = acc[li]["b"] + db
+                new = {"w": dw} if db is None else {"w": dw, "b": db}
+                acc[li] = new if acc[li] is None else {key: acc[li][key] + new[key] for key in new}
             g = grad_of.pop(-1, None)
             dxs.append(g)
         self.grads = acc

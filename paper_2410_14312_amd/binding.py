@@ -11,8 +11,8 @@ _lib = None
 TMPS_F32, TMPS_BF16_F32MASTER = 0, 1
 TMPS_LINEAR, TMPS_CONV2D, TMPS_MAXPOOL, TMPS_SOFTMAX_CE, TMPS_LAYERNORM, TMPS_ATTENTION, TMPS_EMBEDDING = 1, 2, 3, 4, 5, 6, 7
 TMPS_AFFINE, TMPS_RESADD, TMPS_AVGPOOL = 8, 9, 10
-TMPS_FLAG_RELU, TMPS_FLAG_GELU, TMPS_FLAG_RMS, TMPS_FLAG_GATE = 1, 2, 4, 8
-TMPS_ROTARY_INTERLEAVED, TMPS_ROTARY_OWN_LADDERS = 1, 2
+TMPS_ROTARY, TMPS_NORMJOIN, TMPS_DISTILL = 11, 12, 13
+TMPS_FLAG_RELU, TMPS_FLAG_GELU, TMPS_FLAG_RMS, TMPS_FLAG_GATE, TMPS_FLAG_INTERLEAVED, TMPS_FLAG_OWN_LADDERS = 1, 2, 4, 8, 16, 32
 
 
 class TmpsError(RuntimeError):
@@ -189,6 +189,21 @@ def pointwise_forward_joint(dtype, positions, cin, cout):
     return bool(lib().tmps_pointwise_forward_joint(TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, int(positions), cin, cout))
 
 
+def _rotary_flags(interleaved, own_ladders):
+    return (TMPS_FLAG_INTERLEAVED if interleaved else 0) | (TMPS_FLAG_OWN_LADDERS if own_ladders else 0)
+
+
+def _float_bits(v):
+    return int(np.float32(v).view(np.int32))
+
+
+def distill_records(labels, ids, teacher):
+    """The labels of a distillation layer: int32 [..., 1 + 2 k] from labels [...], a teacher's classes ids [..., k] and its logits [..., k]."""
+    ids = np.asarray(ids, dtype=np.int32)
+    bits = np.ascontiguousarray(np.asarray(teacher, dtype=np.float32)).view(np.int32)
+    return np.concatenate([np.asarray(labels, dtype=np.int32)[..., None], ids, bits], axis=-1)
+
+
 def layer_descs(specs):
     """Neutral layer dicts (workloads.configs) -> array of tmps_layer_desc."""
     arr = (LayerDesc * len(specs))()
@@ -202,6 +217,15 @@ def layer_descs(specs):
             if abs(sp["eps"] - 1e-5) > 1e-12:
                 raise ValueError("the library's layer normalisation uses eps = 1e-5")
             d.kind, dims[:2] = TMPS_LAYERNORM, [sp["d"], sp["rows"]]
+            d.flags = TMPS_FLAG_RMS if sp.get("rms") else 0
+        elif k == "rotary":
+            d.kind, dims[:8] = TMPS_ROTARY, [sp["s"], sp["d"], sp["heads"], sp["height"], sp["width"], sp["pairs_h"], sp["pairs_w"], sp["base"]]
+            d.flags = _rotary_flags(sp["interleaved"], sp["own_ladders"])
+        elif k == "norm_join":
+            d.kind, dims[:3] = TMPS_NORMJOIN, [sp["d"], sp["rows"], sp["src"]]
+            d.flags = _join_flags(sp["rms"], sp["gate"])
+        elif k == "distill":
+            d.kind, dims[:5] = TMPS_DISTILL, [sp["classes"], sp["rows"], sp["k"], _float_bits(sp["temperature"]), _float_bits(sp["alpha"])]
         elif k == "attention":
             d.kind, dims[:3] = TMPS_ATTENTION, [sp["s"], sp["d"], sp["heads"]]
         elif k == "embedding":
@@ -289,7 +313,7 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
         out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
     elif out.dim() != 2 or out.shape[0] != rows or out.shape[1] < width or (out.shape[1] > 1 and out.stride(1) != 1) or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("out: %d rows of at least %d neighbouring %s features on %s are wanted" % (rows, width, x.dtype, x.device))
-    d = RotaryDesc(heads, dh, (C.c_int32 * 3)(*pairs), (TMPS_ROTARY_INTERLEAVED if interleaved else 0) | (TMPS_ROTARY_OWN_LADDERS if own_ladders else 0), base)
+    d = RotaryDesc(heads, dh, (C.c_int32 * 3)(*pairs), _rotary_flags(interleaved, own_ladders), base)
     _call(lib().tmps_rotary, x.device, stream, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
     return out
 
@@ -388,7 +412,7 @@ class Stage:
             specs[0] = dict(specs[0], cin=self.cin_pad)
         self.specs = specs
         self.device = torch.device(device)
-        self.is_last = specs[-1]["kind"] == "softmax_ce"
+        self.is_last = specs[-1]["kind"] in ("softmax_ce", "distill")
         self.cfg = StageCfg(TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, micro_batch, n_micro, max_stash,
                             int(self.is_last), int(borrow_input), lr, momentum)
         self.act_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32

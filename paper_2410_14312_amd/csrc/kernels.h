@@ -6,6 +6,9 @@
 
 #include <vector>
 
+// Layer kinds that a host-only build of the executor may lack: it links without their launchers, and refuses such layers.
+#define TMPS_OPTIONAL __attribute__((weak))
+
 namespace tmps {
 
 // dtype codes match TMPS_F32 / TMPS_BF16_F32MASTER
@@ -181,21 +184,21 @@ hipError_t attention_backward(int dtype, const void* qkv, const void* o, const v
 size_t attention_workspace_elems(int B, int S, int H);
 
 // Rotary positions: every head's pairs of features turned by an angle of the row's positions on up to three axes (inverse: back).  `heads` heads of dh features
-// begin each row of x and y, whose rows are x_stride and y_stride elements apart; pairs[a] pairs turn with axis a, features behind them are copied.  Row r has the
+// begin each row of x and y, whose rows are x_stride and y_stride elements apart, `copied` more heads behind them are copied (nothing where y is x); pairs[a] pairs
+// turn with axis a, features behind them are copied.  flags: TMPS_FLAG_INTERLEAVED, TMPS_FLAG_OWN_LADDERS.  Row r has the
 // positions pos[r % pos_rows][0..2] or, without pos, those of a grid: row r % grid_rows is (time, height, width) in row-major order.  y may be x.
-enum { kRotaryInterleaved = 1, kRotaryOwnLadders = 2 };   // pairs are neighbours (else i and i + all pairs); frequencies begin anew on each axis
 struct Rotary {
     const void* x;
     void* y;
     int64_t x_stride, y_stride, rows;
-    int heads, dh, pairs[3], flags;
+    int heads, copied, dh, pairs[3], flags;
     float base;
     bool inverse;
     const int32_t* pos;
     int64_t pos_rows;
     int grid_rows, grid_h, grid_w;
 };
-hipError_t rotary(int dtype, const Rotary& r, hipStream_t s);
+TMPS_OPTIONAL hipError_t rotary(int dtype, const Rotary& r, hipStream_t s);
 
 // A block's result behind its norm and under its gate, joined with the scaled residual, and the norm in front of the next block:
 //   y = scale r + g gain n(f),  u = n(y) pre_gain + pre_shift,  n(v) = (v - mean) / sqrt(var + 1e-5), with rms v / sqrt(mean(v^2) + 1e-5)
@@ -214,21 +217,22 @@ struct NormJoin {
     int D;
     bool rms, gate;
 };
-hipError_t norm_join_forward(int dtype, const NormJoin& j, hipStream_t s);
-// Its backward pass: dh = dy + gradient through the norm of y (either may be missing); dr = scale dh, dx = the gradient of the rows of x (both may be null; without
-// x, dr receives dh itself), dgain_dscale: D gain gradients and D scale gradients, dpre: D pre_gain gradients and, without rms, D pre_shift gradients.  Results may
-// be operands of the same layout.  part, part_pre: norm_join_part_elems(rows, D) fp32 elements each; their sums may wait.
+TMPS_OPTIONAL hipError_t norm_join_forward(int dtype, const NormJoin& j, hipStream_t s);
+// Its backward pass: dh = dy + gradient through the norm of y (either may be missing); dr = scale dh + add (add may be null), dx = the gradient of the rows of x (dx
+// and dr may be null; without x, dr receives dh itself), dgain_dscale: D gain gradients and D scale gradients, dpre: D pre_gain gradients and, without rms, D pre_shift gradients.  Results may
+// be operands of the same layout (dr: dy, du, add; dx: none).  part, part_pre: norm_join_part_elems(rows, D) fp32 elements each; their sums may wait.
 struct NormJoinBackward {
     const void *dy, *du, *x, *r, *y;
     const float *stats, *pre_stats, *gain, *scale, *pre_gain;
+    const void* add;
     void *dx, *dr;
     float *dgain_dscale, *dpre;
     int64_t stats_stride, rows;
     int D;
     bool rms, gate;
 };
-hipError_t norm_join_backward(int dtype, const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s);
-size_t norm_join_part_elems(int64_t rows, int D);
+TMPS_OPTIONAL hipError_t norm_join_backward(int dtype, const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s);
+TMPS_OPTIONAL size_t norm_join_part_elems(int64_t rows, int D);
 
 // y[row] = wte[tok[row]] + wpe[row % S] (tables in the contraction dtype), and the table gradients
 // (fp32; dwte cleared, then every occurring token's rows of dy added in row order, no atomic adds; dwpe summed over the batch).
@@ -250,7 +254,7 @@ hipError_t softmax_ce_small(int dtype, const float* logits, const int32_t* label
 // Distillation: a row's loss alpha T^2 KL(p | softmax(z / T)) + (1 - alpha) (-log softmax(z)[label]), p the softmax of the teacher's k logits over T, and
 // dlogits (may be null) = grad_scale times its gradient.  ids, teacher, labels: entry_stride and label_stride elements from row to row; an id or label of -1 is none
 // (a row without entries or label lacks that term, without both its loss and gradient are 0 whatever its logits), any other outside the classes a NaN loss.
-// Repeated ids add up.  labels may be null where alpha is 1.  ws: distill_workspace_elems.
+// Repeated ids add up.  labels may be null.  ws: distill_workspace_elems of these rows and those of the plan.
 constexpr int kDistillMaxEntries = 1024;
 struct Distill {
     const float* logits;
@@ -261,10 +265,11 @@ struct Distill {
     float temperature, alpha, grad_scale;
     void* dlogits;
     float* row_loss;
+    int64_t plan_rows;   // rows of the loss that these are part of: its passes run the same kernel, however they are cut
 };
-hipError_t distill(int dtype, const Distill& d, float* ws, hipStream_t s);
-size_t distill_workspace_elems(int64_t rows, int classes);
-int check_distill(int64_t classes, int64_t k, float temperature, float alpha);   // TMPS_OK, or the refusal
+TMPS_OPTIONAL hipError_t distill(int dtype, const Distill& d, float* ws, hipStream_t s);
+TMPS_OPTIONAL size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes);
+TMPS_OPTIONAL int check_distill(int64_t classes, int64_t k, float temperature, float alpha);   // TMPS_OK, or the refusal
 // out[0] = scale * sum(in[0..n))   (deterministic single-block tree)
 hipError_t reduce_scaled_sum(const float* in, int n, float scale, float* out, hipStream_t s);
 

@@ -145,8 +145,9 @@ template <typename T> __global__ __launch_bounds__(256) void distill_kernel(Dist
     }
 }
 
-size_t distill_workspace_elems(int64_t rows, int classes) {
+size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes) {
     (void)rows;
+    (void)plan_rows;
     (void)classes;
     return 0;
 }

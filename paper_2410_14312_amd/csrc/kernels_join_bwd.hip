@@ -1,6 +1,6 @@
 // Norm joins, backward.  With the rows' statistics of the forward pass, fh = (f - m1) i1 and yh = (y - m2) i2:
 //   t = du pre_gain, dh = dy + i2 (t - mean(t) - yh mean(t yh))                 (means of t only where the norm subtracts one)
-//   dr = scale dh;  da = dh gain fh g (1 - g);  v = dh g gain, df = i1 (v - mean(v) - fh mean(v fh))
+//   dr = scale dh (+ what others have given r);  da = dh gain fh g (1 - g);  v = dh g gain, df = i1 (v - mean(v) - fh mean(v fh))
 //   dpre_gain = sum du yh, dpre_shift = sum du, dscale = sum dh r, dgain = sum dh g fh over the rows
 // One pass over memory: dy, du, x, r, y are read and dx, dr written once each.  A team goes over its share of the rows and keeps its sums over them in registers, which
 // leave as one row of partial results; those are added up in a fixed order behind.
@@ -82,6 +82,12 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
                     fh[i][e] = (fh[i][e] - mean) * rstd;
                     dscale[i][e] = fmaf(dh[i][e], r[e], dscale[i][e]);
                     o[e] = dh[i][e] * sc[e];
+                }
+                if (a.add) {
+                    float b[V];
+                    load_piece<V>((const T*)a.add + row * D + c, b);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) o[e] += b[e];
                 }
                 if (a.gate) {
                     float at[V], da[V];

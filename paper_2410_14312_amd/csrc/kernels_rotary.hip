@@ -3,6 +3,7 @@
 //
 // Angles are formed as turns in 64 bits: a position of a million times a frequency of one is 1.6e5 turns, of which fp32 keeps 1/64 of a turn.  What is left of whole
 // turns goes to fp32 (2^-25 of a turn at most), its sine and cosine from there.
+#include "../../include/tmps.h"
 #include "gemm.hip.h"
 #include "kernels.h"
 #include "launch.h"
@@ -17,7 +18,7 @@ struct Ladders {
 
 struct RotaryShape {
     int64_t x_stride, y_stride, rows, pos_rows;
-    int heads, dh, pairs, interleaved;
+    int heads, turned, dh, pairs, interleaved;   // heads from `turned` on are copied
     const int32_t* pos;
     int grid_rows, grid_h, grid_w;
     float sign;   // -1: back
@@ -61,6 +62,11 @@ template <typename T> __global__ __launch_bounds__(256) void rotary_kernel(const
         const int h = (int)(rest % a.heads) * a.dh;
         const T* const xr = x + row * a.x_stride + h;
         T* const yr = y + row * a.y_stride + h;
+        if (h >= a.turned * a.dh) {
+            yr[i] = xr[i];
+            if (i < a.pairs) yr[per_head + i] = xr[per_head + i];
+            continue;
+        }
         if (i >= a.pairs) {
             yr[a.pairs + i] = xr[a.pairs + i];
             continue;
@@ -79,12 +85,12 @@ hipError_t rotary(int dtype, const Rotary& r, hipStream_t s) {
     if (r.rows <= 0) return hipSuccess;
     RotaryShape a;
     a.x_stride = r.x_stride; a.y_stride = r.y_stride; a.rows = r.rows; a.pos_rows = r.pos_rows;
-    a.heads = r.heads; a.dh = r.dh; a.pairs = r.pairs[0] + r.pairs[1] + r.pairs[2]; a.interleaved = r.flags & kRotaryInterleaved;
+    a.heads = r.heads + (r.x == r.y ? 0 : r.copied); a.turned = r.heads; a.dh = r.dh; a.pairs = r.pairs[0] + r.pairs[1] + r.pairs[2]; a.interleaved = r.flags & TMPS_FLAG_INTERLEAVED;
     a.pos = r.pos; a.grid_rows = r.grid_rows; a.grid_h = r.grid_h; a.grid_w = r.grid_w;
     a.sign = r.inverse ? -1.0f : 1.0f;
     int at = 0;
     for (int k = 0; k < 3; ++k) {
-        const bool own = r.flags & kRotaryOwnLadders;
+        const bool own = r.flags & TMPS_FLAG_OWN_LADDERS;
         const int n = own ? r.pairs[k] : a.pairs;
         a.l.first[k] = own ? at : 0;
         a.l.ratio[k] = n > 0 ? pow((double)r.base, -1.0 / n) : 1.0;

@@ -53,7 +53,7 @@ extern "C" int tmps_rotary(int dtype, const tmps_rotary_desc* desc, const void* 
         pairs += desc->pairs[k];
     }
     if (pairs < 1 || 2 * pairs > desc->dh) return fail(TMPS_ESHAPE, "%lld pairs of features in a head of %d", (long long)pairs, desc->dh);
-    if (desc->flags & ~(TMPS_ROTARY_INTERLEAVED | TMPS_ROTARY_OWN_LADDERS)) return fail(TMPS_EINVAL, "unknown flags %d", desc->flags);
+    if (desc->flags & ~(TMPS_FLAG_INTERLEAVED | TMPS_FLAG_OWN_LADDERS)) return fail(TMPS_EINVAL, "unknown flags %d", desc->flags);
     if (!(desc->base > 0.0f) || !isfinite(desc->base)) return fail(TMPS_EINVAL, "base must be positive");
     const int64_t width = (int64_t)desc->heads * desc->dh, esz = (int64_t)act_bytes(dtype);
     if (width > INT32_MAX) return fail(TMPS_EUNSUPPORTED, "rows of more than 2^31 features");
@@ -74,7 +74,7 @@ extern "C" int tmps_rotary(int dtype, const tmps_rotary_desc* desc, const void* 
     Rotary r;
     r.x = x; r.y = y; r.x_stride = x_stride; r.y_stride = y_stride; r.rows = rows; r.heads = desc->heads; r.dh = desc->dh;
     for (int k = 0; k < 3; ++k) r.pairs[k] = desc->pairs[k];
-    r.flags = ((desc->flags & TMPS_ROTARY_INTERLEAVED) ? kRotaryInterleaved : 0) | ((desc->flags & TMPS_ROTARY_OWN_LADDERS) ? kRotaryOwnLadders : 0);
+    r.flags = desc->flags; r.copied = 0;
     r.base = desc->base; r.inverse = inverse != 0; r.pos = positions; r.pos_rows = n_positions;
     r.grid_rows = r.grid_h = r.grid_w = 1;
     TMPS_HIP(rotary(dtype, r, (hipStream_t)hip_stream));
@@ -142,7 +142,7 @@ extern "C" int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D
     if (overlaps(operands, results, dy)) return fail(TMPS_EINVAL, "a result or the workspace overlaps an operand or another result (dr may be dy)");
     NormJoinBackward j;
     j.dy = dy; j.du = du; j.x = x; j.r = r; j.y = y; j.stats = stats; j.pre_stats = stats ? stats + 2 : nullptr; j.gain = gain; j.scale = scale; j.pre_gain = pre_gain;
-    j.dx = dx; j.dr = dr; j.dgain_dscale = dgain_dscale; j.dpre = dpre; j.stats_stride = 4; j.rows = rows; j.D = D; j.rms = rms; j.gate = gate;
+    j.add = nullptr; j.dx = dx; j.dr = dr; j.dgain_dscale = dgain_dscale; j.dpre = dpre; j.stats_stride = 4; j.rows = rows; j.D = D; j.rms = rms; j.gate = gate;
     if (rows == 0) j.x = dgain_dscale, j.du = dpre;   // (the gradients of no rows, which have no address, of which none is read)
     float* const ws = static_cast<float*>(workspace);
     try {
@@ -163,7 +163,7 @@ int tmps::check_distill(int64_t classes, int64_t k, float temperature, float alp
 
 extern "C" size_t tmps_distill_workspace(int64_t rows, int classes) {
     if (rows < 1 || classes < 1) return 0;
-    return distill_workspace_elems(rows, classes) * sizeof(float);
+    return distill_workspace_elems(rows, rows, classes) * sizeof(float);
 }
 
 extern "C" int tmps_distill(int dtype, const tmps_distill_desc* desc, int64_t rows, const float* logits, const int32_t* labels, int64_t label_stride, const int32_t* ids,
@@ -193,6 +193,7 @@ extern "C" int tmps_distill(int dtype, const tmps_distill_desc* desc, int64_t ro
     Distill d;
     d.logits = logits; d.labels = labels; d.ids = ids; d.teacher = teacher; d.label_stride = label_stride; d.entry_stride = entry_stride; d.rows = rows;
     d.classes = desc->classes; d.k = desc->k; d.temperature = desc->temperature; d.alpha = desc->alpha; d.grad_scale = desc->grad_scale; d.dlogits = dlogits; d.row_loss = row_loss;
+    d.plan_rows = rows;
     ProfileScope scope(kcSoftmaxCE, (hipStream_t)hip_stream);
     TMPS_HIP(distill(dtype, d, static_cast<float*>(workspace), (hipStream_t)hip_stream));
     return TMPS_OK;

@@ -178,7 +178,7 @@ int issue(RunCtx& c, const Node& n) {
         if (n.stage < K - 1 && (rc = c.record(c.fwd_ev(n.stage, (size_t)b0 * N + n.j0 + n.count - 1), s)) != TMPS_OK) return rc;
         if (ends && !loss) {
             ProfileScope scope(kcReduce, s);
-            const int rows = c.M * st->label_rps;
+            const int rows = c.M * st->loss_rps;
             TMPS_HIP(reduce_scaled_sum(stage_row_loss(st, group * N), rows, 1.0f / (float)rows, c.losses_out + b0, s));
         }
     } else {

@@ -68,6 +68,35 @@ static bool on16(std::initializer_list<const void*> all) {
     return (bits & 15) == 0;
 }
 
+static bool is_loss(const LayerRT& L) { return L.d.kind == TMPS_SOFTMAX_CE || L.d.kind == TMPS_DISTILL; }
+
+// The second result that a layer reads (its first where it reads one).
+static int second_source(const LayerRT& L) { return L.d.kind == TMPS_RESADD || L.d.kind == TMPS_NORMJOIN ? L.in_b : L.in_t; }
+
+static float float_of(int32_t bits) {
+    float v;
+    memcpy(&v, &bits, 4);
+    return v;
+}
+
+// Whether layer i is a norm of the same kind over the rows of the norm join before it: one launch with it, in both passes.
+static bool norm_of_join(const tmps_stage& st, int i) {
+    if (i < 1 || i >= (int)st.layers.size()) return false;
+    const LayerRT &N = st.layers[i], &J = st.layers[i - 1];
+    return N.d.kind == TMPS_LAYERNORM && J.d.kind == TMPS_NORMJOIN && N.d.dims[0] == J.d.dims[0] && N.rps == J.rps && N.rms == J.rms;
+}
+
+static Rotary rotary_of(const tmps_layer_desc& d, int samples, const void* x, void* y, bool inverse) {
+    Rotary r;
+    const int S = d.dims[0], D = d.dims[1], heads = d.dims[2];
+    r.x = x; r.y = y; r.x_stride = r.y_stride = 3 * (int64_t)D; r.rows = (int64_t)samples * S;
+    r.heads = 2 * heads; r.copied = heads; r.dh = D / heads;
+    r.pairs[1] = d.dims[5]; r.pairs[2] = d.dims[6]; r.pairs[0] = r.dh / 2 - r.pairs[1] - r.pairs[2];
+    r.flags = d.flags; r.base = d.dims[7] > 0 ? (float)d.dims[7] : 10000.0f; r.inverse = inverse;
+    r.pos = nullptr; r.pos_rows = 0; r.grid_rows = S; r.grid_h = d.dims[3] > 0 ? d.dims[3] : 1; r.grid_w = d.dims[4] > 0 ? d.dims[4] : 1;
+    return r;
+}
+
 // Whether layer i is an affine layer over the channels of the convolution that it reads.  (Layers that follow each other agree in the number of their values
 // only: one may read a result as a map of other channels, and is then a launch of its own.)
 static bool affine_of_conv(const tmps_stage& st, int i) {
@@ -219,10 +248,51 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
                 if (d[0] < 1 || d[1] < 0) return fail(TMPS_EINVAL, "layer %d: bad layer-normalisation dims", i);
                 L.rps = d[1] > 0 ? d[1] : 1;
                 L.in_elems = L.out_elems = (int64_t)L.rps * d[0];
+                L.rms = (L.d.flags & TMPS_FLAG_RMS) != 0;
+                L.w_count = d[0]; L.b_count = L.rms ? 0 : d[0];
+                L.relu = false; L.act = 0;
+                if (L.rms) {
+                    if (!norm_join_part_elems) return fail(TMPS_EUNSUPPORTED, "layer %d: norms without a mean are not built", i);
+                    if (d[0] > kJoinMaxFeatures) return fail(TMPS_EUNSUPPORTED, "layer %d: rows of more than %d features", i, kJoinMaxFeatures);
+                    L.ws_elems = L.part_elems = norm_join_part_elems((int64_t)M * L.rps, d[0]);
+                } else {
+                    L.ws_elems = L.part_elems = layernorm_workspace_elems((int64_t)M * L.rps, d[0]);
+                }
+                break;
+            case TMPS_NORMJOIN:
+                if (d[0] < 1 || d[1] < 0 || d[2] < 2) return fail(TMPS_EINVAL, "layer %d: bad norm-join dims", i);
+                if (!norm_join_part_elems) return fail(TMPS_EUNSUPPORTED, "layer %d: norm joins are not built", i);
+                if (d[0] > kJoinMaxFeatures) return fail(TMPS_EUNSUPPORTED, "layer %d: rows of more than %d features", i, kJoinMaxFeatures);
+                if (L.d.flags & ~(TMPS_FLAG_RMS | TMPS_FLAG_GATE)) return fail(TMPS_EINVAL, "layer %d: unknown flags %d", i, L.d.flags);
+                if (i - d[2] < -1) return fail(TMPS_ESHAPE, "layer %d: the residual's source lies before the stage input", i);
+                L.in_b = i - d[2];
+                if (st.layers[i - 1].act != 0 || (L.in_b >= 0 && st.layers[L.in_b].act != 0))
+                    return fail(TMPS_EUNSUPPORTED, "layer %d: the sources of a norm join must have no activation", i);
+                if (L.in_b < 0 && st.in_esize != st.asz) return fail(TMPS_EUNSUPPORTED, "layer %d: tokens are no residual", i);
+                L.rps = d[1] > 0 ? d[1] : 1;
+                L.rms = (L.d.flags & TMPS_FLAG_RMS) != 0;
+                L.out_elems = (int64_t)L.rps * d[0];
+                L.in_elems = (L.d.flags & TMPS_FLAG_GATE) ? 2 * L.out_elems : L.out_elems;
                 L.w_count = d[0]; L.b_count = d[0];
                 L.relu = false; L.act = 0;
-                L.ws_elems = L.part_elems = layernorm_workspace_elems((int64_t)M * L.rps, d[0]);
+                L.part_elems = norm_join_part_elems((int64_t)M * L.rps, d[0]);
+                L.ws_elems = 2 * L.part_elems;   // (its own and those of the norm behind it)
+                any_join = true;
                 break;
+            case TMPS_ROTARY: {
+                if (d[0] < 1 || d[1] < 1 || d[2] < 1 || d[1] % d[2] != 0 || (d[1] / d[2]) % 2 != 0)
+                    return fail(TMPS_EINVAL, "layer %d: rotary positions need S, D, heads positive and heads of an even number of features", i);
+                if (!rotary) return fail(TMPS_EUNSUPPORTED, "layer %d: rotary positions are not built", i);
+                if (d[3] < 0 || d[4] < 0 || d[5] < 0 || d[6] < 0 || d[7] < 0 || (int64_t)d[5] + d[6] > d[1] / d[2] / 2)
+                    return fail(TMPS_EINVAL, "layer %d: bad grid or pairs of rotary positions", i);
+                if (L.d.flags & ~(TMPS_FLAG_INTERLEAVED | TMPS_FLAG_OWN_LADDERS)) return fail(TMPS_EINVAL, "layer %d: unknown flags %d", i, L.d.flags);
+                if (i > 0 && st.layers[i - 1].act != 0) return fail(TMPS_EUNSUPPORTED, "layer %d: rotary positions must follow a layer without activation", i);
+                if (d[1] > INT32_MAX / 3) return fail(TMPS_EUNSUPPORTED, "layer %d: rows of more than 2^31 features", i);
+                L.rps = d[0];
+                L.in_elems = L.out_elems = (int64_t)d[0] * 3 * d[1];
+                L.relu = false; L.act = 0;
+                break;
+            }
             case TMPS_ATTENTION:
                 if (d[0] < 1 || d[1] < 1 || d[2] < 1 || d[1] % d[2] != 0)
                     return fail(TMPS_EINVAL, "layer %d: attention needs S, D, heads positive and D a multiple of heads", i);
@@ -243,6 +313,7 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
                 st.in_esize = 4;
                 break;
             case TMPS_SOFTMAX_CE:
+            case TMPS_DISTILL:
                 if (i != n_layers - 1 || !cfg->is_last || i == 0)
                     return fail(TMPS_ESHAPE, "softmax-CE must be the last layer of the last stage, after another layer");
                 if (d[0] < 1 || d[1] < 0) return fail(TMPS_EINVAL, "layer %d: classes must be positive", i);
@@ -253,17 +324,28 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
                     return fail(TMPS_ESHAPE, "softmax-CE has %d rows per sample, the layer before it %d", L.rps, st.layers.back().rps);
                 L.in_elems = L.out_elems = (int64_t)L.rps * d[0];
                 L.relu = false; L.act = 0;
-                st.label_rps = L.rps;
+                st.loss_rps = st.label_rps = L.rps;
+                if (L.d.kind == TMPS_DISTILL) {
+                    if (!distill) return fail(TMPS_EUNSUPPORTED, "layer %d: distillation is not built", i);
+                    const int rc = check_distill(d[0], d[2], float_of(d[3]), float_of(d[4]));
+                    if (rc != TMPS_OK) return rc;
+                    if ((int64_t)L.rps * (1 + 2 * (int64_t)d[2]) > INT32_MAX) return fail(TMPS_EUNSUPPORTED, "layer %d: too many labels a sample", i);
+                    st.label_rps = L.rps * (1 + 2 * d[2]);
+                    const int64_t all = (int64_t)M * L.rps;
+                    L.ws_fwd_elems = distill_workspace_elems((int64_t)mb * L.rps, all, d[0]);
+                    for (int r = 1; r <= cfg->n_micro; ++r) L.ws_elems = std::max(L.ws_elems, distill_workspace_elems((int64_t)r * mb * L.rps, all, d[0]));
+                }
                 break;
             default:
                 return fail(TMPS_EUNSUPPORTED, "layer %d: kind %d not built", i, L.d.kind);
         }
         if (i == 0) st.in_elems = L.in_elems;
-        for (int t : {L.in_t, L.d.kind == TMPS_RESADD ? L.in_b : L.in_t}) {
+        for (int t : {L.in_t, second_source(L)}) {
             const int64_t have = t < 0 ? st.in_elems : st.layers[t].out_elems;
-            if (have != L.in_elems)
+            const int64_t want = L.d.kind == TMPS_NORMJOIN && t == L.in_b ? L.out_elems : L.in_elems;
+            if (have != want)
                 return fail(TMPS_ESHAPE, "layer %d expects %lld input elements per sample, its source gives %lld", i,
-                            (long long)L.in_elems, (long long)have);
+                            (long long)want, (long long)have);
         }
         if (L.w_count) {
             L.w_off = poff;
@@ -274,8 +356,8 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
         st.ws_fwd_bytes = std::max(st.ws_fwd_bytes, L.ws_fwd_elems * 4);
         st.layers.push_back(L);
     }
-    if (cfg->is_last && st.layers.back().d.kind != TMPS_SOFTMAX_CE)
-        return fail(TMPS_ESHAPE, "the last stage must end in softmax-CE");
+    if (cfg->is_last && !is_loss(st.layers.back()))
+        return fail(TMPS_ESHAPE, "the last stage must end in softmax-CE or a distillation");
     if (cfg->is_last) st.layers[n_layers - 2].out_f32 = true;
     if (!cfg->is_last) {
         if (st.layers.back().act == 2) return fail(TMPS_EUNSUPPORTED, "a stage cannot end in a GELU layer");
@@ -284,16 +366,32 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
     st.in_elems = st.layers.front().in_elems;
     st.out_elems = cfg->is_last ? st.layers[n_layers - 2].out_elems : st.layers.back().out_elems;
 
+    // how many layers read each result (the backward pass collects one gradient contribution per reader)
+    st.readers.assign(n_layers + 1, 0);
+    for (int i = 0; i < n_layers; ++i) {
+        const LayerRT& L = st.layers[i];
+        if (L.d.kind == TMPS_EMBEDDING) continue;
+        ++st.readers[L.in_t + 1];
+        if (L.d.kind == TMPS_RESADD || L.d.kind == TMPS_NORMJOIN) ++st.readers[L.in_b + 1];
+        if (L.d.kind == TMPS_LINEAR && L.skip) ++st.readers[st.layers[i - L.skip].in_t + 1];
+    }
+
     // stash: [copied inputs] then every layer's output array over all slots, and what else the backward pass needs
     st.in_off = 0;
     if (!cfg->borrow_input) soff = align_up((size_t)rows_all * st.in_elems * st.in_esize, 256);
     for (LayerRT& L : st.layers) {
-        L.out_off = soff;
         L.out_esize = L.out_f32 ? 4 : st.asz;
-        soff = align_up(soff + (size_t)rows_all * L.out_elems * L.out_esize, 256);
+        // (turned where they lie: a dense layer's backward pass reads its input, not its result)
+        L.in_place = L.d.kind == TMPS_ROTARY && L.in_t >= 0 && st.layers[L.in_t].d.kind == TMPS_LINEAR && st.readers[L.in_t + 1] == 1;
+        if (L.in_place) {
+            L.out_off = st.layers[L.in_t].out_off;
+        } else {
+            L.out_off = soff;
+            soff = align_up(soff + (size_t)rows_all * L.out_elems * L.out_esize, 256);
+        }
         size_t aux = 0;
-        if (L.d.kind == TMPS_SOFTMAX_CE) aux = (size_t)rows_all * L.rps * 4;                  // per-row losses
-        if (L.d.kind == TMPS_LAYERNORM) aux = (size_t)rows_all * L.rps * 8;                   // (mean, 1/std) per row
+        if (is_loss(L)) aux = (size_t)rows_all * L.rps * 4;                  // per-row losses
+        if (L.d.kind == TMPS_LAYERNORM || L.d.kind == TMPS_NORMJOIN) aux = (size_t)rows_all * L.rps * 8;                   // (mean, 1/std) per row
         if (L.d.kind == TMPS_ATTENTION) aux = (size_t)rows_all * L.d.dims[2] * L.d.dims[0] * 4;  // log-sum-exp per head and query
         if (L.d.kind == TMPS_MAXPOOL) aux = (size_t)rows_all * L.out_elems * maxpool_winner_bytes(L.d.dims[3]);   // every window's winner
         if (aux) {
@@ -321,6 +419,9 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
         C.part_elems = std::max<size_t>(C.part_elems, slabs * (size_t)(O * I + O));
         st.layers[i].part_elems = std::max<size_t>(st.layers[i].part_elems, slabs * 2 * (size_t)O);
     }
+
+    for (int i = 1; i < n_layers; ++i)   // (a norm behind a join: partial results as the join's)
+        if (norm_of_join(st, i)) st.layers[i].part_elems = std::max(st.layers[i].part_elems, st.layers[i - 1].part_elems);
 
     // Weight gradients that the backward pass leaves to its end, in groups of one launch each.  The gradient of such a layer's
     // result then has to last that long: it gets memory of its own, unless it is the upstream gradient or the loss's.
@@ -351,23 +452,16 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
     if (!cfg->is_last && st.layers.back().relu) gmax = st.layers.back().out_elems;
     for (int i = 1; i < n_layers; ++i) {
         const LayerRT& L = st.layers[i];
-        if (L.d.kind == TMPS_SOFTMAX_CE) continue;
-        for (int t : {L.in_t, L.d.kind == TMPS_RESADD ? L.in_b : L.in_t})
+        if (is_loss(L)) continue;
+        for (int t : {L.in_t, second_source(L)})
             if (t >= 0 && !kept(t)) gmax = std::max(gmax, st.layers[t].out_elems);
+        if (L.d.kind == TMPS_NORMJOIN && st.readers[L.in_t + 1] > 1) gmax = std::max(gmax, L.in_elems);
+        if (L.d.kind == TMPS_NORMJOIN) gmax = std::max(gmax, L.out_elems);   // (the gradient of a residual that is the stage input, until the end of the pass)
     }
 
     // scratch: gradient buffers of M rows, two boundary-gradient buffers, fp32 workspace
     size_t o = 0;
     st.n_gbuf = any_join ? 6 : (any_skip ? 4 : 2);
-    // how many layers read each result (the backward pass collects one gradient contribution per reader)
-    st.readers.assign(n_layers + 1, 0);
-    for (int i = 0; i < n_layers; ++i) {
-        const LayerRT& L = st.layers[i];
-        if (L.d.kind == TMPS_EMBEDDING) continue;
-        ++st.readers[L.in_t + 1];
-        if (L.d.kind == TMPS_RESADD) ++st.readers[L.in_b + 1];
-        if (L.d.kind == TMPS_LINEAR && L.skip) ++st.readers[st.layers[i - L.skip].in_t + 1];
-    }
     st.gbuf_bytes = align_up((size_t)M * std::max<int64_t>(gmax, 1) * st.asz, 256);
     for (int k = 0; k < st.n_gbuf; ++k) { st.gbuf_off[k] = o; o += st.gbuf_bytes; }
     st.dxout_bytes = align_up((size_t)M * st.in_elems * st.asz, 256);
@@ -378,6 +472,8 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
             st.layers[i].keep_off = o;   // (not 0: the gradient buffers come first)
             o += align_up((size_t)M * st.layers[i].out_elems * st.asz, 256);
         }
+    for (LayerRT& L : st.layers)   // (the gradient of a result turned in place is where that of the result below it is kept)
+        if (L.in_place) L.keep_off = st.layers[L.in_t].keep_off;
     // (larger ones had better be added up while the caches hold them)
     for (LayerRT& L : st.layers) {
         if (L.grouped || L.part_elems * 4 > kLatePartBytes) L.part_elems = 0;
@@ -596,7 +692,8 @@ int tmps::forward_with_workspace(tmps_stage* st, int slot, int count, const void
     const tmps_stage::GraphKey key = {1 + 2 * ((uintptr_t)count + 128 * (uintptr_t)before), (uintptr_t)slot, (uintptr_t)x0, (uintptr_t)labels, (uintptr_t)loss_out, (uintptr_t)ws,
                                       (uintptr_t)st->master, (uintptr_t)st->wcopy};
     // (asked of a whole mini-batch's rows: all of its passes then run the same kernel, however they are cut)
-    const bool small_loss = st->cfg.is_last && softmax_ce_small_takes((int64_t)st->M() * st->label_rps, st->layers.back().d.dims[0]);
+    const bool small_loss = st->cfg.is_last && st->layers.back().d.kind == TMPS_SOFTMAX_CE &&
+                            softmax_ce_small_takes((int64_t)st->M() * st->loss_rps, st->layers.back().d.dims[0]);
     float* const y_by_loss = small_loss && !st->use_graphs ? static_cast<float*>(y) : nullptr;
     // The result for the next worker leaves the kernel that forms it in two places, where that is a contraction (a copy afterwards reads it once more: 1.5 MB
     // 3.4 us, 20 MB of logits 8.4, 13 MB 5.1).  Not into what the pass still reads, and not from a captured graph, whose addresses are fixed.
@@ -616,6 +713,7 @@ int tmps::forward_with_workspace(tmps_stage* st, int slot, int count, const void
         if (!st->layers[li].skip) return nullptr;
         return src == 0 ? x0 : (const void*)st->out_ptr(st->layers[src - 1], row0);
     };
+    auto row_stats = [&](const LayerRT& L) { return reinterpret_cast<float*>(st->stash + L.aux_off) + (size_t)row0 * L.rps * 2; };
     const int rc = run_or_replay(st, key, s, [&]() -> int {
     for (size_t li = 0; li < st->layers.size(); ++li) {
         const LayerRT& L = st->layers[li];
@@ -683,8 +781,30 @@ int tmps::forward_with_workspace(tmps_stage* st, int slot, int count, const void
             case TMPS_AVGPOOL:
                 TMPS_GEMM(avgpool_forward(dt, in, out, mb, d[0] * d[1], d[2], s));
                 break;
+            case TMPS_NORMJOIN: {
+                NormJoin j{};
+                j.x = in; j.r = L.in_b < 0 ? x0 : (const void*)st->out_ptr(st->layers[L.in_b], row0);
+                j.gain = st->master + L.w_off; j.scale = st->master + L.b_off; j.y = out; j.stats = row_stats(L);
+                j.stats_stride = 2; j.rows = (int64_t)mb * L.rps; j.D = d[0]; j.rms = L.rms; j.gate = (L.d.flags & TMPS_FLAG_GATE) != 0;
+                if (norm_of_join(*st, (int)li + 1)) {
+                    const LayerRT& F = st->layers[++li];
+                    j.pre_gain = st->master + F.w_off; j.pre_shift = F.rms ? nullptr : st->master + F.b_off; j.u = st->out_ptr(F, row0); j.pre_stats = row_stats(F);
+                }
+                TMPS_GEMM(norm_join_forward(dt, j, s));
+                break;
+            }
+            case TMPS_ROTARY:
+                TMPS_GEMM(rotary(dt, rotary_of(L.d, mb, in, out, false), s));
+                break;
             case TMPS_LAYERNORM: {
-                float* stats = reinterpret_cast<float*>(st->stash + L.aux_off) + (size_t)row0 * L.rps * 2;
+                float* stats = row_stats(L);
+                if (L.rms) {
+                    NormJoin j{};
+                    j.y = const_cast<void*>(in); j.pre_gain = st->master + L.w_off; j.u = out; j.pre_stats = stats; j.stats_stride = 2;
+                    j.rows = (int64_t)mb * L.rps; j.D = d[0]; j.rms = true;
+                    TMPS_GEMM(norm_join_forward(dt, j, s));
+                    break;
+                }
                 if (li + 1 < st->layers.size() && st->layers[li + 1].d.kind == TMPS_LINEAR && st->layers[li + 1].rps == L.rps &&
                     norm_dense_takes(dt, (int64_t)mb * L.rps, d[0], st->layers[li + 1].d.dims[1])) {
                     const LayerRT& F = st->layers[++li];
@@ -705,6 +825,18 @@ int tmps::forward_with_workspace(tmps_stage* st, int slot, int count, const void
                 TMPS_GEMM(embedding_forward(dt, (const int32_t*)in, st->wptr(L), st->bptr_c(L), out, (int64_t)mb * d[1], d[1],
                                             d[2], d[0], s));
                 break;
+            case TMPS_DISTILL: {
+                const int64_t rows = (int64_t)mb * L.rps, rows_before = (int64_t)before * st->cfg.micro_batch * L.rps, all = rows_before + rows;
+                float* rl = stage_row_loss(st, slot - before);
+                Distill q;
+                q.logits = (const float*)in; q.labels = labels; q.ids = labels + 1; q.teacher = reinterpret_cast<const float*>(labels + 1 + d[2]);
+                q.label_stride = q.entry_stride = 1 + 2 * (int64_t)d[2]; q.rows = rows; q.classes = d[0]; q.k = d[2];
+                q.temperature = float_of(d[3]); q.alpha = float_of(d[4]); q.grad_scale = 1.0f / ((float)st->M() * (float)L.rps);
+                q.dlogits = out; q.row_loss = rl + rows_before; q.plan_rows = (int64_t)st->M() * L.rps;
+                TMPS_RUN(kcSoftmaxCE, s, distill(dt, q, ws, s));
+                if (loss_out) TMPS_RUN(kcReduce, s, reduce_scaled_sum(rl, (int)all, 1.0f / (float)all, loss_out, s));
+                break;
+            }
             case TMPS_SOFTMAX_CE: {
                 const int rows = mb * L.rps, rows_before = before * st->cfg.micro_batch * L.rps, all = rows_before + rows;
                 float* rl = stage_row_loss(st, slot - before);   // (of the rows before, then this pass's)
@@ -736,7 +868,7 @@ extern "C" int tmps_backward(tmps_stage* st, const int* slots, int n_slots, cons
 bool tmps::can_mask_dx(const tmps_stage& st) {
     bool reads = false;
     for (const LayerRT& L : st.layers) {
-        const bool first = L.in_t < 0, joins = L.d.kind == TMPS_RESADD && L.in_b < 0;
+        const bool first = L.in_t < 0, joins = (L.d.kind == TMPS_RESADD || L.d.kind == TMPS_NORMJOIN) && L.in_b < 0;
         if (joins || (first && L.d.kind != TMPS_LINEAR && L.d.kind != TMPS_CONV2D)) return false;
         reads = reads || first;
         // (a residual connection from the stage input starts at a layer normalisation, which is no such reader)
@@ -950,6 +1082,57 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     };
     auto strided_is_last = [&]() { return strided.li >= 0 && remaining[st->layers[strided.li].in_t + 1] == 1; };
 
+    auto row_stats = [&](const LayerRT& L) { return reinterpret_cast<const float*>(st->stash + L.aux_off) + (size_t)row0 * L.rps * 2; };
+    // The norm join ji: dy its result's gradient without the norm behind it (may not be set), du that norm's (not set: no such norm).
+    auto join_backward = [&](int ji, const Grad& dy_, const Grad& du_) -> int {
+        const LayerRT& J = st->layers[ji];
+        Target X, R;
+        int rc = target(J.in_t, X);
+        if (rc != TMPS_OK) return rc;
+        const int beside = X.add ? take() : -1;   // (others have given that result a gradient: this one's is added behind the launch)
+        if (X.add && beside < 0) return fail(TMPS_EUNSUPPORTED, "out of gradient buffers (too many open residual connections)");
+        if (J.in_b < 0 && dx && in_order) {
+            // (dx may be what later kernels still read: the residual's gradient waits in memory of the pass)
+            const Grad& G = grads[0];
+            R.wanted = true;
+            R.add = G.set ? G.ptr : nullptr;
+            if ((R.buf = take()) < 0) return fail(TMPS_EUNSUPPORTED, "out of gradient buffers (too many open residual connections)");
+            R.dst = gbuf[R.buf];
+        } else if ((rc = target(J.in_b, R)) != TMPS_OK) {
+            return rc;
+        }
+        NormJoinBackward j{};
+        j.dy = dy_.set ? dy_.ptr : nullptr;
+        j.x = st->out_ptr(st->layers[J.in_t], row0);
+        j.r = J.in_b < 0 ? (const void*)x0 : (const void*)st->out_ptr(st->layers[J.in_b], row0);
+        j.y = st->out_ptr(J, row0); j.stats = row_stats(J); j.gain = st->master + J.w_off; j.scale = st->master + J.b_off;
+        j.add = R.add; j.dx = X.add ? gbuf[beside] : X.dst; j.dr = R.wanted ? R.dst : nullptr; j.dgain_dscale = st->grad + J.w_off;
+        j.stats_stride = 2; j.rows = (int64_t)M * J.rps; j.D = J.d.dims[0]; j.rms = J.rms; j.gate = (J.d.flags & TMPS_FLAG_GATE) != 0;
+        Partials of_pre(nullptr);
+        if (du_.set) {
+            const LayerRT& F = st->layers[ji + 1];
+            j.du = du_.ptr; j.pre_stats = row_stats(F); j.pre_gain = st->master + F.w_off; j.dpre = st->grad + F.w_off;
+            of_pre = partials(F);
+            if (!of_pre.later) of_pre.ws = ws + norm_join_part_elems(j.rows, j.D);   // (the workspace's first half may be the join's)
+        }
+        TMPS_GEMM(norm_join_backward(dt, j, partials(J), of_pre, s));
+        if (X.add) {
+            TMPS_GEMM(resadd_forward(dt, X.add, gbuf[beside], X.dst, (int64_t)M * J.in_elems, 0, s));
+            release(beside);
+        }
+        commit(J.in_t, X);
+        if (R.wanted) {
+            commit(J.in_b, R);
+            grads[J.in_b + 1].masked = false;
+        }
+        if (du_.set) {
+            --remaining[ji + 1];
+            release(dy_.set ? dy_.buf : -1);
+            grads[ji + 1].set = false;
+        }
+        return TMPS_OK;
+    };
+
     int top = nl - 1;
     if (st->cfg.is_last) {
         // the loss layer's contribution to the logits: the softmax error signal stored by the forward passes
@@ -1082,8 +1265,44 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
                 if ((rc = share(L.in_b, g)) != TMPS_OK) return rc;
                 if ((rc = share(t_in, g)) != TMPS_OK) return rc;
                 break;
+            case TMPS_NORMJOIN:
+                if ((rc = join_backward(li, g, Grad())) != TMPS_OK) return rc;
+                break;
+            case TMPS_ROTARY: {
+                // turned back where it lies, where that is memory of the pass
+                Grad& G = grads[t_in + 1];
+                if (t_in >= 0 && !G.set && g.buf >= 0 && refs[g.buf] == 1) {
+                    TMPS_GEMM(rotary(dt, rotary_of(L.d, M, g.ptr, gbuf[g.buf], true), s));
+                    G = g;
+                    ++refs[g.buf];
+                    --remaining[t_in + 1];
+                    break;
+                }
+                if ((rc = target(t_in, T)) != TMPS_OK) return rc;
+                if (!T.wanted) break;
+                if (T.add) return fail(TMPS_EUNSUPPORTED, "rotary positions on a shared input");
+                const size_t bytes = (size_t)M * L.in_elems * st->asz;
+                if (T.dst != g.ptr && overlap(T.dst, bytes, g.ptr, bytes)) return fail(TMPS_EINVAL, "dx overlaps dy without being dy");
+                TMPS_GEMM(rotary(dt, rotary_of(L.d, M, g.ptr, T.dst, true), s));
+                commit(t_in, T);
+                break;
+            }
             case TMPS_LAYERNORM:
+                if (norm_of_join(*st, li) && remaining[li] == 1) {   // with the join below, whose result's gradient is complete with this one's
+                    if ((rc = join_backward(li - 1, grads[li], g)) != TMPS_OK) return rc;
+                    with_below = 1;
+                    break;
+                }
                 if (mask) return fail(TMPS_EUNSUPPORTED, "layer normalisation directly after an activation");
+                if (L.rms) {
+                    if ((rc = target(t_in, T)) != TMPS_OK) return rc;
+                    NormJoinBackward j{};
+                    j.dy = T.add; j.du = g.ptr; j.y = in; j.pre_stats = row_stats(L); j.pre_gain = st->master + L.w_off; j.dr = T.wanted ? T.dst : nullptr; j.dpre = gw;
+                    j.stats_stride = 2; j.rows = (int64_t)M * L.rps; j.D = d[0]; j.rms = true;
+                    TMPS_GEMM(norm_join_backward(dt, j, Partials(nullptr), partials(L), s));
+                    if (T.wanted) commit(t_in, T);
+                    break;
+                }
                 if ((rc = target(t_in, T)) != TMPS_OK) return rc;
                 TMPS_GEMM(layernorm_backward(dt, g.ptr, in, reinterpret_cast<const float*>(st->stash + L.aux_off) + (size_t)row0 * L.rps * 2,
                                              st->master + L.w_off, T.add, T.wanted ? T.dst : nullptr, gw, partials(L), (int64_t)M * L.rps,

@@ -22,7 +22,9 @@ struct LayerRT {
     int rps = 1;           // rows per sample the layer works on (sequence positions)
     int skip = 0;          // linear: > 0 adds the input of layer (index - skip)
     int in_t = -1;         // which result the layer reads: index of the producing layer, -1 = the stage input
-    int in_b = -1;         // residual join: the second result it reads
+    int in_b = -1;         // residual join, norm join: the second result it reads
+    bool rms = false;      // a norm without a mean
+    bool in_place = false; // rotary positions: the result is where the layer before left its own, which nobody else reads
     bool out_f32 = false;  // the logits layer (followed by softmax-CE) writes fp32
     bool grouped = false;  // linear: its weight gradient waits for the end of the backward pass, to be one launch with others'
     size_t keep_off = 0;   // scratch byte offset of the gradient of its result, kept until then (0: memory that lasts anyway)
@@ -39,7 +41,8 @@ struct tmps_stage {
     int64_t in_elems = 0, out_elems = 0;
     size_t asz = 4;  // bytes per activation / gradient element
     size_t in_esize = 4;  // bytes per element of the stage input (int32 tokens in front of an embedding)
-    int label_rps = 1;    // labels per sample on the last stage
+    int loss_rps = 1;     // rows per sample of the loss on the last stage
+    int label_rps = 1;    // int32 labels per sample there (a distillation's rows have several)
     int n_gbuf = 2;       // gradient buffers in scratch
     int max_run = 1;      // micro-batches that one forward pass can cover (tensors within the convolutions' index range)
     std::vector<int> readers;  // readers[t + 1] = number of layers that read result t (t = -1: the stage input)

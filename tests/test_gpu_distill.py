@@ -14,6 +14,16 @@ DEV = "cuda:0"
 STEP = 2.0 ** -24
 
 
+@pytest.fixture(autouse=True)
+def single_precision_by_default():
+    """(tests of the oracle leave their process at doubles)"""
+    import torch
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def problem(rows, C, k, seed=0, spread=2.0, repeated=False):
     gen = torch.Generator().manual_seed(seed)
     z = spread * torch.randn(rows, C, generator=gen)

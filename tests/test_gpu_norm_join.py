@@ -17,6 +17,16 @@ STEP = 2.0 ** -24
 WIDTHS = [1, 2, 7, 8, 63, 64, 65, 200, 256, 511, 512, 520, 768, 1000, 1024, 1025, 1032, 2040, 2048, 2049, 4096, 4100, 5003, 8192, 8200, 16384]
 
 
+@pytest.fixture(autouse=True)
+def single_precision_by_default():
+    """(tests of the oracle leave their process at doubles)"""
+    import torch
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def norm_parts(v, rms):
     m = np.zeros((len(v), 1)) if rms else v.mean(1, keepdims=True)
     i = 1.0 / np.sqrt(((v - m) ** 2).mean(1, keepdims=True) + 1e-5)

@@ -13,6 +13,16 @@ DEV = "cuda:0"
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
+@pytest.fixture(autouse=True)
+def single_precision_by_default():
+    """(tests of the oracle leave their process at doubles)"""
+    import torch
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 def turned(x, pos, heads, dh, pairs, base, interleaved, own, inverse):
     """x, pos: numpy, rows of heads of dh features; 64 bits."""
     n, out = sum(pairs), x.astype(np.float64).reshape(len(x), heads, dh).copy()

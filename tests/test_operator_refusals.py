@@ -92,7 +92,8 @@ def test_distill_refuses(kw, code):
 
 def test_the_binding_refuses():
     """Shapes, types, layouts and places, before the library is asked."""
-    f = torch.zeros
+    def f(*shape, dtype=torch.float32):
+        return torch.zeros(*shape, dtype=dtype)
     x, pos = f(4, 128), f(4, 3, dtype=torch.int32)
     for bad in (lambda: tmps.rotary(x, pos, 2, 64, (32, 0, 0)), lambda: tmps.rotary(x.double(), pos, 2, 64, (32, 0, 0)), lambda: tmps.rotary(x.t(), pos, 1, 4, (2, 0, 0)),
                 lambda: tmps.rotary(x, pos.long(), 2, 64, (32, 0, 0)), lambda: tmps.rotary(x, pos[:, :2], 2, 64, (32, 0, 0)), lambda: tmps.rotary(x, pos, 3, 64, (32, 0, 0)),

@@ -17,13 +17,41 @@ def linear(din, dout, relu, act=None, rows=1, skip=0):
             "rows": int(rows), "skip": int(skip)}
 
 
-def layernorm(d, rows=1, eps=1e-5):
-    return {"kind": "layernorm", "d": int(d), "rows": int(rows), "eps": float(eps)}
+def layernorm(d, rows=1, eps=1e-5, rms=False):
+    """rms: without a mean and without a shift, x / sqrt(mean(x^2) + eps) times the gain."""
+    return {"kind": "layernorm", "d": int(d), "rows": int(rows), "eps": float(eps), "rms": bool(rms)}
+
+
+def norm_join(d, rows, src, rms=False, gate=False):
+    """scale * r + g * gain * norm(f): f is the result of the layer before (with gate rows [f | a], g = sigmoid(a)), r that of the layer src >= 2
+    positions before (one position before the first layer of a stage is the stage input); parameters gain (w) and scale (b), [d]."""
+    return {"kind": "norm_join", "d": int(d), "rows": int(rows), "src": int(src), "rms": bool(rms), "gate": bool(gate)}
+
+
+def rotary(s, d, heads, height=1, width=1, pairs_h=0, pairs_w=0, base=10000, interleaved=False, own_ladders=False):
+    """Rotary positions on packed [s, 3d] = (q | k | v) rows: row (t * height + h) * width + w has the positions (t, h, w); pairs_h and pairs_w of a head's
+    d / heads / 2 pairs turn with h and w, the others, which come first, with t."""
+    return {"kind": "rotary", "s": int(s), "d": int(d), "heads": int(heads), "height": int(height), "width": int(width), "pairs_h": int(pairs_h),
+            "pairs_w": int(pairs_w), "base": int(base), "interleaved": bool(interleaved), "own_ladders": bool(own_ladders)}
+
+
+def distill(classes, rows=1, k=1, temperature=1.0, alpha=1.0):
+    """Loss against a teacher's k largest logits a row, in the place of softmax_ce; labels are records of 1 + 2k int32 a row (label, ids, bits of the
+    teacher's logits)."""
+    return {"kind": "distill", "classes": int(classes), "rows": int(rows), "k": int(k), "temperature": float(temperature), "alpha": float(alpha)}
 
 
 def attention(s, d, heads):
     """Causal multi-head self-attention on packed [s, 3d] = (q | k | v) rows; output [s, d]."""
     return {"kind": "attention", "s": int(s), "d": int(d), "heads": int(heads)}
+
+
+def gated_block(s, d, heads, ffn, rms=True, **positions):
+    """Block between norms: n = norm(x); x = scale x + g gain norm([f | a] = proj(attn(rotary(qkv(n))))), then the same around fc2(gelu(fc1(norm(x)))).
+    positions: as rotary's."""
+    return [layernorm(d, s, rms=rms), linear(d, 3 * d, False, rows=s), rotary(s, d, heads, **positions), attention(s, d, heads),
+            linear(d, 2 * d, False, rows=s), norm_join(d, s, 6, rms=rms, gate=True),
+            layernorm(d, s, rms=rms), linear(d, ffn, False, act="gelu", rows=s), linear(ffn, 2 * d, False, rows=s), norm_join(d, s, 4, rms=rms, gate=True)]
 
 
 def embedding(vocab, s, d):
@@ -238,8 +266,10 @@ def layer_out_shape(layer, in_shape):
     k = layer["kind"]
     if k == "linear":
         return (layer["dout"],) if layer.get("rows", 1) == 1 else (layer["rows"], layer["dout"])
-    if k == "layernorm":
+    if k in ("layernorm", "rotary"):
         return tuple(in_shape)
+    if k == "norm_join":
+        return (layer["d"],) if layer["rows"] == 1 else (layer["rows"], layer["d"])
     if k == "attention":
         return (layer["s"], layer["d"])
     if k == "embedding":
@@ -256,7 +286,7 @@ def layer_out_shape(layer, in_shape):
         return (layer["h"], layer["w"], layer["c"])
     if k == "avgpool":
         return (layer["c"],)
-    if k == "softmax_ce":
+    if k in ("softmax_ce", "distill"):
         return (layer["classes"],) if layer.get("rows", 1) == 1 else (layer["rows"], layer["classes"])
     raise ValueError(k)
 

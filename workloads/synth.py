@@ -39,6 +39,10 @@ def param_shapes(layer):
         return {"w": (layer["dout"], layer["din"]), "b": (layer["dout"],)}
     if layer["kind"] == "conv":
         return {"w": (layer["cout"], layer["r"], layer["s"], layer["cin"]), "b": (layer["cout"],)}
+    if layer["kind"] == "layernorm" and layer.get("rms"):   # w = gain
+        return {"w": (layer["d"],)}
+    if layer["kind"] == "norm_join":      # w = gain, b = scale of the residual
+        return {"w": (layer["d"],), "b": (layer["d"],)}
     if layer["kind"] == "layernorm":      # w = gain, b = shift
         return {"w": (layer["d"],), "b": (layer["d"],)}
     if layer["kind"] == "affine":         # w = gain, b = shift, per channel
@@ -57,7 +61,9 @@ def init_params(cfg, bias_std=0.0):
         for layer in st:
             shp = param_shapes(layer)
             p = {}
-            if shp and layer["kind"] in ("layernorm", "affine"):
+            if shp and (layer["kind"] == "norm_join" or layer.get("rms")):
+                p = {k: np.ones(v, dtype=np.float32) for k, v in shp.items()}
+            elif shp and layer["kind"] in ("layernorm", "affine"):
                 g = _rng(cfg.seed, 1, idx)
                 p["w"] = np.full(shp["w"], layer.get("init_gain", 1.0), dtype=np.float32)
                 p["b"] = np.zeros(shp["b"], dtype=np.float32)
