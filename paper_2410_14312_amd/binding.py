@@ -261,45 +261,60 @@ def stage_bytes(specs, cfg):
 
 
 # ------------------------------------------------------------------------------------ operators on their own
+def _torch():
+    global _torch_of
+    if _torch_of is None:
+        import torch
+        _torch_of = torch
+    return _torch_of
+
+
+_torch_of = None
+
+
 def _dtype_code(t):
-    import torch
-    codes = {torch.float32: TMPS_F32, torch.bfloat16: TMPS_BF16_F32MASTER}
-    if t.dtype not in codes:
-        raise ValueError("%s: the library computes in float32 and bfloat16" % t.dtype)
-    return codes[t.dtype]
+    torch = _torch()
+    if t.dtype is torch.float32:
+        return TMPS_F32
+    if t.dtype is torch.bfloat16:
+        return TMPS_BF16_F32MASTER
+    raise ValueError("%s: the library computes in float32 and bfloat16" % t.dtype)
 
 
 def _operand(name, t, shape, dtype, device):
     """A tensor's address, after a check of what it is (rows contiguous); None stays None."""
     if t is None:
         return None
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError("%s: a contiguous %s tensor of shape %s on %s is wanted, not %s %s on %s"
-                         % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
-    return t.data_ptr()
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.device == device:
+        return t.data_ptr()
+    raise ValueError("%s: a contiguous %s tensor of shape %s on %s is wanted, not %s %s on %s"
+                     % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
 
 def _call(fn, device, stream, *args):
     """fn(..., stream) on a GPU's current stream, or on `stream`, with that GPU current."""
-    import torch
+    torch = _torch()
+    cuda = torch.cuda
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are wanted, not on %s" % device)
-    if stream is None:
-        handle = torch.cuda.current_stream(device).cuda_stream
+    if stream is None:   # (current_stream(device).cuda_stream without the object: 0.1 us instead of 1.9)
+        handle = torch._C._cuda_getCurrentRawStream(device.index)
     else:
         handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, handle))
+    if device.index == cuda.current_device():
+        rc = fn(*args, handle)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, handle))
+        with cuda.device(device):
+            rc = fn(*args, handle)
+    if rc < 0:
+        _check(rc)
 
 
 def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_ladders=False, inverse=False, out=None, stream=None):
     """Rotary positions (tmps_rotary) of the `heads` heads of dh features that begin each row of x [rows, features]: pairs = (time, height, width)
     pairs of features that turn with each axis of positions, int32 [n, 3], which the rows take in turn.  inverse: back, the gradient's way.
     out (default: a new tensor [rows, heads * dh]) may be x, or a view of rows of its own stride.  Returns out."""
-    import torch
+    torch = _torch()
     code, width = _dtype_code(x), heads * dh
     if x.dim() != 2 or x.shape[1] < width or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("x: rows of at least %d neighbouring features are wanted, not shape %s, strides %s" % (width, tuple(x.shape), x.stride()))
@@ -314,7 +329,7 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
     elif out.dim() != 2 or out.shape[0] != rows or out.shape[1] < width or (out.shape[1] > 1 and out.stride(1) != 1) or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("out: %d rows of at least %d neighbouring %s features on %s are wanted" % (rows, width, x.dtype, x.device))
     d = RotaryDesc(heads, dh, (C.c_int32 * 3)(*pairs), _rotary_flags(interleaved, own_ladders), base)
-    _call(lib().tmps_rotary, x.device, stream, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
+    _call(load_library().tmps_rotary, x.device, stream, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
     return out
 
 
@@ -326,7 +341,7 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
     """y = scale r + g gain n(f), u = n(y) pre_gain + pre_shift over rows of r [rows, D] (tmps_norm_join_forward): x holds f, with `gate` rows [f | a] with
     g = 1 / (1 + exp(-a)); n is layer normalisation, with `rms` without its mean (then without pre_shift); without pre_gain u is None.  Returns
     (y, u, stats); y may be given as r."""
-    import torch
+    torch = _torch()
     code = _dtype_code(r)
     if r.dim() != 2:
         raise ValueError("r: [rows, features] is wanted, not %s" % (tuple(r.shape),))
@@ -337,7 +352,7 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
         u = torch.empty(rows, D, dtype=t, device=dev)
     if stats is None:
         stats = torch.empty(rows, 4, dtype=torch.float32, device=dev)
-    _call(lib().tmps_norm_join_forward, dev, stream, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
+    _call(load_library().tmps_norm_join_forward, dev, stream, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
           _operand("r", r, (rows, D), t, dev), _operand("gain", gain, (D,), torch.float32, dev), _operand("scale", scale, (D,), torch.float32, dev),
           _operand("y", y, (rows, D), t, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev),
           _operand("pre_shift", pre_shift, (D,), torch.float32, dev), _operand("u", u, (rows, D), t, dev),
@@ -348,7 +363,7 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
 def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=False, gate=False, dx=None, dr=None, stream=None):
     """Gradients of norm_join from dy and du (one of them may be None; with du also y and pre_gain are needed): (dx, dr, dgain, dscale, dpre_gain,
     dpre_shift), those of parameters fp32, the last two None without du, the last with `rms`.  dr may be given as dy."""
-    import torch
+    torch = _torch()
     code = _dtype_code(r)
     if r.dim() != 2:
         raise ValueError("r: [rows, features] is wanted, not %s" % (tuple(r.shape),))
@@ -359,22 +374,25 @@ def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=F
     if dr is None:
         dr = torch.empty(rows, D, dtype=t, device=dev)
     grads = torch.empty(4, D, dtype=torch.float32, device=dev)
-    need = lib().tmps_norm_join_workspace(rows, D)
+    need = load_library().tmps_norm_join_workspace(rows, D)
     ws = torch.empty(max(need, 4), dtype=torch.uint8, device=dev)
     at = grads.data_ptr()
-    _call(lib().tmps_norm_join_backward, dev, stream, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
+    _call(load_library().tmps_norm_join_backward, dev, stream, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
           _operand("x", x, (rows, wide), t, dev), _operand("r", r, (rows, D), t, dev), _operand("y", y, (rows, D), t, dev),
           _operand("stats", stats, (rows, 4), torch.float32, dev), _operand("gain", gain, (D,), torch.float32, dev),
           _operand("scale", scale, (D,), torch.float32, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev), _operand("dx", dx, (rows, wide), t, dev),
           _operand("dr", dr, (rows, D), t, dev), at, at + 8 * D if du is not None else None, ws.data_ptr(), need)
-    return dx, dr, grads[0], grads[1], grads[2] if du is not None else None, grads[3] if du is not None and not rms else None
+    dgain, dscale, dpre_gain, dpre_shift = grads.unbind(0)
+    if du is None:
+        return dx, dr, dgain, dscale, None, None
+    return dx, dr, dgain, dscale, dpre_gain, None if rms else dpre_shift
 
 
 def distill(logits, labels, ids, teacher, temperature=1.0, alpha=1.0, grad_scale=None, dtype="f32", gradient=True, stream=None):
     """Distillation loss of each row of fp32 logits [rows, classes] against a teacher's logits [rows, k] of the classes ids (int32 [rows, k], -1: no entry)
     and labels (int32 [rows], -1: none; may be None), with its gradient times grad_scale (default: 1 / rows, for the mean) in `dtype` (tmps_distill).
     Returns (row_loss, dlogits); dlogits is None without `gradient`."""
-    import torch
+    torch = _torch()
     if logits.dim() != 2 or ids.dim() != 2:
         raise ValueError("logits: [rows, classes], ids: [rows, k] are wanted")
     if dtype not in ("f32", "bf16"):
@@ -383,9 +401,9 @@ def distill(logits, labels, ids, teacher, temperature=1.0, alpha=1.0, grad_scale
     row_loss = torch.empty(rows, dtype=torch.float32, device=dev)
     dlogits = torch.empty(rows, classes, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device=dev) if gradient else None
     d = DistillDesc(classes, k, temperature, alpha, 1.0 / max(rows, 1) if grad_scale is None else grad_scale)
-    need = lib().tmps_distill_workspace(rows, classes)
+    need = load_library().tmps_distill_workspace(rows, classes)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(lib().tmps_distill, dev, stream, TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, C.byref(d), rows,
+    _call(load_library().tmps_distill, dev, stream, TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, C.byref(d), rows,
           _operand("logits", logits, (rows, classes), torch.float32, dev), _operand("labels", labels, (rows,), torch.int32, dev), 1,
           _operand("ids", ids, (rows, k), torch.int32, dev), _operand("teacher", teacher, (rows, k), torch.float32, dev), k,
           dlogits.data_ptr() if gradient else None, row_loss.data_ptr(), ws.data_ptr() if need else None, need)
