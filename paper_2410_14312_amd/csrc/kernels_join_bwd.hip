@@ -3,21 +3,29 @@
 //   dr = scale dh (+ what others have given r);  da = dh gain fh g (1 - g);  v = dh g gain, df = i1 (v - mean(v) - fh mean(v fh))
 //   dpre_gain = sum du yh, dpre_shift = sum du, dscale = sum dh r, dgain = sum dh g fh over the rows
 // One pass over memory: dy, du, x, r, y are read and dx, dr written once each.  A team goes over its share of the rows and keeps its sums over them in registers, which
-// leave as one row of partial results; those are added up in a fixed order behind.
+// leave as one row of partial results; those are added up in a fixed order behind.  In bf16, with the norm, both launches (us; a copy of as many bytes at 5.1 TB/s): 8192 x 768
+// 25.8 (17.4) and gated 33.5 (22.4), 8192 x 2048 51 (46), 16384 x 4096 177 (186), 8192 x 8192 204 (186); in fp32 4096 x 1024 gated 36.5 (30).  What short rows lack are waves: a
+// SIMD's registers hold two or three.  Rows of more than 8192 features spill (2048 x 16384: 312, 57).
 #include "launch.h"
 #include "norm_join.hip.h"
 
 namespace tmps {
 
-constexpr int kBwdGroups = 512;
+// Threads of a launch at most: two waves to a SIMD, which is what its registers hold, each with its next row under way.
+constexpr int kBwdThreads = 131072;
 
-template <typename T, int TEAM, int V, int N, bool JOIN, bool PRE, bool GATE>
+// NEXT (8192 x 768 gated 31.3 us without, 28.0 with; 16384 x 4096 197 and 171): a row's operands are requested as soon as those of the row before are taken, in two parts: what the norm of y needs, and what comes behind its sums.  (Workgroups of
+// 1024 threads have no registers for that, nor, with two pieces a thread, for parameters.)
+template <typename T, int TEAM, int N, bool WHOLE, bool JOIN, bool PRE, bool GATE>
 __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(NormJoinBackward a, float* part, float* part_pre) {
-    __shared__ float red[2][4 * 16];
-    __shared__ float fold[Team<TEAM>::kRows > 1 ? Team<TEAM>::kRows : 1][Team<TEAM>::kRows > 1 ? TEAM * V * N : 1];
+    constexpr int kRows = Team<TEAM>::kRows, V = kPiece<T>;
+    constexpr bool KEEP = N * V == 8, NEXT = KEEP && TEAM < 1024;
+    __shared__ float red[2][2 * 16];
+    __shared__ float fold[kRows > 1 ? kRows : 1][kRows > 1 ? TEAM * V * N : 1];
     const int D = a.D;
     constexpr int wide = GATE ? 2 : 1;
     const float over_d = 1.0f / (float)D;
+    const Pieces<TEAM, N, V, WHOLE> p{D};
     int place = 0;
     float dgain[JOIN ? N : 1][V], dscale[JOIN ? N : 1][V], dpg[PRE ? N : 1][V], dps[PRE ? N : 1][V];
 #pragma unroll
@@ -27,108 +35,144 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
             if constexpr (JOIN) dgain[i][e] = dscale[i][e] = 0.0f;
             if constexpr (PRE) dpg[i][e] = dps[i][e] = 0.0f;
         }
-    float gain[JOIN ? N : 1][V], scale[JOIN ? N : 1][V], pre_gain[PRE ? N : 1][V];
-    if constexpr (JOIN) {
-        load_vector<TEAM, V, N>(gain, a.gain, D);
-        load_vector<TEAM, V, N>(scale, a.scale, D);
+    float gain[KEEP ? N : 1][V], scale[KEEP ? N : 1][V], pre_gain[KEEP ? N : 1][V];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (JOIN) {
+                load_vector(gain[i], a.gain, p, i);
+                load_vector(scale[i], a.scale, p, i);
+            }
+            if constexpr (PRE) load_vector(pre_gain[i], a.pre_gain, p, i);
+        }
     }
-    if constexpr (PRE) load_vector<TEAM, V, N>(pre_gain, a.pre_gain, D);
-    const int64_t step = (int64_t)gridDim.x * Team<TEAM>::kRows;
-    for (int64_t row = (int64_t)blockIdx.x * Team<TEAM>::kRows + threadIdx.x / TEAM; row < a.rows; row += step) {
-        RawPiece<T, V> rdy[N], rdu[PRE ? N : 1], ry[PRE ? N : 1], rf[JOIN ? N : 1], ra[GATE ? N : 1], rr[JOIN ? N : 1], radd[JOIN ? N : 1];
-        const bool has_dy = !PRE || a.dy;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TEAM;
+    uint4 rdy[N], rdu[PRE ? N : 1], ry[PRE ? N : 1], rf[JOIN ? N : 1], ra[GATE ? N : 1], rr[JOIN ? N : 1], radd[JOIN ? N : 1];
+    float st[2], pre_st[2];
+    const bool has_dy = !PRE || a.dy;
+    auto request_first = [&](int64_t at) {
         if constexpr (PRE) {
-            request_row<T, TEAM, V, N>(rdu, (const T*)a.du + row * D, D);
-            request_row<T, TEAM, V, N>(ry, (const T*)a.y + row * D, D);
+            request_row(rdu, (const T*)a.du + at * D, p);
+            request_row(ry, (const T*)a.y + at * D, p);
+            pre_st[0] = a.pre_stats[at * a.stats_stride];
+            pre_st[1] = a.pre_stats[at * a.stats_stride + 1];
         }
-        if (has_dy) request_row<T, TEAM, V, N>(rdy, (const T*)a.dy + row * D, D);
+        if (has_dy) request_row(rdy, (const T*)a.dy + at * D, p);
+    };
+    auto request_second = [&](int64_t at) {
         if constexpr (JOIN) {
-            request_row<T, TEAM, V, N>(rf, (const T*)a.x + row * D * wide, D);
-            request_row<T, TEAM, V, N>(rr, (const T*)a.r + row * D, D);
-            if constexpr (GATE) request_row<T, TEAM, V, N>(ra, (const T*)a.x + row * D * wide + D, D);
-            if (a.add) request_row<T, TEAM, V, N>(radd, (const T*)a.add + row * D, D);
+            request_row(rf, (const T*)a.x + at * D * wide, p);
+            request_row(rr, (const T*)a.r + at * D, p);
+            if constexpr (GATE) request_row(ra, (const T*)a.x + at * D * wide + D, p);
+            if (a.add) request_row(radd, (const T*)a.add + at * D, p);
+            st[0] = a.stats[at * a.stats_stride];
+            st[1] = a.stats[at * a.stats_stride + 1];
         }
-        float dh[N][V];
+    };
+    if (NEXT && row < a.rows) {
+        request_first(row);
+        request_second(row);
+    }
+    for (; row < a.rows; row += step) {
+        const bool more = NEXT && row + step < a.rows;
+        if constexpr (!NEXT) {
+            request_first(row);
+            request_second(row);
+        }
+        float dh[N][V], dy[N][V];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) dy[i][e] = 0.0f;
+            if (has_dy) unpack(rdy[i], dy[i]);
+        }
         if constexpr (PRE) {
-            const float mean = a.pre_stats[row * a.stats_stride], rstd = a.pre_stats[row * a.stats_stride + 1];
+            const float mean = pre_st[0], rstd = pre_st[1];
             float yh[N][V], s[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (join_column<TEAM, V>(i) >= D) continue;
+                if (!p.any(i)) continue;
                 float du[V];
-                rdu[i].get(du);
-                ry[i].get(yh[i]);
+                if constexpr (!KEEP) load_vector(pre_gain[0], a.pre_gain, p, i);
+                unpack(rdu[i], du);
+                unpack(ry[i], yh[i]);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     yh[i][e] = (yh[i][e] - mean) * rstd;
-                    dh[i][e] = du[e] * pre_gain[i][e];
-                    s[0] = fmaf(dh[i][e], yh[i][e], s[0]);
-                    s[1] += dh[i][e];
+                    dh[i][e] = du[e] * pre_gain[KEEP ? i : 0][e];
+                    const float t = p.own(i, e) ? dh[i][e] : 0.0f;
+                    s[0] = fmaf(t, yh[i][e], s[0]);
+                    s[1] += t;
                     dpg[i][e] = fmaf(du[e], yh[i][e], dpg[i][e]);
                     dps[i][e] += du[e];
                 }
             }
+            if (more) request_first(row + step);
             Team<TEAM>::sums(s, red, place);
             const float m = a.rms ? 0.0f : s[1] * over_d, q = s[0] * over_d;
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (join_column<TEAM, V>(i) < D) {
+                if (p.any(i)) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) dh[i][e] = rstd * fmaf(-yh[i][e], q, dh[i][e] - m);
+                    for (int e = 0; e < V; ++e) dh[i][e] = fmaf(rstd, fmaf(-yh[i][e], q, dh[i][e] - m), dy[i][e]);
                 }
-        }
-        if (has_dy) {
+        } else {
+            if (more) request_first(row + step);
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (join_column<TEAM, V>(i) < D) {
-                    float dy[V];
-                    rdy[i].get(dy);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) dh[i][e] = PRE ? dh[i][e] + dy[e] : dy[e];
-                }
+                for (int e = 0; e < V; ++e) dh[i][e] = dy[i][e];
         }
         if constexpr (JOIN) {
-            const float mean = a.stats[row * a.stats_stride], rstd = a.stats[row * a.stats_stride + 1];
+            const float mean = st[0], rstd = st[1];
             T* const dxr = (T*)a.dx + row * D * wide;
-            float fh[N][V], s[2] = {0.0f, 0.0f};
+            float fh[N][V], r_[N][V], at_[GATE ? N : 1][V], add_[N][V], s[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int c = join_column<TEAM, V>(i);
-                if (c >= D) continue;
-                float r[V], o[V];
-                rf[i].get(fh[i]);
-                rr[i].get(r);
+                unpack(rf[i], fh[i]);
+                unpack(rr[i], r_[i]);
+                if constexpr (GATE) unpack(ra[i], at_[i]);
+                if (a.add) unpack(radd[i], add_[i]);
+            }
+            if (more) request_second(row + step);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (!p.any(i)) continue;
+                if constexpr (!KEEP) {
+                    load_vector(gain[0], a.gain, p, i);
+                    load_vector(scale[0], a.scale, p, i);
+                }
+                float o[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     fh[i][e] = (fh[i][e] - mean) * rstd;
-                    dscale[i][e] = fmaf(dh[i][e], r[e], dscale[i][e]);
-                    o[e] = dh[i][e] * scale[i][e];
+                    dscale[i][e] = fmaf(dh[i][e], r_[i][e], dscale[i][e]);
+                    o[e] = dh[i][e] * scale[KEEP ? i : 0][e];
                 }
                 if (a.add) {
-                    float b[V];
-                    radd[i].get(b);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) o[e] += b[e];
+                    for (int e = 0; e < V; ++e) o[e] += add_[i][e];
                 }
-                if (a.dr) store_piece<V>((T*)a.dr + row * D + c, o);
+                if (a.dr) store_piece((T*)a.dr + row * D, p, i, o);
                 if constexpr (GATE) {
-                    float at[V], da[V];
-                    ra[i].get(at);
+                    float da[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         float sg, rest;
-                        gate_of<T>(at[e], sg, rest);
-                        da[e] = dh[i][e] * gain[i][e] * fh[i][e] * (sg * rest);
+                        gate_of<T>(at_[i][e], sg, rest);
+                        da[e] = dh[i][e] * gain[KEEP ? i : 0][e] * fh[i][e] * (sg * rest);
                         dh[i][e] *= sg;
                     }
-                    if (a.dx) store_piece<V>(dxr + D + c, da);
+                    if (a.dx) store_piece(dxr + D, p, i, da);
                 }
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     dgain[i][e] = fmaf(dh[i][e], fh[i][e], dgain[i][e]);
-                    dh[i][e] *= gain[i][e];
-                    s[0] = fmaf(dh[i][e], fh[i][e], s[0]);
-                    s[1] += dh[i][e];
+                    dh[i][e] *= gain[KEEP ? i : 0][e];
+                    const float t = p.own(i, e) ? dh[i][e] : 0.0f;
+                    s[0] = fmaf(t, fh[i][e], s[0]);
+                    s[1] += t;
                 }
             }
             if (a.dx) {
@@ -136,40 +180,44 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
                 const float m = a.rms ? 0.0f : s[1] * over_d, q = s[0] * over_d;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int c = join_column<TEAM, V>(i);
-                    if (c >= D) continue;
+                    if (!p.any(i)) continue;
                     float o[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) o[e] = rstd * fmaf(-fh[i][e], q, dh[i][e] - m);
-                    store_piece<V>(dxr + c, o);
+                    store_piece(dxr, p, i, o);
                 }
             }
         } else if (a.dr) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = join_column<TEAM, V>(i);
-                if (c < D) store_piece<V>((T*)a.dr + row * D + c, dh[i]);
-            }
+            for (int i = 0; i < N; ++i) store_piece((T*)a.dr + row * D, p, i, dh[i]);
         }
     }
-    // The workgroup's row of partial results; its waves' sums, where they are teams of their own, are added up through LDS.
+    // The workgroup's row of partial results; its teams' sums, where it has several, are added up through LDS.
     auto leave = [&](const float (&v)[N][V], float* to) {
-        if constexpr (Team<TEAM>::kRows > 1) {
+        if constexpr (kRows > 1) {
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < N; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) fold[threadIdx.x / TEAM][join_column<TEAM, V>(i) + e] = v[i][e];
+                for (int e = 0; e < V; ++e)
+                    if (p.any(i) && p.own(i, e)) fold[threadIdx.x / TEAM][p.at(i) + e] = v[i][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < D; c += Team<TEAM>::kThreads) to[c] = (fold[0][c] + fold[1][c]) + (fold[2][c] + fold[3][c]);
+            for (int c = threadIdx.x; c < D; c += Team<TEAM>::kThreads) {
+                float t[kRows];
+#pragma unroll
+                for (int k = 0; k < kRows; ++k) t[k] = fold[k][c];
+#pragma unroll
+                for (int h = kRows / 2; h > 0; h >>= 1)
+#pragma unroll
+                    for (int k = 0; k < h; ++k) t[k] += t[k + h];
+                to[c] = t[0];
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = join_column<TEAM, V>(i);
-                if (c >= D) continue;
+            for (int i = 0; i < N; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) to[c + e] = v[i][e];
-            }
+                for (int e = 0; e < V; ++e)
+                    if (p.any(i) && p.own(i, e)) to[p.at(i) + e] = v[i][e];
         }
     };
     if constexpr (JOIN) {
@@ -183,20 +231,31 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
     }
 }
 
-// Workgroups of the launch: enough to fill the device, and few enough that their partial results are little beside the rows.
-static int bwd_groups(int64_t rows, int teams) {
-    const int64_t groups = (rows + teams - 1) / teams;
-    return (int)(groups < kBwdGroups ? groups : kBwdGroups);
+// The team that takes rows of D features, and the launch's workgroups: no more than the device holds at a time, and as many rows to each.
+static int bwd_team(int D, bool whole) {
+    if (D <= 128) return 16;
+    if (D <= 256 && whole) return 32;
+    if (D <= 512) return 64;
+    if (D <= 1024) return 128;
+    if (D <= 2048) return 256;
+    return D <= 4096 ? 512 : 1024;
+}
+static int bwd_groups(int64_t rows, int team) {
+    const int threads = team <= 64 ? 256 : team, teams = threads / team, most = (team == 1024 ? 2 : 1) * kBwdThreads / threads;
+    const int64_t groups = (rows + teams - 1) / teams, each = (groups + most - 1) / most;
+    return (int)((groups + each - 1) / each);
 }
 
-// (any kernel's: the one whose teams are workgroups)
-size_t norm_join_part_elems(int64_t rows, int D) { return (size_t)bwd_groups(rows, 1) * 2 * (size_t)D; }
+size_t norm_join_part_elems(int64_t rows, int D) {
+    const int a = bwd_groups(rows, bwd_team(D, true)), b = bwd_groups(rows, bwd_team(D, false));
+    return (size_t)(a > b ? a : b) * 2 * (size_t)D;
+}
 
-template <typename T, int TEAM, int V, int N> static hipError_t bwd_launch(const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s) {
-    const int groups = bwd_groups(j.rows, Team<TEAM>::kRows);
-    auto kern = !j.x ? norm_join_bwd_kernel<T, TEAM, V, N, false, true, false>
-                : !j.du ? (j.gate ? norm_join_bwd_kernel<T, TEAM, V, N, true, false, true> : norm_join_bwd_kernel<T, TEAM, V, N, true, false, false>)
-                        : (j.gate ? norm_join_bwd_kernel<T, TEAM, V, N, true, true, true> : norm_join_bwd_kernel<T, TEAM, V, N, true, true, false>);
+template <typename T, int TEAM, int N, bool WHOLE> static hipError_t bwd_launch(const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s) {
+    const int groups = bwd_groups(j.rows, TEAM);
+    auto kern = !j.x ? norm_join_bwd_kernel<T, TEAM, N, WHOLE, false, true, false>
+                : !j.du ? (j.gate ? norm_join_bwd_kernel<T, TEAM, N, WHOLE, true, false, true> : norm_join_bwd_kernel<T, TEAM, N, WHOLE, true, false, false>)
+                        : (j.gate ? norm_join_bwd_kernel<T, TEAM, N, WHOLE, true, true, true> : norm_join_bwd_kernel<T, TEAM, N, WHOLE, true, true, false>);
     hipError_t e = launch_timed(kcLayerNorm, kern, dim3(groups), dim3(Team<TEAM>::kThreads), 0, s, j, part.ws, part_pre.ws);
     if (e != hipSuccess) return e;
     const Reduction of_join{part.ws, j.dgain_dscale, 2 * (int64_t)j.D, groups, true}, of_pre{part_pre.ws, j.dpre, (j.rms ? 1 : 2) * (int64_t)j.D, groups, true};
@@ -206,19 +265,17 @@ template <typename T, int TEAM, int V, int N> static hipError_t bwd_launch(const
 }
 
 template <typename T> static hipError_t bwd_type(const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s) {
-    if (join_wide(j.D, {j.dy, j.du, j.x, j.r, j.y, j.gain, j.scale, j.pre_gain, j.add, j.dx, j.dr})) {
-        if (j.D <= 512) return bwd_launch<T, 64, 8, 1>(j, part, part_pre, s);
-        if (j.D <= 1024) return bwd_launch<T, 64, 8, 2>(j, part, part_pre, s);
-        if (j.D <= 2048) return bwd_launch<T, 256, 8, 1>(j, part, part_pre, s);
-        if (j.D <= 4096) return bwd_launch<T, 256, 8, 2>(j, part, part_pre, s);
-        if (j.D <= 8192) return bwd_launch<T, 1024, 8, 1>(j, part, part_pre, s);
-        return bwd_launch<T, 1024, 8, 2>(j, part, part_pre, s);
+    const bool whole = join_whole<T>(j.D, {j.dy, j.du, j.x, j.r, j.y, j.gain, j.scale, j.pre_gain, j.add, j.dx, j.dr});
+    switch (bwd_team(j.D, whole)) {
+        case 16: return whole ? bwd_launch<T, 16, kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 16, kOne<T>, false>(j, part, part_pre, s);
+        case 32: return bwd_launch<T, 32, kOne<T>, true>(j, part, part_pre, s);
+        case 64: return whole ? bwd_launch<T, 64, kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 64, kOne<T>, false>(j, part, part_pre, s);
+        case 128: return whole ? bwd_launch<T, 128, kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 128, kOne<T>, false>(j, part, part_pre, s);
+        case 256: return whole ? bwd_launch<T, 256, kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 256, kOne<T>, false>(j, part, part_pre, s);
+        case 512: return whole ? bwd_launch<T, 512, kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 512, kOne<T>, false>(j, part, part_pre, s);
     }
-    if (j.D <= 64) return bwd_launch<T, 64, 1, 1>(j, part, part_pre, s);
-    if (j.D <= 256) return bwd_launch<T, 64, 1, 4>(j, part, part_pre, s);
-    if (j.D <= 1024) return bwd_launch<T, 256, 1, 4>(j, part, part_pre, s);
-    if (j.D <= 4096) return bwd_launch<T, 1024, 1, 4>(j, part, part_pre, s);
-    return bwd_launch<T, 1024, 1, 16>(j, part, part_pre, s);
+    if (j.D <= 8192) return whole ? bwd_launch<T, 1024, kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 1024, kOne<T>, false>(j, part, part_pre, s);
+    return whole ? bwd_launch<T, 1024, 2 * kOne<T>, true>(j, part, part_pre, s) : bwd_launch<T, 1024, 2 * kOne<T>, false>(j, part, part_pre, s);
 }
 
 // Sums over no rows.

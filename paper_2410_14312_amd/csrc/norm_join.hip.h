@@ -1,4 +1,4 @@
-// What the forward and the backward kernel of norm joins share: a row held in the registers of a team of threads, V neighbouring features N times a thread.
+// What the forward and the backward kernel of norm joins share: a row held in the registers of a team of threads, 16 bytes of neighbouring features N times a thread.
 #pragma once
 #include <initializer_list>
 
@@ -11,16 +11,28 @@
 
 namespace tmps {
 
-// A team is a wave, of which a workgroup has four, or a whole workgroup.
+// A team is 16, 32 or 64 lanes of a wave, in workgroups of four waves, or a whole workgroup.
 template <int TEAM> struct Team {
-    static constexpr int kThreads = TEAM < 256 ? 256 : TEAM;
+    static constexpr int kThreads = TEAM <= 64 ? 256 : TEAM;
     static constexpr int kRows = kThreads / TEAM;   // teams of a workgroup
-    static constexpr int kWaves = TEAM / 64;
+    static constexpr int kWaves = TEAM <= 64 ? 1 : TEAM / 64;
+    static __device__ __forceinline__ float lanes_sum(float v) {
+        if constexpr (TEAM >= 64) return wsum(v);
+        if constexpr (TEAM == 32) {
+            const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+        }
+        v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false));   // row_ror:8
+        v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xF, 0xF, false));   // row_ror:4
+        v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xF, 0xF, false));   // row_ror:2
+        v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xF, 0xF, false));   // row_ror:1
+        return v;
+    }
     // Sums of K values over the team, the same in every thread.  red: K kWaves floats in LDS for each of two alternating places, so that one barrier a sum is enough: who
     // writes a place again has passed the barrier of the sum between, which nobody reaches before reading this one.
-    template <int K> static __device__ __forceinline__ void sums(float (&v)[K], float (*red)[4 * 16], int& place) {
+    template <int K> static __device__ __forceinline__ void sums(float (&v)[K], float (*red)[2 * 16], int& place) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[k] = wsum(v[k]);
+        for (int k = 0; k < K; ++k) v[k] = lanes_sum(v[k]);
         if constexpr (kWaves > 1) {
             const int wave = threadIdx.x >> 6;
             if ((threadIdx.x & 63) == 0) {
@@ -40,57 +52,110 @@ template <int TEAM> struct Team {
     }
 };
 
-// Features of piece i of a thread begin at column(i); all of them are inside the row, or none.
-template <int TEAM, int V> __device__ __forceinline__ int join_column(int i) { return ((int)(threadIdx.x % TEAM) + TEAM * i) * V; }
+// A piece: V neighbouring features, 16 bytes.
+template <typename T> constexpr int kPiece = 16 / sizeof(T);
+template <typename T> constexpr int kOne = 8 / kPiece<T>;   // pieces of 8 features
 
-// A piece as it lies in memory: requested for the next row while this one is worked on, converted when its turn comes.
-template <typename T, int V> struct RawPiece;
-template <typename T> struct RawPiece<T, 8> : Raw8<T> {};
-template <typename T> struct RawPiece<T, 1> {
-    T v;
-    __device__ __forceinline__ void load(const T* p) { v = p[0]; }
-    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(v); }
+// The pieces of a thread in every row.  WHOLE: all of the launch's pieces are on 16 bytes, and inside a row or behind it.  Otherwise they are 16 bytes at any address, which the
+// memory unit takes in a request or two, and the piece that a row ends in begins as much earlier as it would reach beyond: its first features are also the piece's before it, which
+// has them for its own.  (Loads of the last features one by one would have to be put together, and so waited for, where they are requested: 8000 x 1003 in bf16, backward, 52 us
+// instead of 35.)  A row of fewer features than a piece is one that is put together all the same.
+template <int TEAM, int N, int V, bool WHOLE> struct Pieces {
+    int D;
+    __device__ __forceinline__ int column(int i) const { return ((int)(threadIdx.x % TEAM) + TEAM * i) * V; }   // the first feature of its own
+    __device__ __forceinline__ bool any(int i) const { return column(i) < D; }
+    __device__ __forceinline__ int at(int i) const { return WHOLE ? column(i) : min(column(i), max(D - V, 0)); }   // the first feature it holds
+    __device__ __forceinline__ bool own(int i, int e) const { return WHOLE || (at(i) + e >= column(i) && (D >= V || e < D)); }   // (of a piece that has any)
 };
-template <typename T, int TEAM, int V, int N> __device__ __forceinline__ void request_row(RawPiece<T, V> (&r)[N], const void* row, int D) {
+
+typedef uint32_t any_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
+
+// 16 bytes of a row from feature c on, as they lie in memory: requested for the next row while this one is worked on, unpacked when their turn comes.
+template <bool WHOLE, typename T> __device__ __forceinline__ void request16(uint4& u, const T* row, int c, int D) {
+    if constexpr (WHOLE) {
+        u = *reinterpret_cast<const uint4*>(row + c);
+    } else if (c + kPiece<T> <= D) {
+        const any_u32x4_t v = *reinterpret_cast<const any_u32x4_t*>(row + c);
+        u = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+        struct Features { T v[kPiece<T>]; } f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = join_column<TEAM, V>(i);
-        if (c < D) r[i].load((const T*)row + c);
+        for (int e = 0; e < kPiece<T>; ++e) f.v[e] = c + e < D ? row[c + e] : T(0.0f);
+        u = __builtin_bit_cast(uint4, f);
     }
 }
-template <int V, typename T> __device__ __forceinline__ void load_piece(const T* p, float (&v)[V]) {
-    if constexpr (V == 8) load8(p, v);
-    else v[0] = to_f32(p[0]);
+template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void request_row(uint4 (&u)[N], const T* row, const Pieces<TEAM, N, V, WHOLE>& p) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (p.any(i)) request16<WHOLE>(u[i], row, p.at(i), p.D);
 }
-template <int V, typename T> __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
-    if constexpr (V == 8) store8(p, v);
-    else p[0] = from_f32<T>(v[0]);
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+        v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[4]) {
+    const float4 f = __builtin_bit_cast(float4, u);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+}
+// (rounded to bf16 in pairs: one conversion makes two values in the halves of a register)
+__device__ __forceinline__ uint4 pack(const float (&v)[8]) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{v[2 * e], v[2 * e + 1]}), bf16x2_t));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 pack(const float (&v)[4]) { return __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3])); }
+
+// The features of piece i that are its own.
+template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void store_packed(T* row, const Pieces<TEAM, N, V, WHOLE>& p, int i, const uint4& u) {
+    if (!p.any(i)) return;
+    if constexpr (WHOLE) {
+        *reinterpret_cast<uint4*>(row + p.at(i)) = u;
+    } else if (p.column(i) + V <= p.D) {
+        *reinterpret_cast<any_u32x4_t*>(row + p.at(i)) = any_u32x4_t{u.x, u.y, u.z, u.w};
+    } else {
+        struct Features { T v[V]; } f = __builtin_bit_cast(Features, u);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (p.own(i, e)) row[p.at(i) + e] = f.v[e];
+    }
+}
+template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void store_piece(T* row, const Pieces<TEAM, N, V, WHOLE>& p, int i, const float (&v)[V]) {
+    store_packed(row, p, i, pack(v));
 }
 
-// A parameter's values of a thread's features (0 behind the row's end).
-template <int TEAM, int V, int N> __device__ __forceinline__ void load_vector(float (&v)[N][V], const float* p, int D) {
+// A parameter's values of piece i (zeros where it has none).
+template <int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void load_vector(float (&v)[V], const float* from, const Pieces<TEAM, N, V, WHOLE>& p, int i) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = join_column<TEAM, V>(i);
+    for (int h = 0; h < V; h += 4) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        float f[4];
+        if (from && p.any(i)) request16<WHOLE>(u, from, p.at(i) + h, p.D);
+        unpack(u, f);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
-        if (c < D) load_piece<V>(p + c, v[i]);
+        for (int e = 0; e < 4; ++e) v[h + e] = f[e];
     }
 }
 
-// A gate and one minus it, each to its own last places (the difference of large a would lose them).  The hardware's exponential is off by |a| 2^-24: enough for results
-// of 8 bits, not for fp32.
+// A gate and one minus it, each to its own last places (the difference of large a would lose them).  The hardware's exponential is off by |a| 2^-24 and its reciprocal by a step:
+// enough for results of 8 bits, not for fp32.
 template <typename T> __device__ __forceinline__ void gate_of(float a, float& g, float& rest) {
     const float e = sizeof(T) == 2 ? __expf(-a) : expf(-a);
-    g = 1.0f / (1.0f + e);
+    g = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
     rest = a < 0.0f ? 1.0f - g : e * g;
 }
 
-// Whether rows can be taken in pieces of 8 features: all of them on 16 bytes.
-inline bool join_wide(int D, std::initializer_list<const void*> all) {
+// Whether all of a launch's pieces are on 16 bytes.
+template <typename T> bool join_whole(int D, std::initializer_list<const void*> all) {
     uintptr_t bits = 0;
     for (const void* p : all) bits |= reinterpret_cast<uintptr_t>(p);
-    return D % 8 == 0 && (bits & 15) == 0;
+    return D % kPiece<T> == 0 && (bits & 15) == 0;
 }
 
 }  // namespace tmps
