@@ -2,8 +2,8 @@
 #pragma once
 #include <initializer_list>
 
-#include "gemm.hip.h"
 #include "kernels.h"
+#include "pieces.hip.h"
 #include "wave.hip.h"
 
 // Products and sums are fused where fmaf says so and nowhere else: a row's results are then the same bit for bit whatever else its launch forms.
@@ -52,8 +52,6 @@ template <int TEAM> struct Team {
     }
 };
 
-// A piece: V neighbouring features, 16 bytes.
-template <typename T> constexpr int kPiece = 16 / sizeof(T);
 template <typename T> constexpr int kOne = 8 / kPiece<T>;   // pieces of 8 features
 
 // The pieces of a thread in every row.  WHOLE: all of the launch's pieces are on 16 bytes, and inside a row or behind it.  Otherwise they are 16 bytes at any address, which the
@@ -68,15 +66,12 @@ template <int TEAM, int N, int V, bool WHOLE> struct Pieces {
     __device__ __forceinline__ bool own(int i, int e) const { return WHOLE || (at(i) + e >= column(i) && (D >= V || e < D)); }   // (of a piece that has any)
 };
 
-typedef uint32_t any_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
-
 // 16 bytes of a row from feature c on, as they lie in memory: requested for the next row while this one is worked on, unpacked when their turn comes.
 template <bool WHOLE, typename T> __device__ __forceinline__ void request16(uint4& u, const T* row, int c, int D) {
     if constexpr (WHOLE) {
         u = *reinterpret_cast<const uint4*>(row + c);
     } else if (c + kPiece<T> <= D) {
-        const any_u32x4_t v = *reinterpret_cast<const any_u32x4_t*>(row + c);
-        u = make_uint4(v[0], v[1], v[2], v[3]);
+        u = load16_any(row + c);
     } else {
         struct Features { T v[kPiece<T>]; } f;
 #pragma unroll
@@ -89,36 +84,13 @@ template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinli
     for (int i = 0; i < N; ++i)
         if (p.any(i)) request16<WHOLE>(u[i], row, p.at(i), p.D);
 }
-__device__ __forceinline__ void unpack(const uint4& u, float (&v)[8]) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
-        v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void unpack(const uint4& u, float (&v)[4]) {
-    const float4 f = __builtin_bit_cast(float4, u);
-    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-}
-// (rounded to bf16 in pairs: one conversion makes two values in the halves of a register)
-__device__ __forceinline__ uint4 pack(const float (&v)[8]) {
-    typedef float f32x2_t __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{v[2 * e], v[2 * e + 1]}), bf16x2_t));
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ uint4 pack(const float (&v)[4]) { return __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3])); }
-
 // The features of piece i that are its own.
 template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void store_packed(T* row, const Pieces<TEAM, N, V, WHOLE>& p, int i, const uint4& u) {
     if (!p.any(i)) return;
     if constexpr (WHOLE) {
         *reinterpret_cast<uint4*>(row + p.at(i)) = u;
     } else if (p.column(i) + V <= p.D) {
-        *reinterpret_cast<any_u32x4_t*>(row + p.at(i)) = any_u32x4_t{u.x, u.y, u.z, u.w};
+        store16_any(row + p.at(i), u);
     } else {
         struct Features { T v[V]; } f = __builtin_bit_cast(Features, u);
 #pragma unroll

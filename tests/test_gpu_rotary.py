@@ -61,7 +61,8 @@ def base_of(base):
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("rows,heads,dh,pairs,own", [(1, 1, 2, (1, 0, 0), False), (1, 24, 64, (32, 0, 0), False), (5, 3, 7, (1, 1, 1), True), (33, 4, 64, (8, 12, 12), False),
                                                       (130, 5, 48, (8, 8, 8), True), (17, 2, 80, (0, 16, 16), True), (9, 3, 36, (2, 0, 5), False), (64, 40, 128, (16, 24, 24), False),
-                                                      (300, 1, 256, (128, 0, 0), False), (257, 2, 16, (0, 0, 8), True), (3, 130, 40, (20, 0, 0), False), (7, 2, 513, (3, 250, 1), True)])
+                                                      (300, 1, 256, (128, 0, 0), False), (257, 2, 16, (0, 0, 8), True), (3, 130, 40, (20, 0, 0), False), (7, 2, 513, (3, 250, 1), True), (3, 2, 1024, (256, 100, 155), False), (3, 1, 1016, (200, 200, 107), True),
+                                                      (40, 3, 24, (4, 3, 4), False), (11, 7, 22, (11, 0, 0), False)])
 def test_turns(dtype, interleaved, rows, heads, dh, pairs, own):
     x, pos = make(rows, heads * dh, dtype, seed=rows + dh)
     for inverse in (False, True):
