@@ -315,7 +315,7 @@ int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D, const voi
                             const float* stats, const float* gain, const float* scale, const float* pre_gain, void* dx, void* dr, float* dgain_dscale,
                             float* dpre, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Distillation from a teacher's k <= 1024 largest logits: with q = softmax(z / T), T = temperature, and p the softmax of the row's teacher entries over T,
+/* Distillation from a teacher's k <= 1024 largest logits of at most 2^23 classes: with q = softmax(z / T), T = temperature, and p the softmax of the row's teacher entries over T,
  *   loss = alpha T^2 sum_j p_j (log p_j - log q[id_j]) + (1 - alpha) (-log softmax(z)[label])
  * row_loss receives each row's, dlogits (may be NULL; gradient dtype) grad_scale times its gradient w.r.t. the row's fp32 logits z.  ids and teacher hold k entries a row,
  * entry_stride elements apart from row to row, labels (NULL: none) one a row, label_stride apart.  An id of -1 is no entry (its logit is not looked at), a label

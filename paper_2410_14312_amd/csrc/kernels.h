@@ -255,7 +255,7 @@ hipError_t softmax_ce_small(int dtype, const float* logits, const int32_t* label
 // dlogits (may be null) = grad_scale times its gradient.  ids, teacher, labels: entry_stride and label_stride elements from row to row; an id or label of -1 is none
 // (a row without entries or label lacks that term, without both its loss and gradient are 0 whatever its logits), any other outside the classes a NaN loss.
 // Repeated ids add up.  labels may be null.  ws: distill_workspace_elems of these rows and those of the plan.
-constexpr int kDistillMaxEntries = 1024;
+constexpr int kDistillMaxEntries = 1024, kDistillMaxClasses = 1 << 23;
 struct Distill {
     const float* logits;
     const int32_t *labels, *ids;

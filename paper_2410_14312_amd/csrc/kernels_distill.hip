@@ -3,162 +3,329 @@
 //   loss = alpha T^2 sum_j p_j (log p_j - log q[id_j]) + (1 - alpha) (-log s[label])
 //   d loss / dz = alpha T (q - sum_j p_j e[id_j]) + (1 - alpha) (s - e[label])
 // Bound by memory: a row of logits is read, a row of gradients written.
-#include "gemm.hip.h"
 #include "kernels.h"
+#include "pieces.hip.h"
 #include "wave.hip.h"
 
 namespace tmps {
 
-// The sum and maximum over a workgroup, the same in every thread; red: a float per wave.
-template <int THREADS> __device__ __forceinline__ float block_sum(float v, float* red) {
-    v = wsum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float t = red[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) t += red[w];
-    return t;
-}
-template <int THREADS> __device__ __forceinline__ float block_max(float v, float* red) {
-    v = wmax(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float t = red[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) t = fmaxf(t, red[w]);
-    return t;
-}
+// What a launch does with its rows: all of it, or one of two launches over slices of rows: the slices' largest logits and sums, and everything else.
+enum { kWholeRows = 0, kSliceSums = 1, kSliceRest = 2 };
 
-// A row's teacher: entries in LDS, their probabilities, and what the row has to learn from.
-struct RowTeacher {
-    bool taught, labelled, bad;   // bad: an id or label that is neither a class nor -1
-    int label;
-    float log_norm;               // of the teacher's logits over T
+// How rows are cut: `slices` of `length` logits each (the last may be shorter).
+struct Slices {
+    int slices, length;
 };
 
-// ids: the entries' classes (-1: none); t: their logits over T; p: their probabilities.  Every thread of the workgroup takes part.
-template <int THREADS> __device__ __forceinline__ RowTeacher read_teacher(const Distill& d, int64_t row, int* ids, float* t, float* p, float* red) {
-    RowTeacher w;
-    w.label = d.labels && d.alpha < 1.0f ? d.labels[row * d.label_stride] : -1;
-    w.labelled = w.label >= 0 && w.label < d.classes;
-    w.bad = !w.labelled && w.label != -1;
-    w.taught = false;
-    w.log_norm = 0.0f;
-    if (d.alpha <= 0.0f) return w;
-    const float over_t = 1.0f / d.temperature;
-    float mx = -INFINITY, wrong = 0.0f;
-    for (int j = threadIdx.x; j < d.k; j += THREADS) {
-        const int id = d.ids[row * d.entry_stride + j];
-        const bool entry = id >= 0 && id < d.classes;
-        wrong = entry || id == -1 ? wrong : 1.0f;
-        const float v = entry ? d.teacher[row * d.entry_stride + j] * over_t : -INFINITY;
-        ids[j] = entry ? id : -1;
-        t[j] = v;
-        mx = v > mx || v != v ? v : mx;
+// A team's reductions, the result in every thread: one barrier each, by alternating between two places in LDS (who writes a place again has passed the barrier between).  Teams
+// of a wave need neither.
+template <int TEAM> struct Reduce {
+    static constexpr int kWaves = TEAM / 64;
+    float (*red)[3 * 16];
+    int place = 0;
+    // v[0], or with MAX the largest v[0] (NaN is passed over), and the sums of the others
+    template <bool MAX, int K> __device__ __forceinline__ void all(float (&v)[K]) {
+        v[0] = MAX ? wmax(v[0]) : wsum(v[0]);
+#pragma unroll
+        for (int k = 1; k < K; ++k) v[k] = wsum(v[k]);
+        if constexpr (kWaves > 1) {
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) red[place][k * 16 + (threadIdx.x >> 6)] = v[k];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = red[place][k * 16];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) {
+                    const float o = red[place][k * 16 + w];
+                    v[k] = MAX && k == 0 ? fmaxf(v[k], o) : v[k] + o;
+                }
+            }
+            place ^= 1;
+        }
     }
-    w.bad |= block_max<THREADS>(wrong, red) > 0.0f;
-    mx = block_max<THREADS>(mx, red);
-    w.taught = mx != -INFINITY;
-    if (!w.taught) return w;
-    float sum = 0.0f;
-    for (int j = threadIdx.x; j < d.k; j += THREADS) {
-        p[j] = ids[j] >= 0 ? expf(t[j] - mx) : 0.0f;
-        sum += p[j];
+};
+
+// What a team's lanes have written to LDS or memory is there for the others.  (A wave's operations on either complete in order; the compiler is kept from moving them.)
+template <int TEAM> __device__ __forceinline__ void team_sync() {
+    if constexpr (TEAM > 64) {
+        __syncthreads();
+    } else {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
     }
-    sum = block_sum<THREADS>(sum, red);
-    for (int j = threadIdx.x; j < d.k; j += THREADS) p[j] /= sum;
-    w.log_norm = mx + logf(sum);
-    __syncthreads();
-    return w;
 }
 
-// A workgroup to a row, which it reads for the maximum, for the sums and for the gradient.
-template <typename T> __global__ __launch_bounds__(256) void distill_kernel(Distill d) {
-    __shared__ int ids[kDistillMaxEntries];
-    __shared__ float t[kDistillMaxEntries], p[kDistillMaxEntries], red[4];
-    const int C = d.classes;
-    const float over_t = 1.0f / d.temperature, alpha = d.alpha;
-    for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
-        __syncthreads();   // (the row before is done with the entries)
-        const RowTeacher w = read_teacher<256>(d, row, ids, t, p, red);
-        const float* const z = d.logits + row * C;
-        T* const g = d.dlogits ? (T*)d.dlogits + row * C : nullptr;
-        if (!w.taught && !w.labelled) {   // nothing to learn: whatever the logits are
-            if (g)
-                for (int c = threadIdx.x; c < C; c += 256) g[c] = from_f32<T>(0.0f);
-            if (threadIdx.x == 0) d.row_loss[row] = w.bad ? NAN : 0.0f;
+__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{v[0], v[1]}), bf16x2_t));
+    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{v[2], v[3]}), bf16x2_t));
+    *reinterpret_cast<any_u32x2_t*>(p) = any_u32x2_t{a, b};
+}
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) { store16_any(p, pack(v)); }
+
+// A team to a row (or a slice of one) at a time, whose logits it keeps in registers: NV pieces of 4 a thread, and of the up to three behind the last whole piece one to a lane.
+// What a thread has no logit for is minus infinity: pieces are loaded, compared and added up without a branch.  The classes of the entries and of the label get their gradients
+// once more, behind the others: the first entry of a class writes it, with what all of them and the label take away.
+template <typename T, int TEAM, int NV, int MODE>
+__global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, NV <= 16 ? 4 : 2) void distill_rows_kernel(Distill d, Slices cut, float* sums) {
+    constexpr int kTeams = TEAM == 64 ? 4 : 1;
+    constexpr float kLog2e = 1.4426950408889634f;
+    extern __shared__ float entries[];   // of every team two rows' in turn: classes, exponentials, the student's logits; k and the label's
+    __shared__ float red[2][3 * 16];
+    Reduce<TEAM> reduce{red};
+    const int lane = threadIdx.x % TEAM, team = TEAM == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, k = d.k, C = d.classes;
+    const float over_t = 1.0f / d.temperature, alpha = d.alpha, at_q = kLog2e * over_t, at_s = kLog2e;
+    const bool same = d.temperature == 1.0f;   // q is s
+    int turn = 0;
+    const int64_t units = d.rows * cut.slices, step = (int64_t)gridDim.x * kTeams;
+    for (int64_t unit = (int64_t)blockIdx.x * kTeams + team; unit < units; unit += step, turn ^= 1) {
+        const int64_t row = MODE == kWholeRows ? unit : unit / cut.slices;
+        const int slice = MODE == kWholeRows ? 0 : (int)(unit - row * cut.slices), from = slice * cut.length, n = MODE == kWholeRows ? C : min(cut.length, C - from);
+        int* const ids = reinterpret_cast<int*>(entries) + (team * 2 + turn) * 3 * (k + 1);
+        float* const p = reinterpret_cast<float*>(ids) + (k + 1);
+        float* const zs = p + (k + 1);
+        const float* const zrow = d.logits + row * C;
+        T* const g = d.dlogits ? (T*)d.dlogits + row * C + from : nullptr;
+        const int whole = n & ~3;   // logits in whole pieces
+
+        // What the row has to learn from.  top: the teacher's largest logit over T; how many ids are no class.  (A NaN among the teacher's logits makes the row one.)
+        const int label = d.labels && alpha < 1.0f ? d.labels[row * d.label_stride] : -1;
+        const bool labelled = label >= 0 && label < C;
+        float top[2] = {-INFINITY, labelled || label == -1 ? 0.0f : 1.0f};
+        if (alpha > 0.0f) {
+            for (int j = lane; j < k; j += TEAM) {
+                const int id = d.ids[row * d.entry_stride + j];
+                const bool entry = id >= 0 && id < C;
+                const float t = entry ? d.teacher[row * d.entry_stride + j] * over_t : -INFINITY;
+                ids[j] = entry ? id : -1;
+                p[j] = t;
+                top[0] = fmaxf(top[0], t != t ? INFINITY : t);
+                top[1] += entry || id == -1 ? 0.0f : 1.0f;
+            }
+            reduce.template all<true>(top);
+        }
+        const bool taught = top[0] != -INFINITY, bad = top[1] != 0.0f;
+        if (!taught && !labelled) {   // nothing to learn, whatever the logits are
+            if (MODE != kSliceSums) {
+                if (g) {
+                    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        if ((i * TEAM + lane) * 4 < whole) store4(g + (i * TEAM + lane) * 4, zero);
+                    if (lane < n - whole) g[whole + lane] = from_f32<T>(0.0f);
+                }
+                if (slice == 0 && lane == 0) d.row_loss[row] = bad ? NAN : 0.0f;
+            }
             continue;
         }
-        float mx = -INFINITY;
-        for (int c = threadIdx.x; c < C; c += 256) mx = fmaxf(mx, z[c]);
-        mx = block_max<256>(mx, red);
-        float sq = 0.0f, ss = 0.0f;
-        for (int c = threadIdx.x; c < C; c += 256) {
-            const float v = z[c] - mx;
-            sq += expf(v * over_t);
-            ss += expf(v);
+        // (the student's logits of the entries before the row's: what is requested first is there first)
+        const bool first = MODE != kSliceSums && taught && lane < k && ids[lane] >= 0;
+        const float z_first = first ? zrow[ids[lane]] : 0.0f, z_label = MODE != kSliceSums && labelled ? zrow[label] : 0.0f;
+        uint4 raw[NV];
+        const float* const z = zrow + from;
+        if (whole > 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) raw[i] = load16_any(z + (unsigned)min((i * TEAM + lane) * 4, whole - 4));
         }
-        sq = block_sum<256>(sq, red);
-        ss = block_sum<256>(ss, red);
-        const float wq = w.taught ? alpha * d.temperature / sq * d.grad_scale : 0.0f, ws = w.labelled ? (1.0f - alpha) / ss * d.grad_scale : 0.0f;
-        const float on_label = (1.0f - alpha) * d.grad_scale, on_entry = alpha * d.temperature * d.grad_scale;
-        float kl = 0.0f;
-        if (w.taught) {
-            const float log_q = logf(sq);
-            for (int j = threadIdx.x; j < d.k; j += 256)
-                if (p[j] != 0.0f) kl += p[j] * ((t[j] - w.log_norm) - ((z[ids[j]] - mx) * over_t - log_q));
-            kl = block_sum<256>(kl, red);
+        float extra = lane < n - whole ? z[whole + lane] : -INFINITY;
+        float kl = 0.0f, most[2] = {-INFINITY, 0.0f};   // the row's largest logit; the sum of the teacher's exponentials
+        if (MODE != kSliceSums) {
+            if (taught) {
+                for (int j = lane; j < k; j += TEAM) {
+                    const float t = p[j] - top[0], e = ids[j] >= 0 ? expf(t) : 0.0f;
+                    zs[j] = j == lane ? z_first : ids[j] >= 0 ? zrow[ids[j]] : 0.0f;
+                    p[j] = e;
+                    most[1] += e;
+                    kl += e != 0.0f ? e * t : 0.0f;
+                }
+            }
+            if (lane == 0) {
+                ids[k] = labelled ? label : -1;
+                p[k] = 0.0f;
+                zs[k] = z_label;
+            }
         }
-        if (threadIdx.x == 0) {
-            float loss = w.taught ? alpha * d.temperature * d.temperature * kl : 0.0f;
-            if (w.labelled) loss += (1.0f - alpha) * (logf(ss) - (z[w.label] - mx));
-            d.row_loss[row] = w.bad ? NAN : loss;
+        float m, sq = 0.0f, ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool any = (i * TEAM + lane) * 4 < whole;
+            float v[4];
+            unpack(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = any ? v[e] : -INFINITY;
+            most[0] = fmaxf(most[0], fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+            raw[i] = pack(v);
+        }
+        most[0] = fmaxf(most[0], extra);
+        if constexpr (MODE == kSliceRest) {
+            // (at most 256 slices: one to a thread)
+            const float* const part = sums + (row * cut.slices + lane) * 3;
+            const bool any = lane < cut.slices;
+            const float mine = any ? part[0] : -INFINITY;
+            most[0] = mine;
+            reduce.template all<true>(most);
+            m = most[0];
+            sq = any ? part[1] * __builtin_amdgcn_exp2f((mine - m) * at_q) : 0.0f;
+            ss = any ? part[2] * __builtin_amdgcn_exp2f((mine - m) * at_s) : 0.0f;
+        } else {
+            reduce.template all<true>(most);
+            m = most[0];
+        }
+        const float teacher = most[1];
+        const bool need_s = labelled && !(same && taught);
+        // (left to itself the compiler has many pieces' exponentials under way at once, in registers that the row needs: hence the barriers to its scheduling)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float v[4];
+            unpack(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] -= m;
+            raw[i] = pack(v);
+        }
+        extra -= m;
+        auto add_up = [&](float scale) {
+            float t = __builtin_amdgcn_exp2f(extra * scale);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float v[4];
+                unpack(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t += __builtin_amdgcn_exp2f(v[e] * scale);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return t;
+        };
+        if constexpr (MODE != kSliceRest) {
+            if (taught) sq = add_up(at_q);
+            if (need_s) ss = add_up(at_s);
+        }
+        if (MODE != kSliceSums && taught) {
+            for (int j = lane; j < k; j += TEAM)
+                if (p[j] != 0.0f) kl -= p[j] * ((zs[j] - m) * over_t);
+        }
+        float total[3] = {sq, ss, kl};
+        reduce.template all<false>(total);
+        sq = total[0];
+        ss = same && taught ? sq : total[1];
+        if constexpr (MODE == kSliceSums) {
+            if (lane == 0) {
+                sums[unit * 3] = m;
+                sums[unit * 3 + 1] = sq;
+                sums[unit * 3 + 2] = ss;
+            }
+            continue;
+        }
+        const float T_ = d.temperature, on_entry = taught ? alpha * T_ * d.grad_scale : 0.0f, on_label = labelled ? (1.0f - alpha) * d.grad_scale : 0.0f;
+        if (slice == 0 && lane == 0) {
+            float loss = taught ? alpha * T_ * T_ * (total[2] / teacher - logf(teacher) + logf(sq)) : 0.0f;
+            if (labelled) loss += (1.0f - alpha) * (logf(ss) - (z_label - m));
+            d.row_loss[row] = bad ? NAN : loss;
         }
         if (!g) continue;
-        for (int c = threadIdx.x; c < C; c += 256) {
-            const float v = z[c] - mx;
-            float o = wq * expf(v * over_t) + ws * expf(v);
-            if (w.labelled && c == w.label) o -= on_label;
-            g[c] = from_f32<T>(o);
-        }
-        if (!w.taught) continue;
-        __syncthreads();
-        // The entries' classes once more, with what the teacher gives them: the first entry of a class writes it, with the sum of all.
-        for (int j = threadIdx.x; j < d.k; j += 256) {
+        // one exponential to a logit, or two
+        const float w1 = taught ? on_entry / sq + (same && labelled ? on_label / ss : 0.0f) : on_label / ss, at1 = taught ? at_q : at_s, w2 = need_s && taught ? on_label / ss : 0.0f;
+        auto gradient = [&](float v, bool two) {
+            float o = w1 * __builtin_amdgcn_exp2f(v * at1);
+            if (two) o = fmaf(w2, __builtin_amdgcn_exp2f(v * at_s), o);
+            return o;
+        };
+        auto write = [&](bool two) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float v[4];
+                unpack(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = gradient(v[e], two);
+                if ((i * TEAM + lane) * 4 < whole) store4(g + (unsigned)((i * TEAM + lane) * 4), v);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const bool two = need_s && taught;
+        if (two) write(true);
+        else write(false);
+        if (lane < n - whole) g[whole + lane] = from_f32<T>(gradient(extra, two));
+        team_sync<TEAM>();
+        const float share = taught ? on_entry / teacher : 0.0f;
+        const int begin = taught ? 0 : k;
+        for (int j = begin + lane; j <= k; j += TEAM) {
             const int id = ids[j];
-            if (id < 0) continue;
+            if (id < from || id >= from + n) continue;
             float sum = 0.0f;
-            bool first = true;
-            for (int i = 0; i < d.k; ++i)
+            int firsts = j;
+            for (int i = begin; i <= k; ++i)
                 if (ids[i] == id) {
-                    first = first && i >= j;
+                    firsts = min(firsts, i);
                     sum += p[i];
                 }
-            if (!first) continue;
-            const float v = z[id] - mx;
-            float o = wq * expf(v * over_t) + ws * expf(v) - on_entry * sum;
-            if (w.labelled && id == w.label) o -= on_label;
-            g[id] = from_f32<T>(o);
+            if (firsts != j) continue;
+            float o = gradient(zs[j] - m, two);
+            if (id == label) o -= on_label;
+            g[id - from] = from_f32<T>(fmaf(-share, sum, o));
         }
     }
+}
+
+// Rows of more than 98304 logits are cut into slices that registers hold, and few wide rows into as many as give every compute unit two.
+constexpr int kWholeMax = 98304, kSliceMax = 32768;
+static Slices cut_rows(int64_t rows, int classes) {
+    const int64_t fit = classes > kWholeMax ? (classes + kSliceMax - 1) / kSliceMax : 1;
+    int64_t slices = fit;
+    if (rows < 256 && classes > 8192) {
+        const int64_t wanted = (512 + rows - 1) / rows, most = (classes + 4095) / 4096 < 256 ? (classes + 4095) / 4096 : 256;
+        slices = wanted < most ? wanted : most;
+        if (slices < fit) slices = fit;
+    }
+    const int64_t length = ((classes + slices - 1) / slices + 3) / 4 * 4;
+    return Slices{(int)((classes + length - 1) / length), (int)length};
 }
 
 size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes) {
-    (void)rows;
-    (void)plan_rows;
-    (void)classes;
-    return 0;
+    const Slices cut = cut_rows(plan_rows, classes);
+    return cut.slices > 1 ? (size_t)rows * cut.slices * 3 : 0;
+}
+
+template <typename T, int TEAM, int NV, int MODE> static hipError_t launch_rows(const Distill& d, const Slices& cut, float* ws, hipStream_t s) {
+    constexpr int teams = TEAM == 64 ? 4 : 1;
+    const int64_t groups = (d.rows * cut.slices + teams - 1) / teams;
+    hipLaunchKernelGGL((distill_rows_kernel<T, TEAM, NV, MODE>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(TEAM == 64 ? 256 : TEAM), (size_t)teams * 2 * 3 * (d.k + 1) * 4, s, d, cut,
+                       ws);
+    return hipGetLastError();
+}
+
+template <typename T, int MODE> static hipError_t launch_slices(const Distill& d, const Slices& cut, float* ws, hipStream_t s) {
+    if (cut.length <= 4096) return launch_rows<T, 256, 4, MODE>(d, cut, ws, s);
+    if (cut.length <= 8192) return launch_rows<T, 256, 8, MODE>(d, cut, ws, s);
+    return launch_rows<T, 512, 16, MODE>(d, cut, ws, s);
+}
+
+template <typename T> static hipError_t distill_type(const Distill& d, float* ws, hipStream_t s) {
+    const Slices cut = cut_rows(d.plan_rows, d.classes);
+    if (cut.slices > 1) {
+        const hipError_t e = launch_slices<T, kSliceSums>(d, cut, ws, s);
+        return e != hipSuccess ? e : launch_slices<T, kSliceRest>(d, cut, ws, s);
+    }
+    const int C = d.classes;
+    if (d.k <= 500) {   // (four rows' entries in LDS)
+        if (C <= 256) return launch_rows<T, 64, 1, kWholeRows>(d, cut, ws, s);
+        if (C <= 512) return launch_rows<T, 64, 2, kWholeRows>(d, cut, ws, s);
+        if (C <= 1024) return launch_rows<T, 64, 4, kWholeRows>(d, cut, ws, s);
+        if (C <= 2048) return launch_rows<T, 64, 8, kWholeRows>(d, cut, ws, s);
+    }
+    if (C <= 4096) return launch_rows<T, 256, 4, kWholeRows>(d, cut, ws, s);
+    if (C <= 8192) return launch_rows<T, 256, 8, kWholeRows>(d, cut, ws, s);
+    if (C <= 16384) return launch_rows<T, 512, 8, kWholeRows>(d, cut, ws, s);
+    if (C <= 32768) return launch_rows<T, 512, 16, kWholeRows>(d, cut, ws, s);
+    if (C <= 65536) return launch_rows<T, 512, 32, kWholeRows>(d, cut, ws, s);
+    return launch_rows<T, 512, 48, kWholeRows>(d, cut, ws, s);
 }
 
 hipError_t distill(int dtype, const Distill& d, float* ws, hipStream_t s) {
-    (void)ws;
     if (d.rows <= 0) return hipSuccess;
-    const dim3 grid((unsigned)(d.rows < (1 << 20) ? d.rows : 1 << 20));
-    if (dtype == kBF16) hipLaunchKernelGGL(distill_kernel<bf16_t>, grid, dim3(256), 0, s, d);
-    else hipLaunchKernelGGL(distill_kernel<float>, grid, dim3(256), 0, s, d);
-    return hipGetLastError();
+    return dtype == kBF16 ? distill_type<bf16_t>(d, ws, s) : distill_type<float>(d, ws, s);
 }
 
 }  // namespace tmps

@@ -54,36 +54,6 @@ template <int TEAM> struct Team {
 
 template <typename T> constexpr int kOne = 8 / kPiece<T>;   // pieces of 8 features
 
-// The pieces of a thread in every row.  WHOLE: all of the launch's pieces are on 16 bytes, and inside a row or behind it.  Otherwise they are 16 bytes at any address, which the
-// memory unit takes in a request or two, and the piece that a row ends in begins as much earlier as it would reach beyond: its first features are also the piece's before it, which
-// has them for its own.  (Loads of the last features one by one would have to be put together, and so waited for, where they are requested: 8000 x 1003 in bf16, backward, 52 us
-// instead of 35.)  A row of fewer features than a piece is one that is put together all the same.
-template <int TEAM, int N, int V, bool WHOLE> struct Pieces {
-    int D;
-    __device__ __forceinline__ int column(int i) const { return ((int)(threadIdx.x % TEAM) + TEAM * i) * V; }   // the first feature of its own
-    __device__ __forceinline__ bool any(int i) const { return column(i) < D; }
-    __device__ __forceinline__ int at(int i) const { return WHOLE ? column(i) : min(column(i), max(D - V, 0)); }   // the first feature it holds
-    __device__ __forceinline__ bool own(int i, int e) const { return WHOLE || (at(i) + e >= column(i) && (D >= V || e < D)); }   // (of a piece that has any)
-};
-
-// 16 bytes of a row from feature c on, as they lie in memory: requested for the next row while this one is worked on, unpacked when their turn comes.
-template <bool WHOLE, typename T> __device__ __forceinline__ void request16(uint4& u, const T* row, int c, int D) {
-    if constexpr (WHOLE) {
-        u = *reinterpret_cast<const uint4*>(row + c);
-    } else if (c + kPiece<T> <= D) {
-        u = load16_any(row + c);
-    } else {
-        struct Features { T v[kPiece<T>]; } f;
-#pragma unroll
-        for (int e = 0; e < kPiece<T>; ++e) f.v[e] = c + e < D ? row[c + e] : T(0.0f);
-        u = __builtin_bit_cast(uint4, f);
-    }
-}
-template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void request_row(uint4 (&u)[N], const T* row, const Pieces<TEAM, N, V, WHOLE>& p) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (p.any(i)) request16<WHOLE>(u[i], row, p.at(i), p.D);
-}
 // The features of piece i that are its own.
 template <typename T, int TEAM, int N, int V, bool WHOLE> __device__ __forceinline__ void store_packed(T* row, const Pieces<TEAM, N, V, WHOLE>& p, int i, const uint4& u) {
     if (!p.any(i)) return;

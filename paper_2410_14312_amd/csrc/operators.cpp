@@ -155,6 +155,7 @@ extern "C" int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D
 
 int tmps::check_distill(int64_t classes, int64_t k, float temperature, float alpha) {
     if (classes < 1 || k < 1) return fail(TMPS_EINVAL, "classes and k must be positive");
+    if (classes > kDistillMaxClasses) return fail(TMPS_EUNSUPPORTED, "more than %d classes", kDistillMaxClasses);
     if (k > kDistillMaxEntries) return fail(TMPS_EUNSUPPORTED, "more than %d teacher entries a row", kDistillMaxEntries);
     if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature)) return fail(TMPS_EINVAL, "temperature must be positive");
     if (!(alpha >= 0.0f && alpha <= 1.0f)) return fail(TMPS_EINVAL, "alpha must lie in 0..1");
@@ -162,7 +163,7 @@ int tmps::check_distill(int64_t classes, int64_t k, float temperature, float alp
 }
 
 extern "C" size_t tmps_distill_workspace(int64_t rows, int classes) {
-    if (rows < 1 || classes < 1) return 0;
+    if (rows < 1 || classes < 1 || classes > kDistillMaxClasses) return 0;
     return distill_workspace_elems(rows, rows, classes) * sizeof(float);
 }
 
