@@ -3,6 +3,7 @@
 //   loss = alpha T^2 sum_j p_j (log p_j - log q[id_j]) + (1 - alpha) (-log s[label])
 //   d loss / dz = alpha T (q - sum_j p_j e[id_j]) + (1 - alpha) (s - e[label])
 // Bound by memory: a row of logits is read, a row of gradients written.
+#include <cstdlib>
 #include "kernels.h"
 #include "pieces.hip.h"
 #include "wave.hip.h"
@@ -71,23 +72,24 @@ __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { store16_
 // What a thread has no logit for is minus infinity: pieces are loaded, compared and added up without a branch.  The classes of the entries and of the label get their gradients
 // once more, behind the others: the first entry of a class writes it, with what all of them and the label take away.
 template <typename T, int TEAM, int NV, int MODE>
-__global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, NV <= 16 ? 4 : 2) void distill_rows_kernel(Distill d, Slices cut, float* sums) {
+__global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 256 && NV == 32 ? 3 : NV <= 16 ? 4 : 2) void distill_rows_kernel(Distill d, Slices cut, float* sums) {
     constexpr int kTeams = TEAM == 64 ? 4 : 1;
     constexpr float kLog2e = 1.4426950408889634f;
-    extern __shared__ float entries[];   // of every team two rows' in turn: classes, exponentials, the student's logits; k and the label's
+    extern __shared__ __attribute__((aligned(16))) float entries[];   // of every team two rows' in turn: classes, exponentials, the student's logits
     __shared__ float red[2][3 * 16];
     Reduce<TEAM> reduce{red};
     const int lane = threadIdx.x % TEAM, team = TEAM == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, k = d.k, C = d.classes;
     const float over_t = 1.0f / d.temperature, alpha = d.alpha, at_q = kLog2e * over_t, at_s = kLog2e;
+    const int slots = (k + 3) & ~3;   // (entries in whole fours)
     const bool same = d.temperature == 1.0f;   // q is s
     int turn = 0;
     const int64_t units = d.rows * cut.slices, step = (int64_t)gridDim.x * kTeams;
     for (int64_t unit = (int64_t)blockIdx.x * kTeams + team; unit < units; unit += step, turn ^= 1) {
         const int64_t row = MODE == kWholeRows ? unit : unit / cut.slices;
         const int slice = MODE == kWholeRows ? 0 : (int)(unit - row * cut.slices), from = slice * cut.length, n = MODE == kWholeRows ? C : min(cut.length, C - from);
-        int* const ids = reinterpret_cast<int*>(entries) + (team * 2 + turn) * 3 * (k + 1);
-        float* const p = reinterpret_cast<float*>(ids) + (k + 1);
-        float* const zs = p + (k + 1);
+        int* const ids = reinterpret_cast<int*>(entries) + (team * 2 + turn) * 3 * slots;
+        float* const p = reinterpret_cast<float*>(ids) + slots;
+        float* const zs = p + slots;
         const float* const zrow = d.logits + row * C;
         T* const g = d.dlogits ? (T*)d.dlogits + row * C + from : nullptr;
         const int whole = n & ~3;   // logits in whole pieces
@@ -143,11 +145,7 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, NV <= 16 ? 4 : 2) void dis
                     kl += e != 0.0f ? e * t : 0.0f;
                 }
             }
-            if (lane == 0) {
-                ids[k] = labelled ? label : -1;
-                p[k] = 0.0f;
-                zs[k] = z_label;
-            }
+            if (lane < slots - k) ids[k + lane] = -1;
         }
         float m, sq = 0.0f, ss = 0.0f;
 #pragma unroll
@@ -250,19 +248,29 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, NV <= 16 ? 4 : 2) void dis
         if (lane < n - whole) g[whole + lane] = from_f32<T>(gradient(extra, two));
         team_sync<TEAM>();
         const float share = taught ? on_entry / teacher : 0.0f;
-        const int begin = taught ? 0 : k;
-        for (int j = begin + lane; j <= k; j += TEAM) {
-            const int id = ids[j];
+        for (int j = taught ? lane : k + lane; j <= k; j += TEAM) {   // (the last is the label, for a class that no entry has)
+            const int id = j < k ? ids[j] : label;
             if (id < from || id >= from + n) continue;
+            int alike = 0;
+            for (int i = 0; taught && i < slots; i += 4) {
+                const int4 v = *reinterpret_cast<const int4*>(ids + i);
+                alike += (v.x == id) + (v.y == id) + (v.z == id) + (v.w == id);
+            }
             float sum = 0.0f;
-            int firsts = j;
-            for (int i = begin; i <= k; ++i)
-                if (ids[i] == id) {
-                    firsts = min(firsts, i);
-                    sum += p[i];
-                }
-            if (firsts != j) continue;
-            float o = gradient(zs[j] - m, two);
+            if (j == k) {
+                if (alike) continue;
+            } else if (alike == 1) {
+                sum = p[j];
+            } else {   // (the sum in the entries' order)
+                int firsts = j;
+                for (int i = 0; i < k; ++i)
+                    if (ids[i] == id) {
+                        firsts = min(firsts, i);
+                        sum += p[i];
+                    }
+                if (firsts != j) continue;
+            }
+            float o = gradient((j < k ? zs[j] : z_label) - m, two);
             if (id == label) o -= on_label;
             g[id - from] = from_f32<T>(fmaf(-share, sum, o));
         }
@@ -291,7 +299,7 @@ size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes) {
 template <typename T, int TEAM, int NV, int MODE> static hipError_t launch_rows(const Distill& d, const Slices& cut, float* ws, hipStream_t s) {
     constexpr int teams = TEAM == 64 ? 4 : 1;
     const int64_t groups = (d.rows * cut.slices + teams - 1) / teams;
-    hipLaunchKernelGGL((distill_rows_kernel<T, TEAM, NV, MODE>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(TEAM == 64 ? 256 : TEAM), (size_t)teams * 2 * 3 * (d.k + 1) * 4, s, d, cut,
+    hipLaunchKernelGGL((distill_rows_kernel<T, TEAM, NV, MODE>), dim3((unsigned)(groups < (1 << 20) ? groups : 1 << 20)), dim3(TEAM == 64 ? 256 : TEAM), (size_t)teams * 2 * 3 * ((d.k + 3) & ~3) * 4, s, d, cut,
                        ws);
     return hipGetLastError();
 }
@@ -318,6 +326,9 @@ template <typename T> static hipError_t distill_type(const Distill& d, float* ws
     if (C <= 4096) return launch_rows<T, 256, 4, kWholeRows>(d, cut, ws, s);
     if (C <= 8192) return launch_rows<T, 256, 8, kWholeRows>(d, cut, ws, s);
     if (C <= 16384) return launch_rows<T, 512, 8, kWholeRows>(d, cut, ws, s);
+    static const int kv = getenv("DV") ? atoi(getenv("DV")) : 0;
+    if (C <= 32768 && kv == 1) return launch_rows<T, 256, 32, kWholeRows>(d, cut, ws, s);
+    if (C <= 32768 && kv == 2) return launch_rows<T, 1024, 8, kWholeRows>(d, cut, ws, s);
     if (C <= 32768) return launch_rows<T, 512, 16, kWholeRows>(d, cut, ws, s);
     if (C <= 65536) return launch_rows<T, 512, 32, kWholeRows>(d, cut, ws, s);
     return launch_rows<T, 512, 48, kWholeRows>(d, cut, ws, s);
