@@ -91,7 +91,8 @@ def check(z, labels, ids, teacher, T, alpha, dtype, scale=None):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,C,k", [(1, 1, 1), (3, 2, 2), (5, 10, 3), (64, 100, 10), (9, 255, 64), (7, 256, 256), (4, 1000, 100), (33, 2048, 64), (6, 2052, 33), (5, 4099, 5),
-                                      (3, 8192, 300), (9, 16384, 64), (3, 16388, 64), (300, 5000, 20), (2, 32000, 1024), (270, 32000, 8), (2, 32771, 50), (1, 65536, 64), (5, 70001, 100), (3, 131072, 7),
+                                      (3, 8192, 300), (9, 16384, 64), (3, 16388, 64), (300, 5000, 20), (2, 32000, 1024), (270, 32000, 8),
+                                      (70, 17000, 30), (67, 24580, 200), (68, 32764, 64), (70, 33000, 300), (2, 32771, 50), (1, 65536, 64), (5, 70001, 100), (66, 65540, 100), (65, 98304, 7), (3, 131072, 7),
                                       (1, 200000, 64)])
 def test_sizes(dtype, rows, C, k):
     z, labels, ids, teacher = problem(rows, C, k, seed=C + k)
@@ -140,6 +141,25 @@ def test_masks(dtype, rows, C):
         loss, g = check(z, labels, ids, teacher, 1.5, alpha, dtype)
         for r in (5, 6):
             assert loss[r] == 0 and bool((g[r] == 0).all())
+
+
+@pytest.mark.parametrize("rows,C,k", [(9, 300, 65), (9, 1999, 256), (9, 1999, 257), (9, 5000, 1024), (9, 16001, 128), (66, 33000, 129), (65, 70000, 100), (9, 100001, 1000)])
+def test_many_entries_and_some_of_one_class(rows, C, k):
+    """No class twice, one class twice (the first and the last entry), up to 50 entries of a class, and the label among each (no sum over a class is longer than the bound's 64)."""
+    z, labels, ids, teacher = problem(rows, C, k, seed=k)
+    ids[1, -1] = ids[1, 0]
+    ids[2, 10:60] = ids[2, 0]
+    ids[3, -1] = ids[3, 0]
+    labels[3] = ids[3, 0]
+    ids[4, 10:60] = ids[4, 5]
+    labels[4] = ids[4, 5]
+    labels[5] = ids[5, k // 2]
+    ids[6, ::2] = -1
+    labels[6] = ids[6, -1 if k % 2 == 0 else -2]
+    ids[7, k // 2:] = ids[7, :k - k // 2].clone()
+    ids[8] = -1
+    for alpha in (0.7, 1.0):
+        check(z, labels, ids, teacher, 2.0, alpha, "bf16")
 
 
 @pytest.mark.parametrize("C", [30, 6001, 50001])
