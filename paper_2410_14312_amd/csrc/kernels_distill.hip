@@ -320,14 +320,14 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     }
 }
 
-// Rows of more than 98304 logits are cut into slices that registers hold (1024 rows of 131072: 255 us), and few wide rows into as many as give every compute unit two: one row of
-// 98304 logits takes 13 us, whole 24, 64 rows 23 and 31, 128 rows 33 and 33; 8 rows of 50257 15 and 17; 8 rows of 32000 15 and 12.
+// Rows of more than 98304 logits are cut into slices that registers hold (1024 rows of 131072: 255 us), and few wide rows into as many as give every compute unit eight: one row of
+// 98304 logits takes 13 us, whole 24, 64 rows 20 and 31; 8 rows of 50257 14 and 17; 8 rows of 32000 15 and 12.  (48 rows of 131071: 19 us, with two to a compute unit 26.)
 constexpr int kWholeMax = 98304, kSliceMax = 32768;
 static Slices cut_rows(int64_t rows, int classes) {
     const int64_t fit = classes > kWholeMax ? (classes + kSliceMax - 1) / kSliceMax : 1;
     int64_t slices = fit;
     if (rows <= 64 && classes > kSliceMax) {
-        const int64_t wanted = (512 + rows - 1) / rows, most = (classes + 4095) / 4096 < 256 ? (classes + 4095) / 4096 : 256;
+        const int64_t wanted = (2048 + rows - 1) / rows, most = (classes + 4095) / 4096 < 256 ? (classes + 4095) / 4096 : 256;
         slices = wanted < most ? wanted : most;
         if (slices < fit) slices = fit;
     }
