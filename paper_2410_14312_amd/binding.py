@@ -291,16 +291,25 @@ def _operand(name, t, shape, dtype, device):
                      % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
 
-def _call(fn, device, stream, *args):
-    """fn(..., stream) on a GPU's current stream, or on `stream`, with that GPU current."""
+def _within(stream, device):
+    """`stream` (a stream, or its handle) as the current one: what a call allocates there, its results and workspaces, then belongs to the stream that uses it."""
+    cuda = _torch().cuda
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU are wanted, not on %s" % device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = cuda.ExternalStream(int(stream), device=device) if int(stream) else cuda.default_stream(device)
+    if stream.device != device:
+        raise ValueError("stream: one of %s is wanted, not of %s" % (device, stream.device))
+    return cuda.stream(stream)
+
+
+def _call(fn, device, *args):
+    """fn(..., stream) on a GPU's current stream, with that GPU current."""
     torch = _torch()
     cuda = torch.cuda
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are wanted, not on %s" % device)
-    if stream is None:   # (current_stream(device).cuda_stream without the object: 0.1 us instead of 1.9)
-        handle = torch._C._cuda_getCurrentRawStream(device.index)
-    else:
-        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    handle = torch._C._cuda_getCurrentRawStream(device.index)   # (current_stream(device).cuda_stream without the object: 0.1 us instead of 1.9)
     if device.index == cuda.current_device():
         rc = fn(*args, handle)
     else:
@@ -313,7 +322,11 @@ def _call(fn, device, stream, *args):
 def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_ladders=False, inverse=False, out=None, stream=None):
     """Rotary positions (tmps_rotary) of the `heads` heads of dh features that begin each row of x [rows, features]: pairs = (time, height, width)
     pairs of features that turn with each axis of positions, int32 [n, 3], which the rows take in turn.  inverse: back, the gradient's way.
-    out (default: a new tensor [rows, heads * dh]) may be x, or a view of rows of its own stride.  Returns out."""
+    out (default: a new tensor [rows, heads * dh]) may be x, or a view of rows of its own stride.  Returns out.  On the current stream, or on `stream`, which a new tensor then
+    belongs to; it waits for no other."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return rotary(x, positions, heads, dh, pairs, base, interleaved, own_ladders, inverse, out)
     torch = _torch()
     code, width = _dtype_code(x), heads * dh
     if x.dim() != 2 or x.shape[1] < width or (x.shape[1] > 1 and x.stride(1) != 1):
@@ -329,7 +342,7 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
     elif out.dim() != 2 or out.shape[0] != rows or out.shape[1] < width or (out.shape[1] > 1 and out.stride(1) != 1) or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("out: %d rows of at least %d neighbouring %s features on %s are wanted" % (rows, width, x.dtype, x.device))
     d = RotaryDesc(heads, dh, (C.c_int32 * 3)(*pairs), _rotary_flags(interleaved, own_ladders), base)
-    _call(load_library().tmps_rotary, x.device, stream, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
+    _call(load_library().tmps_rotary, x.device, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
     return out
 
 
@@ -340,7 +353,10 @@ def _join_flags(rms, gate):
 def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=False, y=None, u=None, stats=None, stream=None):
     """y = scale r + g gain n(f), u = n(y) pre_gain + pre_shift over rows of r [rows, D] (tmps_norm_join_forward): x holds f, with `gate` rows [f | a] with
     g = 1 / (1 + exp(-a)); n is layer normalisation, with `rms` without its mean (then without pre_shift); without pre_gain u is None.  Returns
-    (y, u, stats); y may be given as r."""
+    (y, u, stats); y may be given as r.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, r.device):
+            return norm_join(x, r, gain, scale, pre_gain, pre_shift, rms, gate, y, u, stats)
     torch = _torch()
     code = _dtype_code(r)
     if r.dim() != 2:
@@ -352,7 +368,7 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
         u = torch.empty(rows, D, dtype=t, device=dev)
     if stats is None:
         stats = torch.empty(rows, 4, dtype=torch.float32, device=dev)
-    _call(load_library().tmps_norm_join_forward, dev, stream, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
+    _call(load_library().tmps_norm_join_forward, dev, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
           _operand("r", r, (rows, D), t, dev), _operand("gain", gain, (D,), torch.float32, dev), _operand("scale", scale, (D,), torch.float32, dev),
           _operand("y", y, (rows, D), t, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev),
           _operand("pre_shift", pre_shift, (D,), torch.float32, dev), _operand("u", u, (rows, D), t, dev),
@@ -362,7 +378,10 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
 
 def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=False, gate=False, dx=None, dr=None, stream=None):
     """Gradients of norm_join from dy and du (one of them may be None; with du also y and pre_gain are needed): (dx, dr, dgain, dscale, dpre_gain,
-    dpre_shift), those of parameters fp32, the last two None without du, the last with `rms`.  dr may be given as dy."""
+    dpre_shift), those of parameters fp32, the last two None without du, the last with `rms`.  dr may be given as dy.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, r.device):
+            return norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain, rms, gate, dx, dr)
     torch = _torch()
     code = _dtype_code(r)
     if r.dim() != 2:
@@ -377,7 +396,7 @@ def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=F
     need = load_library().tmps_norm_join_workspace(rows, D)
     ws = torch.empty(max(need, 4), dtype=torch.uint8, device=dev)
     at = grads.data_ptr()
-    _call(load_library().tmps_norm_join_backward, dev, stream, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
+    _call(load_library().tmps_norm_join_backward, dev, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
           _operand("x", x, (rows, wide), t, dev), _operand("r", r, (rows, D), t, dev), _operand("y", y, (rows, D), t, dev),
           _operand("stats", stats, (rows, 4), torch.float32, dev), _operand("gain", gain, (D,), torch.float32, dev),
           _operand("scale", scale, (D,), torch.float32, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev), _operand("dx", dx, (rows, wide), t, dev),
@@ -391,7 +410,10 @@ def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=F
 def distill(logits, labels, ids, teacher, temperature=1.0, alpha=1.0, grad_scale=None, dtype="f32", gradient=True, stream=None):
     """Distillation loss of each row of fp32 logits [rows, classes] against a teacher's logits [rows, k] of the classes ids (int32 [rows, k], -1: no entry)
     and labels (int32 [rows], -1: none; may be None), with its gradient times grad_scale (default: 1 / rows, for the mean) in `dtype` (tmps_distill).
-    Returns (row_loss, dlogits); dlogits is None without `gradient`."""
+    Returns (row_loss, dlogits); dlogits is None without `gradient`.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, logits.device):
+            return distill(logits, labels, ids, teacher, temperature, alpha, grad_scale, dtype, gradient)
     torch = _torch()
     if logits.dim() != 2 or ids.dim() != 2:
         raise ValueError("logits: [rows, classes], ids: [rows, k] are wanted")
@@ -403,7 +425,7 @@ def distill(logits, labels, ids, teacher, temperature=1.0, alpha=1.0, grad_scale
     d = DistillDesc(classes, k, temperature, alpha, 1.0 / max(rows, 1) if grad_scale is None else grad_scale)
     need = load_library().tmps_distill_workspace(rows, classes)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(load_library().tmps_distill, dev, stream, TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, C.byref(d), rows,
+    _call(load_library().tmps_distill, dev, TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, C.byref(d), rows,
           _operand("logits", logits, (rows, classes), torch.float32, dev), _operand("labels", labels, (rows,), torch.int32, dev), 1,
           _operand("ids", ids, (rows, k), torch.int32, dev), _operand("teacher", teacher, (rows, k), torch.float32, dev), k,
           dlogits.data_ptr() if gradient else None, row_loss.data_ptr(), ws.data_ptr() if need else None, need)

@@ -98,7 +98,7 @@ def test_the_binding_refuses():
     for bad in (lambda: tmps.rotary(x, pos, 2, 64, (32, 0, 0)), lambda: tmps.rotary(x.double(), pos, 2, 64, (32, 0, 0)), lambda: tmps.rotary(x.t(), pos, 1, 4, (2, 0, 0)),
                 lambda: tmps.rotary(x, pos.long(), 2, 64, (32, 0, 0)), lambda: tmps.rotary(x, pos[:, :2], 2, 64, (32, 0, 0)), lambda: tmps.rotary(x, pos, 3, 64, (32, 0, 0)),
                 lambda: tmps.rotary(x, pos, 2, 64, (32, 0)), lambda: tmps.rotary(x, pos, 2, 64, (32, 0, 0), out=f(3, 128)), lambda: tmps.rotary(x[0], pos, 2, 64, (32, 0, 0)),
-                lambda: tmps.rotary(x, pos, 2, 64, (32, 0, 0), out=x.bfloat16())):
+                lambda: tmps.rotary(x, pos, 2, 64, (32, 0, 0), out=x.bfloat16()), lambda: tmps.rotary(x, pos, 2, 64, (32, 0, 0), stream=0)):
         with pytest.raises(ValueError):
             bad()
     r, v, st = f(4, 8), f(8), f(4, 4)
