@@ -4,8 +4,8 @@
 //   dpre_gain = sum du yh, dpre_shift = sum du, dscale = sum dh r, dgain = sum dh g fh over the rows
 // One pass over memory: dy, du, x, r, y are read and dx, dr written once each.  A team goes over its share of the rows and keeps its sums over them in registers, which
 // leave as one row of partial results; those are added up in a fixed order behind.  In bf16, with the norm, both launches (us; a copy of as many bytes at 5.1 TB/s): 8192 x 768
-// 25.8 (17.4) and gated 33.5 (22.4), 8192 x 2048 51 (46), 16384 x 4096 177 (186), 8192 x 8192 204 (186); in fp32 4096 x 1024 gated 36.5 (30).  What short rows lack are waves: a
-// SIMD's registers hold two or three.  Rows of more than 8192 features spill (2048 x 16384: 312, 57).
+// 25.8 (17.4) and gated 33.5 (22.4), 8192 x 2048 51 (46), 16384 x 4096 177 (186), 8192 x 8192 195 (186); in fp32 4096 x 1024 gated 36.5 (30).  What short rows lack are waves: a
+// SIMD's registers hold two or three.  Rows of more than 8192 features have more values than registers and spill some (2048 x 16384: 168, 93).
 #include "launch.h"
 #include "norm_join.hip.h"
 
@@ -14,27 +14,105 @@ namespace tmps {
 // Threads of a launch at most: two waves to a SIMD, which is what its registers hold, each with its next row under way.
 constexpr int kBwdThreads = 131072;
 
-// NEXT (8192 x 768 gated 31.3 us without, 28.0 with; 16384 x 4096 197 and 171): a row's operands are requested as soon as those of the row before are taken, in two parts: what the norm of y needs, and what comes behind its sums.  (Workgroups of
-// 1024 threads have no registers for that, nor, with two pieces a thread, for parameters.)
+// A thread's sums over its rows, of N pieces of V: in registers, or (SHARED) in LDS, where nobody else touches them.
+template <int TEAM, int N, int V, bool SHARED> struct RowSums {
+    float kept[SHARED ? 1 : N][V];
+    float4* mine;
+    __device__ __forceinline__ void get(int i, float (&v)[V]) const {
+        if constexpr (SHARED) {
+#pragma unroll
+            for (int h = 0; h < V / 4; ++h) {
+                const float4 u = mine[(i * (V / 4) + h) * TEAM];
+                v[4 * h] = u.x, v[4 * h + 1] = u.y, v[4 * h + 2] = u.z, v[4 * h + 3] = u.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = kept[i][e];
+        }
+    }
+    __device__ __forceinline__ void put(int i, const float (&v)[V]) {
+        if constexpr (SHARED) {
+#pragma unroll
+            for (int h = 0; h < V / 4; ++h) mine[(i * (V / 4) + h) * TEAM] = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) kept[i][e] = v[e];
+        }
+    }
+    __device__ __forceinline__ void start(float4* at) {
+        mine = at + threadIdx.x;
+        const float zeros[V] = {};
+#pragma unroll
+        for (int i = 0; i < N; ++i) put(i, zeros);
+    }
+    // sum += a b, or a
+    __device__ __forceinline__ void add(int i, const float (&a)[V], const float (&b)[V]) {
+        float v[V];
+        get(i, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = fmaf(a[e], b[e], v[e]);
+        put(i, v);
+    }
+    __device__ __forceinline__ void add(int i, const float (&a)[V]) {
+        float v[V];
+        get(i, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += a[e];
+        put(i, v);
+    }
+};
+
+// A row's operand as numbers, of N pieces of V: formed once (KEPT, where the next row's pieces take its registers), or wherever it is wanted.
+template <int N, int V, bool KEPT, typename F> struct Numbers {
+    F form;
+    float kept[KEPT ? N : 1][V];
+    __device__ __forceinline__ explicit Numbers(F f) : form(f) {
+        if constexpr (KEPT) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) form(i, kept[i]);
+        }
+    }
+    __device__ __forceinline__ void get(int i, float (&v)[V]) const {
+        if constexpr (KEPT) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = kept[i][e];
+        } else {
+            form(i, v);
+        }
+    }
+};
+template <int N, int V, bool KEPT, typename F> __device__ __forceinline__ Numbers<N, V, KEPT, F> numbers(F f) { return Numbers<N, V, KEPT, F>(f); }
+
+// NEXT (8192 x 768 gated 31.3 us without, 28.0 with; 16384 x 4096 197 and 171): a row's operands are requested as soon as those of the row before are taken, in two parts: what the
+// norm of y needs, and what comes behind its sums.  Workgroups of 1024 threads have no registers for that: they form an operand's numbers again wherever they are used, hold two of
+// the sums in LDS and take a join's parameters, with a norm behind, from the cache (not KEEP; 4096 x 5120 gated 84 us, 97 in registers; 8192 x 8192 185 and 186).  Sums in LDS
+// and numbers formed again against registers for both, first launch: 8192 x 8192 185 and 201 us, 3000 x 5001 gated 91 and 152, 2048 x 16384 152 and 297, 2048 x 8193 with means 130
+// and 376.  (Of a row of odd length the compiler would keep in registers which features are whose, of all pieces at once: hence the row's length anew in every row.)
 template <typename T, int TEAM, int N, bool WHOLE, bool JOIN, bool PRE, bool GATE>
 __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(NormJoinBackward a, float* part, float* part_pre) {
     constexpr int kRows = Team<TEAM>::kRows, V = kPiece<T>;
-    constexpr bool KEEP = N * V == 8, NEXT = KEEP && TEAM < 1024;
+    constexpr bool KEEP = N * V == 8 && !(TEAM == 1024 && JOIN && PRE), NEXT = KEEP && TEAM < 1024;
     __shared__ float red[2][2 * 16];
     __shared__ float fold[kRows > 1 ? kRows : 1][kRows > 1 ? TEAM * V * N : 1];
     const int D = a.D;
     constexpr int wide = GATE ? 2 : 1;
     const float over_d = 1.0f / (float)D;
-    const Pieces<TEAM, N, V, WHOLE> p{D};
+    Pieces<TEAM, N, V, WHOLE> p{D};
     int place = 0;
-    float dgain[JOIN ? N : 1][V], dscale[JOIN ? N : 1][V], dpg[PRE ? N : 1][V], dps[PRE ? N : 1][V];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            if constexpr (JOIN) dgain[i][e] = dscale[i][e] = 0.0f;
-            if constexpr (PRE) dpg[i][e] = dps[i][e] = 0.0f;
-        }
+    // (two of the sums of a workgroup of 1024 threads are in LDS)
+    constexpr bool SHARED = TEAM == 1024;
+    constexpr int kEach = N * V / 4 * TEAM;
+    __shared__ float4 shared_sums[SHARED ? 2 * kEach : 1];
+    RowSums<TEAM, N, V, SHARED> dgain, dscale;
+    RowSums<TEAM, N, V, SHARED && !JOIN> dpg, dps;
+    if constexpr (JOIN) {
+        dgain.start(shared_sums);
+        dscale.start(shared_sums + (SHARED ? kEach : 0));
+    }
+    if constexpr (PRE) {
+        dpg.start(shared_sums);
+        dps.start(shared_sums + (SHARED ? kEach : 0));
+    }
     float gain[KEEP ? N : 1][V], scale[KEEP ? N : 1][V], pre_gain[KEEP ? N : 1][V];
     if constexpr (KEEP) {
 #pragma unroll
@@ -76,65 +154,75 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
     }
     for (; row < a.rows; row += step) {
         const bool more = NEXT && row + step < a.rows;
-        if constexpr (!NEXT) {
-            request_first(row);
-            request_second(row);
-        }
-        float dh[N][V], dy[N][V];
+        if constexpr (TEAM == 1024) asm volatile("" : "+s"(p.D));
+        if constexpr (!NEXT) request_first(row);
+        if constexpr (!NEXT && KEEP) request_second(row);
+        float dh[N][V];
+        auto dy = numbers<N, V, NEXT>([&](int i, float (&v)[V]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) dy[i][e] = 0.0f;
-            if (has_dy) unpack(rdy[i], dy[i]);
-        }
+            for (int e = 0; e < V; ++e) v[e] = 0.0f;
+            if (has_dy) unpack(rdy[i], v);
+        });
         if constexpr (PRE) {
             const float mean = pre_st[0], rstd = pre_st[1];
-            float yh[N][V], s[2] = {0.0f, 0.0f};
+            auto yh = numbers<N, V, NEXT>([&](int i, float (&v)[V]) {
+                unpack(ry[i], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd;
+            });
+            float s[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 if (!p.any(i)) continue;
-                float du[V];
+                float du[V], y[V];
                 if constexpr (!KEEP) load_vector(pre_gain[0], a.pre_gain, p, i);
                 unpack(rdu[i], du);
-                unpack(ry[i], yh[i]);
+                yh.get(i, y);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    yh[i][e] = (yh[i][e] - mean) * rstd;
                     dh[i][e] = du[e] * pre_gain[KEEP ? i : 0][e];
                     const float t = p.own(i, e) ? dh[i][e] : 0.0f;
-                    s[0] = fmaf(t, yh[i][e], s[0]);
+                    s[0] = fmaf(t, y[e], s[0]);
                     s[1] += t;
-                    dpg[i][e] = fmaf(du[e], yh[i][e], dpg[i][e]);
-                    dps[i][e] += du[e];
                 }
+                dpg.add(i, du, y);
+                dps.add(i, du);
             }
             if (more) request_first(row + step);
+            if constexpr (!KEEP) request_second(row);
             Team<TEAM>::sums(s, red, place);
             const float m = a.rms ? 0.0f : s[1] * over_d, q = s[0] * over_d;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (p.any(i)) {
+            for (int i = 0; i < N; ++i) {
+                if (!p.any(i)) continue;
+                float d[V], y[V];
+                dy.get(i, d);
+                yh.get(i, y);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) dh[i][e] = fmaf(rstd, fmaf(-yh[i][e], q, dh[i][e] - m), dy[i][e]);
-                }
+                for (int e = 0; e < V; ++e) dh[i][e] = fmaf(rstd, fmaf(-y[e], q, dh[i][e] - m), d[e]);
+            }
         } else {
             if (more) request_first(row + step);
+            if constexpr (!KEEP) request_second(row);
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int e = 0; e < V; ++e) dh[i][e] = dy[i][e];
+            for (int i = 0; i < N; ++i) dy.get(i, dh[i]);
         }
         if constexpr (JOIN) {
             const float mean = st[0], rstd = st[1];
             T* const dxr = (T*)a.dx + row * D * wide;
-            float fh[N][V], r_[N][V], at_[GATE ? N : 1][V], add_[N][V], s[2] = {0.0f, 0.0f};
+            auto fh = numbers<N, V, NEXT>([&](int i, float (&v)[V]) {
+                unpack(rf[i], v);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                unpack(rf[i], fh[i]);
-                unpack(rr[i], r_[i]);
-                if constexpr (GATE) unpack(ra[i], at_[i]);
-                if (a.add) unpack(radd[i], add_[i]);
-            }
+                for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd;
+            });
+            auto from_r = numbers<N, V, NEXT>([&](int i, float (&v)[V]) { unpack(rr[i], v); });
+            auto gate = numbers<N, V, NEXT>([&](int i, float (&v)[V]) {
+                if constexpr (GATE) unpack(ra[i], v);
+            });
+            auto given = numbers<N, V, NEXT>([&](int i, float (&v)[V]) {
+                if (a.add) unpack(radd[i], v);
+            });
+            float s[2] = {0.0f, 0.0f};
             if (more) request_second(row + step);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -143,35 +231,37 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
                     load_vector(gain[0], a.gain, p, i);
                     load_vector(scale[0], a.scale, p, i);
                 }
-                float o[V];
+                float o[V], r[V], f[V];
+                from_r.get(i, r);
+                fh.get(i, f);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    fh[i][e] = (fh[i][e] - mean) * rstd;
-                    dscale[i][e] = fmaf(dh[i][e], r_[i][e], dscale[i][e]);
-                    o[e] = dh[i][e] * scale[KEEP ? i : 0][e];
-                }
+                for (int e = 0; e < V; ++e) o[e] = dh[i][e] * scale[KEEP ? i : 0][e];
+                dscale.add(i, dh[i], r);
                 if (a.add) {
+                    float v[V];
+                    given.get(i, v);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) o[e] += add_[i][e];
+                    for (int e = 0; e < V; ++e) o[e] += v[e];
                 }
                 if (a.dr) store_piece((T*)a.dr + row * D, p, i, o);
                 if constexpr (GATE) {
-                    float da[V];
+                    float da[V], at[V];
+                    gate.get(i, at);
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         float sg, rest;
-                        gate_of<T>(at_[i][e], sg, rest);
-                        da[e] = dh[i][e] * gain[KEEP ? i : 0][e] * fh[i][e] * (sg * rest);
+                        gate_of<T>(at[e], sg, rest);
+                        da[e] = dh[i][e] * gain[KEEP ? i : 0][e] * f[e] * (sg * rest);
                         dh[i][e] *= sg;
                     }
                     if (a.dx) store_piece(dxr + D, p, i, da);
                 }
+                dgain.add(i, dh[i], f);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    dgain[i][e] = fmaf(dh[i][e], fh[i][e], dgain[i][e]);
                     dh[i][e] *= gain[KEEP ? i : 0][e];
                     const float t = p.own(i, e) ? dh[i][e] : 0.0f;
-                    s[0] = fmaf(t, fh[i][e], s[0]);
+                    s[0] = fmaf(t, f[e], s[0]);
                     s[1] += t;
                 }
             }
@@ -181,9 +271,10 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     if (!p.any(i)) continue;
-                    float o[V];
+                    float o[V], f[V];
+                    fh.get(i, f);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) o[e] = rstd * fmaf(-fh[i][e], q, dh[i][e] - m);
+                    for (int e = 0; e < V; ++e) o[e] = rstd * fmaf(-f[e], q, dh[i][e] - m);
                     store_piece(dxr, p, i, o);
                 }
             }
@@ -193,14 +284,17 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
         }
     }
     // The workgroup's row of partial results; its teams' sums, where it has several, are added up through LDS.
-    auto leave = [&](const float (&v)[N][V], float* to) {
+    auto leave = [&](const auto& sums, float* to) {
         if constexpr (kRows > 1) {
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+            for (int i = 0; i < N; ++i) {
+                float v[V];
+                sums.get(i, v);
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    if (p.any(i) && p.own(i, e)) fold[threadIdx.x / TEAM][p.at(i) + e] = v[i][e];
+                    if (p.any(i) && p.own(i, e)) fold[threadIdx.x / TEAM][p.at(i) + e] = v[e];
+            }
             __syncthreads();
             for (int c = threadIdx.x; c < D; c += Team<TEAM>::kThreads) {
                 float t[kRows];
@@ -214,10 +308,13 @@ __global__ __launch_bounds__(Team<TEAM>::kThreads) void norm_join_bwd_kernel(Nor
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
+            for (int i = 0; i < N; ++i) {
+                float v[V];
+                sums.get(i, v);
 #pragma unroll
                 for (int e = 0; e < V; ++e)
-                    if (p.any(i) && p.own(i, e)) to[p.at(i) + e] = v[i][e];
+                    if (p.any(i) && p.own(i, e)) to[p.at(i) + e] = v[e];
+            }
         }
     };
     if constexpr (JOIN) {

@@ -149,6 +149,16 @@ def test_forms(dtype, rms, gate, pre, dy, rows, D):
     check_backward(p, y, stats, D, dtype, rms, gate, pre, dy)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("gate,pre,dy", [(True, True, True), (False, True, True), (True, False, True), (False, True, False)])
+@pytest.mark.parametrize("rows,D", [(600, 5003), (530, 8192), (270, 8201), (258, 16384)])
+def test_wide_rows_several_to_a_workgroup(dtype, rms, gate, pre, dy, rows, D):
+    p = problem(rows, D, dtype, rms, gate, pre, seed=D)
+    y, _, stats = check_forward(p, D, dtype, rms, gate, pre)
+    check_backward(p, y, stats, D, dtype, rms, gate, pre, dy)
+
+
 @pytest.mark.parametrize("rms", [False, True])
 def test_large_means_and_tiny_rows(rms):
     """Rows far from zero (the variance is that of differences), rows of zeros, rows of one value: finite results, the bounds as they are."""
