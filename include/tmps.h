@@ -119,7 +119,7 @@ typedef struct {
     int32_t micro_batch;  /* M/N samples per forward */
     int32_t n_micro;      /* N */
     int32_t max_stash;    /* stash capacity in micro-batches; a positive multiple of n_micro */
-    int32_t is_last;      /* stage ends in TMPS_SOFTMAX_CE */
+    int32_t is_last;      /* stage ends in TMPS_SOFTMAX_CE or TMPS_DISTILL */
     int32_t borrow_input; /* 1: the stage keeps only the pointer x given to tmps_forward_micro,
                              which must stay valid and unchanged until the slot's backward pass,
                              and the N inputs of a mini-batch must be consecutive in memory;
@@ -394,8 +394,9 @@ int tmps_streams_destroy(void** streams, int n);
  * kernel's execution.  TMPS_KC_EVENT_PAIR is an empty bracket recorded before every update launch, the
  * cost of such a pair by itself.  tmps_profile_read() waits for the recorded events, adds the elapsed
  * milliseconds and launch counts per class into total_ms[] / launches[] (host arrays of n_classes >=
- * TMPS_KERNEL_CLASSES entries), clears the record and returns TMPS_KERNEL_CLASSES.  Timing adds host
- * overhead: measure throughput with profiling off. */
+ * TMPS_KERNEL_CLASSES entries), clears the record and returns TMPS_KERNEL_CLASSES.  Rotary positions count
+ * under TMPS_KC_EMBEDDING, norm joins under TMPS_KC_LAYERNORM, distillation under TMPS_KC_SOFTMAX_CE.
+ * Timing adds host overhead: measure throughput with profiling off. */
 enum {
     TMPS_KC_DENSE_FWD = 0, TMPS_KC_DENSE_DGRAD, TMPS_KC_DENSE_WGRAD, TMPS_KC_CONV_FWD,
     TMPS_KC_CONV_DGRAD, TMPS_KC_CONV_WGRAD, TMPS_KC_SOFTMAX_CE, TMPS_KC_UPDATE, TMPS_KC_POOL_FWD,
