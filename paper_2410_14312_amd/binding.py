@@ -303,13 +303,14 @@ def _within(stream, device):
     return cuda.stream(stream)
 
 
-def _call(fn, device, *args):
-    """fn(..., stream) on a GPU's current stream, with that GPU current."""
+def _call(fn, device, stream, *args):
+    """fn(..., stream) on a GPU's current stream, or on the stream whose handle is given, with that GPU current."""
     torch = _torch()
     cuda = torch.cuda
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are wanted, not on %s" % device)
-    handle = torch._C._cuda_getCurrentRawStream(device.index)   # (current_stream(device).cuda_stream without the object: 0.1 us instead of 1.9)
+    # (current_stream(device).cuda_stream without the object: 0.1 us instead of 1.9)
+    handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else int(stream)
     if device.index == cuda.current_device():
         rc = fn(*args, handle)
     else:
@@ -342,7 +343,7 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
     elif out.dim() != 2 or out.shape[0] != rows or out.shape[1] < width or (out.shape[1] > 1 and out.stride(1) != 1) or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("out: %d rows of at least %d neighbouring %s features on %s are wanted" % (rows, width, x.dtype, x.device))
     d = RotaryDesc(heads, dh, (C.c_int32 * 3)(*pairs), _rotary_flags(interleaved, own_ladders), base)
-    _call(load_library().tmps_rotary, x.device, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
+    _call(load_library().tmps_rotary, x.device, None, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
     return out
 
 
@@ -368,7 +369,7 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
         u = torch.empty(rows, D, dtype=t, device=dev)
     if stats is None:
         stats = torch.empty(rows, 4, dtype=torch.float32, device=dev)
-    _call(load_library().tmps_norm_join_forward, dev, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
+    _call(load_library().tmps_norm_join_forward, dev, None, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
           _operand("r", r, (rows, D), t, dev), _operand("gain", gain, (D,), torch.float32, dev), _operand("scale", scale, (D,), torch.float32, dev),
           _operand("y", y, (rows, D), t, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev),
           _operand("pre_shift", pre_shift, (D,), torch.float32, dev), _operand("u", u, (rows, D), t, dev),
@@ -396,7 +397,7 @@ def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=F
     need = load_library().tmps_norm_join_workspace(rows, D)
     ws = torch.empty(max(need, 4), dtype=torch.uint8, device=dev)
     at = grads.data_ptr()
-    _call(load_library().tmps_norm_join_backward, dev, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
+    _call(load_library().tmps_norm_join_backward, dev, None, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
           _operand("x", x, (rows, wide), t, dev), _operand("r", r, (rows, D), t, dev), _operand("y", y, (rows, D), t, dev),
           _operand("stats", stats, (rows, 4), torch.float32, dev), _operand("gain", gain, (D,), torch.float32, dev),
           _operand("scale", scale, (D,), torch.float32, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev), _operand("dx", dx, (rows, wide), t, dev),
@@ -425,7 +426,7 @@ def distill(logits, labels, ids, teacher, temperature=1.0, alpha=1.0, grad_scale
     d = DistillDesc(classes, k, temperature, alpha, 1.0 / max(rows, 1) if grad_scale is None else grad_scale)
     need = load_library().tmps_distill_workspace(rows, classes)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(load_library().tmps_distill, dev, TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, C.byref(d), rows,
+    _call(load_library().tmps_distill, dev, None, TMPS_BF16_F32MASTER if dtype == "bf16" else TMPS_F32, C.byref(d), rows,
           _operand("logits", logits, (rows, classes), torch.float32, dev), _operand("labels", labels, (rows,), torch.int32, dev), 1,
           _operand("ids", ids, (rows, k), torch.int32, dev), _operand("teacher", teacher, (rows, k), torch.float32, dev), k,
           dlogits.data_ptr() if gradient else None, row_loss.data_ptr(), ws.data_ptr() if need else None, need)

@@ -214,6 +214,8 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
         m = most[0];
     }
     const float teacher = most[1];
+    // (of a slice without a finite logit the sums are those of what its logits are: nothing, or NaN)
+    const float off = MODE == kSliceSums && m == -INFINITY ? 0.0f : m;
     const bool need_s = labelled && !(same && taught);
     // (left to itself the compiler has many pieces' exponentials under way at once, in registers that the row needs: hence the barriers to its scheduling)
 #pragma unroll
@@ -221,10 +223,10 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
         float v[4];
         unpack(raw[i], v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] -= m;
+        for (int e = 0; e < 4; ++e) v[e] -= off;
         raw[i] = pack(v);
     }
-    extra -= m;
+    extra -= off;
     auto add_up = [&](float scale) {
         float t = __builtin_amdgcn_exp2f(extra * scale);
 #pragma unroll

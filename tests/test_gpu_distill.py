@@ -179,6 +179,23 @@ def test_wrong_ids_and_what_cannot_be_learned(C):
     assert torch.equal(g, g1)
 
 
+@pytest.mark.parametrize("rows,C,cut", [(12, 50000, 30000), (3, 200000, 100), (70, 130000, 40000), (9, 3000, 10), (9, 20000, 5)])
+def test_long_runs_of_masked_classes(rows, C, cut):
+    """Whole slices of a row whose logits are minus infinity (classes that the student does not have), and of NaN."""
+    z, labels, ids, teacher = problem(rows, cut, 5, seed=C)
+    wide = torch.full((rows, C), -float("inf"))
+    wide[::2, :cut] = z[::2]
+    wide[1::2, C - cut:] = z[1::2]
+    ids[1::2] += C - cut
+    labels[1::2] += C - cut
+    loss, g = check(wide, labels, ids, teacher, 2.0, 0.6, "f32")
+    assert bool(torch.isfinite(loss).all()) and bool((g.cpu()[wide == -float("inf")] == 0).all())
+    wide[0, cut:] = float("nan")
+    wide[1] = -float("inf")
+    loss, _ = tmps.distill(wide.to(DEV), labels.to(DEV), ids.to(DEV), teacher.to(DEV), temperature=2.0, alpha=0.6)
+    assert bool(torch.isnan(loss[:2]).all()) and bool(torch.isfinite(loss[2:]).all())
+
+
 @pytest.mark.parametrize("C", [50, 7000, 40001])
 def test_large_logits(C):
     """Spread of hundreds: the smallest probabilities vanish, nothing overflows."""
