@@ -320,7 +320,7 @@ int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D, const voi
  * row_loss receives each row's, dlogits (may be NULL; gradient dtype) grad_scale times its gradient w.r.t. the row's fp32 logits z.  ids and teacher hold k entries a row,
  * entry_stride elements apart from row to row, labels (NULL: none) one a row, label_stride apart.  An id of -1 is no entry (its logit is not looked at), a label
  * of -1 no label: a row without entries lacks the first term, one without a label the second, one without both has loss and gradient 0 whatever its logits are.  Entries
- * of the same class add up.  Any other id or label outside the classes gives a NaN loss, and no part in the gradient.  0 <= alpha <= 1; at 0 the teacher, at 1
+ * of the same class add up, one whose logit is minus infinity is none.  Any other id or label outside the classes gives a NaN loss, and no part in the gradient.  0 <= alpha <= 1; at 0 the teacher, at 1
  * the labels are not looked at.  workspace: tmps_distill_workspace bytes (may be 0). */
 typedef struct {
     int32_t classes, k;

@@ -157,7 +157,8 @@ int tmps::check_distill(int64_t classes, int64_t k, float temperature, float alp
     if (classes < 1 || k < 1) return fail(TMPS_EINVAL, "classes and k must be positive");
     if (classes > kDistillMaxClasses) return fail(TMPS_EUNSUPPORTED, "more than %d classes", kDistillMaxClasses);
     if (k > kDistillMaxEntries) return fail(TMPS_EUNSUPPORTED, "more than %d teacher entries a row", kDistillMaxEntries);
-    if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature)) return fail(TMPS_EINVAL, "temperature must be positive");
+    if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature) || !isfinite(temperature * temperature))
+        return fail(TMPS_EINVAL, "temperature must be positive, its inverse and its square finite");
     if (!(alpha >= 0.0f && alpha <= 1.0f)) return fail(TMPS_EINVAL, "alpha must lie in 0..1");
     return TMPS_OK;
 }

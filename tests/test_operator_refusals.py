@@ -82,7 +82,7 @@ def distill(**kw):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(dtype=3), EINVAL), (dict(classes=0), EINVAL), (dict(k=0), EINVAL), (dict(k=1025, es=1025), EUNSUPPORTED), (dict(classes=(1 << 23) + 1), EUNSUPPORTED), (dict(T=0.0), EINVAL), (dict(T=-1.0), EINVAL), (dict(T=float("nan")), EINVAL), (dict(T=1e-45), EINVAL),
+    (dict(dtype=3), EINVAL), (dict(classes=0), EINVAL), (dict(k=0), EINVAL), (dict(k=1025, es=1025), EUNSUPPORTED), (dict(classes=(1 << 23) + 1), EUNSUPPORTED), (dict(T=0.0), EINVAL), (dict(T=-1.0), EINVAL), (dict(T=float("nan")), EINVAL), (dict(T=1e-45), EINVAL), (dict(T=1e30), EINVAL),
     (dict(T=float("inf")), EINVAL), (dict(alpha=-0.1), EINVAL), (dict(alpha=1.5), EINVAL), (dict(alpha=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(rows=-1), EINVAL),
     (dict(z=None), EINVAL), (dict(loss=None), EINVAL), (dict(ids=None), EINVAL), (dict(teacher=None), EINVAL), (dict(es=7), ESHAPE), (dict(ls=0), ESHAPE), (dict(rows=2 ** 60), EUNSUPPORTED),
     (dict(z=M + 2), ESHAPE), (dict(g=M + 2), ESHAPE), (dict(ids=M + 1), ESHAPE), (dict(g=M), EINVAL), (dict(g=M + 400), EINVAL), (dict(loss=3 * M + 4), EINVAL), (dict(loss=5 * M), EINVAL)])
