@@ -31,8 +31,11 @@ class StageCfg(C.Structure):
                 ("lr", C.c_float), ("momentum", C.c_float)]
 
 
+Axes = C.c_int32 * 3
+
+
 class RotaryDesc(C.Structure):
-    _fields_ = [("heads", C.c_int32), ("dh", C.c_int32), ("pairs", C.c_int32 * 3), ("flags", C.c_int32), ("base", C.c_float)]
+    _fields_ = [("heads", C.c_int32), ("dh", C.c_int32), ("pairs", Axes), ("flags", C.c_int32), ("base", C.c_float)]
 
 
 class DistillDesc(C.Structure):
@@ -306,15 +309,15 @@ def _within(stream, device):
 def _call(fn, device, stream, *args):
     """fn(..., stream) on a GPU's current stream, or on the stream whose handle is given, with that GPU current."""
     torch = _torch()
-    cuda = torch.cuda
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are wanted, not on %s" % device)
-    # (current_stream(device).cuda_stream without the object: 0.1 us instead of 1.9)
-    handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else int(stream)
-    if device.index == cuda.current_device():
+    # (current_stream(device).cuda_stream without the object, 0.1 us instead of 1.9, and current_device() of a process that has tensors on a GPU)
+    index = device.index
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else int(stream)
+    if index == torch._C._cuda_getDevice():
         rc = fn(*args, handle)
     else:
-        with cuda.device(device):
+        with torch.cuda.device(device):
             rc = fn(*args, handle)
     if rc < 0:
         _check(rc)
@@ -338,12 +341,15 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
         raise ValueError("pairs: a number for each of three axes is wanted")
     rows = x.shape[0]
     pos = _operand("positions", positions, positions.shape, torch.int32, x.device)
+    out_stride = width
     if out is None:
         out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
     elif out.dim() != 2 or out.shape[0] != rows or out.shape[1] < width or (out.shape[1] > 1 and out.stride(1) != 1) or out.dtype != x.dtype or out.device != x.device:
         raise ValueError("out: %d rows of at least %d neighbouring %s features on %s are wanted" % (rows, width, x.dtype, x.device))
-    d = RotaryDesc(heads, dh, (C.c_int32 * 3)(*pairs), _rotary_flags(interleaved, own_ladders), base)
-    _call(load_library().tmps_rotary, x.device, None, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out.stride(0), pos, positions.shape[0], rows, int(inverse))
+    else:
+        out_stride = out.stride(0)
+    d = RotaryDesc(heads, dh, Axes(*pairs), _rotary_flags(interleaved, own_ladders), base)
+    _call(load_library().tmps_rotary, x.device, None, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out_stride, pos, positions.shape[0], rows, int(inverse))
     return out
 
 
@@ -362,18 +368,26 @@ def norm_join(x, r, gain, scale, pre_gain=None, pre_shift=None, rms=False, gate=
     code = _dtype_code(r)
     if r.dim() != 2:
         raise ValueError("r: [rows, features] is wanted, not %s" % (tuple(r.shape),))
-    (rows, D), t, dev = r.shape, r.dtype, r.device
+    (rows, D), t, dev, f32 = r.shape, r.dtype, r.device, torch.float32
+    # (what is allocated here needs no check)
     if y is None:
         y = torch.empty(rows, D, dtype=t, device=dev)
+        to_y = y.data_ptr()
+    else:
+        to_y = _operand("y", y, (rows, D), t, dev)
     if u is None and pre_gain is not None:
         u = torch.empty(rows, D, dtype=t, device=dev)
+        to_u = u.data_ptr()
+    else:
+        to_u = _operand("u", u, (rows, D), t, dev)
     if stats is None:
-        stats = torch.empty(rows, 4, dtype=torch.float32, device=dev)
+        stats = torch.empty(rows, 4, dtype=f32, device=dev)
+        to_stats = stats.data_ptr()
+    else:
+        to_stats = _operand("stats", stats, (rows, 4), f32, dev)
     _call(load_library().tmps_norm_join_forward, dev, None, code, _join_flags(rms, gate), rows, D, _operand("x", x, (rows, 2 * D if gate else D), t, dev),
-          _operand("r", r, (rows, D), t, dev), _operand("gain", gain, (D,), torch.float32, dev), _operand("scale", scale, (D,), torch.float32, dev),
-          _operand("y", y, (rows, D), t, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev),
-          _operand("pre_shift", pre_shift, (D,), torch.float32, dev), _operand("u", u, (rows, D), t, dev),
-          _operand("stats", stats, (rows, 4), torch.float32, dev))
+          _operand("r", r, (rows, D), t, dev), _operand("gain", gain, (D,), f32, dev), _operand("scale", scale, (D,), f32, dev), to_y,
+          _operand("pre_gain", pre_gain, (D,), f32, dev), _operand("pre_shift", pre_shift, (D,), f32, dev), to_u, to_stats)
     return y, u, stats
 
 
@@ -391,8 +405,14 @@ def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=F
     wide = 2 * D if gate else D
     if dx is None:
         dx = torch.empty(rows, wide, dtype=t, device=dev)
+        to_dx = dx.data_ptr()
+    else:
+        to_dx = _operand("dx", dx, (rows, wide), t, dev)
     if dr is None:
         dr = torch.empty(rows, D, dtype=t, device=dev)
+        to_dr = dr.data_ptr()
+    else:
+        to_dr = _operand("dr", dr, (rows, D), t, dev)
     grads = torch.empty(4, D, dtype=torch.float32, device=dev)
     need = load_library().tmps_norm_join_workspace(rows, D)
     ws = torch.empty(max(need, 4), dtype=torch.uint8, device=dev)
@@ -400,8 +420,7 @@ def norm_join_backward(dy, du, x, r, y, stats, gain, scale, pre_gain=None, rms=F
     _call(load_library().tmps_norm_join_backward, dev, None, code, _join_flags(rms, gate), rows, D, _operand("dy", dy, (rows, D), t, dev), _operand("du", du, (rows, D), t, dev),
           _operand("x", x, (rows, wide), t, dev), _operand("r", r, (rows, D), t, dev), _operand("y", y, (rows, D), t, dev),
           _operand("stats", stats, (rows, 4), torch.float32, dev), _operand("gain", gain, (D,), torch.float32, dev),
-          _operand("scale", scale, (D,), torch.float32, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev), _operand("dx", dx, (rows, wide), t, dev),
-          _operand("dr", dr, (rows, D), t, dev), at, at + 8 * D if du is not None else None, ws.data_ptr(), need)
+          _operand("scale", scale, (D,), torch.float32, dev), _operand("pre_gain", pre_gain, (D,), torch.float32, dev), to_dx, to_dr, at, at + 8 * D if du is not None else None, ws.data_ptr(), need)
     dgain, dscale, dpre_gain, dpre_shift = grads.unbind(0)
     if du is None:
         return dx, dr, dgain, dscale, None, None
