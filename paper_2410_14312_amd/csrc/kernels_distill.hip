@@ -5,7 +5,7 @@
 // Bound by memory: a row of logits is read, a row of gradients written.  Hence a row stays in registers between its largest logit, its two sums and its gradients, each of which takes
 // every logit's exponentials again.  Of 8192 rows of 32000 logits, 64 entries, bf16 gradients: 317 us, 4.6 TB/s (a copy of as many bytes 285 us; 291 us where T is 1 and one exponential
 // does for both, 253 us without a teacher); the same of 1, 16, 256 entries: 306, 306, 343 us; 4096 rows of 16000 logits: 79 us, 5.0 TB/s; 16384 rows of 1000: 26 us; 2048 rows of
-// 50257: 176 us (one workgroup to a compute unit: nothing runs beside its loads); 64 rows of 100: 7 us, mostly the launch.
+// 50257: 136 us, 4.2 TB/s; of 65000 207 us, 3.6 TB/s (one workgroup to a compute unit: nothing runs beside its loads); 64 rows of 100: 7 us, mostly the launch.
 #include "kernels.h"
 #include "pieces.hip.h"
 #include "wave.hip.h"
@@ -98,18 +98,20 @@ __device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) {
 }
 __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { store16_any(p, pack(v)); }
 
-// (a base that all lanes share and a 32-bit offset: no address in registers)
-template <typename T> __device__ __forceinline__ T* at_bytes(T* base, uint32_t bytes) { return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes); }
+// (A base that all lanes share, one for every piece, and a 32-bit offset, the same for all pieces: no address and no offset in registers from a piece's load to its store.)
+template <typename T> __device__ __forceinline__ T* at_bytes(T* base, uint32_t bytes) { return (T*)((char*)base + bytes); }
 
-// A team to a row (or a slice of one), whose logits it keeps in registers: NV pieces of 4 a thread, and of the up to three behind the last whole piece one to a lane.
+// A team to a row (or a slice of one), whose logits it keeps in registers and LDS: NV pieces of 4 a thread and NL in LDS, which nobody else touches, and of the up to three behind the
+// last whole piece one to a lane.
 // What a thread has no logit for is minus infinity: pieces are loaded, compared and added up without a branch.  The classes of the entries and of the label get their gradients
 // once more, behind the others: the first entry of a class writes it, with what all of them and the label take away.
-template <typename T, int TEAM, int NV, int MODE>
+template <typename T, int TEAM, int NV, int NL, int MODE>
 __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 16 ? 4 : 2) void distill_rows_kernel(Distill d, Slices cut, float* sums, int64_t unit0) {
     constexpr int kTeams = TEAM == 64 ? 4 : 1;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __attribute__((aligned(16))) float entries[];   // of every team: classes, exponentials, the student's logits
     __shared__ float red[2][3 * 16];
+    __shared__ uint4 stash[NL > 0 ? NL * TEAM : 1];
     Reduce<TEAM> reduce{red};
     const int lane = threadIdx.x % TEAM, team = TEAM == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, k = d.k, C = d.classes;
     const float over_t = 1.0f / d.temperature, alpha = d.alpha, at_q = kLog2e * over_t, at_s = kLog2e;
@@ -156,8 +158,8 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
             if (g) {
                 const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if ((i * TEAM + lane) * 4 < whole) store4(at_bytes(g, (i * TEAM + lane) * 4 * (int)sizeof(T)), zero);
+                for (int i = 0; i < NV + NL; ++i)
+                    if (lane * 4 < whole - i * TEAM * 4) store4(at_bytes(g + i * TEAM * 4, lane * 4 * (int)sizeof(T)), zero);
                 if (lane < n - whole) g[whole + lane] = from_f32<T>(0.0f);
             }
             if (slice == 0 && lane == 0) d.row_loss[row] = bad ? NAN : 0.0f;
@@ -167,14 +169,41 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     // (the student's logits of the entries before the row's: what is requested first is there first)
     const bool first = MODE != kSliceSums && taught && lane < k && ids[lane] >= 0;
     const float z_first = first ? zrow[ids[lane]] : 0.0f, z_label = MODE != kSliceSums && labelled ? zrow[label] : 0.0f;
-    uint4 raw[NV];
+    uint4 raw[NV], aside[NL > 0 ? NL : 1];
     const float* const z = zrow + from;
-    if (whole > 0) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) raw[i] = load16_any(reinterpret_cast<const char*>(z) + (uint32_t)min((i * TEAM + lane) * 16, whole * 4 - 16));
-    }
-    float extra = lane < n - whole ? z[whole + lane] : -INFINITY;
+    float extra = -INFINITY;
     float kl = 0.0f, most[2] = {-INFINITY, 0.0f};   // the row's largest logit; the sum of the teacher's exponentials
+    auto request = [&](uint4& u, int i) {
+        const int last = whole * 4 - 16, base = min(i * TEAM * 16, last);
+        u = load16_any(at_bytes(reinterpret_cast<const char*>(z) + base, (uint32_t)min(lane * 16, last - base)));
+    };
+    auto finite = [&](uint4& u, int i) {
+        const bool any = lane * 4 < whole - i * TEAM * 4;
+        float v[4];
+        unpack(u, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = any ? v[e] : -INFINITY;
+        most[0] = fmaxf(most[0], fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+        u = pack(v);
+    };
+    if (lane < n - whole) extra = z[whole + lane];
+    if constexpr (NL > 0) {   // (at most NV pieces under way: the registers that the row has; such a row has whole pieces)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) request(aside[i], NV + i);
+#pragma unroll
+        for (int i = 0; i < NV - NL; ++i) request(raw[i], i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            finite(aside[i], NV + i);
+            stash[i * TEAM + lane] = aside[i];
+            request(raw[NV - NL + i], NV - NL + i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else if (whole > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) request(raw[i], i);
+    }
     if (MODE != kSliceSums) {
         if (taught) {
             for (int j = lane; j < k; j += TEAM) {
@@ -189,15 +218,7 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     }
     float m, sq = 0.0f, ss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const bool any = (i * TEAM + lane) * 4 < whole;
-        float v[4];
-        unpack(raw[i], v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = any ? v[e] : -INFINITY;
-        most[0] = fmaxf(most[0], fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
-        raw[i] = pack(v);
-    }
+    for (int i = 0; i < NV; ++i) finite(raw[i], i);
     most[0] = fmaxf(most[0], extra);
     if constexpr (MODE == kSliceRest) {
         // (at most 256 slices: one to a thread)
@@ -227,12 +248,21 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
         raw[i] = pack(v);
     }
     extra -= off;
+    auto piece = [&](int i, float (&v)[4]) {   // a piece's logits minus the largest
+        if (i < NV) {
+            unpack(raw[i], v);
+        } else {
+            unpack(stash[(i - NV) * TEAM + lane], v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] -= off;
+        }
+    };
     auto add_up = [&](float scale) {
         float t = __builtin_amdgcn_exp2f(extra * scale);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < NV + NL; ++i) {
             float v[4];
-            unpack(raw[i], v);
+            piece(i, v);
 #pragma unroll
             for (int e = 0; e < 4; ++e) t += __builtin_amdgcn_exp2f(v[e] * scale);
             __builtin_amdgcn_sched_barrier(0);
@@ -275,12 +305,12 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     };
     auto write = [&](bool two) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < NV + NL; ++i) {
             float v[4];
-            unpack(raw[i], v);
+            piece(i, v);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = gradient(v[e], two);
-            if ((i * TEAM + lane) * 4 < whole) store4(at_bytes(g, (i * TEAM + lane) * 4 * (int)sizeof(T)), v);
+            if (lane * 4 < whole - i * TEAM * 4) store4(at_bytes(g + i * TEAM * 4, lane * 4 * (int)sizeof(T)), v);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -343,12 +373,12 @@ size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes) {
 }
 
 // (A launch takes no loop over rows: what a lane has in each of them would be kept in registers that the row needs.)
-template <typename T, int TEAM, int NV, int MODE> static hipError_t launch_rows(const Distill& d, const Slices& cut, float* ws, hipStream_t s) {
+template <typename T, int TEAM, int NV, int MODE, int NL = 0> static hipError_t launch_rows(const Distill& d, const Slices& cut, float* ws, hipStream_t s) {
     constexpr int teams = TEAM == 64 ? 4 : 1;
     const int64_t units = d.rows * cut.slices, at_once = int64_t(teams) << 20;
     for (int64_t unit = 0; unit < units; unit += at_once) {
         const int64_t n = units - unit < at_once ? units - unit : at_once;
-        hipLaunchKernelGGL((distill_rows_kernel<T, TEAM, NV, MODE>), dim3((unsigned)((n + teams - 1) / teams)), dim3(TEAM == 64 ? 256 : TEAM), (size_t)teams * entry_words(d.k) * 4, s, d, cut,
+        hipLaunchKernelGGL((distill_rows_kernel<T, TEAM, NV, NL, MODE>), dim3((unsigned)((n + teams - 1) / teams)), dim3(TEAM == 64 ? 256 : TEAM), (size_t)teams * entry_words(d.k) * 4, s, d, cut,
                            ws, unit);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -371,7 +401,9 @@ template <typename T> static hipError_t distill_type(const Distill& d, float* ws
     const int C = d.classes;
     // A wave to a row needs no barriers: 16384 rows of 1000 logits take 26 us, with 256 threads 58 us, rows of 2000 39 and 65 us.  With many entries it loses: 4096 rows of 2000,
     // 10 entries 15 and 21 us, 500 entries 32 and 31 us, 1000 entries 64 and 40 us.  The other teams, where two were measured: 8192 rows of 12000 by 256 threads 122 us, 512 133 us;
-    // of 32000 by 512 317 us, 1024 (fewer registers to each, some spilled) 366 us; 2048 of 65000 by 512 202 us, 1024 206 us; of 90000 by 1024 329 us, 512 364 us, in slices 350 us.
+    // of 32000 by 512 317 us, 1024 (fewer registers to each, some spilled) 366 us; 2048 of 65000 by 512 202 us, 1024 206 us; of 90000 by 1024 329 us
+    // (270 since a lane's offset is one for all pieces), 512 364 us, in slices 350 us.  Up to 51200 classes part of the row lies in LDS and a compute unit holds two rows: 2048 of 50257 136 us,
+    // of 40000 111, by registers alone 176 and 159.  (Wider rows held so, 22 or 24 pieces in registers, spill: 2048 of 63000 235 to 282 us, by registers alone 204.)
     if (d.k <= 256) {
         if (C <= 256) return launch_rows<T, 64, 1, kWholeRows>(d, cut, ws, s);
         if (C <= 512) return launch_rows<T, 64, 2, kWholeRows>(d, cut, ws, s);
@@ -382,6 +414,7 @@ template <typename T> static hipError_t distill_type(const Distill& d, float* ws
     if (C <= 8192) return launch_rows<T, 256, 8, kWholeRows>(d, cut, ws, s);
     if (C <= 16384) return launch_rows<T, 256, 16, kWholeRows>(d, cut, ws, s);
     if (C <= 32768) return launch_rows<T, 512, 16, kWholeRows>(d, cut, ws, s);
+    if (C <= 51200) return launch_rows<T, 512, 16, kWholeRows, 9>(d, cut, ws, s);
     if (C <= 65536) return launch_rows<T, 512, 32, kWholeRows>(d, cut, ws, s);
     return launch_rows<T, 1024, 24, kWholeRows>(d, cut, ws, s);
 }

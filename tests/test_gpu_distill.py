@@ -92,7 +92,7 @@ def check(z, labels, ids, teacher, T, alpha, dtype, scale=None):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,C,k", [(1, 1, 1), (3, 2, 2), (5, 10, 3), (64, 100, 10), (9, 255, 64), (7, 256, 256), (4, 1000, 100), (33, 2048, 64), (6, 2052, 33), (5, 4099, 5),
                                       (3, 8192, 300), (9, 16384, 64), (3, 16388, 64), (300, 5000, 20), (2, 32000, 1024), (270, 32000, 8),
-                                      (70, 17000, 30), (67, 24580, 200), (68, 32764, 64), (70, 33000, 300), (2, 32771, 50), (1, 65536, 64), (5, 70001, 100), (66, 65540, 100), (65, 98304, 7), (3, 131072, 7),
+                                      (70, 17000, 30), (67, 24580, 200), (68, 32764, 64), (70, 33000, 300), (66, 51200, 64), (66, 51201, 20), (67, 49999, 1024), (2, 32771, 50), (1, 65536, 64), (5, 70001, 100), (66, 65540, 100), (65, 98304, 7), (3, 131072, 7),
                                       (1, 200000, 64)])
 def test_sizes(dtype, rows, C, k):
     z, labels, ids, teacher = problem(rows, C, k, seed=C + k)
