@@ -306,3 +306,34 @@ def test_rows_beyond_32_bit_offsets():
     dx, dr, dgain, _, _, _ = tmps.norm_join_backward(r, None, x, y, None, st, p["gain"], p["scale"], rms=True, dr=r)
     want = tmps.norm_join_backward(p["dy"], None, p["x"], one, None, st1, p["gain"], p["scale"], rms=True)
     assert torch.equal(dx[-1], want[0][0]) and torch.equal(dr[-1], want[1][0]) and torch.equal(dgain, want[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,D", [(3, 1), (7, 5), (40, 129), (33, 1001), (9, 4097), (270, 5003), (3, 8193), (2, 16383)])
+def test_memory_around_results_and_workspace(dtype, rows, D):
+    """Results and the workspace between guards, at addresses of whole elements: what is not theirs stays as it was, and results are those of arrays of their own."""
+    from paper_2410_14312_amd import binding
+    p = problem(rows, D, dtype, False, True, True, seed=D)
+    t, flags = TYPES[dtype], binding.TMPS_FLAG_GATE
+    code = binding.TMPS_F32 if dtype == "f32" else binding.TMPS_BF16_F32MASTER
+    y, u, stats = tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], p["pre_gain"], p["pre_shift"], gate=True)
+    want = tmps.norm_join_backward(p["dy"], p["du"], p["x"], p["r"], y, stats, p["gain"], p["scale"], pre_gain=p["pre_gain"], gate=True)
+    guarded = []
+
+    def between(shape, dt):
+        n = int(np.prod(shape))
+        buf = torch.full((n + 130,), 7.0, dtype=dt, device=DEV)
+        guarded.append((buf, n))
+        return buf[65:65 + n].view(shape)
+    y2, u2, st2 = between((rows, D), t), between((rows, D), t), between((rows, 4), torch.float32)
+    tmps.norm_join(p["x"], p["r"], p["gain"], p["scale"], p["pre_gain"], p["pre_shift"], gate=True, y=y2, u=u2, stats=st2)
+    assert torch.equal(y2, y) and torch.equal(u2, u) and torch.equal(st2, stats)
+    need = binding.lib().tmps_norm_join_workspace(rows, D)
+    dx, dr, own, pre = between((rows, 2 * D), t), between((rows, D), t), between((2 * D,), torch.float32), between((2 * D,), torch.float32)
+    ws = between((need // 4,), torch.float32)
+    binding._call(binding.lib().tmps_norm_join_backward, p["dy"].device, None, code, flags, rows, D, *(v.data_ptr() for v in (
+        p["dy"], p["du"], p["x"], p["r"], y, stats, p["gain"], p["scale"], p["pre_gain"], dx, dr, own, pre, ws)), need)
+    for got, w in zip((dx, dr, own[:D], own[D:], pre[:D], pre[D:]), want):
+        assert torch.equal(got, w)
+    for buf, n in guarded:
+        assert bool((buf[:65] == 7.0).all()) and bool((buf[65 + n:] == 7.0).all())

@@ -58,3 +58,16 @@ def test_a_stream_for_tensors_on_the_host_is_refused():
     z = torch.zeros(4, 4)
     with pytest.raises(ValueError):
         tmps.norm_join(z, z, z[0], z[0], stream=torch.cuda.Stream())
+
+
+@pytest.mark.parametrize("name", ["norm_join_backward", "distill"])
+def test_calls_on_two_streams_at_once(name):
+    """Calls whose kernels may overlap, each with a workspace of its own."""
+    call = calls()[name]
+    want = call()
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [call(stream=sides[k % 2]) for k in range(20)]
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
