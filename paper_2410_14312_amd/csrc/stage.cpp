@@ -456,7 +456,6 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
         for (int t : {L.in_t, second_source(L)})
             if (t >= 0 && !kept(t)) gmax = std::max(gmax, st.layers[t].out_elems);
         if (L.d.kind == TMPS_NORMJOIN && st.readers[L.in_t + 1] > 1) gmax = std::max(gmax, L.in_elems);
-        if (L.d.kind == TMPS_NORMJOIN) gmax = std::max(gmax, L.out_elems);   // (the gradient of a residual that is the stage input, until the end of the pass)
     }
 
     // scratch: gradient buffers of M rows, two boundary-gradient buffers, fp32 workspace
@@ -918,6 +917,16 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
 
     const tmps_stage::GraphKey key = {2, (uintptr_t)g0, (uintptr_t)x0, (uintptr_t)dy, (uintptr_t)dx, (uintptr_t)flags,
                                       (uintptr_t)st->master, (uintptr_t)st->wcopy};
+    // A caller may have the gradient w.r.t. the input written over the upstream gradient or the input: then every kernel that reads
+    // those comes, as they are called, before the one that writes.
+    const size_t dx_bytes = (size_t)M * st->in_elems * st->asz;
+    auto over_operand = [&]() {
+        return overlap(dx, dx_bytes, dy, (size_t)M * st->out_elems * st->asz) || overlap(dx, dx_bytes, x0, (size_t)M * st->in_elems * st->in_esize);
+    };
+    // A gradient that is added up from several layers is begun long before the last kernel has read them: it is formed in memory of the stage then and copied at the end.
+    void* const dx_wanted = dx;
+    if (std::any_of(st->layers.begin(), st->layers.end(), [](const LayerRT& L) { return L.d.kind == TMPS_NORMJOIN && L.in_b < 0; }) && over_operand()) dx = stage_dxout(st, 0);
+    const bool in_order = over_operand();
     return run_or_replay(st, key, s, [&]() -> int {
     // Gradients are kept per result: grads[t + 1] is the gradient w.r.t. the result of layer t (t = -1: the stage
     // input).  Layers are visited last to first; every layer that reads a result contributes to its gradient: the
@@ -1011,10 +1020,6 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
         G.masked = true;   // (by the kernel that wrote it)
         --remaining[t + 1];
     };
-    // A caller may have the gradient w.r.t. the input written over the upstream gradient or the input: then every kernel that reads
-    // those comes, as they are called, before the one that writes.
-    const size_t dx_bytes = (size_t)M * st->in_elems * st->asz;
-    const bool in_order = overlap(dx, dx_bytes, dy, (size_t)M * st->out_elems * st->asz) || overlap(dx, dx_bytes, x0, (size_t)M * st->in_elems * st->in_esize);
     // hand an existing gradient (g) to result t as its contribution, without a kernel when it is the first
     auto share = [&](int t, const Grad& g) -> int {
         if (t < 0 && !dx) return TMPS_OK;
@@ -1091,16 +1096,7 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
         if (rc != TMPS_OK) return rc;
         const int beside = X.add ? take() : -1;   // (others have given that result a gradient: this one's is added behind the launch)
         if (X.add && beside < 0) return fail(TMPS_EUNSUPPORTED, "out of gradient buffers (too many open residual connections)");
-        if (J.in_b < 0 && dx && in_order) {
-            // (dx may be what later kernels still read: the residual's gradient waits in memory of the pass)
-            const Grad& G = grads[0];
-            R.wanted = true;
-            R.add = G.set ? G.ptr : nullptr;
-            if ((R.buf = take()) < 0) return fail(TMPS_EUNSUPPORTED, "out of gradient buffers (too many open residual connections)");
-            R.dst = gbuf[R.buf];
-        } else if ((rc = target(J.in_b, R)) != TMPS_OK) {
-            return rc;
-        }
+        if ((rc = target(J.in_b, R)) != TMPS_OK) return rc;
         NormJoinBackward j{};
         j.dy = dy_.set ? dy_.ptr : nullptr;
         j.x = st->out_ptr(st->layers[J.in_t], row0);
@@ -1347,6 +1343,7 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     int rc = flush_group();
     if (rc != TMPS_OK) return rc;
     TMPS_GEMM(reduce_all(sums, s));
+    if (dx != dx_wanted) TMPS_RUN(kcCopy, s, copy_bytes(dx_wanted, dx, dx_bytes, s));
     return TMPS_OK;
     });   // (free_slots releases the group)
 }
