@@ -925,7 +925,7 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     };
     // A gradient that is added up from several layers is begun long before the last kernel has read them: it is formed in memory of the stage then and copied at the end.
     void* const dx_wanted = dx;
-    if (std::any_of(st->layers.begin(), st->layers.end(), [](const LayerRT& L) { return L.d.kind == TMPS_NORMJOIN && L.in_b < 0; }) && over_operand()) dx = stage_dxout(st, 0);
+    if (st->readers[0] > 1 && over_operand()) dx = stage_dxout(st, 0);
     const bool in_order = over_operand();
     return run_or_replay(st, key, s, [&]() -> int {
     // Gradients are kept per result: grads[t + 1] is the gradient w.r.t. the result of layer t (t = -1: the stage
@@ -1025,7 +1025,7 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
         if (t < 0 && !dx) return TMPS_OK;
         Grad& G = grads[t + 1];
         const int64_t n = (int64_t)M * st->tensor_elems(t);
-        if (t < 0 && (G.set || in_order || remaining[0] == 1)) {
+        if (t < 0 && (G.set || remaining[0] == 1)) {
             if (G.set) TMPS_GEMM(resadd_forward(dt, G.ptr, g.ptr, dx, n, 0, s));
             else TMPS_RUN(kcCopy, s, copy_bytes(dx, g.ptr, (size_t)n * st->asz, s));
             release(G.buf);

@@ -29,6 +29,7 @@ static tmps_layer_desc L(int kind, std::initializer_list<int> dims, int flags = 
 }
 static unsigned rnd_state = 4242;
 static int rnd(int n) {
+    if (n < 1) return 0;
     rnd_state = rnd_state * 1664525u + 1013904223u;
     return (int)((rnd_state >> 8) % (unsigned)n);
 }
@@ -213,10 +214,10 @@ int main(int argc, char** argv) {
             for (int it = 0; it < 4000; ++it) {
                 Layers ls;
                 const int n = 1 + rnd(10);
-                for (int i = 0; i < n; ++i) switch (rnd(8)) {
+                for (int i = 0; i < n; ++i) switch (ls.empty() && rnd(2) ? 0 : rnd(8)) {
                         case 0: ls.push_back(L(TMPS_LAYERNORM, {D, S}, rnd(2) ? TMPS_FLAG_RMS : 0)); break;
-                        case 1: case 2: ls.push_back(join(2 + rnd(i + 1), rnd(2) ? TMPS_FLAG_RMS : 0)); break;
-                        case 3: case 4: ls.push_back(add(2 + rnd(i + 1))); break;
+                        case 1: case 2: ls.push_back(join(2 + rnd((int)ls.size()), rnd(2) ? TMPS_FLAG_RMS : 0)); break;
+                        case 3: case 4: ls.push_back(add(2 + rnd((int)ls.size()))); break;
                         case 5: ls.push_back(wide); ls.push_back(turned); ls.push_back(narrow); break;
                         case 6: ls.push_back(L(TMPS_LINEAR, {D, D, rnd(4) ? 0 : 1 + rnd(3), S})); break;
                         default: ls.push_back(dense);

@@ -22,3 +22,7 @@ def run(driver, which):
 
 def test_joins_of_the_stage_input(driver):
     run(driver, "joins")
+
+
+def test_additions_of_the_stage_input(driver):
+    run(driver, "additions")
