@@ -219,7 +219,7 @@ int tmps_forward_micro_static(tmps_stage* stage, int slot, const void* x, void* 
  * gradient of the average of the N micro-batch losses) is propagated through the layers in
  * reverse using the stashed activations and the weights AS THEY ARE NOW; weight gradients are
  * summed over the N micro-batches into `state`; dx (device, M rows of the input shape; may be
- * NULL) receives the gradient w.r.t. the stage input.  Frees the slots, also when the pass fails after its arguments
+ * NULL, and may lie over dy or over the inputs) receives the gradient w.r.t. the stage input.  Frees the slots, also when the pass fails after its arguments
  * were accepted (TMPS_EUNSUPPORTED, TMPS_EHIP): the gradients are then incomplete and tmps_update must not follow. */
 int tmps_backward(tmps_stage* stage, const int* slots, int n_slots, const void* dy, void* dx,
                   void* hip_stream);

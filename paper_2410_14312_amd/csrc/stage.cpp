@@ -923,9 +923,11 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     auto over_operand = [&]() {
         return overlap(dx, dx_bytes, dy, (size_t)M * st->out_elems * st->asz) || overlap(dx, dx_bytes, x0, (size_t)M * st->in_elems * st->in_esize);
     };
-    // A gradient that is added up from several layers is begun long before the last kernel has read them: it is formed in memory of the stage then and copied at the end.
+    // A gradient that is added up from several layers is begun long before the last kernel has read them, and one kernel cannot write over the dy that all of its workgroups read
+    // (rotary positions can, where the two are the same): it is formed in memory of the stage then and copied at the end.
     void* const dx_wanted = dx;
-    if (st->readers[0] > 1 && over_operand()) dx = stage_dxout(st, 0);
+    const bool one_kernel = st->layers.size() == 1 && !(st->layers[0].d.kind == TMPS_ROTARY && dx == dy);
+    if ((st->readers[0] > 1 || one_kernel) && over_operand()) dx = stage_dxout(st, 0);
     const bool in_order = over_operand();
     return run_or_replay(st, key, s, [&]() -> int {
     // Gradients are kept per result: grads[t + 1] is the gradient w.r.t. the result of layer t (t = -1: the stage
@@ -1277,8 +1279,6 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
                 if ((rc = target(t_in, T)) != TMPS_OK) return rc;
                 if (!T.wanted) break;
                 if (T.add) return fail(TMPS_EUNSUPPORTED, "rotary positions on a shared input");
-                const size_t bytes = (size_t)M * L.in_elems * st->asz;
-                if (T.dst != g.ptr && overlap(T.dst, bytes, g.ptr, bytes)) return fail(TMPS_EINVAL, "dx overlaps dy without being dy");
                 TMPS_GEMM(rotary(dt, rotary_of(L.d, M, g.ptr, T.dst, true), s));
                 commit(t_in, T);
                 break;

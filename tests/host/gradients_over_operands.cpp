@@ -81,14 +81,15 @@ struct Result {
                                                 (grads.empty() || !memcmp(grads.data(), o.grads.data(), grads.size() * 4))));
     }
 };
-enum Over { kApart, kOverDy, kOverX };
+enum Over { kApart, kOverDy, kOverX, kAcrossDy };   // kAcrossDy: from the middle of dy on
 static Result run(const Layers& ls, int borrow, Over over, const Numbers& params, const Numbers& x0, const Numbers& dy0) {
     Result r;
     Stage st(ls, borrow);
     if (!st.st) return r;
     Numbers x = x0, dy = dy0, dx(x0.size());
+    if (over == kAcrossDy) dy.resize(dy.size() + x0.size());
     st.forward(params, x);
-    float* const to = over == kApart ? dx.data() : over == kOverDy ? dy.data() : x.data();
+    float* const to = over == kApart ? dx.data() : over == kOverDy ? dy.data() : over == kOverX ? x.data() : dy.data() + dy0.size() / 2;
     r.rc = st.backward(dy, to);
     r.dx.assign(to, to + x0.size());
     r.grads = st.grads();
@@ -117,9 +118,9 @@ static bool same(const Layers& ls, const char* what, bool must_pass) {
     const Result want = run(ls, 1, kApart, params, x, dy);
     expect(!must_pass || want.rc == TMPS_OK, what);
     for (int borrow : {0, 1})
-        for (Over over : {kOverDy, kOverX}) {
+        for (Over over : {kOverDy, kOverX, kAcrossDy}) {
             if (over == kOverDy && dy.size() != x.size()) continue;
-            expect(run(ls, borrow, over, params, x, dy) == want, std::string(what) + (over == kOverDy ? ", dx over dy" : ", dx over x"));
+            expect(run(ls, borrow, over, params, x, dy) == want, std::string(what) + (over == kOverDy ? ", dx over dy" : over == kOverX ? ", dx over x" : ", dx across the end of dy"));
         }
     return want.rc == TMPS_OK;
 }

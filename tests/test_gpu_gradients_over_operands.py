@@ -66,3 +66,30 @@ def test_a_convolution_of_the_stage_input_beside_others(dtype, in_place):
         torch.cuda.synchronize()
         got.append((dx.clone(), st._flat(1, 1).clone()))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and float(got[0][0].float().abs().max()) > 0
+
+
+@both
+@over
+@pytest.mark.parametrize("kind", ["linear", "norm", "conv"])
+def test_a_stage_of_one_layer(dtype, in_place, kind):
+    """One kernel's workgroups read all of what the result lies over: bit for bit what separate arrays give, at a size of many workgroups."""
+    import torch
+    from paper_2410_14312_amd import Stage
+
+    d, rows, M = 256, 64, 8
+    specs, shapes = {"linear": ([linear(d, d, False, rows=rows)], {"w": (d, d), "b": (d,)}), "norm": ([layernorm(d, rows)], {"w": (d,), "b": (d,)}),
+                     "conv": ([conv(8, 8, d, d, relu=False)], {"w": (d, 3, 3, d), "b": (d,)})}[kind]
+    rng = np.random.default_rng(6)
+    p = [{k: (0.05 * rng.standard_normal(v)).astype(np.float32) for k, v in shapes.items()}]
+    x, dy = (rng.standard_normal((M, rows * d)).astype(np.float32) for _ in range(2))
+    got = []
+    for place in (None, in_place):
+        st = Stage(specs, dtype, M, 1, 1, 0.1, 0.9, borrow_input=True)
+        st.set_params(p)
+        xd, dyd = (torch.from_numpy(a).to(st.act_dtype).to(st.device) for a in (x, dy))
+        dx = {None: torch.empty_like(xd), "dy": dyd, "x": xd}[place]
+        st.forward_micro(0, xd)
+        st.backward([0], dy=dyd, dx=dx)
+        torch.cuda.synchronize()
+        got.append((dx.clone(), st._flat(1, 1).clone()))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])

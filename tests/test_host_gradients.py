@@ -26,3 +26,11 @@ def test_joins_of_the_stage_input(driver):
 
 def test_additions_of_the_stage_input(driver):
     run(driver, "additions")
+
+
+def test_stages_of_one_layer(driver):
+    run(driver, "alone")
+
+
+def test_random_layers(driver):
+    run(driver, "random")
