@@ -458,6 +458,9 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
         if (L.d.kind == TMPS_NORMJOIN && st.readers[L.in_t + 1] > 1) gmax = std::max(gmax, L.in_elems);
     }
 
+    for (const LayerRT& L : st.layers)   // (a contribution that waits beside what others have given)
+        if (L.d.kind == TMPS_ROTARY && st.readers[L.in_t + 1] > 1) gmax = std::max(gmax, L.in_elems);
+
     // scratch: gradient buffers of M rows, two boundary-gradient buffers, fp32 workspace
     size_t o = 0;
     st.n_gbuf = any_join ? 6 : (any_skip ? 4 : 2);
@@ -1278,8 +1281,17 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
                 }
                 if ((rc = target(t_in, T)) != TMPS_OK) return rc;
                 if (!T.wanted) break;
-                if (T.add) return fail(TMPS_EUNSUPPORTED, "rotary positions on a shared input");
-                TMPS_GEMM(rotary(dt, rotary_of(L.d, M, g.ptr, T.dst, true), s));
+                if (!T.add) {
+                    TMPS_GEMM(rotary(dt, rotary_of(L.d, M, g.ptr, T.dst, true), s));
+                } else {
+                    // (others have given that result a gradient: this one's, rounded to its type as theirs, is added behind the launch)
+                    const bool mine = g.buf >= 0 && refs[g.buf] == 1;
+                    const int beside = mine ? g.buf : take();
+                    if (beside < 0) return fail(TMPS_EUNSUPPORTED, "out of gradient buffers (too many open residual connections)");
+                    TMPS_GEMM(rotary(dt, rotary_of(L.d, M, g.ptr, gbuf[beside], true), s));
+                    TMPS_GEMM(resadd_forward(dt, T.add, gbuf[beside], T.dst, (int64_t)M * L.in_elems, 0, s));
+                    if (!mine) release(beside);
+                }
                 commit(t_in, T);
                 break;
             }

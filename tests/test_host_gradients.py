@@ -34,3 +34,7 @@ def test_stages_of_one_layer(driver):
 
 def test_random_layers(driver):
     run(driver, "random")
+
+
+def test_rotary_positions_on_a_shared_input(driver):
+    run(driver, "rotary")
