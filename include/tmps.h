@@ -282,7 +282,7 @@ int tmps_update(tmps_stage* stage, void* hip_stream);
  * What stands between the contractions of a transformer's stage, for programs that call it over arrays of their own: rotary positions, the norms around a
  * block, a distillation loss.  Activations and their gradients are of `dtype` (fp32, or bf16 with TMPS_BF16_F32MASTER), parameters, their gradients, statistics and
  * losses fp32; sums are fp32.  Rows are contiguous unless a stride (in elements) is given.  All pointers are device memory of the stream's device, on whole elements (on
- * 16 bytes and with widths of whole 8 elements the calls are faster); workspaces belong to one call at a time.  Zero rows are nothing to do (arrays of rows may then be
+ * 16 bytes and with widths of whole 8 elements the calls are faster); workspaces belong to one call at a time, and one of the bytes asked for some rows is enough for fewer.  Zero rows are nothing to do (arrays of rows may then be
  * NULL; gradients of parameters, where given, are zeros).  Errors: TMPS_EINVAL, TMPS_ESHAPE, TMPS_EUNSUPPORTED, TMPS_ECAP (workspace too small), TMPS_EHIP. */
 
 /* Rotary positions with several axes (time, height, width).  Each of the `heads` heads of dh features that begin a row has pairs[0] + pairs[1] + pairs[2] pairs of

@@ -233,6 +233,7 @@ struct NormJoinBackward {
 };
 TMPS_OPTIONAL hipError_t norm_join_backward(int dtype, const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s);
 TMPS_OPTIONAL size_t norm_join_part_elems(int64_t rows, int D);
+size_t norm_join_part_elems_up_to(int64_t rows, int D);   // what any number of rows up to `rows` needs
 
 // y[row] = wte[tok[row]] + wpe[row % S] (tables in the contraction dtype), and the table gradients
 // (fp32; dwte cleared, then every occurring token's rows of dy added in row order, no atomic adds; dwpe summed over the batch).
@@ -269,6 +270,7 @@ struct Distill {
 };
 TMPS_OPTIONAL hipError_t distill(int dtype, const Distill& d, float* ws, hipStream_t s);
 TMPS_OPTIONAL size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes);
+size_t distill_workspace_elems_up_to(int64_t rows, int classes);   // what any number of rows up to `rows` needs, each its own plan
 TMPS_OPTIONAL int check_distill(int64_t classes, int64_t k, float temperature, float alpha);   // TMPS_OK, or the refusal
 // out[0] = scale * sum(in[0..n))   (deterministic single-block tree)
 hipError_t reduce_scaled_sum(const float* in, int n, float scale, float* out, hipStream_t s);

@@ -6,6 +6,8 @@
 // every logit's exponentials again.  Of 8192 rows of 32000 logits, 64 entries, bf16 gradients: 317 us, 4.6 TB/s (a copy of as many bytes 285 us; 291 us where T is 1 and one exponential
 // does for both, 253 us without a teacher); the same of 1, 16, 256 entries: 306, 306, 343 us; 4096 rows of 16000 logits: 79 us, 5.0 TB/s; 16384 rows of 1000: 26 us; 2048 rows of
 // 50257: 136 us, 4.2 TB/s; of 65000 207 us, 3.6 TB/s (one workgroup to a compute unit: nothing runs beside its loads); 64 rows of 100: 7 us, mostly the launch.
+#include <algorithm>
+
 #include "kernels.h"
 #include "pieces.hip.h"
 #include "wave.hip.h"
@@ -355,10 +357,11 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
 // Rows of more than 98304 logits are cut into slices that registers hold (1024 rows of 131072: 255 us), and few wide rows into as many as give every compute unit eight: one row of
 // 98304 logits takes 13 us, whole 24, 64 rows 20 and 31; 8 rows of 50257 14 and 17; 8 rows of 32000 15 and 12.  (48 rows of 131071: 19 us, with two to a compute unit 26.)
 constexpr int kWholeMax = 98304, kSliceMax = 32768;
+constexpr int64_t kFewRows = 64;
 static Slices cut_rows(int64_t rows, int classes) {
     const int64_t fit = classes > kWholeMax ? (classes + kSliceMax - 1) / kSliceMax : 1;
     int64_t slices = fit;
-    if (rows <= 64 && classes > kSliceMax) {
+    if (rows <= kFewRows && classes > kSliceMax) {
         const int64_t wanted = (2048 + rows - 1) / rows, most = (classes + 4095) / 4096 < 256 ? (classes + 4095) / 4096 : 256;
         slices = wanted < most ? wanted : most;
         if (slices < fit) slices = fit;
@@ -370,6 +373,14 @@ static Slices cut_rows(int64_t rows, int classes) {
 size_t distill_workspace_elems(int64_t rows, int64_t plan_rows, int classes) {
     const Slices cut = cut_rows(plan_rows, classes);
     return cut.slices > 1 ? (size_t)rows * cut.slices * 3 : 0;
+}
+
+// (few rows are cut into more slices than many)
+size_t distill_workspace_elems_up_to(int64_t rows, int classes) {
+    if (classes <= kSliceMax) return 0;
+    size_t elems = distill_workspace_elems(rows, rows, classes);
+    for (int64_t r = std::min(rows, kFewRows); r > 0; --r) elems = std::max(elems, distill_workspace_elems(r, r, classes));
+    return elems;
 }
 
 // (A launch takes no loop over rows: what a lane has in each of them would be kept in registers that the row needs.)

@@ -6,6 +6,8 @@
 // leave as one row of partial results; those are added up in a fixed order behind.  In bf16, with the norm, both launches (us; a copy of as many bytes at 5.1 TB/s): 8192 x 768
 // 25.8 (17.4) and gated 33.5 (22.4), 8192 x 2048 51 (46), 16384 x 4096 177 (186), 8192 x 8192 195 (186); in fp32 4096 x 1024 gated 36.5 (30).  What short rows lack are waves: a
 // SIMD's registers hold two or three.  Rows of more than 8192 features have more values than registers and spill some (2048 x 16384: 168, 93).
+#include <algorithm>
+
 #include "launch.h"
 #include "norm_join.hip.h"
 
@@ -337,9 +339,14 @@ static int bwd_team(int D, bool whole) {
     if (D <= 2048) return 256;
     return D <= 4096 ? 512 : 1024;
 }
+static int bwd_most(int team) { return (team == 1024 ? 2 : 1) * kBwdThreads / (team <= 64 ? 256 : team); }
+static int64_t bwd_full_groups(int64_t rows, int team) {
+    const int teams = team <= 64 ? 256 / team : 1;
+    return (rows + teams - 1) / teams;
+}
 static int bwd_groups(int64_t rows, int team) {
-    const int threads = team <= 64 ? 256 : team, teams = threads / team, most = (team == 1024 ? 2 : 1) * kBwdThreads / threads;
-    const int64_t groups = (rows + teams - 1) / teams, few = groups / 512 < 6 ? groups / 512 : 6;
+    const int most = bwd_most(team);
+    const int64_t groups = bwd_full_groups(rows, team), few = groups / 512 < 6 ? groups / 512 : 6;
     // (up to six, where that still leaves two workgroups to a compute unit: a row of partial results is two to four of 4-byte values, written and read; 2999 x 1001 in fp32 20.6 and 9.7 us
     // for the two launches with three rows to a workgroup, 20.7 and 6.4 with six)
     const int64_t each = (groups + most - 1) / most > few ? (groups + most - 1) / most : few > 1 ? few : 1;
@@ -349,6 +356,17 @@ static int bwd_groups(int64_t rows, int team) {
 size_t norm_join_part_elems(int64_t rows, int D) {
     const int a = bwd_groups(rows, bwd_team(D, true)), b = bwd_groups(rows, bwd_team(D, false));
     return (size_t)(a > b ? a : b) * 2 * (size_t)D;
+}
+
+// (fewer rows may take more workgroups: 1023 of 768 features 1023, 1024 of them 512)
+size_t norm_join_part_elems_up_to(int64_t rows, int D) {
+    int64_t groups = 0;
+    for (bool whole : {true, false}) {
+        const int team = bwd_team(D, whole);
+        const int64_t most = std::min<int64_t>(bwd_full_groups(rows, team), bwd_most(team));
+        groups = std::max(groups, most);
+    }
+    return (size_t)groups * 2 * (size_t)D;
 }
 
 template <typename T, int TEAM, int N, bool WHOLE> static hipError_t bwd_launch(const NormJoinBackward& j, const Partials& part, const Partials& part_pre, hipStream_t s) {

@@ -116,7 +116,7 @@ extern "C" int tmps_norm_join_forward(int dtype, int flags, int64_t rows, int D,
 
 extern "C" size_t tmps_norm_join_workspace(int64_t rows, int D) {
     if (rows < 1 || D < 1 || D > kJoinMaxFeatures) return 0;
-    return 2 * norm_join_part_elems(rows, D) * sizeof(float);
+    return 2 * norm_join_part_elems_up_to(rows, D) * sizeof(float);
 }
 
 extern "C" int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D, const void* dy, const void* du, const void* x, const void* r, const void* y,
@@ -126,7 +126,7 @@ extern "C" int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D
     if (rc != TMPS_OK) return rc;
     const bool rms = flags & TMPS_FLAG_RMS, gate = flags & TMPS_FLAG_GATE;
     if (!dgain_dscale || (du && !dpre)) return fail(TMPS_EINVAL, "an argument is null");
-    const size_t need = tmps_norm_join_workspace(rows, D);
+    const size_t part = rows > 0 ? norm_join_part_elems(rows, D) : 0, need = 2 * part * sizeof(float);   // (what the query gives is enough for fewer rows too)
     const size_t esz = act_bytes(dtype), n = (size_t)rows * D * esz, v = (size_t)D * 4;
     if (rows > 0) {
         if (!dy && !du) return fail(TMPS_EINVAL, "neither dy nor du is given");
@@ -146,7 +146,7 @@ extern "C" int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D
     if (rows == 0) j.x = dgain_dscale, j.du = dpre;   // (the gradients of no rows, which have no address, of which none is read)
     float* const ws = static_cast<float*>(workspace);
     try {
-        TMPS_HIP(norm_join_backward(dtype, j, Partials(ws), Partials(ws ? ws + need / 8 : nullptr), (hipStream_t)hip_stream));
+        TMPS_HIP(norm_join_backward(dtype, j, Partials(ws), Partials(ws ? ws + part : nullptr), (hipStream_t)hip_stream));
     } catch (const std::bad_alloc&) {
         return fail(TMPS_EINVAL, "out of host memory");
     }
@@ -165,7 +165,7 @@ int tmps::check_distill(int64_t classes, int64_t k, float temperature, float alp
 
 extern "C" size_t tmps_distill_workspace(int64_t rows, int classes) {
     if (rows < 1 || classes < 1 || classes > kDistillMaxClasses) return 0;
-    return distill_workspace_elems(rows, rows, classes) * sizeof(float);
+    return distill_workspace_elems_up_to(rows, classes) * sizeof(float);
 }
 
 extern "C" int tmps_distill(int dtype, const tmps_distill_desc* desc, int64_t rows, const float* logits, const int32_t* labels, int64_t label_stride, const int32_t* ids,
@@ -185,7 +185,7 @@ extern "C" int tmps_distill(int dtype, const tmps_distill_desc* desc, int64_t ro
     for (const void* p : {(const void*)logits, (const void*)labels, (const void*)ids, (const void*)teacher, (const void*)row_loss, (const void*)workspace})
         if (!aligned(p, 4)) return fail(TMPS_ESHAPE, "a pointer is not on a whole element");
     if (!aligned(dlogits, act_bytes(dtype))) return fail(TMPS_ESHAPE, "a pointer is not on a whole element");
-    const size_t need = tmps_distill_workspace(rows, desc->classes), n = (size_t)rows * desc->classes;
+    const size_t need = distill_workspace_elems(rows, rows, desc->classes) * sizeof(float), n = (size_t)rows * desc->classes;
     if (need && (!workspace || workspace_bytes < need))
         return fail(TMPS_ECAP, "the workspace holds %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need);
     const size_t entries = desc->alpha > 0.0f ? ((size_t)(rows - 1) * entry_stride + desc->k) * 4 : 0;
