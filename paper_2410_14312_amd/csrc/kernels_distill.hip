@@ -132,7 +132,7 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     T* const g = d.dlogits ? (T*)d.dlogits + row * C + from : nullptr;
     const int whole = n & ~3;   // logits in whole pieces
 
-    // What the row has to learn from.  top: the teacher's largest logit over T; how many ids are no class; how many repeat one.  (A NaN among the teacher's logits makes the row one.)
+    // What the row has to learn from.  top: the teacher's largest logit (over T come differences from it: a common part of large logits takes no places from them); how many ids are no class; how many repeat one.  (A NaN among the teacher's logits makes the row one.)
     const int label = d.labels && alpha < 1.0f ? d.labels[row * d.label_stride] : -1;
     const bool labelled = label >= 0 && label < C;
     float top[3] = {-INFINITY, labelled || label == -1 ? 0.0f : 1.0f, 0.0f};
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
         for (int j = lane; j < k; j += TEAM) {
             const int id = d.ids[row * d.entry_stride + j];
             const bool entry = id >= 0 && id < C;
-            const float t = entry ? d.teacher[row * d.entry_stride + j] * over_t : -INFINITY;
+            const float t = entry ? d.teacher[row * d.entry_stride + j] : -INFINITY;
             ids[j] = entry ? id : -1;
             p[j] = t;
             top[0] = fmaxf(top[0], t != t ? INFINITY : t);
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     if (MODE != kSliceSums) {
         if (taught) {
             for (int j = lane; j < k; j += TEAM) {
-                const float t = p[j] - top[0], e = ids[j] >= 0 ? expf(t) : 0.0f;
+                const float t = (p[j] - top[0]) * over_t, e = ids[j] >= 0 ? expf(t) : 0.0f;
                 zs[j] = j == lane ? z_first : ids[j] >= 0 ? zrow[ids[j]] : 0.0f;
                 p[j] = e;
                 most[1] += e;
