@@ -321,7 +321,7 @@ int tmps_norm_join_backward(int dtype, int flags, int64_t rows, int D, const voi
  * entry_stride elements apart from row to row, labels (NULL: none) one a row, label_stride apart.  An id of -1 is no entry (its logit is not looked at), a label
  * of -1 no label: a row without entries lacks the first term, one without a label the second, one without both has loss and gradient 0 whatever its logits are.  Entries
  * of the same class add up, one whose logit is minus infinity is none.  Any other id or label outside the classes gives a NaN loss, and no part in the gradient.  0 <= alpha <= 1; at 0 the teacher, at 1
- * the labels are not looked at.  workspace: tmps_distill_workspace bytes (may be 0). */
+ * the labels are not looked at.  T lies between 1.1e-19 and 1.8e19 (its square is a normal float).  workspace: tmps_distill_workspace bytes (may be 0). */
 typedef struct {
     int32_t classes, k;
     float temperature, alpha, grad_scale;

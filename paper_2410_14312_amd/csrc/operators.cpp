@@ -1,5 +1,6 @@
 // Operators as calls of their own, over the caller's memory: rotary positions, norm joins, distillation.  Arguments are checked here; the launchers are those that the
 // layers of a stage use.
+#include <float.h>
 #include <math.h>
 
 #include <new>
@@ -157,8 +158,9 @@ int tmps::check_distill(int64_t classes, int64_t k, float temperature, float alp
     if (classes < 1 || k < 1) return fail(TMPS_EINVAL, "classes and k must be positive");
     if (classes > kDistillMaxClasses) return fail(TMPS_EUNSUPPORTED, "more than %d classes", kDistillMaxClasses);
     if (k > kDistillMaxEntries) return fail(TMPS_EUNSUPPORTED, "more than %d teacher entries a row", kDistillMaxEntries);
-    if (!(temperature > 0.0f) || !isfinite(temperature) || !isfinite(1.0f / temperature) || !isfinite(temperature * temperature))
-        return fail(TMPS_EINVAL, "temperature must be positive, its inverse and its square finite");
+    // (the loss has its square for a factor: one that is nothing, or has lost places, would take the term along)
+    const float square = temperature * temperature;
+    if (!(temperature > 0.0f) || !isfinite(square) || square < FLT_MIN) return fail(TMPS_EINVAL, "temperature must be positive, its square within the range of a float");
     if (!(alpha >= 0.0f && alpha <= 1.0f)) return fail(TMPS_EINVAL, "alpha must lie in 0..1");
     return TMPS_OK;
 }
