@@ -6,8 +6,13 @@
 
 #include <vector>
 
-// Layer kinds that a host-only build of the executor may lack: it links without their launchers, and refuses such layers.
+// Launchers of layer kinds that a host-only build of the executor may lack: it links without them, and refuses such layers.  The library is built with TMPS_WHOLE: there
+// they are symbols like any others, and a source that is left out is an error of the link.
+#ifdef TMPS_WHOLE
+#define TMPS_OPTIONAL
+#else
 #define TMPS_OPTIONAL __attribute__((weak))
+#endif
 
 namespace tmps {
 

@@ -68,6 +68,9 @@ static bool on16(std::initializer_list<const void*> all) {
     return (bits & 15) == 0;
 }
 
+// Whether a launcher is linked.
+template <typename F> static bool is_built(F* launcher) { return launcher != nullptr; }
+
 static bool is_loss(const LayerRT& L) { return L.d.kind == TMPS_SOFTMAX_CE || L.d.kind == TMPS_DISTILL; }
 
 // The second result that a layer reads (its first where it reads one).
@@ -252,7 +255,7 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
                 L.w_count = d[0]; L.b_count = L.rms ? 0 : d[0];
                 L.relu = false; L.act = 0;
                 if (L.rms) {
-                    if (!norm_join_part_elems) return fail(TMPS_EUNSUPPORTED, "layer %d: norms without a mean are not built", i);
+                    if (!is_built(norm_join_part_elems)) return fail(TMPS_EUNSUPPORTED, "layer %d: norms without a mean are not built", i);
                     if (d[0] > kJoinMaxFeatures) return fail(TMPS_EUNSUPPORTED, "layer %d: rows of more than %d features", i, kJoinMaxFeatures);
                     L.ws_elems = L.part_elems = norm_join_part_elems((int64_t)M * L.rps, d[0]);
                 } else {
@@ -261,7 +264,7 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
                 break;
             case TMPS_NORMJOIN:
                 if (d[0] < 1 || d[1] < 0 || d[2] < 2) return fail(TMPS_EINVAL, "layer %d: bad norm-join dims", i);
-                if (!norm_join_part_elems) return fail(TMPS_EUNSUPPORTED, "layer %d: norm joins are not built", i);
+                if (!is_built(norm_join_part_elems)) return fail(TMPS_EUNSUPPORTED, "layer %d: norm joins are not built", i);
                 if (d[0] > kJoinMaxFeatures) return fail(TMPS_EUNSUPPORTED, "layer %d: rows of more than %d features", i, kJoinMaxFeatures);
                 if (L.d.flags & ~(TMPS_FLAG_RMS | TMPS_FLAG_GATE)) return fail(TMPS_EINVAL, "layer %d: unknown flags %d", i, L.d.flags);
                 if (i - d[2] < -1) return fail(TMPS_ESHAPE, "layer %d: the residual's source lies before the stage input", i);
@@ -282,7 +285,7 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
             case TMPS_ROTARY: {
                 if (d[0] < 1 || d[1] < 1 || d[2] < 1 || d[1] % d[2] != 0 || (d[1] / d[2]) % 2 != 0)
                     return fail(TMPS_EINVAL, "layer %d: rotary positions need S, D, heads positive and heads of an even number of features", i);
-                if (!rotary) return fail(TMPS_EUNSUPPORTED, "layer %d: rotary positions are not built", i);
+                if (!is_built(rotary)) return fail(TMPS_EUNSUPPORTED, "layer %d: rotary positions are not built", i);
                 if (d[3] < 0 || d[4] < 0 || d[5] < 0 || d[6] < 0 || d[7] < 0 || (int64_t)d[5] + d[6] > d[1] / d[2] / 2)
                     return fail(TMPS_EINVAL, "layer %d: bad grid or pairs of rotary positions", i);
                 if (L.d.flags & ~(TMPS_FLAG_INTERLEAVED | TMPS_FLAG_OWN_LADDERS)) return fail(TMPS_EINVAL, "layer %d: unknown flags %d", i, L.d.flags);
@@ -326,7 +329,7 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
                 L.relu = false; L.act = 0;
                 st.loss_rps = st.label_rps = L.rps;
                 if (L.d.kind == TMPS_DISTILL) {
-                    if (!distill) return fail(TMPS_EUNSUPPORTED, "layer %d: distillation is not built", i);
+                    if (!is_built(distill)) return fail(TMPS_EUNSUPPORTED, "layer %d: distillation is not built", i);
                     const int rc = check_distill(d[0], d[2], float_of(d[3]), float_of(d[4]));
                     if (rc != TMPS_OK) return rc;
                     if ((int64_t)L.rps * (1 + 2 * (int64_t)d[2]) > INT32_MAX) return fail(TMPS_EUNSUPPORTED, "layer %d: too many labels a sample", i);
