@@ -307,13 +307,16 @@ def _within(stream, device):
 
 
 def _call(fn, device, stream, *args):
-    """fn(..., stream) on a GPU's current stream, or on the stream whose handle is given, with that GPU current."""
+    """fn(..., stream) on a GPU's current stream, with that GPU current.  stream is None: another stream is made the current one (_within) before results and workspaces are
+    allocated, which belong to the stream that is current then."""
     torch = _torch()
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are wanted, not on %s" % device)
+    if stream is not None:
+        raise ValueError("a call runs on the current stream")
     # (current_stream(device).cuda_stream without the object, 0.1 us instead of 1.9, and current_device() of a process that has tensors on a GPU)
     index = device.index
-    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else int(stream)
+    handle = torch._C._cuda_getCurrentRawStream(index)
     if index == torch._C._cuda_getDevice():
         rc = fn(*args, handle)
     else:
