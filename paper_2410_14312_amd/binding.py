@@ -264,6 +264,8 @@ def stage_bytes(specs, cfg):
 
 
 # ------------------------------------------------------------------------------------ operators on their own
+# Gradients are calls as well (rotary's inverse, norm_join_backward, distill's second result): nothing is recorded for torch's backward pass, and tensors that ask for it are refused
+# outside of torch.no_grad().
 def _torch():
     global _torch_of
     if _torch_of is None:
@@ -284,11 +286,18 @@ def _dtype_code(t):
     raise ValueError("%s: the library computes in float32 and bfloat16" % t.dtype)
 
 
+def _unrecorded(name, t):
+    if t.requires_grad and _torch().is_grad_enabled():
+        raise ValueError("%s asks for a gradient, which is a call of its own here and not recorded: call with detached tensors or under torch.no_grad()" % name)
+
+
 def _operand(name, t, shape, dtype, device):
     """A tensor's address, after a check of what it is (rows contiguous); None stays None."""
     if t is None:
         return None
     if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.device == device:
+        if t.requires_grad:
+            _unrecorded(name, t)
         return t.data_ptr()
     raise ValueError("%s: a contiguous %s tensor of shape %s on %s is wanted, not %s %s on %s"
                      % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
@@ -330,7 +339,7 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
     """Rotary positions (tmps_rotary) of the `heads` heads of dh features that begin each row of x [rows, features]: pairs = (time, height, width)
     pairs of features that turn with each axis of positions, int32 [n, 3], which the rows take in turn.  inverse: back, the gradient's way.
     out (default: a new tensor [rows, heads * dh]) may be x, or a view of rows of its own stride.  Returns out.  On the current stream, or on `stream`, which a new tensor then
-    belongs to; it waits for no other."""
+    belongs to; it waits for no other.  A tensor that asks for a gradient is refused while gradients are recorded (all of these calls do so)."""
     if stream is not None:
         with _within(stream, x.device):
             return rotary(x, positions, heads, dh, pairs, base, interleaved, own_ladders, inverse, out)
@@ -351,6 +360,8 @@ def rotary(x, positions, heads, dh, pairs, base=10000.0, interleaved=False, own_
         raise ValueError("out: %d rows of at least %d neighbouring %s features on %s are wanted" % (rows, width, x.dtype, x.device))
     else:
         out_stride = out.stride(0)
+    if x.requires_grad or out.requires_grad:
+        _unrecorded("x" if x.requires_grad else "out", x if x.requires_grad else out)
     d = RotaryDesc(heads, dh, Axes(*pairs), _rotary_flags(interleaved, own_ladders), base)
     _call(load_library().tmps_rotary, x.device, None, code, C.byref(d), x.data_ptr(), x.stride(0), out.data_ptr(), out_stride, pos, positions.shape[0], rows, int(inverse))
     return out

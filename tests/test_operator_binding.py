@@ -14,3 +14,25 @@ def test_a_call_takes_no_stream_beside_the_current_one():
     for stream in (0, 1 << 20):
         with pytest.raises(ValueError, match="current stream"):
             binding._call(never, torch.device("cuda:0"), stream)
+
+
+def asking(*tensors):
+    return [[t.clone().requires_grad_(i == k) if t.is_floating_point() else t for i, t in enumerate(tensors)] for k in range(len(tensors)) if tensors[k].is_floating_point()]
+
+
+def test_tensors_that_ask_for_a_gradient_are_refused_while_gradients_are_recorded():
+    """Every operand of every call; under torch.no_grad() such tensors are taken (and then refused for being on the host)."""
+    import paper_2410_14312_amd as tmps
+
+    f, v, pos = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4, 3, dtype=torch.int32)
+    st, ids = torch.zeros(4, 4), torch.zeros(4, 2, dtype=torch.int32)
+    calls = [(lambda x: tmps.rotary(x, pos, 1, 8, (4, 0, 0)), (f,)), (lambda out: tmps.rotary(f, pos, 1, 8, (4, 0, 0), out=out), (f,)),
+             (lambda x, r, g, s, p, q: tmps.norm_join(x, r, g, s, pre_gain=p, pre_shift=q), (f, f, v, v, v, v)), (lambda y: tmps.norm_join(f, f, v, v, y=y), (f,)),
+             (lambda dy, du, x, r, y, stats, g, s, p: tmps.norm_join_backward(dy, du, x, r, y, stats, g, s, pre_gain=p), (f, f, f, f, f, st, v, v, v)),
+             (lambda z, t: tmps.distill(z, None, ids, t), (f, torch.zeros(4, 2)))]
+    for call, operands in calls:
+        for given in asking(*operands):
+            with pytest.raises(ValueError, match="asks for a gradient"):
+                call(*given)
+            with torch.no_grad(), pytest.raises(ValueError, match="on a GPU"):
+                call(*given)
