@@ -267,14 +267,22 @@ def stage_bytes(specs, cfg):
 # Gradients are calls as well (rotary's inverse, norm_join_backward, distill's second result): nothing is recorded for torch's backward pass, and tensors that ask for it are refused
 # outside of torch.no_grad().
 def _torch():
-    global _torch_of
+    global _torch_of, _raw_stream, _current_device
     if _torch_of is None:
         import torch
+        _raw_stream, _current_device = _short_ways(torch, torch._C)
         _torch_of = torch
     return _torch_of
 
 
-_torch_of = None
+def _short_ways(torch, private):
+    """(a GPU's index -> its current stream's handle, () -> the current GPU's index).  The private ones, where this torch has them, make no object (0.1 us instead of 1.9) and ask
+    less (a process that has tensors on a GPU has initialised it)."""
+    return (getattr(private, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream),
+            getattr(private, "_cuda_getDevice", None) or torch.cuda.current_device)
+
+
+_torch_of = _raw_stream = _current_device = None
 
 
 def _dtype_code(t):
@@ -323,10 +331,9 @@ def _call(fn, device, stream, *args):
         raise ValueError("tensors on a GPU are wanted, not on %s" % device)
     if stream is not None:
         raise ValueError("a call runs on the current stream")
-    # (current_stream(device).cuda_stream without the object, 0.1 us instead of 1.9, and current_device() of a process that has tensors on a GPU)
     index = device.index
-    handle = torch._C._cuda_getCurrentRawStream(index)
-    if index == torch._C._cuda_getDevice():
+    handle = _raw_stream(index)
+    if index == _current_device():
         rc = fn(*args, handle)
     else:
         with torch.cuda.device(device):

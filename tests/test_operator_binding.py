@@ -36,3 +36,18 @@ def test_tensors_that_ask_for_a_gradient_are_refused_while_gradients_are_recorde
                 call(*given)
             with torch.no_grad(), pytest.raises(ValueError, match="on a GPU"):
                 call(*given)
+
+
+def test_streams_are_found_without_private_names(monkeypatch):
+    class Stream:
+        cuda_stream = 77
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index: Stream if index == 3 else None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    stream, device = binding._short_ways(torch, object())
+    assert stream(3) == 77 and device() == 3
+    binding._torch()
+    monkeypatch.setattr(binding, "_raw_stream", stream)
+    monkeypatch.setattr(binding, "_current_device", device)
+    seen = []
+    binding._call(lambda *a: seen.append(a) or 0, torch.device("cuda:3"), None, 5)
+    assert seen == [(5, 77)]
