@@ -1,8 +1,9 @@
 // Rotary positions: pairs (u, v) of a head's features turned by an angle, u' = u cos - v sin, v' = v cos + u sin.  The angle of pair i is the row's position on the
 // pair's axis times base^(-j/n), j and n counted over all pairs or over the axis's own.
 //
-// Angles are formed as turns in 64 bits: a position of a million times a frequency of one is 1.6e5 turns, of which fp32 keeps 1/64 of a turn.  What is left of whole
-// turns goes to fp32 (2^-25 of a turn at most), its sine and cosine from there.
+// Angles are formed as turns in 64 bits: a position of a million times a frequency of one is 1.6e5 turns, of which fp32 keeps 1/64 of a turn.  A frequency is off by less than 2^-50
+// of itself, whatever its place on the ladder, so turns are off by 2^-50 of their number.  What is left of whole turns goes to fp32 (2^-25 of a turn at most, which is the larger part up
+// to positions of 2^27), its sine and cosine from there.
 //
 // Bound by memory: the heads are read and written once.  (us; a copy of as many bytes at the 5.1 TB/s that one of a gigabyte reaches; a thread to a pair of one head): 16384 rows of
 // 40 heads of 128 in bf16 66 (66; 238), 8192 of 24 of 64 13.4 (9.9; 31), in fp32 19.4 (19.8).  One row is a launch and one latency, 4.1 us.
@@ -14,9 +15,10 @@
 
 namespace tmps {
 
-// What a launch's threads share.  ratio: base^(-1/n) of the ladder that each axis uses, first: the pair that stands at the ladder's top.
+// What a launch's threads share.  step + rest: log2(base) / n of the ladder that each axis uses, the first with 24 bits, so that a pair's multiple of it is exact; first: the pair that
+// stands at the ladder's top.
 struct Ladders {
-    double ratio[3];
+    double step[3], rest[3];
     int first[3], end[3];   // end: the first pair behind axis a's
 };
 
@@ -29,20 +31,15 @@ struct RotaryShape {
     Ladders l;
 };
 
-// x^n by squaring: the relative error of its at most 2 log2(n) products is below 2^-48.
-__device__ __forceinline__ double power(double x, int n) {
-    double r = 1.0;
-    for (; n > 0; n >>= 1) {
-        if (n & 1) r *= x;
-        x *= x;
-    }
-    return r;
-}
-
 __device__ __forceinline__ int axis_of(const RotaryShape& a, int i) { return i < a.l.end[0] ? 0 : i < a.l.end[1] ? 1 : 2; }
 
-// turns of pair i for a position of one
-__device__ __forceinline__ double turns_of(const RotaryShape& a, int i, int axis) { return 0.15915494309189533577 * power(a.l.ratio[axis], i - a.l.first[axis]); }
+// turns of pair i for a position of one: base^(-j/n) / (2 pi) as 2^(-j step) 2^(-j rest), the second, of an exponent below 2^-17, by its series (its third term is below 2^-54).  A step of
+// 2^-52 of the exponential and three of 2^-53 of the products and the constant.  (Powers of base^(-1/n) would be off by its rounding j times over, 2^-44 at 4096 pairs.)
+__device__ __forceinline__ double turns_of(const RotaryShape& a, int i, int axis) {
+    const int j = i - a.l.first[axis];
+    const double r = -0.69314718055994530942 * (j * a.l.rest[axis]);
+    return 0.15915494309189533577 * exp2(-j * a.l.step[axis]) * fma(r, fma(0.5, r, 1.0), 1.0);
+}
 
 __device__ __forceinline__ int position(const RotaryShape& a, int64_t row, int axis) {
     if (a.pos) return a.pos[row % a.pos_rows * 3 + axis];
@@ -237,7 +234,9 @@ hipError_t rotary(int dtype, const Rotary& r, hipStream_t s) {
         const bool own = r.flags & TMPS_FLAG_OWN_LADDERS;
         const int n = own ? r.pairs[k] : a.pairs;
         a.l.first[k] = own ? at : 0;
-        a.l.ratio[k] = n > 0 ? pow((double)r.base, -1.0 / n) : 1.0;
+        const long double step = n > 0 ? log2l((long double)r.base) / n : 0.0L;
+        a.l.step[k] = (double)(float)step;
+        a.l.rest[k] = (double)(step - (long double)a.l.step[k]);
         a.l.end[k] = at += r.pairs[k];
     }
     const int most = dtype == kBF16 ? 8 : 4;
