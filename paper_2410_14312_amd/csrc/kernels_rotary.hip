@@ -53,8 +53,13 @@ __device__ __forceinline__ void turn(double turns, float sign, float& c, float& 
     s *= sign;
 }
 
-// A thread to a pair (or to a feature behind the pairs) of one head of one row: heads of few pairs.
-template <typename T> __global__ __launch_bounds__(256) void rotary_kernel(const T* x, T* y, RotaryShape a) {
+// A thread to a pair (or to a feature behind the pairs) of one head of one row: heads of few pairs, and wide ones.  TABLE: frequencies are formed once a workgroup, in LDS.
+template <typename T, bool TABLE> __global__ __launch_bounds__(256) void rotary_kernel(const T* x, T* y, RotaryShape a) {
+    extern __shared__ double frequency[];
+    if constexpr (TABLE) {
+        for (int i = threadIdx.x; i < a.pairs; i += 256) frequency[i] = turns_of(a, i, axis_of(a, i));
+        __syncthreads();
+    }
     const int per_head = a.pairs + (a.dh - 2 * a.pairs);
     const int64_t n = a.rows * a.heads * per_head, step = (int64_t)gridDim.x * 256;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < n; t += step) {
@@ -74,7 +79,7 @@ template <typename T> __global__ __launch_bounds__(256) void rotary_kernel(const
         }
         const int axis = axis_of(a, i);
         float c, s;
-        turn(position(a, row, axis) * turns_of(a, i, axis), a.sign, c, s);
+        turn(position(a, row, axis) * (TABLE ? frequency[i] : turns_of(a, i, axis)), a.sign, c, s);
         const int at = a.interleaved ? 2 * i : i, to = a.interleaved ? 2 * i + 1 : i + a.pairs;
         const float u = to_f32(xr[at]), v = to_f32(xr[to]);
         yr[at] = from_f32<T>(u * c - v * s);
@@ -244,10 +249,15 @@ hipError_t rotary(int dtype, const Rotary& r, hipStream_t s) {
         if (dtype == kBF16) return a.interleaved ? rotary_pieces<bf16_t, true>(r, a, s) : rotary_pieces<bf16_t, false>(r, a, s);
         return a.interleaved ? rotary_pieces<float, true>(r, a, s) : rotary_pieces<float, false>(r, a, s);
     }
-    const int64_t n = a.rows * a.heads * (a.dh - a.pairs);
-    const dim3 grid((unsigned)(n + 255 > (int64_t(1) << 28) ? 1 << 20 : (n + 255) / 256));
-    if (dtype == kBF16) return launch_timed(kcEmbedding, rotary_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)r.x, (bf16_t*)r.y, a);
-    return launch_timed(kcEmbedding, rotary_kernel<float>, grid, dim3(256), 0, s, (const float*)r.x, (float*)r.y, a);
+    const int64_t blocks = (a.rows * a.heads * (a.dh - a.pairs) + 255) / 256;
+    // A table of more pairs than a workgroup has threads would cost each of them several frequencies for its one.  With a table, as many workgroups as the device holds, so that each
+    // forms it once for many rows: 8192 rows of 24 heads of 64, 4 pairs, bf16 59 us, 65 with a workgroup to 256 features, 72 with a frequency formed for every turn.
+    const bool table = a.pairs <= 256;
+    const int64_t cap = table ? 2048 : 1 << 20;
+    const dim3 grid((unsigned)(blocks < cap ? blocks : cap));
+    const size_t lds = table ? (size_t)a.pairs * 8 : 0;
+    if (dtype == kBF16) return launch_timed(kcEmbedding, table ? rotary_kernel<bf16_t, true> : rotary_kernel<bf16_t, false>, grid, dim3(256), lds, s, (const bf16_t*)r.x, (bf16_t*)r.y, a);
+    return launch_timed(kcEmbedding, table ? rotary_kernel<float, true> : rotary_kernel<float, false>, grid, dim3(256), lds, s, (const float*)r.x, (float*)r.y, a);
 }
 
 }  // namespace tmps
