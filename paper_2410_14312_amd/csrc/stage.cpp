@@ -467,8 +467,23 @@ int stage_layout(tmps_stage& st, const tmps_layer_desc* layers, int n_layers, co
     // scratch: gradient buffers of M rows, two boundary-gradient buffers, fp32 workspace
     size_t o = 0;
     st.n_gbuf = any_join ? 6 : (any_skip ? 4 : 2);
+    if (std::any_of(st.layers.begin(), st.layers.end(), [](const LayerRT& L) { return L.d.kind == TMPS_NORMJOIN; })) {
+        // Norm joins write a gradient of their own to each source: as many as are open at a layer (results before it that a layer behind it reads), its result's, its two sources' and one
+        // that is added behind its launch.
+        std::vector<int> last(n_layers + 1, -1);   // the last layer that reads each result
+        for (int i = 0; i < n_layers; ++i) {
+            const LayerRT& L = st.layers[i];
+            for (int t : {L.in_t, second_source(L), L.skip ? st.layers[i - L.skip].in_t : L.in_t}) last[t + 1] = i;
+        }
+        for (int i = 0; i < n_layers; ++i) {
+            int open = 0;
+            for (int t = -1; t < i; ++t) open += last[t + 1] > i;
+            st.n_gbuf = std::max(st.n_gbuf, open + 4);
+        }
+    }
     st.gbuf_bytes = align_up((size_t)M * std::max<int64_t>(gmax, 1) * st.asz, 256);
-    for (int k = 0; k < st.n_gbuf; ++k) { st.gbuf_off[k] = o; o += st.gbuf_bytes; }
+    st.gbuf_off.clear();
+    for (int k = 0; k < st.n_gbuf; ++k) { st.gbuf_off.push_back(o); o += st.gbuf_bytes; }
     st.dxout_bytes = align_up((size_t)M * st.in_elems * st.asz, 256);
     st.dxout_off[0] = o; o += st.dxout_bytes;
     st.dxout_off[1] = o; o += st.dxout_bytes;
@@ -950,8 +965,8 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     const int nl = (int)st->layers.size();
     std::vector<Grad> grads(nl + 1);
     std::vector<int> remaining(st->readers);
-    char* gbuf[8];
-    int refs[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    std::vector<char*> gbuf(st->n_gbuf);
+    std::vector<int> refs(st->n_gbuf, 0);
     for (int k = 0; k < st->n_gbuf; ++k) gbuf[k] = st->scratch + st->gbuf_off[k];
     auto take = [&]() -> int {
         for (int k = 0; k < st->n_gbuf; ++k)
@@ -1091,7 +1106,7 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     auto can_wait = [&](const LayerRT& L) {
         const int32_t* d = L.d.dims;
         return strided.li < 0 && !in_order && d[4] == 1 && d[5] == 1 && d[6] > 1 && d[7] == 0 && remaining[L.in_t + 1] > 1 && !grads[L.in_t + 1].set &&
-               (L.in_t >= 0 || dx) && std::count(refs, refs + st->n_gbuf, 0) >= 3;
+               (L.in_t >= 0 || dx) && std::count(refs.begin(), refs.end(), 0) >= 3;
     };
     auto strided_is_last = [&]() { return strided.li >= 0 && remaining[st->layers[strided.li].in_t + 1] == 1; };
 

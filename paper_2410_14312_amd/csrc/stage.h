@@ -56,7 +56,8 @@ struct tmps_stage {
     float* grad = nullptr;
     size_t in_off = 0;  // stash offset of the copied inputs (borrow_input == 0)
     size_t stash_bytes = 0, scratch_bytes = 0;
-    size_t gbuf_off[8] = {0, 0, 0, 0, 0, 0, 0, 0}, gbuf_bytes = 0;  // gradient buffers (M rows each)
+    std::vector<size_t> gbuf_off;  // gradient buffers (M rows each)
+    size_t gbuf_bytes = 0;
     size_t dxout_off[2] = {0, 0}, dxout_bytes = 0;  // boundary gradient buffers used by the scheduler
     size_t ws_off = 0, ws_bytes = 0;
     size_t ws_fwd_bytes = 0;  // fp32 workspace bytes a forward pass needs (the k-split partial sums of its contractions)

@@ -1,5 +1,5 @@
 // Stand-ins for the kernel launchers (paper_2410_14312_amd/csrc/kernels.h) that compute, on fp32 host memory and at once: dense layers without activation, residual joins, layer
-// normalisation, norm joins, rotary positions by a quarter turn.  The other launchers are those of kernel_stubs.cpp.  What no kernel promises is not kept here either: a dense layer's
+// normalisation, norm joins, rotary positions.  The other launchers are those of kernel_stubs.cpp.  What no kernel promises is not kept here either: a dense layer's
 // input gradient is written column by column while its operands are still read, and comes before the weight gradient where the two share a launch.
 #include "arithmetic.h"
 
@@ -203,24 +203,25 @@ hipError_t norm_join_backward(int, const NormJoinBackward& j, const Partials&, c
     return hipSuccess;
 }
 
-// (a quarter turn a row of its time, exact: what is tested is where results go)
 hipError_t rotary(int, const Rotary& r, hipStream_t) {
-    const int half = r.dh / 2;
+    const int pairs = r.pairs[0] + r.pairs[1] + r.pairs[2];
+    const bool interleaved = r.flags & TMPS_FLAG_INTERLEAVED, own = r.flags & TMPS_FLAG_OWN_LADDERS;
     for (int64_t k = 0; k < r.rows; ++k) {
-        const int time = (int)(k % r.grid_rows % 4), quarter = r.inverse ? (4 - time) % 4 : time;
-        for (int h = 0; h < r.heads + r.copied; ++h)
-            for (int i = 0; i < half; ++i) {
-                const float* x = (const float*)r.x + k * r.x_stride + h * r.dh;
-                float* y = (float*)r.y + k * r.y_stride + h * r.dh;
-                float u = x[i], v = x[half + i];
-                for (int q = 0; q < (h < r.heads ? quarter : 0); ++q) {
-                    const float w = -v;
-                    v = u;
-                    u = w;
-                }
-                y[i] = u;
-                y[half + i] = v;
+        const int place = (int)(k % r.grid_rows), across = r.grid_w * r.grid_h, at[3] = {place / across, place / r.grid_w % r.grid_h, place % r.grid_w};
+        for (int h = 0; h < r.heads + (r.x == r.y ? 0 : r.copied); ++h) {
+            const float* x = (const float*)r.x + k * r.x_stride + h * r.dh;
+            float* y = (float*)r.y + k * r.y_stride + h * r.dh;
+            for (int i = 0; i < pairs; ++i) {
+                const int axis = i < r.pairs[0] ? 0 : i < r.pairs[0] + r.pairs[1] ? 1 : 2, first = axis == 0 ? 0 : axis == 1 ? r.pairs[0] : r.pairs[0] + r.pairs[1];
+                const double angle = at[axis] * pow((double)r.base, own ? -(double)(i - first) / r.pairs[axis] : -(double)i / pairs) * (r.inverse ? -1.0 : 1.0);
+                const double c = h < r.heads ? cos(angle) : 1.0, s = h < r.heads ? sin(angle) : 0.0;
+                const int a = interleaved ? 2 * i : i, b = interleaved ? 2 * i + 1 : i + pairs;
+                const double u = x[a], v = x[b];
+                y[a] = (float)(u * c - v * s);
+                y[b] = (float)(v * c + u * s);
             }
+            for (int i = 2 * pairs; i < r.dh; ++i) y[i] = x[i];
+        }
     }
     return hipSuccess;
 }

@@ -13,12 +13,12 @@ over = pytest.mark.parametrize("in_place", ["dy", "x"])
 
 @both
 @over
-@pytest.mark.parametrize("opened", [1, 4])
+@pytest.mark.parametrize("opened", [1, 4, 8])
 def test_a_join_of_the_stage_input_among_others(dtype, in_place, opened):
     """Joins that read the first results leave their gradients open when the one of the stage input comes."""
     d, rows = 32, 3
-    specs = [linear(d, d, False, rows=rows) for _ in range(6)]
-    specs += [norm_join(d, rows, 6) for _ in range(opened)]
+    specs = [linear(d, d, False, rows=rows) for _ in range(10)]
+    specs += [norm_join(d, rows, 10) for _ in range(opened)]
     specs += [norm_join(d, rows, len(specs) + 1), layernorm(d, rows), linear(d, d, False, rows=rows)]
     for borrow in (True, False):
         run(specs, d * rows, dtype, 3, 2, seed=opened, borrow=borrow, in_place=in_place)
