@@ -3,9 +3,9 @@
 //   loss = alpha T^2 sum_j p_j (log p_j - log q[id_j]) + (1 - alpha) (-log s[label])
 //   d loss / dz = alpha T (q - sum_j p_j e[id_j]) + (1 - alpha) (s - e[label])
 // Bound by memory: a row of logits is read, a row of gradients written.  Hence a row stays in registers between its largest logit, its two sums and its gradients, each of which takes
-// every logit's exponentials again.  Of 8192 rows of 32000 logits, 64 entries, bf16 gradients: 317 us, 4.6 TB/s (a copy of as many bytes 285 us; 291 us where T is 1 and one exponential
-// does for both, 253 us without a teacher); the same of 1, 16, 256 entries: 306, 306, 343 us; 4096 rows of 16000 logits: 79 us, 5.0 TB/s; 16384 rows of 1000: 26 us; 2048 rows of
-// 50257: 136 us, 4.2 TB/s; of 65000 207 us, 3.6 TB/s (one workgroup to a compute unit: nothing runs beside its loads); 64 rows of 100: 7 us, mostly the launch.
+// every logit's exponentials again.  Of 8192 rows of 32000 logits, 64 entries, bf16 gradients, between two time stamps: 319 us, 4.5 TB/s (a copy of as many bytes 285 us; 293 us where T is 1 and one exponential
+// does for both, 253 us without a teacher); the same of 1, 16, 256 entries: 301, 304, 338 us; 4096 rows of 16000 logits: 77 us, 4.7 TB/s; 16384 rows of 1000: 26 us; 2048 rows of
+// 50257: 137 us, 4.1 TB/s; of 65000 207 us, 3.5 TB/s (one workgroup to a compute unit: nothing runs beside its loads); 64 rows of 100: 7 us, mostly the launch.
 #include <algorithm>
 
 #include "kernels.h"
@@ -354,8 +354,8 @@ __global__ __launch_bounds__(TEAM == 64 ? 256 : TEAM, TEAM == 1024 ? 4 : NV <= 1
     }
 }
 
-// Rows of more than 98304 logits are cut into slices that registers hold (1024 rows of 131072: 255 us), and few wide rows into as many as give every compute unit eight: one row of
-// 98304 logits takes 13 us, whole 24, 64 rows 20 and 31; 8 rows of 50257 14 and 17; 8 rows of 32000 15 and 12.  (48 rows of 131071: 19 us, with two to a compute unit 26.)
+// Rows of more than 98304 logits are cut into slices that registers hold (1024 rows of 131072: 259 us), and few wide rows into as many as give every compute unit eight: one row of
+// 98304 logits takes 13 us, whole 24, 64 rows 20 and 31; 8 rows of 50257 14 and 17; 8 rows of 32000 15 and 12.  (48 rows of 131071: 20 us, with two to a compute unit 26.)
 constexpr int kWholeMax = 98304, kSliceMax = 32768;
 constexpr int64_t kFewRows = 64;
 static Slices cut_rows(int64_t rows, int classes) {

@@ -1,6 +1,6 @@
 // Norm joins, forward: y = scale r + g gain n(f) and u = n(y) pre_gain + pre_shift in one pass over memory.  Bound by memory: f, r (and the gate's argument) are
-// read, y and u written once each.  With the norm behind it, in bf16 (us; a copy of as many bytes at the 5.1 TB/s that one of a gigabyte reaches): 8192 x 768 gated 16.5 (12.4),
-// 16384 x 4096 103 (106), 8192 x 8192 99 (106), 32768 x 256 13.8 (13.3); in fp32 4096 x 1024 gated 15.6 (16.6).  Small ones are a launch and two or three sums over
+// read, y and u written once each.  With the norm behind it, in bf16 (us of a launch between two time stamps; a copy of as many bytes at the 5.1 TB/s that one of a gigabyte reaches):
+// 8192 x 768 gated 16.9 (12.4), 16384 x 4096 103 (106), 8192 x 8192 100 (106), 32768 x 256 13.9 (13.3); in fp32 4096 x 1024 gated 15.2 (16.6).  Small ones are a launch and two or three sums over
 // a team: 256 x 64 4 us.
 #include "launch.h"
 #include "norm_join.hip.h"

@@ -3,9 +3,9 @@
 //   dr = scale dh (+ what others have given r);  da = dh gain fh g (1 - g);  v = dh g gain, df = i1 (v - mean(v) - fh mean(v fh))
 //   dpre_gain = sum du yh, dpre_shift = sum du, dscale = sum dh r, dgain = sum dh g fh over the rows
 // One pass over memory: dy, du, x, r, y are read and dx, dr written once each.  A team goes over its share of the rows and keeps its sums over them in registers, which
-// leave as one row of partial results; those are added up in a fixed order behind.  In bf16, with the norm, both launches (us; a copy of as many bytes at 5.1 TB/s): 8192 x 768
-// 25.8 (17.4) and gated 33.5 (22.4), 8192 x 2048 51 (46), 16384 x 4096 177 (186), 8192 x 8192 195 (186); in fp32 4096 x 1024 gated 36.5 (30).  What short rows lack are waves: a
-// SIMD's registers hold two or three.  Rows of more than 8192 features have more values than registers and spill some (2048 x 16384: 168, 93).
+// leave as one row of partial results; those are added up in a fixed order behind.  In bf16, with the norm, both launches, each between two time stamps (us; a copy of as many
+// bytes at 5.1 TB/s): 8192 x 768 26.6 (17.4) and gated 31.9 (22.4), 8192 x 2048 53 (46), 16384 x 4096 177 (186), 8192 x 8192 189 (186); in fp32 4096 x 1024 gated 36.1 (30).  What short rows lack are waves: a
+// SIMD's registers hold two or three.  Rows of more than 8192 features have more values than registers and spill some (2048 x 16384: 167, 93).
 #include <algorithm>
 
 #include "launch.h"

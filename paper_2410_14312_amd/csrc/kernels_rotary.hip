@@ -5,8 +5,8 @@
 // of itself, whatever its place on the ladder, so turns are off by 2^-50 of their number.  What is left of whole turns goes to fp32 (2^-25 of a turn at most, which is the larger part up
 // to positions of 2^27), its sine and cosine from there.
 //
-// Bound by memory: the heads are read and written once.  (us; a copy of as many bytes at the 5.1 TB/s that one of a gigabyte reaches; a thread to a pair of one head): 16384 rows of
-// 40 heads of 128 in bf16 66 (66; 238), 8192 of 24 of 64 13.4 (9.9; 31), in fp32 19.4 (19.8).  One row is a launch and one latency, 4.1 us.
+// Bound by memory: the heads are read and written once.  (us of a launch between two time stamps; a copy of as many bytes at the 5.1 TB/s that one of a gigabyte reaches; a thread to a
+// pair of one head): 16384 rows of 40 heads of 128 in bf16 67 (66; 238), 8192 of 24 of 64 14.4 (9.9; 31), in fp32 19.0 (19.8).  One row is a launch and one latency, 4.4 us.
 #include "../../include/tmps.h"
 #include "gemm.hip.h"
 #include "kernels.h"
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void rotary_pieces_kernel(const T* x, T* y, Ro
     }
 }
 
-// Workgroups of a launch at most: four to a compute unit, each with its frequencies formed once.  (8192 rows of 24 heads of 64 in bf16 14.6 us with twice as many, 13.4 so.)
+// Workgroups of a launch at most: four to a compute unit, each with its frequencies formed once.  (8192 rows of 24 heads of 64 in bf16 a twelfth more with twice as many.)
 constexpr int kRotaryGroups = 1024;
 
 template <typename T, bool INTERLEAVED> static hipError_t rotary_pieces(const Rotary& r, const RotaryShape& a, hipStream_t s) {
