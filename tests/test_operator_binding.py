@@ -24,12 +24,14 @@ def test_tensors_that_ask_for_a_gradient_are_refused_while_gradients_are_recorde
     """Every operand of every call; under torch.no_grad() such tensors are taken (and then refused for being on the host)."""
     import paper_2410_14312_amd as tmps
 
-    f, v, pos = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4, 3, dtype=torch.int32)
-    st, ids = torch.zeros(4, 4), torch.zeros(4, 2, dtype=torch.int32)
+    def zeros(*shape):
+        return torch.zeros(*shape, dtype=torch.float32)
+    f, v, pos = zeros(4, 8), zeros(8), torch.zeros(4, 3, dtype=torch.int32)
+    st, ids = zeros(4, 4), torch.zeros(4, 2, dtype=torch.int32)
     calls = [(lambda x: tmps.rotary(x, pos, 1, 8, (4, 0, 0)), (f,)), (lambda out: tmps.rotary(f, pos, 1, 8, (4, 0, 0), out=out), (f,)),
              (lambda x, r, g, s, p, q: tmps.norm_join(x, r, g, s, pre_gain=p, pre_shift=q), (f, f, v, v, v, v)), (lambda y: tmps.norm_join(f, f, v, v, y=y), (f,)),
              (lambda dy, du, x, r, y, stats, g, s, p: tmps.norm_join_backward(dy, du, x, r, y, stats, g, s, pre_gain=p), (f, f, f, f, f, st, v, v, v)),
-             (lambda z, t: tmps.distill(z, None, ids, t), (f, torch.zeros(4, 2)))]
+             (lambda z, t: tmps.distill(z, None, ids, t), (f, zeros(4, 2)))]
     for call, operands in calls:
         for given in asking(*operands):
             with pytest.raises(ValueError, match="asks for a gradient"):
