@@ -947,7 +947,8 @@ int tmps::backward_between(tmps_stage* st, const int* slots, int n_slots, const 
     // A gradient that is added up from several layers is begun long before the last kernel has read them, and one kernel cannot write over the dy that all of its workgroups read
     // (rotary positions can, where the two are the same): it is formed in memory of the stage then and copied at the end.
     void* const dx_wanted = dx;
-    const bool one_kernel = st->layers.size() == 1 && !(st->layers[0].d.kind == TMPS_ROTARY && dx == dy);
+    const int first = st->layers[0].d.kind;
+    const bool one_kernel = st->layers.size() == 1 && first != TMPS_EMBEDDING && !(first == TMPS_ROTARY && dx == dy);
     if ((st->readers[0] > 1 || one_kernel) && over_operand()) dx = stage_dxout(st, 0);
     const bool in_order = over_operand();
     return run_or_replay(st, key, s, [&]() -> int {

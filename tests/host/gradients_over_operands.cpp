@@ -199,6 +199,13 @@ int main(int argc, char** argv) {
             same({L(TMPS_LAYERNORM, {D, S}, TMPS_FLAG_RMS)}, "one norm without a mean", true);
             same({turned}, "rotary positions", true);
             same({dense, dense}, "two dense layers", true);
+            // tokens have no gradient: nothing is written
+            Numbers params, x, dy;
+            const Layers tokens = {L(TMPS_EMBEDDING, {50, S, D})};
+            inputs(tokens, params, x, dy);
+            const Numbers before(dy.begin(), dy.begin() + (int)x.size());
+            const Result r = run(tokens, 1, kOverDy, params, x, dy);
+            expect(r.rc == TMPS_OK && r.dx == before, "an embedding alone, dx over dy");
         } else if (which == "rotary") {
             differences({wide, turned, narrow}, "in place");
             differences({turned, narrow}, "first");
