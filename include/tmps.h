@@ -99,7 +99,8 @@ enum {
     TMPS_FLAG_RMS = 4,  /* a norm without a mean: v / sqrt(mean(v^2) + 1e-5) */
     TMPS_FLAG_GATE = 8, /* rows [f | a]: f under the gate 1 / (1 + exp(-a)) */
     TMPS_FLAG_INTERLEAVED = 16, /* rotary positions: pairs of neighbours 2i and 2i + 1 (else i and i + all pairs) */
-    TMPS_FLAG_OWN_LADDERS = 32  /* rotary positions: frequencies begin anew on each axis (else one ladder over all pairs) */
+    TMPS_FLAG_OWN_LADDERS = 32, /* rotary positions: frequencies begin anew on each axis (else one ladder over all pairs) */
+    TMPS_FLAG_SILU = 64         /* z / (1 + exp(-z)) (operators on their own) */
 };
 /* A convolution normally reads the result of the layer before it.  TMPS_FLAG_SRC(k), k = 2..255, in its flags
  * makes it read the result of the layer k positions before it instead (one position before the first layer of a
@@ -330,6 +331,69 @@ size_t tmps_distill_workspace(int64_t rows, int classes);
 int tmps_distill(int dtype, const tmps_distill_desc* desc, int64_t rows, const float* logits, const int32_t* labels, int64_t label_stride, const int32_t* ids,
                  const float* teacher, int64_t entry_stride, void* dlogits, float* row_loss, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- operators of blocks that mix positions by a recurrence ----
+ *
+ * Conventions as above; workspaces are on 16 bytes.  Rows come sample by sample, `positions` rows each.  Rows of operands and results may be columns of wider rows (strides), also
+ * of the same ones, as long as none lies over another.  Without samples a forward pass has nothing to do and a backward pass is refused. */
+
+/* A causal convolution of 1 to 8 taps along the positions, channels apart, and with TMPS_FLAG_SILU the activation behind it:
+ *   z[t][c] = bias[c] + sum_j weight[c][j] u[t - taps + 1 + j][c],   y = z, or z / (1 + exp(-z))
+ * u: the rows of x and, before a sample's first, those of tail ([samples, taps - 1, channels], of the activations' type; NULL: zeros).  bias may be NULL.  tail_out (NULL: not wanted):
+ * the last taps - 1 inputs, the tail of the positions that follow; for one position it may be tail. */
+int tmps_short_conv_forward(int dtype, int flags, int64_t samples, int64_t positions, int channels, int taps, const void* x, int64_t x_stride,
+                            const float* weight, const float* bias, const void* tail, void* y, int64_t y_stride, void* tail_out, void* hip_stream);
+/* Its gradients from dy and, w.r.t. tail_out, dtail (NULL: none): dx, dtail_in w.r.t. tail (NULL: not wanted) and dparams: those of the weights [channels, taps], then, with a
+ * bias, of it [channels].  Sums over rows are in a fixed order.  workspace: tmps_short_conv_workspace bytes. */
+size_t tmps_short_conv_workspace(int64_t samples, int64_t positions, int channels, int taps);
+int tmps_short_conv_backward(int dtype, int flags, int64_t samples, int64_t positions, int channels, int taps, const void* dy, int64_t dy_stride, const void* x,
+                             int64_t x_stride, const float* weight, const float* bias, const void* tail, const void* dtail, void* dx, int64_t dx_stride,
+                             void* dtail_in, float* dparams, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Selective state space of `heads` heads of dh features with states of n <= 128 features, heads / groups neighbouring heads with the same B and C.  Per sample and head, position by
+ * position, S a matrix [dh, n]:
+ *   delta = log(1 + exp(dt + dt_bias)),   S <- exp(-delta exp(a_log)) S + delta x B',   y = S C + skip x
+ * Rows of x: [x (heads * dh) | B (groups * n) | C (groups * n)]; of dt: heads; of y: heads * dh.  a_log, skip, dt_bias: [heads].  state (NULL: zeros) and state_out (NULL: not
+ * wanted), float [samples, heads, dh, n]: before the first position and behind the last; state_out may be state.  A number of x, dt, B or C that is not finite reaches the results of its
+ * own and later positions of its sample alone.  workspace: tmps_scan_workspace bytes (may be 0). */
+typedef struct {
+    int32_t heads, dh, groups, n;
+} tmps_scan_desc;
+size_t tmps_scan_workspace(const tmps_scan_desc* desc, int64_t samples, int64_t positions);
+int tmps_scan_forward(int dtype, const tmps_scan_desc* desc, int64_t samples, int64_t positions, const void* x, int64_t x_stride, const void* dt, int64_t dt_stride,
+                      const float* a_log, const float* skip, const float* dt_bias, const float* state, void* y, int64_t y_stride, float* state_out,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Its gradients from dy and, w.r.t. state_out, dstate (NULL: none): dx (rows as x's), ddt, dparams: [heads] of a_log, of skip and of dt_bias; dstate_in w.r.t. state (NULL: not wanted;
+ * zeros stand for a state of NULL).  Sums are in a fixed order.  A number that is not finite may reach all gradients of the 64 positions around it and those of earlier ones.
+ * workspace: tmps_scan_backward_workspace bytes (the states and their gradients of every 64th position, fp32, are kept there). */
+size_t tmps_scan_backward_workspace(int dtype, const tmps_scan_desc* desc, int64_t samples, int64_t positions);
+int tmps_scan_backward(int dtype, const tmps_scan_desc* desc, int64_t samples, int64_t positions, const void* dy, int64_t dy_stride, const float* dstate, const void* x,
+                       int64_t x_stride, const void* dt, int64_t dt_stride, const float* a_log, const float* skip, const float* dt_bias, const float* state, void* dx,
+                       int64_t dx_stride, void* ddt, int64_t ddt_stride, float* dparams, float* dstate_in, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Group norm of maps [samples, positions, channels], channels last (one position: each row's groups of neighbouring features), and the activation behind it (TMPS_FLAG_RELU, TMPS_FLAG_GELU,
+ * TMPS_FLAG_SILU or none): mean and variance are those of a sample's positions and the channels / groups channels of a group,
+ *   xhat = (x - mean) / sqrt(var + 1e-5), with TMPS_FLAG_RMS x / sqrt(mean(x^2) + 1e-5),   y = act(gain xhat + shift)
+ * At most 65536 channels.  shift may be NULL.  stats: float [samples, groups, 2], mean (0 with TMPS_FLAG_RMS) and 1/std, for the backward pass.  workspace: tmps_group_norm_workspace
+ * bytes (may be 0). */
+size_t tmps_group_norm_workspace(int dtype, int64_t samples, int64_t positions, int channels, int groups, int backward);
+int tmps_group_norm_forward(int dtype, int flags, int64_t samples, int64_t positions, int channels, int groups, const void* x, const float* gain, const float* shift,
+                            void* y, float* stats, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Its gradients from dy: dx, and dparams: [channels] of gain and [channels] of shift (the latter written without a shift too).  Sums over rows are in a fixed order. */
+int tmps_group_norm_backward(int dtype, int flags, int64_t samples, int64_t positions, int channels, int groups, const void* dy, const void* x, const float* stats,
+                             const float* gain, const float* shift, void* dx, float* dparams, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The norm of all arrays together, *norm = sqrt(sum of all squares) (formed in 64 bits, in a fixed order), and each array times limit / norm in its `out` where the norm is over the
+ * limit (limit >= 0; infinity: never).  out may be data; it is NULL in all arrays where the norm alone is wanted.  A norm that is not finite leaves the arrays' values as they are.
+ * Results lie over no other array.  workspace: tmps_clip_workspace bytes. */
+typedef struct {
+    const void* data;
+    void* out;
+    int64_t n;
+    int32_t dtype;   /* TMPS_F32 or TMPS_BF16_F32MASTER (bf16) */
+} tmps_array;
+size_t tmps_clip_workspace(const tmps_array* arrays, int n);
+int tmps_clip_gradients(const tmps_array* arrays, int n, float limit, float* norm, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ---- nF1B schedule (sections "Work Scheduling" and "Multiple Sequence Problem") ----
  *
  * Host-only time-point simulation of W workers, N micro-batches per mini-batch.  Each task is
@@ -395,7 +459,9 @@ int tmps_streams_destroy(void** streams, int n);
  * cost of such a pair by itself.  tmps_profile_read() waits for the recorded events, adds the elapsed
  * milliseconds and launch counts per class into total_ms[] / launches[] (host arrays of n_classes >=
  * TMPS_KERNEL_CLASSES entries), clears the record and returns TMPS_KERNEL_CLASSES.  Rotary positions count
- * under TMPS_KC_EMBEDDING, norm joins under TMPS_KC_LAYERNORM, distillation under TMPS_KC_SOFTMAX_CE.
+ * under TMPS_KC_EMBEDDING, norm joins and group norm under TMPS_KC_LAYERNORM, distillation under TMPS_KC_SOFTMAX_CE, short
+ * convolutions under TMPS_KC_CONV_FWD and TMPS_KC_CONV_DGRAD, state spaces under TMPS_KC_ATTN_FWD and TMPS_KC_ATTN_BWD, the
+ * norm of gradients under TMPS_KC_REDUCE and their scaling under TMPS_KC_UPDATE.
  * Timing adds host overhead: measure throughput with profiling off. */
 enum {
     TMPS_KC_DENSE_FWD = 0, TMPS_KC_DENSE_DGRAD, TMPS_KC_DENSE_WGRAD, TMPS_KC_CONV_FWD,

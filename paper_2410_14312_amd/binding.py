@@ -12,7 +12,7 @@ TMPS_F32, TMPS_BF16_F32MASTER = 0, 1
 TMPS_LINEAR, TMPS_CONV2D, TMPS_MAXPOOL, TMPS_SOFTMAX_CE, TMPS_LAYERNORM, TMPS_ATTENTION, TMPS_EMBEDDING = 1, 2, 3, 4, 5, 6, 7
 TMPS_AFFINE, TMPS_RESADD, TMPS_AVGPOOL = 8, 9, 10
 TMPS_ROTARY, TMPS_NORMJOIN, TMPS_DISTILL = 11, 12, 13
-TMPS_FLAG_RELU, TMPS_FLAG_GELU, TMPS_FLAG_RMS, TMPS_FLAG_GATE, TMPS_FLAG_INTERLEAVED, TMPS_FLAG_OWN_LADDERS = 1, 2, 4, 8, 16, 32
+TMPS_FLAG_RELU, TMPS_FLAG_GELU, TMPS_FLAG_RMS, TMPS_FLAG_GATE, TMPS_FLAG_INTERLEAVED, TMPS_FLAG_OWN_LADDERS, TMPS_FLAG_SILU = 1, 2, 4, 8, 16, 32, 64
 
 
 class TmpsError(RuntimeError):
@@ -40,6 +40,14 @@ class RotaryDesc(C.Structure):
 
 class DistillDesc(C.Structure):
     _fields_ = [("classes", C.c_int32), ("k", C.c_int32), ("temperature", C.c_float), ("alpha", C.c_float), ("grad_scale", C.c_float)]
+
+
+class ScanDesc(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("dh", C.c_int32), ("groups", C.c_int32), ("n", C.c_int32)]
+
+
+class Array(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
 EXPORTS = {
@@ -93,6 +101,22 @@ EXPORTS = {
     "tmps_distill_workspace": (C.c_size_t, [C.c_int64, C.c_int]),
     "tmps_distill": (C.c_int, [C.c_int, C.POINTER(DistillDesc), C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tmps_short_conv_forward": (C.c_int, [C.c_int, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_int64] + [C.c_void_p] * 4 +
+                                [C.c_int64, C.c_void_p, C.c_void_p]),
+    "tmps_short_conv_workspace": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int, C.c_int]),
+    "tmps_short_conv_backward": (C.c_int, [C.c_int, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] +
+                                 [C.c_void_p] * 5 + [C.c_int64] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]),
+    "tmps_scan_workspace": (C.c_size_t, [C.POINTER(ScanDesc), C.c_int64, C.c_int64]),
+    "tmps_scan_forward": (C.c_int, [C.c_int, C.POINTER(ScanDesc), C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 5 +
+                          [C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tmps_scan_backward_workspace": (C.c_size_t, [C.c_int, C.POINTER(ScanDesc), C.c_int64, C.c_int64]),
+    "tmps_scan_backward": (C.c_int, [C.c_int, C.POINTER(ScanDesc), C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                                     C.c_int64] + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]),
+    "tmps_group_norm_workspace": (C.c_size_t, [C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int]),
+    "tmps_group_norm_forward": (C.c_int, [C.c_int, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]),
+    "tmps_group_norm_backward": (C.c_int, [C.c_int, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+    "tmps_clip_workspace": (C.c_size_t, [C.POINTER(Array), C.c_int]),
+    "tmps_clip_gradients": (C.c_int, [C.POINTER(Array), C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tmps_last_error": (C.c_char_p, []),
 }
 
@@ -471,6 +495,229 @@ def distill(logits, labels, ids, teacher, temperature=1.0, alpha=1.0, grad_scale
           _operand("ids", ids, (rows, k), torch.int32, dev), _operand("teacher", teacher, (rows, k), torch.float32, dev), k,
           dlogits.data_ptr() if gradient else None, row_loss.data_ptr(), ws.data_ptr() if need else None, need)
     return row_loss, dlogits
+
+
+def _rows_of(name, t, width, dtype, device, rows=None):
+    """(address, stride) of rows of `width` neighbouring elements, which may be columns of wider rows."""
+    if t.dim() != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows) or t.dtype is not dtype or t.device != device or \
+            (width > 1 and t.stride(1) != 1 and t.shape[0] > 0):
+        raise ValueError("%s: %s rows of %d neighbouring %s elements on %s are wanted, not %s %s of strides %s on %s"
+                         % (name, "some" if rows is None else rows, width, dtype, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    if t.requires_grad:
+        _unrecorded(name, t)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+
+
+def _new_rows(name, t, rows, width, dtype, device):
+    """(tensor, address, stride) of a result's rows: those given, or new ones."""
+    if t is None:
+        t = _torch().empty(rows, width, dtype=dtype, device=device)
+        return t, t.data_ptr(), width
+    return (t,) + _rows_of(name, t, width, dtype, device, rows)
+
+
+def _samples(rows, positions):
+    if positions < 1 or rows % positions:
+        raise ValueError("positions: rows are samples of as many positions each, not %d rows of %d" % (rows, positions))
+    return rows // positions
+
+
+def _workspace(need, device):
+    return _torch().empty(max(need, 16), dtype=_torch().uint8, device=device) if need else None
+
+
+def short_conv(x, weight, bias=None, positions=1, tail=None, want_tail=False, silu=True, out=None, tail_out=None, stream=None):
+    """A causal convolution along the positions of each sample, channels apart, with SiLU behind it (tmps_short_conv_forward): x [samples * positions, channels] (rows may
+    be columns of wider rows), weight fp32 [channels, taps], bias fp32 [channels] or None, tail [samples, taps - 1, channels]: the inputs before the first
+    position (None: zeros).  Returns (y, tail): the last taps - 1 inputs, None unless want_tail or a tensor tail_out for them is given (for one position it may be
+    tail).  out may be columns of wider rows.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return short_conv(x, weight, bias, positions, tail, want_tail, silu, out, tail_out)
+    torch = _torch()
+    code, t, dev = _dtype_code(x), x.dtype, x.device
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x: [rows, channels], weight: [channels, taps] are wanted")
+    (rows, channels), taps = x.shape, weight.shape[1]
+    samples = _samples(rows, positions)
+    at_x, x_stride = _rows_of("x", x, channels, t, dev)
+    out, at_y, y_stride = _new_rows("out", out, rows, channels, t, dev)
+    if tail_out is None and want_tail:
+        tail_out = torch.empty(samples, taps - 1, channels, dtype=t, device=dev)
+    _call(load_library().tmps_short_conv_forward, dev, None, code, TMPS_FLAG_SILU if silu else 0, samples, positions, channels, taps, at_x, x_stride,
+          _operand("weight", weight, (channels, taps), torch.float32, dev), _operand("bias", bias, (channels,), torch.float32, dev),
+          _operand("tail", tail, (samples, taps - 1, channels), t, dev), at_y, y_stride, _operand("tail_out", tail_out, (samples, taps - 1, channels), t, dev))
+    return out, tail_out
+
+
+def short_conv_backward(dy, x, weight, bias=None, positions=1, tail=None, dtail=None, silu=True, dx=None, stream=None):
+    """Gradients of short_conv from dy and, w.r.t. the tail it returned, dtail (None: none): (dx, dweight, dbias, dtail_in), those of parameters fp32, dbias None without a
+    bias, dtail_in None without a tail.  dy, x and dx may be columns of wider rows.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return short_conv_backward(dy, x, weight, bias, positions, tail, dtail, silu, dx)
+    torch = _torch()
+    code, t, dev, f32 = _dtype_code(x), x.dtype, x.device, torch.float32
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x: [rows, channels], weight: [channels, taps] are wanted")
+    (rows, channels), taps = x.shape, weight.shape[1]
+    samples = _samples(rows, positions)
+    at_x, x_stride = _rows_of("x", x, channels, t, dev)
+    at_dy, dy_stride = _rows_of("dy", dy, channels, t, dev, rows)
+    dx, at_dx, dx_stride = _new_rows("dx", dx, rows, channels, t, dev)
+    dtail_in = torch.empty(samples, taps - 1, channels, dtype=t, device=dev) if tail is not None else None
+    grads = torch.empty(channels * (taps + (bias is not None)), dtype=f32, device=dev)
+    need = load_library().tmps_short_conv_workspace(samples, positions, channels, taps)
+    ws = _workspace(need, dev)
+    _call(load_library().tmps_short_conv_backward, dev, None, code, TMPS_FLAG_SILU if silu else 0, samples, positions, channels, taps, at_dy, dy_stride, at_x, x_stride,
+          _operand("weight", weight, (channels, taps), f32, dev), _operand("bias", bias, (channels,), f32, dev),
+          _operand("tail", tail, (samples, taps - 1, channels), t, dev), _operand("dtail", dtail, (samples, taps - 1, channels), t, dev), at_dx, dx_stride,
+          dtail_in.data_ptr() if dtail_in is not None else None, grads.data_ptr(), ws.data_ptr() if need else None, need)
+    return dx, grads[:channels * taps].view(channels, taps), grads[channels * taps:] if bias is not None else None, dtail_in
+
+
+def _scan_shape(x, a_log, positions, groups, state_features):
+    if x.dim() != 2 or a_log.dim() != 1:
+        raise ValueError("x: [rows, features], a_log: [heads] are wanted")
+    (rows, wide), heads = x.shape, a_log.shape[0]
+    inner = wide - 2 * groups * state_features
+    if groups < 1 or state_features < 1 or heads < 1 or inner < 1 or inner % heads:
+        raise ValueError("x: rows [x (heads * features) | B (groups * state_features) | C (groups * state_features)] are wanted, not %d features for %d heads, "
+                         "%d groups and %d state_features" % (wide, heads, groups, state_features))
+    return rows, wide, heads, inner, _samples(rows, positions), ScanDesc(heads, inner // heads, groups, state_features)
+
+
+def selective_scan(x, dt, a_log, skip, dt_bias, positions, state_features, groups=1, state=None, want_state=False, out=None, state_out=None, stream=None):
+    """A selective state space (tmps_scan_forward): per head and position delta = softplus(dt + dt_bias), S <- exp(-delta exp(a_log)) S + delta x B', y = S C + skip x.
+    x: rows [x (heads * features) | B (groups * state_features) | C (groups * state_features)], dt: rows [heads] (both may be columns of wider rows), samples of
+    `positions` rows each; a_log, skip, dt_bias fp32 [heads]; state fp32 [samples, heads, features, state_features] before the first position (None: zeros).
+    Returns (y, state): y [rows, heads * features] (out, where given, may be columns of wider rows) and the state behind the last position, None unless want_state
+    or a tensor state_out for it is given, which may be state.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return selective_scan(x, dt, a_log, skip, dt_bias, positions, state_features, groups, state, want_state, out, state_out)
+    torch = _torch()
+    code, t, dev, f32 = _dtype_code(x), x.dtype, x.device, torch.float32
+    rows, wide, heads, inner, samples, d = _scan_shape(x, a_log, positions, groups, state_features)
+    of_state = (samples, heads, inner // heads, state_features)
+    at_x, x_stride = _rows_of("x", x, wide, t, dev)
+    at_dt, dt_stride = _rows_of("dt", dt, heads, t, dev, rows)
+    out, at_y, y_stride = _new_rows("out", out, rows, inner, t, dev)
+    if state_out is None and want_state:
+        state_out = torch.empty(of_state, dtype=f32, device=dev)
+    need = load_library().tmps_scan_workspace(C.byref(d), samples, positions)
+    ws = _workspace(need, dev)
+    _call(load_library().tmps_scan_forward, dev, None, code, C.byref(d), samples, positions, at_x, x_stride, at_dt, dt_stride,
+          _operand("a_log", a_log, (heads,), f32, dev), _operand("skip", skip, (heads,), f32, dev), _operand("dt_bias", dt_bias, (heads,), f32, dev),
+          _operand("state", state, of_state, f32, dev), at_y, y_stride, _operand("state_out", state_out, of_state, f32, dev), ws.data_ptr() if need else None, need)
+    return out, state_out
+
+
+def selective_scan_backward(dy, x, dt, a_log, skip, dt_bias, positions, state_features, groups=1, state=None, dstate=None, dx=None, ddt=None, stream=None):
+    """Gradients of selective_scan from dy and, w.r.t. the state it returned, dstate (None: none): (dx, ddt, da_log, dskip, ddt_bias, dstate_in), dx rows as x's,
+    those of parameters and of the state fp32, dstate_in None without a state.  dx and ddt, where given, may be columns of wider rows.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return selective_scan_backward(dy, x, dt, a_log, skip, dt_bias, positions, state_features, groups, state, dstate, dx, ddt)
+    torch = _torch()
+    code, t, dev, f32 = _dtype_code(x), x.dtype, x.device, torch.float32
+    rows, wide, heads, inner, samples, d = _scan_shape(x, a_log, positions, groups, state_features)
+    of_state = (samples, heads, inner // heads, state_features)
+    at_dy, dy_stride = _rows_of("dy", dy, inner, t, dev, rows)
+    at_x, x_stride = _rows_of("x", x, wide, t, dev)
+    at_dt, dt_stride = _rows_of("dt", dt, heads, t, dev, rows)
+    dx, at_dx, dx_stride = _new_rows("dx", dx, rows, wide, t, dev)
+    ddt, at_ddt, ddt_stride = _new_rows("ddt", ddt, rows, heads, t, dev)
+    dstate_in = torch.empty(of_state, dtype=f32, device=dev) if state is not None else None
+    grads = torch.empty(3, heads, dtype=f32, device=dev)
+    need = load_library().tmps_scan_backward_workspace(code, C.byref(d), samples, positions)
+    ws = _workspace(need, dev)
+    _call(load_library().tmps_scan_backward, dev, None, code, C.byref(d), samples, positions, at_dy, dy_stride, _operand("dstate", dstate, of_state, f32, dev), at_x, x_stride,
+          at_dt, dt_stride, _operand("a_log", a_log, (heads,), f32, dev), _operand("skip", skip, (heads,), f32, dev), _operand("dt_bias", dt_bias, (heads,), f32, dev),
+          _operand("state", state, of_state, f32, dev), at_dx, dx_stride, at_ddt, ddt_stride, grads.data_ptr(),
+          dstate_in.data_ptr() if dstate_in is not None else None, ws.data_ptr() if need else None, need)
+    return (dx, ddt) + tuple(grads.unbind(0)) + (dstate_in,)
+
+
+def _act_flags(act, rms):
+    acts = {None: 0, "relu": TMPS_FLAG_RELU, "gelu": TMPS_FLAG_GELU, "silu": TMPS_FLAG_SILU}
+    if act not in acts:
+        raise ValueError('act: None, "relu", "gelu" or "silu"')
+    return acts[act] | (TMPS_FLAG_RMS if rms else 0)
+
+
+def group_norm(x, gain, shift=None, groups=1, positions=1, act=None, rms=False, y=None, stats=None, stream=None):
+    """Group norm of maps [samples * positions, channels], channels last, and the activation behind it (tmps_group_norm_forward): y = act(gain xhat + shift), xhat = (x - mean) /
+    sqrt(var + 1e-5) over a sample's positions and the channels / groups channels of a group, with `rms` x / sqrt(mean(x^2) + 1e-5); act: None, "relu", "gelu" or
+    "silu"; shift may be None.  Returns (y, stats): stats fp32 [samples, groups, 2], mean and 1/std.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return group_norm(x, gain, shift, groups, positions, act, rms, y, stats)
+    torch = _torch()
+    code, t, dev, f32 = _dtype_code(x), x.dtype, x.device, torch.float32
+    if x.dim() != 2:
+        raise ValueError("x: [rows, channels] is wanted, not %s" % (tuple(x.shape),))
+    rows, channels = x.shape
+    samples = _samples(rows, positions)
+    if y is None:
+        y = torch.empty(rows, channels, dtype=t, device=dev)
+    if stats is None:
+        stats = torch.empty(samples, max(groups, 0), 2, dtype=f32, device=dev)
+    need = load_library().tmps_group_norm_workspace(code, samples, positions, channels, groups, 0)
+    ws = _workspace(need, dev)
+    _call(load_library().tmps_group_norm_forward, dev, None, code, _act_flags(act, rms), samples, positions, channels, groups, _operand("x", x, (rows, channels), t, dev),
+          _operand("gain", gain, (channels,), f32, dev), _operand("shift", shift, (channels,), f32, dev), _operand("y", y, (rows, channels), t, dev),
+          _operand("stats", stats, (samples, groups, 2), f32, dev), ws.data_ptr() if need else None, need)
+    return y, stats
+
+
+def group_norm_backward(dy, x, stats, gain, shift=None, groups=1, positions=1, act=None, rms=False, dx=None, stream=None):
+    """Gradients of group_norm from dy and the stats that it returned: (dx, dgain, dshift), those of parameters fp32, dshift None without a shift.  `stream` as for rotary."""
+    if stream is not None:
+        with _within(stream, x.device):
+            return group_norm_backward(dy, x, stats, gain, shift, groups, positions, act, rms, dx)
+    torch = _torch()
+    code, t, dev, f32 = _dtype_code(x), x.dtype, x.device, torch.float32
+    if x.dim() != 2:
+        raise ValueError("x: [rows, channels] is wanted, not %s" % (tuple(x.shape),))
+    rows, channels = x.shape
+    samples = _samples(rows, positions)
+    if dx is None:
+        dx = torch.empty(rows, channels, dtype=t, device=dev)
+    grads = torch.empty(2, channels, dtype=f32, device=dev)
+    need = load_library().tmps_group_norm_workspace(code, samples, positions, channels, groups, 1)
+    ws = _workspace(need, dev)
+    _call(load_library().tmps_group_norm_backward, dev, None, code, _act_flags(act, rms), samples, positions, channels, groups, _operand("dy", dy, (rows, channels), t, dev),
+          _operand("x", x, (rows, channels), t, dev), _operand("stats", stats, (samples, groups, 2), f32, dev), _operand("gain", gain, (channels,), f32, dev),
+          _operand("shift", shift, (channels,), f32, dev), _operand("dx", dx, (rows, channels), t, dev), grads.data_ptr(), ws.data_ptr() if need else None, need)
+    dgain, dshift = grads.unbind(0)
+    return dx, dgain, dshift if shift is not None else None
+
+
+def clip_gradients(grads, limit, out=None, stream=None):
+    """The norm of all tensors of `grads` together, fp32 of no dimension, and each of them times limit / norm where that is less than one, in place or in the tensors `out`
+    (tmps_clip_gradients).  limit = inf: the norm alone.  A norm that is not finite leaves the values as they are.  Tensors are contiguous, fp32 or bf16.  `stream` as for rotary."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("grads: one tensor at least is wanted")
+    dev = grads[0].device
+    if stream is not None:
+        with _within(stream, dev):
+            return clip_gradients(grads, limit, out)
+    torch = _torch()
+    to = grads if out is None else list(out)
+    if len(to) != len(grads):
+        raise ValueError("out: %d tensors are wanted, not %d" % (len(grads), len(to)))
+    norm_alone = out is None and limit == float("inf")
+    arrays = (Array * len(grads))()
+    for a, g, o in zip(arrays, grads, to):
+        a.data, a.n, a.dtype = _operand("grads", g, g.shape, g.dtype, dev), g.numel(), _dtype_code(g)
+        a.out = None if norm_alone else a.data if o is g else _operand("out", o, g.shape, g.dtype, dev)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    need = load_library().tmps_clip_workspace(arrays, len(grads))
+    ws = _workspace(need, dev)
+    _call(load_library().tmps_clip_gradients, dev, None, arrays, len(grads), limit, norm.data_ptr(), ws.data_ptr() if need else None, need)
+    return norm
 
 
 # ------------------------------------------------------------------------------------ device side

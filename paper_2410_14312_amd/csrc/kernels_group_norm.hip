@@ -1,0 +1,573 @@
+// Group norm with its activation, and its gradients.  Two forms, both bound by memory:
+//   rows  one position a sample: each group of a sample is a row of its own, held in the registers of a team of threads, one pass;
+//   maps  more positions: sums of slices of positions, the samples' sums, and a second pass over the map.
+// Of a group's values the mean is taken first and the differences from it squared; what several threads or slices have is joined as (number, mean, sum of squared differences).
+#include <algorithm>
+
+#include "launch.h"
+#include "mixer.h"
+#include "norm_join.hip.h"
+
+#pragma clang fp contract(off)
+
+namespace tmps {
+
+// z = gain xhat + shift in single steps, so that both passes have the same bits and a ReLU the same border.
+__device__ __forceinline__ float norm_z(float x, float mean, float rstd, float gain, float shift, float& xhat) {
+    xhat = (x - mean) * rstd;
+    return gain * xhat + shift;
+}
+
+// The hardware's exponential and reciprocal are off by some 2^-23, enough for results of 8 bits, not for fp32.
+template <typename T> __device__ __forceinline__ float norm_sigmoid(float z) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+    return 1.0f / (1.0f + expf(-z));
+}
+template <typename T> __device__ __forceinline__ float norm_act(int act, float z) {
+    if (act == kNormActRelu) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if (act == kNormActGelu) return sizeof(T) == 2 ? gelu_f(z) : z * (0.5f + 0.5f * erff(z * 0.70710678118654752f));
+    if (act == kNormActSilu) return z * norm_sigmoid<T>(z);
+    return z;
+}
+template <typename T> __device__ __forceinline__ float norm_act_grad(int act, float z, float dy) {
+    if (act == kNormActRelu) return z > 0.0f ? dy : 0.0f;
+    if (act == kNormActGelu)
+        return dy * (sizeof(T) == 2 ? gelu_grad_f(z) : 0.5f + 0.5f * erff(z * 0.70710678118654752f) + z * 0.3989422804014327f * expf(-0.5f * z * z));
+    if (act == kNormActSilu) {
+        const float g = norm_sigmoid<T>(z);
+        return dy * (g * (1.0f + z * (1.0f - g)));
+    }
+    return dy;
+}
+
+// (count, mean, sum of squared differences) of two sets as one
+__device__ __forceinline__ void join_moments(float& n, float& mean, float& m2, float n2, float mean2, float m22) {
+    if (n2 == 0.0f) return;
+    const float all = n + n2, d = mean2 - mean;
+    mean += d * (n2 / all);
+    m2 += m22 + d * d * (n * n2 / all);
+    n = all;
+}
+
+// ------------------------------------------------------------------------------------------------ rows
+constexpr int kGroupRowThreads = 524288;   // threads of a launch at most
+
+// The rows are the samples' groups; a team's rows are a whole number of samples apart, so that its group's parameters stay in registers.
+template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(Team<TEAM>::kThreads) void group_rows_fwd_kernel(GroupNorm a, int64_t step) {
+    __shared__ float red[2][2 * 16];
+    constexpr int V = kPiece<T>;
+    const int D = a.channels / a.groups;
+    const Pieces<TEAM, N, V, WHOLE> p{D};
+    const int64_t rows = a.samples * a.groups;
+    int64_t row = (int64_t)blockIdx.x * Team<TEAM>::kRows + threadIdx.x / TEAM;
+    if (row >= step) return;   // (teams of a workgroup with barriers are the whole of it)
+    int place = 0;
+    const int group = (int)(row % a.groups);
+    float gain[N][V], shift[N][V];
+    uint4 next[N];
+    request_row(next, (const T*)a.x + row * D, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        load_vector(gain[i], a.gain + (int64_t)group * D, p, i);
+        load_vector(shift[i], a.shift ? a.shift + (int64_t)group * D : nullptr, p, i);
+    }
+    for (; row < rows; row += step) {
+        float v[N][V];
+        float s[1] = {0.0f}, mean = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            unpack(next[i], v[i]);
+            if (p.any(i)) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[0] += p.own(i, e) ? v[i][e] : 0.0f;
+            }
+        }
+        if (row + step < rows) request_row(next, (const T*)a.x + (row + step) * D, p);
+        if (!a.rms) {
+            Team<TEAM>::sums(s, red, place);
+            mean = s[0] / (float)D;
+        }
+        s[0] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (p.any(i)) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float d = p.own(i, e) ? v[i][e] - mean : 0.0f;
+                    s[0] = fmaf(d, d, s[0]);
+                }
+            }
+        Team<TEAM>::sums(s, red, place);
+        const float rstd = 1.0f / sqrtf(s[0] / (float)D + 1e-5f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (!p.any(i)) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float xhat;
+                v[i][e] = norm_act<T>(a.act, norm_z(v[i][e], mean, rstd, gain[i][e], shift[i][e], xhat));
+            }
+            store_piece((T*)a.y + row * D, p, i, v[i]);
+        }
+        if (threadIdx.x % TEAM == 0) {
+            a.stats[2 * row] = mean;
+            a.stats[2 * row + 1] = rstd;
+        }
+    }
+}
+
+// part: [step / groups][2][channels], the sums of each team's rows.
+template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(Team<TEAM>::kThreads) void group_rows_bwd_kernel(GroupNormBackward a, int64_t step, float* part) {
+    __shared__ float red[2][2 * 16];
+    constexpr int V = kPiece<T>;
+    const int D = a.channels / a.groups;
+    const Pieces<TEAM, N, V, WHOLE> p{D};
+    const int64_t rows = a.samples * a.groups;
+    int64_t row = (int64_t)blockIdx.x * Team<TEAM>::kRows + threadIdx.x / TEAM;
+    if (row >= step) return;
+    int place = 0;
+    const int group = (int)(row % a.groups);
+    float* const mine = part + (row / a.groups) * 2 * (int64_t)a.channels + (int64_t)group * D;
+    float gain[N][V], shift[N][V], dgain[N][V], dshift[N][V];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        load_vector(gain[i], a.gain + (int64_t)group * D, p, i);
+        load_vector(shift[i], a.shift ? a.shift + (int64_t)group * D : nullptr, p, i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) dgain[i][e] = dshift[i][e] = 0.0f;
+    }
+    uint4 nx[N], ng[N];
+    request_row(nx, (const T*)a.x + row * D, p);
+    request_row(ng, (const T*)a.dy + row * D, p);
+    for (; row < rows; row += step) {
+        const float mean = a.stats[2 * row], rstd = a.stats[2 * row + 1];
+        float xhat[N][V], g[N][V];
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            unpack(nx[i], xhat[i]);
+            unpack(ng[i], g[i]);
+        }
+        if (row + step < rows) {
+            request_row(nx, (const T*)a.x + (row + step) * D, p);
+            request_row(ng, (const T*)a.dy + (row + step) * D, p);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (!p.any(i)) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (!p.own(i, e)) continue;
+                const float z = norm_z(xhat[i][e], mean, rstd, gain[i][e], shift[i][e], xhat[i][e]);
+                const float dz = norm_act_grad<T>(a.act, z, g[i][e]);
+                dgain[i][e] = fmaf(dz, xhat[i][e], dgain[i][e]);
+                dshift[i][e] += dz;
+                g[i][e] = dz * gain[i][e];
+                s[0] += g[i][e];
+                s[1] = fmaf(g[i][e], xhat[i][e], s[1]);
+            }
+        }
+        Team<TEAM>::sums(s, red, place);
+        const float of_mean = a.rms ? 0.0f : s[0] / (float)D, of_xhat = s[1] / (float)D;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (!p.any(i)) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[i][e] = (fmaf(-xhat[i][e], of_xhat, g[i][e]) - of_mean) * rstd;
+            store_piece((T*)a.dx + row * D, p, i, g[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (!p.any(i)) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (!p.own(i, e)) continue;
+            mine[p.at(i) + e] = dgain[i][e];
+            mine[a.channels + p.at(i) + e] = dshift[i][e];
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ maps
+// A thread has a piece of channels and every `lanes`-th position of its workgroup's slice.  A workgroup has up to 256 pieces; a last piece that begins earlier comes out the same as
+// the one before it where both hold a channel.
+template <typename T> struct MapPlace {
+    static constexpr int V = kPiece<T>;
+    int C, pieces, width, lanes, lane, at;   // pieces of a row; of this workgroup; positions side by side; this thread's; its first channel
+    bool any;
+    __device__ __forceinline__ MapPlace(int channels, int block, int threads) : C(channels), pieces((channels + V - 1) / V) {
+        width = min(pieces - block * 256, 256);
+        lanes = threads / width;
+        lane = (int)threadIdx.x / width;
+        any = lane < lanes;
+        at = min((block * 256 + (int)threadIdx.x % width) * V, max(C - V, 0));
+    }
+    __device__ __forceinline__ uint4 request(const T* row) const {
+        if (C >= V) return load16_any(row + at);
+        struct Values { T v[V]; } f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) f.v[e] = e < C ? row[e] : T(0.0f);
+        return __builtin_bit_cast(uint4, f);
+    }
+    __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
+        if (C >= V) {
+            store16_any(row + at, pack(v));
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < C) row[e] = from_f32<T>(v[e]);
+        }
+    }
+    template <class F> __device__ __forceinline__ void params(float (&v)[V], F&& f) const {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = f(min(at + e, C - 1));
+    }
+};
+
+constexpr int kMapBlock = 8;   // positions whose values a thread has at a time
+
+// Mean and sum of squared differences of every channel over a slice: part [sample][slice][channels][2].
+template <typename T> __global__ __launch_bounds__(256) void group_map_moments_kernel(const T* x, int64_t positions, int channels, int64_t slice, int slices, bool rms, float* part) {
+    constexpr int V = kPiece<T>;
+    __shared__ float fold[256][2 * V + 1];
+    const MapPlace<T> p(channels, blockIdx.y, 256);
+    const int64_t sample = blockIdx.x / slices, cut = blockIdx.x % slices;
+    const int64_t t0 = cut * slice, t1 = min(t0 + slice, positions);
+    const T* const rows = x + sample * positions * channels;
+    float n = 0.0f, mean[V], m2[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) mean[e] = m2[e] = 0.0f;
+    if (p.any) {
+        for (int64_t t = t0 + p.lane; t < t1; t += (int64_t)p.lanes * kMapBlock) {
+            uint4 u[kMapBlock];
+            const int many = (int)min<int64_t>(kMapBlock, (t1 - t + p.lanes - 1) / p.lanes);
+#pragma unroll
+            for (int k = 0; k < kMapBlock; ++k)
+                if (k < many) u[k] = p.request(rows + (t + (int64_t)k * p.lanes) * channels);
+            float v[kMapBlock][V], bm[V], b2[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) bm[e] = b2[e] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kMapBlock; ++k)
+                if (k < many) {
+                    unpack(u[k], v[k]);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) bm[e] += v[k][e];
+                }
+            const float by = rms ? 0.0f : 1.0f / (float)many;
+#pragma unroll
+            for (int e = 0; e < V; ++e) bm[e] *= by;
+#pragma unroll
+            for (int k = 0; k < kMapBlock; ++k)
+                if (k < many) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float d = v[k][e] - bm[e];
+                        b2[e] = fmaf(d, d, b2[e]);
+                    }
+                }
+            const float all = n + (float)many, share = (float)many / all, between = n * share;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = bm[e] - mean[e];
+                mean[e] = fmaf(d, share, mean[e]);
+                m2[e] += fmaf(d * d, between, b2[e]);
+            }
+            n = all;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        fold[threadIdx.x][e] = mean[e];
+        fold[threadIdx.x][V + e] = m2[e];
+    }
+    fold[threadIdx.x][2 * V] = n;
+    __syncthreads();
+    float* const mine = part + (sample * slices + cut) * channels * 2;
+    for (int i = threadIdx.x; i < p.width * V; i += 256) {
+        const int k = i / V, e = i % V;
+        float c = fold[k][2 * V], m = fold[k][e], s = fold[k][V + e];
+        for (int l = 1; l < p.lanes; ++l) {
+            const float* f = fold[l * p.width + k];
+            join_moments(c, m, s, f[2 * V], f[e], f[V + e]);
+        }
+        const int first = ((int)blockIdx.y * 256 + k) * V, ch = min(first, max(channels - V, 0)) + e;
+        if (ch >= first && ch < channels) {
+            mine[2 * ch] = m;
+            mine[2 * ch + 1] = s;
+        }
+    }
+}
+
+// The groups' means and 1/std from those of the slices' channels: 16 lanes to a group.
+__global__ __launch_bounds__(256) void group_map_stats_kernel(const float* part, int64_t samples, int64_t positions, int channels, int groups, int64_t slice, int slices, bool rms, float* stats) {
+    const int64_t g = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    if (g >= samples * groups) return;
+    const int64_t sample = g / groups;
+    const int size = channels / groups, first = (int)(g % groups) * size;
+    float n = 0.0f, mean = 0.0f, m2 = 0.0f;
+    for (int i = threadIdx.x % 16; i < size * slices; i += 16) {
+        const int cut = i / size;
+        const float many = (float)min<int64_t>(slice, positions - cut * slice);
+        const float* const f = part + ((sample * slices + cut) * channels + first + i % size) * 2;
+        join_moments(n, mean, m2, many, f[0], f[1]);
+    }
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) {
+        const float n2 = __shfl_xor(n, d), mean2 = __shfl_xor(mean, d), m22 = __shfl_xor(m2, d);
+        if (n == 0.0f) n = n2, mean = mean2, m2 = m22;
+        else join_moments(n, mean, m2, n2, mean2, m22);
+    }
+    if (threadIdx.x % 16 == 0) {
+        stats[2 * g] = rms ? 0.0f : mean;
+        stats[2 * g + 1] = 1.0f / sqrtf(m2 / ((float)size * (float)positions) + 1e-5f);
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void group_map_apply_kernel(GroupNorm a, int64_t slice, int slices) {
+    constexpr int V = kPiece<T>;
+    const MapPlace<T> p(a.channels, blockIdx.y, 256);
+    if (!p.any) return;
+    const int64_t sample = blockIdx.x / slices, cut = blockIdx.x % slices;
+    const int64_t t0 = cut * slice, t1 = min(t0 + slice, a.positions);
+    const int size = a.channels / a.groups;
+    const float* const stats = a.stats + sample * a.groups * 2;
+    float mean[V], rstd[V], gain[V], shift[V];
+    p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
+    p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
+    p.params(gain, [&](int c) { return a.gain[c]; });
+    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    const T* const x = (const T*)a.x + sample * a.positions * a.channels;
+    T* const y = (T*)a.y + sample * a.positions * a.channels;
+#pragma unroll 4
+    for (int64_t t = t0 + p.lane; t < t1; t += p.lanes) {
+        float v[V];
+        unpack(p.request(x + t * a.channels), v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float xhat;
+            v[e] = norm_act<T>(a.act, norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat));
+        }
+        p.store(y + t * a.channels, v);
+    }
+}
+
+// Sums of dz xhat and of dz of every channel over a slice: part [sample][slice][2][channels].
+template <typename T> __global__ __launch_bounds__(256) void group_map_sums_kernel(GroupNormBackward a, int64_t slice, int slices, float* part) {
+    constexpr int V = kPiece<T>;
+    __shared__ float fold[256][2 * V];
+    const MapPlace<T> p(a.channels, blockIdx.y, 256);
+    const int64_t sample = blockIdx.x / slices, cut = blockIdx.x % slices;
+    const int64_t t0 = cut * slice, t1 = min(t0 + slice, a.positions);
+    float with_xhat[V], alone[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) with_xhat[e] = alone[e] = 0.0f;
+    if (p.any) {
+        const int size = a.channels / a.groups;
+        const float* const stats = a.stats + sample * a.groups * 2;
+        float mean[V], rstd[V], gain[V], shift[V];
+        p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
+        p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
+        p.params(gain, [&](int c) { return a.gain[c]; });
+        p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+        const T* const x = (const T*)a.x + sample * a.positions * a.channels;
+        const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
+#pragma unroll 4
+        for (int64_t t = t0 + p.lane; t < t1; t += p.lanes) {
+            float v[V], g[V];
+            unpack(p.request(x + t * a.channels), v);
+            unpack(p.request(dy + t * a.channels), g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float xhat;
+                const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
+                const float dz = norm_act_grad<T>(a.act, z, g[e]);
+                with_xhat[e] = fmaf(dz, xhat, with_xhat[e]);
+                alone[e] += dz;
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        fold[threadIdx.x][e] = with_xhat[e];
+        fold[threadIdx.x][V + e] = alone[e];
+    }
+    __syncthreads();
+    float* const mine = part + (sample * slices + cut) * 2 * a.channels;
+    for (int i = threadIdx.x; i < 2 * p.width * V; i += 256) {
+        const int which = i / (p.width * V), k = i / V % p.width, e = i % V;
+        float s = 0.0f;
+        for (int l = 0; l < p.lanes; ++l) s += fold[l * p.width + k][which * V + e];
+        const int first = ((int)blockIdx.y * 256 + k) * V, ch = min(first, max(a.channels - V, 0)) + e;
+        if (ch >= first && ch < a.channels) mine[which * (int64_t)a.channels + ch] = s;
+    }
+}
+
+// Each group's sums of gain dz and of gain dz xhat over its values, divided by their number: means [samples][groups][2].
+__global__ __launch_bounds__(256) void group_map_means_kernel(const float* part, const float* gain, int64_t samples, int64_t positions, int channels, int groups, int slices, bool rms, float* means) {
+    const int64_t g = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    if (g >= samples * groups) return;
+    const int64_t sample = g / groups;
+    const int size = channels / groups, first = (int)(g % groups) * size;
+    float with_xhat = 0.0f, alone = 0.0f;
+    for (int i = threadIdx.x % 16; i < size * slices; i += 16) {
+        const int c = first + i % size;
+        const float* const f = part + (sample * slices + i / size) * 2 * channels + c;
+        with_xhat = fmaf(gain[c], f[0], with_xhat);
+        alone = fmaf(gain[c], f[channels], alone);
+    }
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) {
+        with_xhat += __shfl_xor(with_xhat, d);
+        alone += __shfl_xor(alone, d);
+    }
+    if (threadIdx.x % 16 == 0) {
+        const float n = (float)size * (float)positions;
+        means[2 * g] = rms ? 0.0f : alone / n;
+        means[2 * g + 1] = with_xhat / n;
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void group_map_apply_bwd_kernel(GroupNormBackward a, int64_t slice, int slices, const float* means) {
+    constexpr int V = kPiece<T>;
+    const MapPlace<T> p(a.channels, blockIdx.y, 256);
+    if (!p.any) return;
+    const int64_t sample = blockIdx.x / slices, cut = blockIdx.x % slices;
+    const int64_t t0 = cut * slice, t1 = min(t0 + slice, a.positions);
+    const int size = a.channels / a.groups;
+    const float *const stats = a.stats + sample * a.groups * 2, *const of = means + sample * a.groups * 2;
+    float mean[V], rstd[V], gain[V], shift[V], alone[V], with_xhat[V];
+    p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
+    p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
+    p.params(alone, [&](int c) { return of[2 * (c / size)]; });
+    p.params(with_xhat, [&](int c) { return of[2 * (c / size) + 1]; });
+    p.params(gain, [&](int c) { return a.gain[c]; });
+    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    const T* const x = (const T*)a.x + sample * a.positions * a.channels;
+    const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
+    T* const dx = (T*)a.dx + sample * a.positions * a.channels;
+#pragma unroll 2
+    for (int64_t t = t0 + p.lane; t < t1; t += p.lanes) {
+        float v[V], g[V];
+        unpack(p.request(x + t * a.channels), v);
+        unpack(p.request(dy + t * a.channels), g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float xhat;
+            const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
+            const float dz = norm_act_grad<T>(a.act, z, g[e]) * gain[e];
+            v[e] = (fmaf(-xhat, with_xhat[e], dz) - alone[e]) * rstd[e];
+        }
+        p.store(dx + t * a.channels, v);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+// Slices of a sample's positions: as many as give the chip 2048 workgroups, of 32 positions at least.
+constexpr int kMapGroups = 2048, kMapPositions = 32;
+struct MapPlan {
+    int64_t slice;
+    int slices, blocks;   // blocks: of 256 pieces of channels
+};
+static MapPlan map_plan(int64_t samples, int64_t positions, int channels, int V) {
+    MapPlan m;
+    m.blocks = ((channels + V - 1) / V + 255) / 256;
+    int64_t want = (kMapGroups + samples * m.blocks - 1) / (samples * m.blocks);
+    if (want > (positions + kMapPositions - 1) / kMapPositions) want = (positions + kMapPositions - 1) / kMapPositions;
+    if (want < 1) want = 1;
+    m.slice = (positions + want - 1) / want;
+    m.slices = (int)((positions + m.slice - 1) / m.slice);
+    return m;
+}
+
+// Teams of a launch of rows: a whole number of samples' groups.
+static int64_t row_teams(int64_t samples, int groups, int team, int rows_each) {
+    const int64_t rows = samples * groups, most = kGroupRowThreads / team;
+    int64_t n = (samples + rows_each - 1) / rows_each;
+    if (n * groups > most) n = most / groups;
+    if (n < 1) n = 1;
+    return n * groups < rows ? n * groups : rows;
+}
+constexpr int kRowsEachBack = 8;
+
+constexpr int kRowFeatures = 16384;   // of a group in the form by rows
+static bool by_rows(int64_t positions, int channels, int groups) { return positions == 1 && channels / groups <= kRowFeatures; }
+
+// (as much as any call of no more samples and positions takes)
+size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions, int channels, int groups, bool backward) {
+    if (by_rows(positions, channels, groups)) return backward ? (size_t)row_teams(samples, groups, 16, kRowsEachBack) / groups * 2 * channels * sizeof(float) : 0;
+    const int64_t blocks = map_plan(samples, positions, channels, dtype == kBF16 ? 8 : 4).blocks;
+    const int64_t most = std::min(samples * ((positions + kMapPositions - 1) / kMapPositions), samples + kMapGroups / blocks + 1);
+    return ((size_t)most * 2 * channels + (backward ? (size_t)samples * groups * 2 : 0)) * sizeof(float);
+}
+
+template <typename T, int TEAM, int N, bool WHOLE> static hipError_t rows_fwd(const GroupNorm& a, hipStream_t s) {
+    const int64_t teams = row_teams(a.samples, a.groups, TEAM, 1);
+    const dim3 grid((unsigned)((teams + Team<TEAM>::kRows - 1) / Team<TEAM>::kRows));
+    return launch_timed(kcLayerNorm, group_rows_fwd_kernel<T, TEAM, N, WHOLE>, grid, dim3(Team<TEAM>::kThreads), 0, s, a, teams);
+}
+template <typename T, int TEAM, int N, bool WHOLE> static hipError_t rows_bwd(const GroupNormBackward& a, float* part, hipStream_t s) {
+    const int64_t teams = row_teams(a.samples, a.groups, TEAM, kRowsEachBack);
+    const dim3 grid((unsigned)((teams + Team<TEAM>::kRows - 1) / Team<TEAM>::kRows));
+    const hipError_t e = launch_timed(kcLayerNorm, group_rows_bwd_kernel<T, TEAM, N, WHOLE>, grid, dim3(Team<TEAM>::kThreads), 0, s, a, teams, part);
+    if (e != hipSuccess) return e;
+    return reduce_all(Reductions(1, Reduction{part, a.dparams, 2 * (int64_t)a.channels, (int)(teams / a.groups), true}), s);
+}
+
+#define TMPS_GROUP_ROWS(fn, WHOLE, D, ...)                               \
+    if (D <= 128) return fn<T, 16, kOne<T>, WHOLE>(__VA_ARGS__);         \
+    if (D <= 512) return fn<T, 64, kOne<T>, WHOLE>(__VA_ARGS__);         \
+    if (D <= 2048) return fn<T, 256, kOne<T>, WHOLE>(__VA_ARGS__);       \
+    if (D <= 8192) return fn<T, 1024, kOne<T>, WHOLE>(__VA_ARGS__);      \
+    return fn<T, 1024, 2 * kOne<T>, WHOLE>(__VA_ARGS__)
+
+template <typename T> static hipError_t rows_fwd_type(const GroupNorm& a, hipStream_t s) {
+    const int D = a.channels / a.groups;
+    if (join_whole<T>(D, {a.x, a.gain, a.shift, a.y})) { TMPS_GROUP_ROWS(rows_fwd, true, D, a, s); }
+    TMPS_GROUP_ROWS(rows_fwd, false, D, a, s);
+}
+template <typename T> static hipError_t rows_bwd_type(const GroupNormBackward& a, float* part, hipStream_t s) {
+    const int D = a.channels / a.groups;
+    if (join_whole<T>(D, {a.dy, a.x, a.gain, a.shift, a.dx})) { TMPS_GROUP_ROWS(rows_bwd, true, D, a, part, s); }
+    TMPS_GROUP_ROWS(rows_bwd, false, D, a, part, s);
+}
+
+template <typename T> static hipError_t forward_type(const GroupNorm& a, float* ws, hipStream_t s) {
+    if (by_rows(a.positions, a.channels, a.groups)) return rows_fwd_type<T>(a, s);
+    const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
+    if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
+    hipError_t e = launch_timed(kcLayerNorm, group_map_moments_kernel<T>, grid, dim3(256), 0, s, (const T*)a.x, a.positions, a.channels, m.slice, m.slices, a.rms, ws);
+    if (e != hipSuccess) return e;
+    e = launch_timed(kcLayerNorm, group_map_stats_kernel, dim3((unsigned)((a.samples * a.groups + 15) / 16)), dim3(256), 0, s, (const float*)ws, a.samples, a.positions, a.channels,
+                     a.groups, m.slice, m.slices, a.rms, a.stats);
+    if (e != hipSuccess) return e;
+    return launch_timed(kcLayerNorm, group_map_apply_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices);
+}
+
+template <typename T> static hipError_t backward_type(const GroupNormBackward& a, float* ws, hipStream_t s) {
+    if (by_rows(a.positions, a.channels, a.groups)) return rows_bwd_type<T>(a, ws, s);
+    const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
+    if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
+    float* const means = ws + a.samples * m.slices * 2 * (int64_t)a.channels;
+    const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
+    hipError_t e = launch_timed(kcLayerNorm, group_map_sums_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices, ws);
+    if (e != hipSuccess) return e;
+    e = launch_timed(kcLayerNorm, group_map_means_kernel, dim3((unsigned)((a.samples * a.groups + 15) / 16)), dim3(256), 0, s, (const float*)ws, a.gain, a.samples, a.positions,
+                     a.channels, a.groups, m.slices, a.rms, means);
+    if (e != hipSuccess) return e;
+    e = launch_timed(kcLayerNorm, group_map_apply_bwd_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices, (const float*)means);
+    if (e != hipSuccess) return e;
+    Reductions sums(1, Reduction{ws, a.dparams, 2 * (int64_t)a.channels, (int)(a.samples * m.slices), true});
+    return reduce_all(sums, s);
+}
+
+hipError_t group_norm_forward(int dtype, const GroupNorm& a, void* ws, hipStream_t s) {
+    return dtype == kBF16 ? forward_type<bf16_t>(a, (float*)ws, s) : forward_type<float>(a, (float*)ws, s);
+}
+hipError_t group_norm_backward(int dtype, const GroupNormBackward& a, void* ws, hipStream_t s) {
+    return dtype == kBF16 ? backward_type<bf16_t>(a, (float*)ws, s) : backward_type<float>(a, (float*)ws, s);
+}
+
+}  // namespace tmps

@@ -1,0 +1,114 @@
+// Selective state space, forward: per sample and head S_t = exp(-delta_t e^a) S_{t-1} + delta_t x_t B_t', y_t = S_t C_t + skip x_t.
+//
+// In chunks of 64 positions it is products of matrices: with D[t][s] the decay from s to t, d_t that from before the chunk to t,
+//   y_t = sum_{s <= t} (C_t . B_s) D[t][s] delta_s x_s + d_t S C_t + skip x_t,   S <- d_end S + sum_s D[end][s] delta_s x_s B_s'
+// A workgroup walks the chunks of a head's (or 64 features' of it) positions with the state in its accumulators, fp32; as an operand of a product a state, and the matrix of decayed
+// products, is the sum of bf16 terms.  Where there are few samples and heads the positions are cut into stretches: a first walk leaves each one's own state, which are joined, and a second
+// walk starts from those.  A few positions go one after the other with the state in registers, which is a reading and a writing of it.
+#include <algorithm>
+
+#include "launch.h"
+#include "scan_walk.hip.h"
+#include "wave.hip.h"
+
+namespace tmps {
+
+// ------------------------------------------------------------------------------------------------ single positions
+// 16 lanes to a feature, which share its state's n; four features at a time to each of 16 teams.
+template <typename T> __global__ __launch_bounds__(256) void scan_steps_kernel(Scan a) {
+    constexpr int kPasses = 4;
+    const int64_t unit = blockIdx.x;
+    const int head = (int)(unit % a.heads), group = head / (a.heads / a.groups);
+    const int64_t sample = unit / a.heads;
+    const int lane = threadIdx.x & 15, team = threadIdx.x >> 4;
+    const double rate = exp((double)a.a_log[head]) * kLog2eD;
+    const float skip = a.skip[head], bias = a.dt_bias[head];
+    const int64_t of_head = unit * a.dh * a.n;
+    const T* const xr = (const T*)a.x + sample * a.positions * a.x_stride;
+    const T* const dtr = (const T*)a.dt + sample * a.positions * a.dt_stride + head;
+    T* const yr = (T*)a.y + sample * a.positions * a.y_stride + (int64_t)head * a.dh;
+    const int64_t b_at = (int64_t)a.heads * a.dh + (int64_t)group * a.n, c_at = b_at + (int64_t)a.groups * a.n;
+    for (int p0 = blockIdx.y * (16 * kPasses); p0 < min(a.dh, (int)(blockIdx.y + 1) * (16 * kPasses)); p0 += 16 * kPasses) {
+        float s[kPasses][2][4];
+#pragma unroll
+        for (int k = 0; k < kPasses; ++k) {
+            const int p = p0 + team + 16 * k;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = 4 * lane + 64 * h;
+                if (a.state && p < a.dh && n < a.n) four_any(a.state + of_head + (int64_t)p * a.n + n, s[k][h], a.n - n);
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[k][h][e] = 0.0f;
+            }
+        }
+        for (int64_t t = 0; t < a.positions; ++t) {
+            const T* const row = xr + t * a.x_stride;
+            const float u = to_f32(dtr[t * a.dt_stride]) + bias, delta = u != u ? u : softplus(u);
+            const float decay = __builtin_amdgcn_exp2f((float)(-(double)delta * rate));
+            float b[2][4], c[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int n = 4 * lane + 64 * h + e;
+                    b[h][e] = n < a.n ? to_f32(row[b_at + n]) : 0.0f;
+                    c[h][e] = n < a.n ? to_f32(row[c_at + n]) : 0.0f;
+                }
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const int p = p0 + team + 16 * k;
+                const float x = p < a.dh ? to_f32(row[(int64_t)head * a.dh + p]) : 0.0f;
+                const float add = delta * x;
+                float y = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[k][h][e] = fmaf(decay, s[k][h][e], add * b[h][e]);
+                        y = fmaf(s[k][h][e], c[h][e], y);
+                    }
+                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xF, 0xF, false));   // row_ror:8
+                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x124, 0xF, 0xF, false));   // row_ror:4
+                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x122, 0xF, 0xF, false));   // row_ror:2
+                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x121, 0xF, 0xF, false));   // row_ror:1
+                if (lane == 0 && p < a.dh) yr[t * a.y_stride + p] = from_f32<T>(fmaf(skip, x, y));
+            }
+        }
+        if (a.state_out) {
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const int p = p0 + team + 16 * k;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int n = 4 * lane + 64 * h;
+                    if (p < a.dh && n < a.n) put_four_any(a.state_out + of_head + (int64_t)p * a.n + n, s[k][h], a.n - n);
+                }
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+constexpr int kStepsMost = 8;   // positions that go one after the other
+
+size_t scan_workspace_bytes(const Scan& a) {
+    if (a.positions <= kStepsMost) return 0;
+    return walk_stretch_bytes(a);
+}
+
+template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hipStream_t s) {
+    if (a.positions <= kStepsMost) {
+        const int64_t units = a.samples * a.heads;
+        if (units > INT32_MAX) return hipErrorInvalidValue;
+        return launch_timed(kcAttnFwd, scan_steps_kernel<T>, dim3((unsigned)units, (unsigned)((a.dh + 63) / 64)), dim3(256), 0, s, a);
+    }
+    ScanWalk w = walk_of<T>(a);
+    w.y = a.y; w.y_stride = a.y_stride;
+    w.final_state = a.state_out;
+    return walk_stretches<T, true, false>(w, ws, s);
+}
+
+hipError_t scan_forward(int dtype, const Scan& a, void* ws, hipStream_t s) { return dtype == kBF16 ? forward_type<bf16_t>(a, ws, s) : forward_type<float>(a, ws, s); }
+
+}  // namespace tmps

@@ -1,0 +1,427 @@
+// Gradients of the selective state space.
+//
+// Two walks leave, for every chunk of 64 positions, the state S before it and the gradient G of the state behind it (the recurrence's adjoint: G <- d_end G + sum_t d_t dy_t C_t').  Chunks
+// are independent then.  With Z[t][s] = C_t . B_s, R[t][s] = dy_t . x_s, D the decays, w_s = D[end][s] delta_s, sums over s <= t:
+//   dx_s = sum_t Z D delta_s dy_t + w_s G B_s + skip dy_s      dB_s = sum_t R D delta_s C_t + w_s G' x_s      dC_t = sum_s R D delta_s B_s + d_t S' dy_t
+// The exponent up to t is in the row t of Z R D delta and in d_t with a plus, in the column t and in w_t with a minus: the gradient of position t's own exponent is the sum of those
+// differences over the chunk's positions from t on, and <S behind the chunk, G>.  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
+// once and whose gradients of B and C stay in its accumulators.
+#include "launch.h"
+#include "scan_walk.hip.h"
+#include "wave.hip.h"
+
+namespace tmps {
+
+struct ScanGrad {
+    ScanBackward b;
+    const float *before, *behind;   // S and G: [samples, heads, chunks, dh, n]
+    float* shared;                  // gradients of B and C of each part: [parts][rows][2 groups n] (null: one part, straight to dx)
+    float* sums;                    // [samples * chunks][3 heads]
+    int chunks, parts, each, slices;
+};
+
+// over the 16 lanes of a row
+__device__ __forceinline__ float lane_sum16(float v) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false));   // row_ror:8
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xF, 0xF, false));   // row_ror:4
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xF, 0xF, false));   // row_ror:2
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xF, 0xF, false));   // row_ror:1
+    return v;
+}
+// over the four lanes of a column
+__device__ __forceinline__ float column_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void scan_grad_kernel(ScanGrad a) {
+    constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, MP = kScanChunk + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
+    constexpr int GT = kStateTerms<T>;
+    constexpr int kState = PP * NP / 4 / 256;   // fours of a state of a thread
+    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[kScanChunk * MP];
+    __shared__ __attribute__((aligned(16))) ChunkDecays decays[4];
+    __shared__ float rowq[4][kScanChunk], ya[kScanChunk], gs[kScanChunk], red[4][2];
+    const ScanBackward& b = a.b;
+    const Scan& f = b.f;
+    const int64_t units = f.samples * a.chunks * f.groups * a.parts;
+    int64_t unit = xcd_order(blockIdx.x, gridDim.x);
+    if (unit >= units) return;
+    const int part = (int)(unit % a.parts);
+    unit /= a.parts;
+    const int group = (int)(unit % f.groups);
+    unit /= f.groups;
+    const int chunk = (int)(unit % a.chunks);
+    const int64_t sample = unit / a.chunks;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+    const int rows = (int)min<int64_t>(kScanChunk, f.positions - (int64_t)chunk * kScanChunk);
+    const int64_t row0 = sample * f.positions + (int64_t)chunk * kScanChunk;
+    const int in_group = f.heads / f.groups, first = part * a.each, last = min(first + a.each, in_group);   // heads of the group
+    const int64_t b_at = (int64_t)f.heads * f.dh + (int64_t)group * f.n, c_at = b_at + (int64_t)f.groups * f.n;
+    const int own = 16 * wave + col;   // this lane's column: a position
+
+    {
+        ChunkRows<T, NP, 256> r;
+        r.request((const T*)f.x + row0 * f.x_stride + b_at, f.x_stride, rows, f.n);
+        r.template put<BP>(bs);
+        r.request((const T*)f.x + row0 * f.x_stride + c_at, f.x_stride, rows, f.n);
+        r.template put<BP>(cs);
+    }
+    __syncthreads();
+    f32x4_t z[4];   // rows s, column t
+#pragma unroll
+    for (int st = 0; st < 4; ++st) {
+        z[st] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (st > wave) continue;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) z[st] = mma(along<false>(bs + (16 * st + col) * BP, 32 * k, lane), along<false>(cs + own * BP, 32 * k, lane), z[st]);
+    }
+    f32x4_t db[NT], dc[NT];   // rows n, columns s and t
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) db[nt] = dc[nt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    for (int h = first; h < last; ++h) {
+        const int head = group * in_group + h;
+        const float skip = f.skip[head];
+        float dskip = 0.0f, meet = 0.0f;   // sums of dy x and of S G
+        float end_sum = 0.0f;              // of w_s x_s G B_s (a lane's column)
+        for (int slice = 0; slice < a.slices; ++slice) {
+            const int p0 = slice * 64, width = min(64, f.dh - p0);
+            ChunkRows<T, PP, 256> rx, rd;
+            rx.request((const T*)f.x + row0 * f.x_stride + (int64_t)head * f.dh + p0, f.x_stride, rows, width);
+            rd.request((const T*)b.dy + row0 * b.dy_stride + (int64_t)head * f.dh + p0, b.dy_stride, rows, width);
+            const int64_t of_state = (((sample * f.heads + head) * a.chunks + chunk) * f.dh + p0) * (int64_t)f.n;
+            float s4[kState][4], g4[kState][4];
+#pragma unroll
+            for (int i = 0; i < kState; ++i) {
+                const int k = (int)threadIdx.x + 256 * i, p = k / (NP / 4), n = k % (NP / 4) * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s4[i][e] = g4[i][e] = 0.0f;
+                if (p < width && n < f.n) {
+                    four_any(a.before + of_state + (int64_t)p * f.n + n, s4[i], f.n - n);
+                    four_any(a.behind + of_state + (int64_t)p * f.n + n, g4[i], f.n - n);
+                }
+            }
+            __syncthreads();   // (what the head or slice before has left in LDS has been read)
+            if (slice == 0 && ((h - first) & 3) == 0 && h + wave < last) {
+                const int mine = head + wave;
+                chunk_decays(decays[wave], (const T*)f.dt + row0 * f.dt_stride + mine, f.dt_stride, rows, f.dt_bias[mine], exp((double)f.a_log[mine]) * kLog2eD, lane);
+            }
+            rx.template put<XP>(xs);
+            rd.template put<XP>(dys);
+            const auto put_state = [&](const float (&v)[kState][4]) {
+#pragma unroll
+                for (int i = 0; i < kState; ++i) {
+                    const int k = (int)threadIdx.x + 256 * i, p = k / (NP / 4), n = k % (NP / 4) * 4;
+                    float w[4] = {v[i][0], v[i][1], v[i][2], v[i][3]};
+#pragma unroll
+                    for (int term = 0; term < GT; ++term) {
+                        put_four(sg + (term * PP + p) * BP + n, w);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] -= (float)(T)w[e];
+                    }
+                }
+            };
+            put_state(s4);
+#pragma unroll
+            for (int i = 0; i < kState; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) meet = fmaf(s4[i][e], g4[i][e], meet);
+#pragma unroll
+            for (int i = 0; i < ChunkRows<T, PP, 256>::kMany; ++i) {
+                float vx[V], vd[V];
+                unpack(rx.u[i], vx);
+                unpack(rd.u[i], vd);
+#pragma unroll
+                for (int e = 0; e < V; ++e) dskip = fmaf(vx[e], vd[e], dskip);
+            }
+            __syncthreads();
+            const ChunkDecays& d = decays[(h - first) & 3];
+
+            // by columns t
+            f32x4_t m[4], dz[4];
+            float from_row = 0.0f;
+            Oct<T> dyf[PK];
+#pragma unroll
+            for (int k = 0; k < PK; ++k) dyf[k] = along<false>(dys + own * XP, 32 * k, lane);
+            const float sum_t = d.sum[own], rest_t = d.rest[own];
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+                f32x4_t r = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                m[st] = dz[st] = r;
+                if (st <= wave) {
+#pragma unroll
+                    for (int k = 0; k < PK; ++k) r = mma(along<false>(xs + (16 * st + col) * XP, 32 * k, lane), dyf[k], r);
+                    float sum_s[4], rest_s[4], delta_s[4];
+                    four(d.sum + 16 * st + 4 * g, sum_s);
+                    four(d.rest + 16 * st + 4 * g, rest_s);
+                    four(d.delta + 16 * st + 4 * g, delta_s);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float decay = 16 * st + 4 * g + e <= own ? decay_between(sum_t, rest_t, sum_s[e], rest_s[e]) : 0.0f;
+                        const float zd = z[st][e] * decay;
+                        const float q = r[e] * zd;
+                        m[st][e] = zd * delta_s[e];
+                        dz[st][e] = r[e] * (decay * delta_s[e]);
+                        from_row = fmaf(q, delta_s[e], from_row);
+                        r[e] = q;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float q = lane_sum16(r[e]);
+                    if (col == 0) {
+                        if (slice == 0) rowq[wave][16 * st + 4 * g + e] = q;
+                        else rowq[wave][16 * st + 4 * g + e] += q;
+                    }
+                }
+                const float v[4] = {m[st][0], m[st][1], m[st][2], m[st][3]};
+                put_four(mm + own * MP + 16 * st + 4 * g, v);
+            }
+            float with_c = 0.0f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    if (2 * pair > wave) continue;
+                    Oct<T> zf[1];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) terms_of(dz[2 * pair + e / 4][e % 4], e, zf);
+                    dc[nt] = mma(across<true>(bs, BP, 32 * pair, 16 * nt, lane), zf[0], dc[nt]);
+                }
+                f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int term = GT - 1; term >= 0; --term)
+#pragma unroll
+                    for (int k = 0; k < PK; ++k) v = mma(across<false>(sg + term * PP * BP, BP, 32 * k, 16 * nt, lane), dyf[k], v);
+                float c[4];
+                four(cs + own * BP + 16 * nt + 4 * g, c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) with_c = fmaf(v[e], c[e], with_c);
+                dc[nt] += v * d.from[own];
+            }
+            from_row = column_sum(fmaf(d.from[own], with_c, from_row));
+            if (g == 0) {
+                if (slice == 0) ya[own] = from_row;
+                else ya[own] += from_row;
+            }
+            __syncthreads();   // (S has been read, the decayed products are there)
+
+            // by columns s
+            put_state(g4);
+            f32x4_t dx[PT];
+#pragma unroll
+            for (int j = 0; j < PT; ++j) {
+                dx[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    if (2 * pair + 1 < wave) continue;
+                    dx[j] = mma(across<false>(dys, XP, 32 * pair, 16 * j, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), dx[j]);
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+                const float v[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
+                put_four(mm + own * MP + 16 * st + 4 * g, v);
+            }
+            __syncthreads();
+            Oct<T> xf[PK], bf[NK];
+#pragma unroll
+            for (int k = 0; k < PK; ++k) xf[k] = along<false>(xs + own * XP, 32 * k, lane);
+#pragma unroll
+            for (int k = 0; k < NK; ++k) bf[k] = along<false>(bs + own * BP, 32 * k, lane);
+            const float to = d.to[own];
+#pragma unroll
+            for (int j = 0; j < PT; ++j) {
+                f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int term = GT - 1; term >= 0; --term)
+#pragma unroll
+                    for (int k = 0; k < NK; ++k) v = mma(along<false>(sg + (term * PP + 16 * j + col) * BP, 32 * k, lane), bf[k], v);
+                float dyv[4], out[4];
+                four(dys + own * XP + 16 * j + 4 * g, dyv);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = fmaf(skip, dyv[e], fmaf(to, v[e], dx[j][e]));
+                if (own < rows && 16 * j + 4 * g < width)
+                    put_four_any((T*)b.dx + (row0 + own) * b.dx_stride + (int64_t)head * f.dh + p0 + 16 * j + 4 * g, out, width - 16 * j - 4 * g);
+            }
+            float with_b = 0.0f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    if (2 * pair + 1 < wave) continue;
+                    db[nt] = mma(across<false>(cs, BP, 32 * pair, 16 * nt, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), db[nt]);
+                }
+                f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int term = GT - 1; term >= 0; --term)
+#pragma unroll
+                    for (int k = 0; k < PK; ++k) v = mma(across<false>(sg + term * PP * BP, BP, 32 * k, 16 * nt, lane), xf[k], v);
+                float bv[4];
+                four(bs + own * BP + 16 * nt + 4 * g, bv);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) with_b = fmaf(v[e], bv[e], with_b);
+                db[nt] += v * to;
+            }
+            with_b = column_sum(with_b);
+            if (g == 0) {
+                if (slice == 0) gs[own] = with_b;
+                else gs[own] += with_b;
+                end_sum = fmaf(to, with_b, end_sum);
+            }
+        }
+        // the head's steps and parameters
+        const float meet_all = wsum(meet * decays[(h - first) & 3].end + end_sum), skip_all = wsum(dskip);
+        if (lane == 0) {
+            red[wave][0] = meet_all;
+            red[wave][1] = skip_all;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const ChunkDecays& d = decays[(h - first) & 3];
+            const double rate = exp((double)f.a_log[head]);
+            const float q = (rowq[0][lane] + rowq[1][lane]) + (rowq[2][lane] + rowq[3][lane]), delta = d.delta[lane], with_g = gs[lane];
+            double sum = (double)ya[lane] - ((double)delta * (double)q + (double)d.to[lane] * (double)with_g);
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) {
+                const double behind = __shfl_down(sum, k);
+                if (lane + k < 64) sum += behind;
+            }
+            const double of_exponent = sum + (((double)red[0][0] + (double)red[1][0]) + ((double)red[2][0] + (double)red[3][0]));
+            const float ddelta = (float)((double)q + (double)d.back[lane] * (double)with_g - rate * of_exponent), du = lane < rows ? ddelta * d.slope[lane] : 0.0f;
+            if (lane < rows) ((T*)b.ddt)[(row0 + lane) * b.ddt_stride + head] = from_f32<T>(du);
+            const float drate = wsum(lane < rows ? (float)(-rate * (double)delta * of_exponent) : 0.0f), dbias = wsum(du);
+            if (lane == 0) {
+                float* const to = a.sums + (sample * a.chunks + chunk) * 3 * f.heads + head;
+                to[0] = drate;
+                to[f.heads] = (red[0][1] + red[1][1]) + (red[2][1] + red[3][1]);
+                to[2 * f.heads] = dbias;
+            }
+        }
+    }
+    if (own >= rows) return;
+    const int64_t wide = 2 * (int64_t)f.groups * f.n;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = 16 * nt + 4 * g;
+        if (n >= f.n) continue;
+        const float vb[4] = {db[nt][0], db[nt][1], db[nt][2], db[nt][3]}, vc[4] = {dc[nt][0], dc[nt][1], dc[nt][2], dc[nt][3]};
+        if (a.shared) {
+            float* const to = a.shared + ((int64_t)part * f.samples * f.positions + row0 + own) * wide + (int64_t)group * f.n + n;
+            put_four_any(to, vb, f.n - n);
+            put_four_any(to + (int64_t)f.groups * f.n, vc, f.n - n);
+        } else {
+            T* const to = (T*)b.dx + (row0 + own) * b.dx_stride;
+            put_four_any(to + b_at + n, vb, f.n - n);
+            put_four_any(to + c_at + n, vc, f.n - n);
+        }
+    }
+}
+
+// Gradients of B and C: the parts' sums, rounded once.
+template <typename T> __global__ __launch_bounds__(256) void scan_shared_kernel(ScanGrad a) {
+    const Scan& f = a.b.f;
+    const int64_t wide = 2 * (int64_t)f.groups * f.n, rows = f.samples * f.positions, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= rows * wide) return;
+    const int many = (int)min<int64_t>(4, rows * wide - i);
+    float sum[4];
+    four_any(a.shared + i, sum, many);
+    for (int k = 1; k < a.parts; ++k) {
+        float v[4];
+        four_any(a.shared + k * rows * wide + i, v, many);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+    const int64_t row = i / wide, at = i % wide;
+    T* const to = (T*)a.b.dx + (int64_t)f.heads * f.dh;
+    if (many == 4 && at + 4 <= wide) {
+        put_four_any(to + row * a.b.dx_stride + at, sum, 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < many) to[(i + e) / wide * a.b.dx_stride + (i + e) % wide] = from_f32<T>(sum[e]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+// Parts of a group's heads: as many as give the chip 512 workgroups.
+constexpr int kGradGroups = 512;
+static void grad_plan(ScanGrad& a) {
+    const Scan& f = a.b.f;
+    a.chunks = (int)((f.positions + kScanChunk - 1) / kScanChunk);
+    a.slices = (f.dh + 63) / 64;
+    const int64_t groups = f.samples * a.chunks * f.groups;
+    const int in_group = f.heads / f.groups;
+    int64_t parts = (kGradGroups + groups - 1) / groups;
+    if (parts > in_group) parts = in_group;
+    a.each = (int)((in_group + parts - 1) / parts);
+    a.parts = (in_group + a.each - 1) / a.each;
+}
+
+static size_t on256(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// The stretches' states, S, G, sums, and what the parts leave: as much as any call of no more samples and positions takes.
+struct GradRoom {
+    size_t walk, states, sums, shared;
+    size_t all() const { return walk + 2 * states + sums + shared; }
+};
+static GradRoom grad_room(const Scan& f) {
+    const int64_t chunks = (f.positions + kScanChunk - 1) / kScanChunk, of_chunks = f.samples * chunks;
+    GradRoom r;
+    r.walk = on256(walk_stretch_bytes(f));
+    r.states = on256((size_t)of_chunks * f.heads * f.dh * f.n * sizeof(float));
+    r.sums = on256((size_t)of_chunks * 3 * f.heads * sizeof(float));
+    // (parts x chunks is at most the workgroups wanted and as many again as there are chunks)
+    const int64_t most = std::min<int64_t>(of_chunks * (f.heads / f.groups), kGradGroups / f.groups + of_chunks);
+    r.shared = f.heads == f.groups ? 0 : on256((size_t)most * kScanChunk * 2 * f.groups * f.n * sizeof(float));
+    return r;
+}
+
+size_t scan_backward_workspace_bytes(int, const Scan& a) { return grad_room(a).all(); }
+
+template <typename T> static hipError_t backward_type(const ScanBackward& b, void* ws, hipStream_t s) {
+    const GradRoom room = grad_room(b.f);
+    char* at = static_cast<char*>(ws);
+    ScanGrad a;
+    a.b = b;
+    grad_plan(a);
+    float* const before = reinterpret_cast<float*>(at + room.walk);
+    float* const behind = reinterpret_cast<float*>(at + room.walk + room.states);
+    a.before = before; a.behind = behind;
+    a.sums = reinterpret_cast<float*>(at + room.walk + 2 * room.states);
+    a.shared = a.parts > 1 ? reinterpret_cast<float*>(at + room.walk + 2 * room.states + room.sums) : nullptr;
+    ScanWalk w = walk_of<T>(b.f);
+    w.chunk_states = before;
+    hipError_t e = walk_stretches<T, false, false>(w, ws, s);
+    if (e != hipSuccess) return e;
+    w.x = b.dy; w.x_stride = b.dy_stride; w.b = w.c;
+    w.first_state = b.dstate; w.chunk_states = behind; w.final_state = b.dstate_in;
+    e = walk_stretches<T, false, true>(w, ws, s);
+    if (e != hipSuccess) return e;
+    const Scan& f = b.f;
+    const int64_t units = f.samples * a.chunks * f.groups * a.parts, blocks = (units + 7) / 8 * 8;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks), block(256);
+    if (f.dh > 32) {
+        if (f.n <= 32) e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 32, 4>, grid, block, 0, s, a);
+        else if (f.n <= 64) e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 64, 4>, grid, block, 0, s, a);
+        else e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 128, 4>, grid, block, 0, s, a);
+    } else {
+        if (f.n <= 32) e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 32, 2>, grid, block, 0, s, a);
+        else if (f.n <= 64) e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 64, 2>, grid, block, 0, s, a);
+        else e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 128, 2>, grid, block, 0, s, a);
+    }
+    if (e != hipSuccess) return e;
+    if (a.shared) {
+        const int64_t fours = (f.samples * f.positions * 2 * f.groups * f.n + 3) / 4;
+        if ((fours + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
+        e = launch_timed(kcAttnBwd, scan_shared_kernel<T>, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, s, a);
+        if (e != hipSuccess) return e;
+    }
+    return reduce_all(Reductions(1, Reduction{a.sums, b.dparams, 3 * (int64_t)f.heads, (int)(f.samples * a.chunks), true}), s);
+}
+
+hipError_t scan_backward(int dtype, const ScanBackward& b, void* ws, hipStream_t s) { return dtype == kBF16 ? backward_type<bf16_t>(b, ws, s) : backward_type<float>(b, ws, s); }
+
+}  // namespace tmps

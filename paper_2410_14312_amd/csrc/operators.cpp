@@ -7,41 +7,10 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "operands.h"
 #include "profile.h"
 
 using namespace tmps;
-
-namespace {
-
-bool known(int dtype) { return dtype == TMPS_F32 || dtype == TMPS_BF16_F32MASTER; }
-
-bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
-// Memory of `bytes` bytes at p (null: none).
-struct Range {
-    const void* p;
-    size_t bytes;
-    bool meets(const Range& o) const {
-        const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
-        return p && o.p && bytes && o.bytes && a < b + o.bytes && b < a + bytes;
-    }
-};
-
-// Whether a result overlaps an operand or another result; `same`: operand that results[0] may be, whole.
-template <int NO, int NR> bool overlaps(const Range (&operands)[NO], const Range (&results)[NR], const void* same = nullptr) {
-    for (int i = 0; i < NR; ++i) {
-        for (const Range& o : operands)
-            if (results[i].meets(o) && !(i == 0 && same && o.p == same && results[i].p == same)) return true;
-        for (int k = 0; k < i; ++k)
-            if (results[i].meets(results[k])) return true;
-    }
-    return false;
-}
-
-// Elements that 63 bits of bytes count.
-constexpr int64_t kMaxElems = int64_t(1) << 59;
-
-}  // namespace
 
 extern "C" int tmps_rotary(int dtype, const tmps_rotary_desc* desc, const void* x, int64_t x_stride, void* y, int64_t y_stride, const int32_t* positions,
                            int64_t n_positions, int64_t rows, int inverse, void* hip_stream) {

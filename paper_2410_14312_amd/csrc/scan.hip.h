@@ -1,0 +1,219 @@
+// What the kernels of the selective state space share: tiles of 16 x 16 by the matrix unit, operands from LDS by rows and by columns, the decays of a chunk of positions.
+#pragma once
+#include "mixer.h"
+#include "pieces.hip.h"
+
+namespace tmps {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int16_t s16x4v_t __attribute__((ext_vector_type(4)));
+
+constexpr int kScanChunk = 64;   // positions that a workgroup takes at a time
+
+// Eight of the 32 numbers of a row (first operand) or column (second) that a lane holds: row or column lane % 16, numbers 8 (lane / 16) .. + 7; or, `split`, 4 (lane / 16) .. + 3 and
+// 16 + 4 (lane / 16) .. + 3, which is how the results of two tiles lie (a lane has rows 4 (lane / 16) .. + 3 of column lane % 16).
+template <typename T> struct Oct;
+template <> struct Oct<bf16_t> {
+    bf16x8_t v;
+    __device__ __forceinline__ void set(int e, float x) { v[e] = (bf16_t)x; }
+    __device__ __forceinline__ float get(int e) const { return (float)v[e]; }
+};
+template <> struct Oct<float> {
+    float v[8];
+    __device__ __forceinline__ void set(int e, float x) { v[e] = x; }
+    __device__ __forceinline__ float get(int e) const { return v[e]; }
+};
+
+__device__ __forceinline__ f32x4_t mma(const Oct<bf16_t>& a, const Oct<bf16_t>& b, f32x4_t acc) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, acc, 0, 0, 0); }
+__device__ __forceinline__ f32x4_t mma(const Oct<float>& a, const Oct<float>& b, f32x4_t acc) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], acc, 0, 0, 0);
+    return acc;
+}
+
+// A number as the sum of K numbers of the operands' type (fp32: itself).  One that is not finite is the first of them, the others are 0.
+template <int K> __device__ __forceinline__ void terms_of(float x, int e, Oct<bf16_t> (&out)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        out[k].set(e, x);
+        if (k + 1 < K) {
+            x -= out[k].get(e);
+            x = fabsf(x) < 3.4e38f ? x : 0.0f;
+        }
+    }
+}
+template <int K> __device__ __forceinline__ void terms_of(float x, int e, Oct<float> (&out)[K]) { out[0].set(e, x); }
+
+// Numbers of a row of a tile that lie one behind the other from k0 on.
+template <bool SPLIT> __device__ __forceinline__ Oct<bf16_t> along(const bf16_t* row, int k0, int lane) {
+    Oct<bf16_t> o;
+    if constexpr (SPLIT) {
+        union { uint2 h[2]; bf16x8_t v; } u;
+        u.h[0] = *reinterpret_cast<const uint2*>(row + k0 + 4 * (lane >> 4));
+        u.h[1] = *reinterpret_cast<const uint2*>(row + k0 + 16 + 4 * (lane >> 4));
+        o.v = u.v;
+    } else {
+        o.v = *reinterpret_cast<const bf16x8_t*>(row + k0 + 8 * (lane >> 4));
+    }
+    return o;
+}
+template <bool SPLIT> __device__ __forceinline__ Oct<float> along(const float* row, int k0, int lane) {
+    Oct<float> o;
+    const int first = SPLIT ? 4 * (lane >> 4) : 8 * (lane >> 4), second = SPLIT ? first + 16 : first + 4;
+    const float4 a = *reinterpret_cast<const float4*>(row + k0 + first), b = *reinterpret_cast<const float4*>(row + k0 + second);
+    o.v[0] = a.x; o.v[1] = a.y; o.v[2] = a.z; o.v[3] = a.w;
+    o.v[4] = b.x; o.v[5] = b.y; o.v[6] = b.z; o.v[7] = b.w;
+    return o;
+}
+// Numbers of a column, c0 + lane % 16, in the rows from k0 on.  bf16: transposing reads of four rows by 16 columns to each 16 lanes.
+template <bool SPLIT> __device__ __forceinline__ Oct<bf16_t> across(const bf16_t* tile, int pitch, int k0, int c0, int lane) {
+    typedef __attribute__((address_space(3))) s16x4v_t* lds_t;
+    const int first = SPLIT ? 4 * (lane >> 4) : 8 * (lane >> 4), second = SPLIT ? first + 16 : first + 4;
+    const bf16_t* const p = tile + (k0 + ((lane & 15) >> 2)) * pitch + c0 + (lane & 3) * 4;
+    union { s16x4v_t h[2]; bf16x8_t v; } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p + first * pitch));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p + second * pitch));
+    Oct<bf16_t> o;
+    o.v = u.v;
+    return o;
+}
+template <bool SPLIT> __device__ __forceinline__ Oct<float> across(const float* tile, int pitch, int k0, int c0, int lane) {
+    Oct<float> o;
+    const int first = SPLIT ? 4 * (lane >> 4) : 8 * (lane >> 4), second = SPLIT ? first + 16 : first + 4;
+    const float* const p = tile + k0 * pitch + c0 + (lane & 15);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.v[e] = p[((e < 4 ? first : second - 4) + e) * pitch];
+    return o;
+}
+
+// Four neighbouring numbers.
+__device__ __forceinline__ void four(const bf16_t* p, float (&v)[4]) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    v[0] = __builtin_bit_cast(float, u.x << 16); v[1] = __builtin_bit_cast(float, u.x & 0xffff0000u);
+    v[2] = __builtin_bit_cast(float, u.y << 16); v[3] = __builtin_bit_cast(float, u.y & 0xffff0000u);
+}
+__device__ __forceinline__ void four(const float* p, float (&v)[4]) {
+    const float4 f = *reinterpret_cast<const float4*>(p);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+}
+__device__ __forceinline__ void put_four(bf16_t* p, const float (&v)[4]) {   // (on 8 bytes)
+    union { bf16_t h[4]; uint2 u; } k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k.h[e] = (bf16_t)v[e];
+    *reinterpret_cast<uint2*>(p) = k.u;
+}
+__device__ __forceinline__ void put_four(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+// The same anywhere in memory, those of them before `many`.
+__device__ __forceinline__ void put_four_any(bf16_t* p, const float (&v)[4], int many) {
+    union { bf16_t h[4]; any_u32x2_t u; } k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k.h[e] = (bf16_t)v[e];
+    if (many >= 4) *reinterpret_cast<any_u32x2_t*>(p) = k.u;
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < many) p[e] = k.h[e];
+}
+__device__ __forceinline__ void put_four_any(float* p, const float (&v)[4], int many) {
+    if (many >= 4) store16_any(p, pack(v));
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < many) p[e] = v[e];
+}
+__device__ __forceinline__ void four_any(const float* p, float (&v)[4], int many) {
+    if (many >= 4) unpack(load16_any(p), v);
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < many ? p[e] : 0.0f;
+}
+
+// 16 bytes of a row from column c on, zeros from column `columns` on.
+template <typename T> __device__ __forceinline__ uint4 piece_until(const T* row, int c, int columns) {
+    constexpr int V = kPiece<T>;
+    if (c + V <= columns) return load16_any(row + c);
+    struct Values { T v[V]; } f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) f.v[e] = c + e < columns ? row[c + e] : T(0.0f);
+    return __builtin_bit_cast(uint4, f);
+}
+
+// The rows of a chunk on their way from memory to LDS: requested while the chunk before is worked on.  W columns, zeros behind the valid rows and columns.
+template <typename T, int W, int THREADS> struct ChunkRows {
+    static constexpr int V = kPiece<T>, kEach = W / V, kMany = kScanChunk * kEach / THREADS;
+    static_assert(kScanChunk * kEach % THREADS == 0, "pieces of a chunk");
+    uint4 u[kMany];
+    __device__ __forceinline__ void request(const T* base, int64_t stride, int rows, int columns) {
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) {
+            const int k = (int)threadIdx.x + i * THREADS, r = k / kEach;
+            u[i] = r < rows ? piece_until(base + r * stride, k % kEach * V, columns) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    template <int PITCH> __device__ __forceinline__ void put(T* tile) const {
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) {
+            const int k = (int)threadIdx.x + i * THREADS;
+            *reinterpret_cast<uint4*>(tile + k / kEach * PITCH + k % kEach * V) = u[i];
+        }
+    }
+    // whether a number of this thread's is not finite
+    __device__ __forceinline__ bool odd() const {
+        bool is = false;
+#pragma unroll
+        for (int i = 0; i < kMany; ++i)
+#pragma unroll
+            for (uint32_t w : {u[i].x, u[i].y, u[i].z, u[i].w}) {
+                if constexpr (sizeof(T) == 2) is |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+                else is |= (w & 0x7f800000u) == 0x7f800000u;
+            }
+        return is;
+    }
+};
+
+// The steps and decays of a chunk, a position to a lane: delta, the sum of the exponents up to the position in units of log 2 (in two floats: of sums of hundreds their differences keep
+// their last places), the decay from before the chunk, that to its end and delta times it, and the slope of softplus.  Positions behind the last have delta 0: they change nothing.
+struct ChunkDecays {
+    float delta[kScanChunk], sum[kScanChunk], rest[kScanChunk], from[kScanChunk], back[kScanChunk], to[kScanChunk], slope[kScanChunk];
+    float end;       // the decay over the whole chunk
+    double total;    // its exponent
+};
+constexpr double kLog2eD = 1.4426950408889634074;
+
+__device__ __forceinline__ float softplus(float u) { return fmaxf(u, 0.0f) + log1pf(expf(-fabsf(u))); }
+
+template <typename T> __device__ __forceinline__ void chunk_decays(ChunkDecays& d, const T* dt, int64_t stride, int rows, float bias, double rate, int lane) {
+    float delta = 0.0f, slope = 0.0f;
+    if (lane < rows) {
+        const float u = to_f32(dt[lane * stride]) + bias;
+        delta = u != u ? u : softplus(u);
+        slope = 1.0f / (1.0f + expf(-u));
+    }
+    double sum = -(double)delta * rate;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const double before = __shfl_up(sum, k);
+        if (lane >= k) sum += before;
+    }
+    const double total = __shfl(sum, 63);
+    const float hi = (float)sum;
+    d.delta[lane] = delta;
+    d.sum[lane] = hi;
+    d.rest[lane] = hi - hi == 0.0f ? (float)(sum - (double)hi) : 0.0f;
+    d.from[lane] = __builtin_amdgcn_exp2f(hi) * (1.0f + 0.69314718f * d.rest[lane]);
+    d.back[lane] = __builtin_amdgcn_exp2f((float)(total - sum));
+    d.to[lane] = delta * d.back[lane];
+    d.slope[lane] = slope;
+    if (lane == 63) {
+        d.end = __builtin_amdgcn_exp2f((float)total);
+        d.total = total;
+    }
+}
+
+// The decay from behind position s to behind position t >= s.
+__device__ __forceinline__ float decay_between(float sum_t, float rest_t, float sum_s, float rest_s) { return __builtin_amdgcn_exp2f((sum_t - sum_s) + (rest_t - rest_s)); }
+
+// Which heads, samples and stretches a workgroup has: neighbours, which read the same B and C, on one of the eight XCDs.
+__device__ __forceinline__ int64_t xcd_order(int64_t block, int64_t blocks) { return (block & 7) * (blocks >> 3) + (block >> 3); }
+
+}  // namespace tmps

@@ -1,0 +1,136 @@
+"""Group norm against 64 bits.  Bounds: mean and variance are sums in chains of at most some 100 roundings, joined in pairs, off by 2^-18 of the group's root mean square, and its
+distance from 0 where the mean is far away; z, the activations (the hardware's exponential and reciprocal in bf16) and their slopes add a few 2^-23: 2^-16 of |z| and of |gain| stands
+above both.  Gradients: dx is a difference of terms of the sizes |dz gain| rstd and of its means; 2^-15 of those with the slope's own error, 1.2 |dy|."""
+import pytest
+import torch
+
+import paper_2410_14312_amd as tmps
+from tests import mixers
+from tests.mixers import DEV, TYPES, near
+
+pytestmark = pytest.mark.gpu
+SIZES = [(1, 1, 16, 1), (3, 1, 64, 4), (5, 1, 1536, 24), (2, 1, 99, 3), (2, 1, 20000, 1), (4, 16, 32, 8), (2, 49, 24, 3), (3, 33, 10, 2), (2, 300, 256, 32), (1, 1000, 7, 1), (2, 64, 2060, 5),
+         (1, 4, 4200, 2), (70, 5, 40, 4), (1, 4000, 64, 64)]
+
+
+@pytest.fixture(autouse=True)
+def single_precision_by_default():
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
+def inputs(seed, samples, positions, channels, t, shift=True, mean=0.5):
+    g = mixers.generator(seed)
+
+    def normal(*s):
+        return torch.randn(*s, generator=g)
+    rows = samples * positions
+    return {"x": (normal(rows, channels) + mean).to(t).to(DEV), "gain": (1 + 0.2 * normal(channels)).to(DEV), "shift": (0.3 * normal(channels)).to(DEV) if shift else None,
+            "dy": normal(rows, channels).to(t).to(DEV)}
+
+
+def check(i, groups, positions, act, rms, loose=1.0):
+    kw = dict(groups=groups, positions=positions, act=act, rms=rms)
+    y, stats = tmps.group_norm(i["x"], i["gain"], i["shift"], **kw)
+    want = mixers.group_norm(i["x"], i["gain"], i["shift"], groups, positions, act, rms)
+    near(y, want["y"], (want["z"].abs() + i["gain"].abs().cpu().double()) * loose, 2.0 ** -16, "y")
+    near(stats, want["stats"], want["stats"].abs() + 1.0, 2.0 ** -18 * loose, "stats")
+    # a ReLU's border: values next to it may go either way
+    dy = i["dy"]
+    if act == "relu":
+        dy = torch.where(want["z"].abs().to(DEV) < 1e-4 * loose, torch.zeros_like(dy), dy)
+    dx, dgain, dshift = tmps.group_norm_backward(dy, i["x"], stats, i["gain"], i["shift"], **kw)
+    assert (dshift is None) == (i["shift"] is None)
+    want = mixers.group_norm(i["x"], i["gain"], i["shift"], groups, positions, act, rms, dy)
+    rows, c = i["x"].shape
+    b = rows // positions
+    sizes = (1.2 * dy.double().cpu().abs() * i["gain"].double().cpu().abs()).view(b, positions, groups, c // groups)
+    xhat = want["xhat"].abs().view_as(sizes)
+    total = (sizes + xhat * (sizes * xhat).mean((1, 3), keepdim=True) + sizes.mean((1, 3), keepdim=True)) * want["rstd"].view(b, 1, groups, 1) * (1 + xhat)
+    near(dx, want["dx"], total.reshape(rows, c), 2.0 ** -15 * loose, "dx")
+    size = 1.2 * dy.double().cpu().abs()
+    near(dgain, want["dgain"], (size * (1 + want["xhat"].abs())).sum(0), 2.0 ** -15 * loose, "dgain")
+    if dshift is not None:
+        near(dshift, want["dshift"], size.sum(0), 2.0 ** -15 * loose, "dshift")
+    again = tmps.group_norm_backward(dy, i["x"], stats, i["gain"], i["shift"], **kw)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dgain)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("samples,positions,channels,groups", SIZES)
+def test_values_and_gradients(samples, positions, channels, groups, dtype):
+    i = inputs(1, samples, positions, channels, TYPES[dtype])
+    check(i, groups, positions, "silu", False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", [None, "relu", "gelu", "silu"])
+@pytest.mark.parametrize("rms,shift", [(False, True), (True, False), (True, True), (False, False)])
+@pytest.mark.parametrize("positions", [1, 40])
+def test_forms(act, rms, shift, positions, dtype):
+    check(inputs(2, 6, positions, 72, TYPES[dtype], shift), 3, positions, act, rms)
+
+
+@pytest.mark.parametrize("positions", [1, 500])
+def test_means_far_from_zero(positions):
+    """A mean of 1000 with a deviation of 1: fp32 holds the differences to 2^-14 of the deviation."""
+    check(inputs(3, 3, positions, 64, torch.float32, mean=1000.0), 2, positions, "silu", False, loose=2.0 ** 10)
+
+
+def test_values_that_are_all_the_same():
+    for positions in (1, 100):
+        x = torch.full((2 * positions, 32), 3.0, device=DEV)
+        gain, shift = torch.ones(32, device=DEV), torch.linspace(-1, 1, 32, device=DEV)
+        y, stats = tmps.group_norm(x, gain, shift, groups=4, positions=positions)
+        assert torch.equal(y, shift.expand_as(y)) and torch.equal(stats[..., 0], torch.full((2, 4), 3.0, device=DEV))
+
+
+def test_a_number_that_is_not_finite_stays_in_its_group():
+    for positions in (1, 200):
+        i = inputs(4, 3, positions, 64, torch.float32)
+        kw = dict(groups=8, positions=positions, act="relu")
+        want, _ = tmps.group_norm(i["x"], i["gain"], i["shift"], **kw)
+        x = i["x"].clone()
+        x[positions, 17] = float("nan")   # the second sample's third group
+        y, _ = tmps.group_norm(x, i["gain"], i["shift"], **kw)
+        own = torch.zeros_like(y, dtype=torch.bool)
+        own[positions:2 * positions, 16:24] = True
+        assert torch.equal(y[~own], want[~own]) and bool(torch.isnan(y[own]).all())
+
+
+@pytest.mark.parametrize("positions", [1, 300])
+def test_replays_of_a_graph_and_another_stream(positions):
+    i = inputs(5, 4, positions, 64, torch.bfloat16)
+
+    def work(**k):
+        kw = dict(groups=4, positions=positions, act="silu", **k)
+        y, stats = tmps.group_norm(i["x"], i["gain"], i["shift"], **kw)
+        return [y, stats] + list(tmps.group_norm_backward(i["dy"], i["x"], stats, i["gain"], i["shift"], **kw))
+    want = work()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = work(stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = work()
+    for seed in (6, 7, 8):
+        new = inputs(seed, 4, positions, 64, torch.bfloat16)
+        for k in i:
+            i[k].copy_(new[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, work()))
+
+
+def test_a_workspace_for_more_is_enough_for_fewer():
+    lib = tmps.load_library()
+    for backward in (0, 1):
+        for positions in (1, 33, 500, 3000):
+            sizes = [lib.tmps_group_norm_workspace(1, b, positions, 96, 6, backward) for b in range(1, 300)]
+            assert sizes == sorted(sizes)
+            sizes = [lib.tmps_group_norm_workspace(0, positions, p, 96, 6, backward) for p in range(2, 300)]
+            assert sizes == sorted(sizes)
