@@ -14,7 +14,7 @@ namespace tmps {
 
 struct ScanGrad {
     ScanBackward b;
-    const float *before, *behind;   // S and G: [samples, heads, chunks, dh, n]
+    const float *before, *behind;   // S and G: [samples, heads, chunks, PP * slices, NP]
     float* shared;                  // gradients of B and C of each part: [parts][rows][2 groups n] (null: one part, straight to dx)
     float* sums;                    // [samples * chunks][3 heads]
     int chunks, parts, each, slices;
@@ -52,7 +52,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
     unit /= f.groups;
     const int chunk = (int)(unit % a.chunks);
     const int64_t sample = unit / a.chunks;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
     const int rows = (int)min<int64_t>(kScanChunk, f.positions - (int64_t)chunk * kScanChunk);
     const int64_t row0 = sample * f.positions + (int64_t)chunk * kScanChunk;
     const int in_group = f.heads / f.groups, first = part * a.each, last = min(first + a.each, in_group);   // heads of the group
@@ -61,9 +61,12 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
 
     {
         ChunkRows<T, NP, 256> r;
-        r.request((const T*)f.x + row0 * f.x_stride + b_at, f.x_stride, rows, f.n);
+        r.places_all(f.x_stride, f.n);
+        r.request_all((const T*)f.x + row0 * f.x_stride + b_at, f.x_stride, rows, f.n);
+        r.settle_all(rows, f.n);
         r.template put<BP>(bs);
-        r.request((const T*)f.x + row0 * f.x_stride + c_at, f.x_stride, rows, f.n);
+        r.request_all((const T*)f.x + row0 * f.x_stride + c_at, f.x_stride, rows, f.n);
+        r.settle_all(rows, f.n);
         r.template put<BP>(cs);
     }
     __syncthreads();
@@ -87,25 +90,25 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
         for (int slice = 0; slice < a.slices; ++slice) {
             const int p0 = slice * 64, width = min(64, f.dh - p0);
             ChunkRows<T, PP, 256> rx, rd;
-            rx.request((const T*)f.x + row0 * f.x_stride + (int64_t)head * f.dh + p0, f.x_stride, rows, width);
-            rd.request((const T*)b.dy + row0 * b.dy_stride + (int64_t)head * f.dh + p0, b.dy_stride, rows, width);
-            const int64_t of_state = (((sample * f.heads + head) * a.chunks + chunk) * f.dh + p0) * (int64_t)f.n;
+            rx.places_all(f.x_stride, width);
+            rd.places_all(b.dy_stride, width);
+            rx.request_all((const T*)f.x + row0 * f.x_stride + (int64_t)head * f.dh + p0, f.x_stride, rows, width);
+            rd.request_all((const T*)b.dy + row0 * b.dy_stride + (int64_t)head * f.dh + p0, b.dy_stride, rows, width);
+            const int64_t of_state = (((sample * f.heads + head) * a.chunks + chunk) * a.slices + slice) * (int64_t)(PP * NP);
             float s4[kState][4], g4[kState][4];
 #pragma unroll
             for (int i = 0; i < kState; ++i) {
-                const int k = (int)threadIdx.x + 256 * i, p = k / (NP / 4), n = k % (NP / 4) * 4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s4[i][e] = g4[i][e] = 0.0f;
-                if (p < width && n < f.n) {
-                    four_any(a.before + of_state + (int64_t)p * f.n + n, s4[i], f.n - n);
-                    four_any(a.behind + of_state + (int64_t)p * f.n + n, g4[i], f.n - n);
-                }
+                const int k = (int)threadIdx.x + 256 * i;
+                four(a.before + of_state + 4 * k, s4[i]);
+                four(a.behind + of_state + 4 * k, g4[i]);
             }
             __syncthreads();   // (what the head or slice before has left in LDS has been read)
             if (slice == 0 && ((h - first) & 3) == 0 && h + wave < last) {
                 const int mine = head + wave;
-                chunk_decays(decays[wave], (const T*)f.dt + row0 * f.dt_stride + mine, f.dt_stride, rows, f.dt_bias[mine], exp((double)f.a_log[mine]) * kLog2eD, lane);
+                chunk_decays<true>(decays[wave], (const T*)f.dt + row0 * f.dt_stride + mine, f.dt_stride, rows, f.dt_bias[mine], exp((double)f.a_log[mine]) * kLog2eD, lane);
             }
+            rx.settle_all(rows, width);
+            rd.settle_all(rows, width);
             rx.template put<XP>(xs);
             rd.template put<XP>(dys);
             const auto put_state = [&](const float (&v)[kState][4]) {
@@ -151,17 +154,27 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
                 if (st <= wave) {
 #pragma unroll
                     for (int k = 0; k < PK; ++k) r = mma(along<false>(xs + (16 * st + col) * XP, 32 * k, lane), dyf[k], r);
-                    float sum_s[4], rest_s[4], delta_s[4];
-                    four(d.sum + 16 * st + 4 * g, sum_s);
-                    four(d.rest + 16 * st + 4 * g, rest_s);
+                    float delta_s[4], decay[4];
                     four(d.delta + 16 * st + 4 * g, delta_s);
+                    if (st < wave) {
+                        // (by way of the end of the sixteen positions of s: neither factor is over one)
+                        const float on = decay_between(sum_t, rest_t, d.sum[16 * st + 15], d.rest[16 * st + 15]);
+                        four(d.tile + 16 * st + 4 * g, decay);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) decay[e] *= on;
+                    } else {
+                        float sum_s[4], rest_s[4];
+                        four(d.sum + 16 * st + 4 * g, sum_s);
+                        four(d.rest + 16 * st + 4 * g, rest_s);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) decay[e] = 4 * g + e <= col ? decay_between(sum_t, rest_t, sum_s[e], rest_s[e]) : 0.0f;
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float decay = 16 * st + 4 * g + e <= own ? decay_between(sum_t, rest_t, sum_s[e], rest_s[e]) : 0.0f;
-                        const float zd = z[st][e] * decay;
+                        const float zd = z[st][e] * decay[e];
                         const float q = r[e] * zd;
                         m[st][e] = zd * delta_s[e];
-                        dz[st][e] = r[e] * (decay * delta_s[e]);
+                        dz[st][e] = r[e] * (decay[e] * delta_s[e]);
                         from_row = fmaf(q, delta_s[e], from_row);
                         r[e] = q;
                     }
@@ -242,8 +255,8 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
                 four(dys + own * XP + 16 * j + 4 * g, dyv);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) out[e] = fmaf(skip, dyv[e], fmaf(to, v[e], dx[j][e]));
-                if (own < rows && 16 * j + 4 * g < width)
-                    put_four_any((T*)b.dx + (row0 + own) * b.dx_stride + (int64_t)head * f.dh + p0 + 16 * j + 4 * g, out, width - 16 * j - 4 * g);
+                if (own < rows)
+                    put_four_of((T*)b.dx + (row0 + own) * b.dx_stride + (int64_t)head * f.dh + p0 + 16 * j + 4 * g, out, width - 16 * j - 4 * g, width % 4 == 0);
             }
             float with_b = 0.0f;
 #pragma unroll
@@ -370,7 +383,7 @@ static GradRoom grad_room(const Scan& f) {
     const int64_t chunks = (f.positions + kScanChunk - 1) / kScanChunk, of_chunks = f.samples * chunks;
     GradRoom r;
     r.walk = on256(walk_stretch_bytes(f));
-    r.states = on256((size_t)of_chunks * f.heads * f.dh * f.n * sizeof(float));
+    r.states = on256((size_t)of_chunks * f.heads * padded_dh(f.dh) * padded_n(f.n) * sizeof(float));
     r.sums = on256((size_t)of_chunks * 3 * f.heads * sizeof(float));
     // (parts x chunks is at most the workgroups wanted and as many again as there are chunks)
     const int64_t most = std::min<int64_t>(of_chunks * (f.heads / f.groups), kGradGroups / f.groups + of_chunks);

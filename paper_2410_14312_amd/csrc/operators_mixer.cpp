@@ -124,9 +124,16 @@ static int check_scan(int dtype, const tmps_scan_desc* desc, int64_t samples, in
     if (desc->heads < 1 || desc->dh < 1 || desc->groups < 1 || desc->n < 1) return fail(TMPS_EINVAL, "heads, features, groups and state features must be positive");
     if (desc->heads % desc->groups) return fail(TMPS_ESHAPE, "%d heads in %d groups", desc->heads, desc->groups);
     if (desc->n > kScanMaxState) return fail(TMPS_EUNSUPPORTED, "states of more than %d features", kScanMaxState);
-    if ((int64_t)desc->heads * desc->dh > (1 << 24) || desc->heads > (1 << 20)) return fail(TMPS_EUNSUPPORTED, "rows of more than 2^24 features");
+    if ((int64_t)desc->heads * desc->dh + 2 * (int64_t)desc->groups * desc->n > (1 << 24)) return fail(TMPS_EUNSUPPORTED, "rows of more than 2^24 features");
     const int64_t head_numbers = (int64_t)desc->heads * desc->dh * desc->n;   // (of a sample's states)
     if (samples > ((int64_t)INT32_MAX - 1) * 256 / head_numbers) return fail(TMPS_EUNSUPPORTED, "too many samples");
+    return TMPS_OK;
+}
+
+// (places in a chunk of rows are numbers of 32 bits)
+static int check_strides(int64_t rows, std::initializer_list<int64_t> strides) {
+    for (int64_t s : strides)
+        if (rows > 1 && s > (1 << 24)) return fail(TMPS_EUNSUPPORTED, "rows more than 2^24 elements apart");
     return TMPS_OK;
 }
 
@@ -151,7 +158,7 @@ extern "C" int tmps_scan_forward(int dtype, const tmps_scan_desc* desc, int64_t 
     Scan s = scan_of(desc, samples, positions);
     const int64_t rows = samples * positions, wide = (int64_t)s.heads * s.dh + 2 * (int64_t)s.groups * s.n, inner = (int64_t)s.heads * s.dh;
     if ((rc = check_rows("x", rows, wide, x_stride)) != TMPS_OK || (rc = check_rows("dt", rows, s.heads, dt_stride)) != TMPS_OK ||
-        (rc = check_rows("y", rows, inner, y_stride)) != TMPS_OK)
+        (rc = check_rows("y", rows, inner, y_stride)) != TMPS_OK || (rc = check_strides(rows, {x_stride, dt_stride, y_stride})) != TMPS_OK)
         return rc;
     const size_t esz = act_bytes(dtype), heads = (size_t)s.heads * 4, states = (size_t)samples * inner * s.n * 4, need = scan_workspace_bytes(s);
     if (!whole(esz, {x, dt, y}) || !whole(4, {a_log, skip, dt_bias, state, state_out})) return fail(TMPS_ESHAPE, "a pointer is not on a whole element");
@@ -182,7 +189,7 @@ extern "C" int tmps_scan_backward(int dtype, const tmps_scan_desc* desc, int64_t
     const int64_t rows = samples * positions, wide = (int64_t)s.heads * s.dh + 2 * (int64_t)s.groups * s.n, inner = (int64_t)s.heads * s.dh;
     if ((rc = check_rows("x", rows, wide, x_stride)) != TMPS_OK || (rc = check_rows("dt", rows, s.heads, dt_stride)) != TMPS_OK ||
         (rc = check_rows("dy", rows, inner, dy_stride)) != TMPS_OK || (rc = check_rows("dx", rows, wide, dx_stride)) != TMPS_OK ||
-        (rc = check_rows("ddt", rows, s.heads, ddt_stride)) != TMPS_OK)
+        (rc = check_rows("ddt", rows, s.heads, ddt_stride)) != TMPS_OK || (rc = check_strides(rows, {x_stride, dt_stride, dy_stride, dx_stride, ddt_stride})) != TMPS_OK)
         return rc;
     const size_t esz = act_bytes(dtype), heads = (size_t)s.heads * 4, states = (size_t)samples * inner * s.n * 4, need = scan_backward_workspace_bytes(dtype, s);
     if (!whole(esz, {dy, x, dt, dx, ddt}) || !whole(4, {dstate, a_log, skip, dt_bias, state, dparams, dstate_in})) return fail(TMPS_ESHAPE, "a pointer is not on a whole element");

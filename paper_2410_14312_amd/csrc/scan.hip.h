@@ -31,15 +31,12 @@ __device__ __forceinline__ f32x4_t mma(const Oct<float>& a, const Oct<float>& b,
     return acc;
 }
 
-// A number as the sum of K numbers of the operands' type (fp32: itself).  One that is not finite is the first of them, the others are 0.
+// A number as the sum of K numbers of the operands' type (fp32: itself).
 template <int K> __device__ __forceinline__ void terms_of(float x, int e, Oct<bf16_t> (&out)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         out[k].set(e, x);
-        if (k + 1 < K) {
-            x -= out[k].get(e);
-            x = fabsf(x) < 3.4e38f ? x : 0.0f;
-        }
+        if (k + 1 < K) x -= out[k].get(e);
     }
 }
 template <int K> __device__ __forceinline__ void terms_of(float x, int e, Oct<float> (&out)[K]) { out[0].set(e, x); }
@@ -121,6 +118,14 @@ __device__ __forceinline__ void put_four_any(float* p, const float (&v)[4], int 
         for (int e = 0; e < 4; ++e)
             if (e < many) p[e] = v[e];
 }
+// A row's fours, `many` numbers from this one on (all: the row has whole fours, the same for all).
+template <typename T> __device__ __forceinline__ void put_four_of(T* p, const float (&v)[4], int many, bool all) {
+    if (all) {
+        if (many > 0) put_four_any(p, v, 4);
+    } else if (many > 0) {
+        put_four_any(p, v, many);
+    }
+}
 __device__ __forceinline__ void four_any(const float* p, float (&v)[4], int many) {
     if (many >= 4) unpack(load16_any(p), v);
     else
@@ -128,28 +133,86 @@ __device__ __forceinline__ void four_any(const float* p, float (&v)[4], int many
         for (int e = 0; e < 4; ++e) v[e] = e < many ? p[e] : 0.0f;
 }
 
-// 16 bytes of a row from column c on, zeros from column `columns` on.
-template <typename T> __device__ __forceinline__ uint4 piece_until(const T* row, int c, int columns) {
-    constexpr int V = kPiece<T>;
-    if (c + V <= columns) return load16_any(row + c);
-    struct Values { T v[V]; } f;
+// N pieces of 16 bytes of a chunk's rows, at(i, row, column): piece i's row and first column.  The requests are loads without a branch (one in a branch would be waited for there), their
+// places in a whole chunk a number of 32 bits each that is formed once: where a row ends inside a piece, or before it, the piece begins as much earlier, and settle() moves what is its
+// own to its place and puts zeros behind it.
+template <typename T, int N> struct Requests {
+    static constexpr int V = kPiece<T>;
+    uint4 u[N];
+    uint32_t off[N];
+    static __device__ __forceinline__ uint32_t place(int r, int c, int64_t stride, int columns) { return (uint32_t)(r * (int)stride + (columns >= V ? min(c, columns - V) : 0)) * (uint32_t)sizeof(T); }
+    template <class At> __device__ __forceinline__ void places(int64_t stride, int columns, At&& at) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) f.v[e] = c + e < columns ? row[c + e] : T(0.0f);
-    return __builtin_bit_cast(uint4, f);
-}
-
-// The rows of a chunk on their way from memory to LDS: requested while the chunk before is worked on.  W columns, zeros behind the valid rows and columns.
-template <typename T, int W, int THREADS> struct ChunkRows {
-    static constexpr int V = kPiece<T>, kEach = W / V, kMany = kScanChunk * kEach / THREADS;
-    static_assert(kScanChunk * kEach % THREADS == 0, "pieces of a chunk");
-    uint4 u[kMany];
-    __device__ __forceinline__ void request(const T* base, int64_t stride, int rows, int columns) {
-#pragma unroll
-        for (int i = 0; i < kMany; ++i) {
-            const int k = (int)threadIdx.x + i * THREADS, r = k / kEach;
-            u[i] = r < rows ? piece_until(base + r * stride, k % kEach * V, columns) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < N; ++i) {
+            int r, c;
+            at(i, r, c);
+            off[i] = place(r, c, stride, columns);
         }
     }
+    template <class At> __device__ __forceinline__ void request(const T* base, int64_t stride, int rows, int columns, At&& at) {
+        if (columns < V) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int r, c;
+                at(i, r, c);
+                struct Values { T v[V]; } f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) f.v[e] = base[min(r, rows - 1) * stride + min(e, columns - 1)];
+                u[i] = __builtin_bit_cast(uint4, f);
+            }
+        } else if (rows < kScanChunk) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int r, c;
+                at(i, r, c);
+                u[i] = load16_any(reinterpret_cast<const char*>(base) + place(min(r, rows - 1), c, stride, columns));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) u[i] = load16_any(reinterpret_cast<const char*>(base) + off[i]);
+        }
+    }
+    // rows: those from this one on are zeros.  W: columns that are looked at
+    template <class At> __device__ __forceinline__ void settle(int rows, int columns, int W, At&& at) {
+        if (rows == kScanChunk && columns == W) return;
+        if (columns % V == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int r, c;
+                at(i, r, c);
+                if (r >= rows || c >= columns) u[i] = make_uint4(0, 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int r, c;
+                at(i, r, c);
+                uint64_t lo = u[i].x | (uint64_t)u[i].y << 32, hi = u[i].z | (uint64_t)u[i].w << 32;
+                const int early = columns >= V ? max(c + V - columns, 0) : 0, bits = early * (int)sizeof(T) * 8, keep = (columns - c) * (int)sizeof(T) * 8;
+                if (bits >= 64) lo = hi >> (bits & 63), hi = 0;
+                else if (bits > 0) lo = lo >> bits | hi << (64 - bits), hi >>= bits;
+                if (r >= rows || keep <= 0) lo = hi = 0;
+                else if (columns < V && keep < 64) hi = 0, lo &= (uint64_t(1) << keep) - 1;
+                else if (columns < V && keep < 128) hi &= keep > 64 ? (uint64_t(1) << (keep - 64)) - 1 : 0;
+                u[i] = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+            }
+        }
+    }
+};
+
+// The rows of a chunk on their way from memory to LDS: requested while the chunk before is worked on.  W columns, zeros behind the valid rows and columns.
+template <typename T, int W, int THREADS> struct ChunkRows : Requests<T, kScanChunk * W / kPiece<T> / THREADS> {
+    static constexpr int V = kPiece<T>, kEach = W / V, kMany = kScanChunk * kEach / THREADS;
+    static_assert(kScanChunk * kEach % THREADS == 0, "pieces of a chunk");
+    using Requests<T, kMany>::u;
+    static __device__ __forceinline__ void at(int i, int& r, int& c) {
+        const int k = (int)threadIdx.x + i * THREADS;
+        r = k / kEach;
+        c = k % kEach * V;
+    }
+    __device__ __forceinline__ void places_all(int64_t stride, int columns) { this->places(stride, columns, at); }
+    __device__ __forceinline__ void request_all(const T* base, int64_t stride, int rows, int columns) { this->request(base, stride, rows, columns, at); }
+    __device__ __forceinline__ void settle_all(int rows, int columns) { this->settle(rows, columns, W, at); }
     template <int PITCH> __device__ __forceinline__ void put(T* tile) const {
 #pragma unroll
         for (int i = 0; i < kMany; ++i) {
@@ -159,22 +222,23 @@ template <typename T, int W, int THREADS> struct ChunkRows {
     }
     // whether a number of this thread's is not finite
     __device__ __forceinline__ bool odd() const {
-        bool is = false;
+        uint32_t most = 0;   // exponents of all, the largest in each half
 #pragma unroll
         for (int i = 0; i < kMany; ++i)
 #pragma unroll
             for (uint32_t w : {u[i].x, u[i].y, u[i].z, u[i].w}) {
-                if constexpr (sizeof(T) == 2) is |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-                else is |= (w & 0x7f800000u) == 0x7f800000u;
+                if constexpr (sizeof(T) == 2) most = max(most, max(w & 0x7f800000u, w << 16 & 0x7f800000u));
+                else most = max(most, w & 0x7f800000u);
             }
-        return is;
+        return most == 0x7f800000u;
     }
 };
 
 // The steps and decays of a chunk, a position to a lane: delta, the sum of the exponents up to the position in units of log 2 (in two floats: of sums of hundreds their differences keep
-// their last places), the decay from before the chunk, that to its end and delta times it, and the slope of softplus.  Positions behind the last have delta 0: they change nothing.
+// their last places), the decay from before the chunk, that to its end and delta times it, that to the end of the position's sixteen, and the slope of softplus.  Positions behind the last
+// have delta 0: they change nothing.
 struct ChunkDecays {
-    float delta[kScanChunk], sum[kScanChunk], rest[kScanChunk], from[kScanChunk], back[kScanChunk], to[kScanChunk], slope[kScanChunk];
+    float delta[kScanChunk], sum[kScanChunk], rest[kScanChunk], from[kScanChunk], back[kScanChunk], to[kScanChunk], tile[kScanChunk], slope[kScanChunk];
     float end;       // the decay over the whole chunk
     double total;    // its exponent
 };
@@ -182,30 +246,34 @@ constexpr double kLog2eD = 1.4426950408889634074;
 
 __device__ __forceinline__ float softplus(float u) { return fmaxf(u, 0.0f) + log1pf(expf(-fabsf(u))); }
 
-template <typename T> __device__ __forceinline__ void chunk_decays(ChunkDecays& d, const T* dt, int64_t stride, int rows, float bias, double rate, int lane) {
-    float delta = 0.0f, slope = 0.0f;
-    if (lane < rows) {
-        const float u = to_f32(dt[lane * stride]) + bias;
-        delta = u != u ? u : softplus(u);
-        slope = 1.0f / (1.0f + expf(-u));
-    }
+// 2^e, e <= 0: of an exponent of hundreds what its float has lost is put back, as 1 + its natural multiple.
+__device__ __forceinline__ float exp2_of(double e) {
+    const float hi = (float)e, rest = (float)(e - (double)hi);
+    return __builtin_amdgcn_exp2f(hi) * fmaf(0.69314718f, fabsf(rest) < 1.0f ? rest : 0.0f, 1.0f);
+}
+
+template <bool SLOPE, typename T> __device__ __forceinline__ void chunk_decays(ChunkDecays& d, const T* dt, int64_t stride, int rows, float bias, double rate, int lane) {
+    const float u = to_f32(dt[min(lane, rows - 1) * stride]) + bias;
+    const float delta = lane >= rows ? 0.0f : u != u ? u : softplus(u);
     double sum = -(double)delta * rate;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
         const double before = __shfl_up(sum, k);
         if (lane >= k) sum += before;
     }
-    const double total = __shfl(sum, 63);
+    const double total = __shfl(sum, 63), of_tile = __shfl(sum, lane | 15);
     const float hi = (float)sum;
     d.delta[lane] = delta;
     d.sum[lane] = hi;
     d.rest[lane] = hi - hi == 0.0f ? (float)(sum - (double)hi) : 0.0f;
-    d.from[lane] = __builtin_amdgcn_exp2f(hi) * (1.0f + 0.69314718f * d.rest[lane]);
-    d.back[lane] = __builtin_amdgcn_exp2f((float)(total - sum));
-    d.to[lane] = delta * d.back[lane];
-    d.slope[lane] = slope;
+    d.from[lane] = exp2_of(sum);
+    const float back = exp2_of(total - sum);
+    d.back[lane] = back;
+    d.to[lane] = delta * back;
+    d.tile[lane] = exp2_of(of_tile - sum);
+    if constexpr (SLOPE) d.slope[lane] = lane < rows ? 1.0f / (1.0f + expf(-u)) : 0.0f;
     if (lane == 63) {
-        d.end = __builtin_amdgcn_exp2f((float)total);
+        d.end = exp2_of(total);
         d.total = total;
     }
 }

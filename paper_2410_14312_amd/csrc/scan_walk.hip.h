@@ -7,6 +7,10 @@
 
 namespace tmps {
 
+// States in workspaces have whole tiles, PP features of a slice by NP of n, zeros behind the last.
+inline int padded_n(int n) { return n <= 32 ? 32 : n <= 64 ? 64 : 128; }
+inline int padded_dh(int dh) { return dh <= 32 ? 32 : (dh + 63) / 64 * 64; }
+
 // The walk's operands: "x" and "b" are x and B going forward, dy and C going backward, where the state is the gradient of the state behind a chunk.
 struct ScanWalk {
     const void *x, *b, *c, *dt;
@@ -16,11 +20,11 @@ struct ScanWalk {
     void* y;
     int64_t y_stride;
     float* final_state;          // behind the last chunk (null: not wanted)
-    float* chunk_states;         // before each chunk of the walk: [samples, heads, chunks, dh, n] (null: not wanted)
+    float* chunk_states;         // before each chunk of the walk: [samples, heads, chunks, PP * slices, NP] (null: not wanted)
     int64_t samples, positions;
     int heads, dh, groups, n;
     int chunks, stretches, each, slices;   // chunks of a sample, stretches of them and the chunks of one, slices of a head's features
-    float* stretch_states;       // [samples, heads, stretches, dh, n]: before each stretch, or with `own` left by each
+    float* stretch_states;       // [samples, heads, stretches, PP * slices, NP]: before each stretch, or with `own` left by each
     double* stretch_totals;
     bool own;                    // each stretch from nothing, for its own state and exponent alone
 };
@@ -39,7 +43,7 @@ template <typename T> ScanWalk walk_of(const Scan& a) {
 template <typename T> constexpr int kStateTerms = sizeof(T) == 2 ? 3 : 1;    // of a state's increments: results in fp32
 template <typename T> constexpr int kResultTerms = sizeof(T) == 2 ? 2 : 1;   // of states and decayed products on their way to results of the type
 
-template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bounds__(256) void scan_walk_kernel(ScanWalk a) {
+template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bounds__(256, 2) void scan_walk_kernel(ScanWalk a) {
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, NT = NP / 16, TW = NT * PT / 4, NK = NP / 32;
     constexpr int RT = kResultTerms<T>, ST = kStateTerms<T>;
     __shared__ __attribute__((aligned(16))) T xs[kScanChunk * XP];
@@ -57,7 +61,7 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     const int stretch = (int)(unit % a.stretches);
     const int64_t sample = unit / a.stretches;
     const int group = head / (a.heads / a.groups);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
     const int p0 = slice * 64, width = min(64, a.dh - p0);
     const double rate = exp((double)a.a_log[head]) * kLog2eD;
     const float bias = a.dt_bias[head];
@@ -74,13 +78,18 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     const int p = pt * 16 + col;   // in the slice
     f32x4_t state[TW];
     const int64_t of_head = (sample * a.heads + head) * a.dh * a.n + (int64_t)(p0 + p) * a.n;
-    const int64_t of_stretch = ((sample * a.heads + head) * a.stretches + stretch) * a.dh * a.n + (int64_t)(p0 + p) * a.n;
-    const float* const from = a.own ? nullptr : a.stretches > 1 ? a.stretch_states + of_stretch : a.first_state ? a.first_state + of_head : nullptr;
+    const int64_t whole = (int64_t)a.slices * PP * NP, in_whole = (int64_t)(p0 + p) * NP;
+    const int64_t of_stretch = ((sample * a.heads + head) * a.stretches + stretch) * whole + in_whole;
     const auto n_of = [&](int k) { return (nt0 + k * NSTEP) * 16 + 4 * g; };
 #pragma unroll
     for (int k = 0; k < TW; ++k) {
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (from && p < width && n_of(k) < a.n) four_any(from + n_of(k), v, a.n - n_of(k));
+        if (a.own) {
+        } else if (a.stretches > 1) {
+            four(a.stretch_states + of_stretch + n_of(k), v);
+        } else if (a.first_state && p < width && n_of(k) < a.n) {
+            four_any(a.first_state + of_head + n_of(k), v, a.n - n_of(k));
+        }
         state[k] = f32x4_t{v[0], v[1], v[2], v[3]};
     }
 
@@ -89,12 +98,21 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     const auto rows_of = [&](int chunk) { return (int)min<int64_t>(kScanChunk, a.positions - (int64_t)chunk * kScanChunk); };
     ChunkRows<T, PP, 256> xr;
     ChunkRows<T, NP, 256> br;
-    Oct<T> cf[OUT ? NK : 1];
+    constexpr int kC = (int)sizeof(T) / 2;   // pieces of eight numbers
+    Requests<T, OUT ? NK * kC : 1> cr;
+    xr.places_all(a.x_stride, width);
+    br.places_all(a.bc_stride, a.n);
+    const auto of_c = [&](int k, int& r, int& c) {
+        r = 16 * wave + col;
+        c = 32 * (k / kC) + 8 * g + k % kC * V;
+    };
+    if constexpr (OUT) cr.places(a.bc_stride, a.n, of_c);
     const auto request = [&](int chunk) {
         const int64_t t0 = (int64_t)chunk * kScanChunk;
         const int rows = rows_of(chunk);
-        xr.request(xg + t0 * a.x_stride, a.x_stride, rows, width);
-        br.request(bg + t0 * a.bc_stride, a.bc_stride, rows, a.n);
+        xr.request_all(xg + t0 * a.x_stride, a.x_stride, rows, width);
+        br.request_all(bg + t0 * a.bc_stride, a.bc_stride, rows, a.n);
+        if constexpr (OUT) cr.request(cg + t0 * a.bc_stride, a.bc_stride, rows, a.n, of_c);
     };
     double total = 0.0;
     if (threadIdx.x < 2) odd[threadIdx.x] = 0;
@@ -105,20 +123,22 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
         __syncthreads();   // (the chunk before has been read)
         if ((i & 3) == 0 && i + wave < many) {
             const int mine = chunk_of(i + wave);
-            chunk_decays(decays[wave], dtg + (int64_t)mine * kScanChunk * a.dt_stride, a.dt_stride, rows_of(mine), bias, rate, lane);
+            chunk_decays<false>(decays[wave], dtg + (int64_t)mine * kScanChunk * a.dt_stride, a.dt_stride, rows_of(mine), bias, rate, lane);
         }
+        xr.settle_all(rows, width);
+        br.settle_all(rows, a.n);
         xr.template put<XP>(xs);
         br.template put<BP>(bs);
+        Oct<T> cf[OUT ? NK : 1];
         if constexpr (OUT) {
             if (xr.odd()) odd[i & 1] = 1;
             if (threadIdx.x == 0) odd[(i + 1) & 1] = 0;   // (last read before the barrier above)
-            const int t = 16 * wave + col;
+            cr.settle(rows, a.n, NP, of_c);
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                struct Eight { uint4 u[sizeof(T) / 2]; } e;
+                struct Eight { uint4 u[kC]; } e;
 #pragma unroll
-                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                    e.u[h] = t < rows ? piece_until(cg + (t0 + t) * a.bc_stride, 32 * k + 8 * g + h * V, a.n) : make_uint4(0, 0, 0, 0);
+                for (int h = 0; h < kC; ++h) e.u[h] = cr.u[k * kC + h];
                 cf[k] = __builtin_bit_cast(Oct<T>, e);
             }
             // the state as an operand: [p][n]
@@ -130,10 +150,7 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
                     put_four(ss + h * PP * BP + p * BP + n_of(k), v);
                     if (h + 1 < RT) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float rest = v[e] - (float)(T)v[e];
-                            v[e] = fabsf(rest) < 3.4e38f ? rest : 0.0f;
-                        }
+                        for (int e = 0; e < 4; ++e) v[e] -= (float)(T)v[e];
                     }
                 }
             }
@@ -141,12 +158,12 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
         __syncthreads();
         if (i + 1 < many) request(chunk_of(i + 1));
         const ChunkDecays& d = decays[i & 3];
-        if (a.chunk_states && p < width) {
-            float* const to = a.chunk_states + (((sample * a.heads + head) * a.chunks + chunk) * a.dh + p0 + p) * a.n;
+        if (!OUT && a.chunk_states) {
+            float* const to = a.chunk_states + ((sample * a.heads + head) * a.chunks + chunk) * whole + in_whole;
 #pragma unroll
             for (int k = 0; k < TW; ++k) {
                 const float v[4] = {state[k][0], state[k][1], state[k][2], state[k][3]};
-                if (n_of(k) < a.n) put_four_any(to + n_of(k), v, a.n - n_of(k));
+                put_four(to + n_of(k), v);
             }
         }
         if constexpr (OUT) {
@@ -160,13 +177,23 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
                 if (st > wave) continue;
 #pragma unroll
                 for (int k = 0; k < NK; ++k) m[st] = mma(along<false>(bs + (16 * st + col) * BP, 32 * k, lane), cf[k], m[st]);
-                float sum_s[4], rest_s[4], delta_s[4];
-                four(d.sum + 16 * st + 4 * g, sum_s);
-                four(d.rest + 16 * st + 4 * g, rest_s);
+                float delta_s[4];
                 four(d.delta + 16 * st + 4 * g, delta_s);
+                if (st < wave) {
+                    // (by way of the end of the sixteen positions of s: neither factor is over one)
+                    const float on = decay_between(sum_t, rest_t, d.sum[16 * st + 15], d.rest[16 * st + 15]);
+                    float tile_s[4];
+                    four(d.tile + 16 * st + 4 * g, tile_s);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    m[st][r] = 16 * st + 4 * g + r <= t ? m[st][r] * (decay_between(sum_t, rest_t, sum_s[r], rest_s[r]) * delta_s[r]) : 0.0f;
+                    for (int r = 0; r < 4; ++r) m[st][r] *= on * (tile_s[r] * delta_s[r]);
+                } else {
+                    float sum_s[4], rest_s[4];
+                    four(d.sum + 16 * st + 4 * g, sum_s);
+                    four(d.rest + 16 * st + 4 * g, rest_s);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        m[st][r] = 4 * g + r <= col ? m[st][r] * (decay_between(sum_t, rest_t, sum_s[r], rest_s[r]) * delta_s[r]) : 0.0f;
+                }
             }
             // rows p, column t: what the state before the chunk gives, then the chunk's own
             f32x4_t y[PT];
@@ -200,22 +227,34 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
                 }
             }
             if (some_odd) {
+#pragma clang loop unroll(disable)
+                for (int s = 0; s < 16 * wave + 16; ++s) {
+                    float x[PT][4];
+                    bool here = false;
 #pragma unroll
-                for (int st = 0; st < 4; ++st)
+                    for (int j = 0; j < PT; ++j) {
+                        four(xs + s * XP + 16 * j + 4 * g, x[j]);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        for (int h = 0; h < 4; ++h) {
-                            const int s = 16 * st + 4 * h + r;
-                            const float by = __shfl(m[st][r], 16 * h + col);
-                            if (s > t) continue;
+                        for (int e = 0; e < 4; ++e) here |= !(fabsf(x[j][e]) < __builtin_inff());
+                    }
+                    if (!__any(here)) continue;
+                    float by = 0.0f;   // C_t . B_s
 #pragma unroll
-                            for (int j = 0; j < PT; ++j)
+                    for (int k = 0; k < NK; ++k) {
+                        const Oct<T> b = along<false>(bs + s * BP, 32 * k, lane);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const float x = to_f32(xs[s * XP + 16 * j + 4 * g + e]);
-                                    if (!(fabsf(x) < __builtin_inff())) y[j][e] = fmaf(by, x, y[j][e]);
-                                }
-                        }
+                        for (int e = 0; e < 8; ++e) by = fmaf(b.get(e), cf[k].get(e), by);
+                    }
+                    by += __shfl_xor(by, 16);
+                    by += __shfl_xor(by, 32);
+                    by *= decay_between(sum_t, rest_t, d.sum[s], d.rest[s]) * d.delta[s];
+                    if (s > t) continue;
+#pragma unroll
+                    for (int j = 0; j < PT; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(fabsf(x[j][e]) < __builtin_inff())) y[j][e] = fmaf(by, x[j][e], y[j][e]);
+                }
             }
             if (t < rows) {
                 T* const row = (T*)a.y + (rows0 + t0 + t) * a.y_stride + (int64_t)head * a.dh + p0;
@@ -226,7 +265,7 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
                     four(xs + t * XP + 16 * j + 4 * g, x);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = fmaf(skip, x[e], y[j][e]);
-                    if (16 * j + 4 * g < width) put_four_any(row + 16 * j + 4 * g, v, width - 16 * j - 4 * g);
+                    put_four_of(row + 16 * j + 4 * g, v, width - 16 * j - 4 * g, width % 4 == 0);
                 }
             }
         }
@@ -253,39 +292,46 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
         total += d.total;
     }
     if (a.own && threadIdx.x == 0 && slice == 0) a.stretch_totals[(sample * a.heads + head) * a.stretches + stretch] = total;
-    float* const to = a.own ? a.stretch_states + of_stretch : a.final_state && stretch == (REV ? 0 : a.stretches - 1) ? a.final_state + of_head : nullptr;
-    if (to && p < width) {
+    if (a.own) {
 #pragma unroll
         for (int k = 0; k < TW; ++k) {
             const float v[4] = {state[k][0], state[k][1], state[k][2], state[k][3]};
-            if (n_of(k) < a.n) put_four_any(to + n_of(k), v, a.n - n_of(k));
+            put_four(a.stretch_states + of_stretch + n_of(k), v);
+        }
+    } else if (a.final_state && stretch == (REV ? 0 : a.stretches - 1) && p < width) {
+#pragma unroll
+        for (int k = 0; k < TW; ++k) {
+            const float v[4] = {state[k][0], state[k][1], state[k][2], state[k][3]};
+            if (n_of(k) < a.n) put_four_any(a.final_state + of_head + n_of(k), v, a.n - n_of(k));
         }
     }
 }
 
 // The stretches' own states become those before them: a thread to a number of a state.
-template <bool REV> __global__ __launch_bounds__(256) void scan_join_kernel(ScanWalk a) {
-    const int64_t size = (int64_t)a.dh * a.n, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.samples * a.heads * size) return;
-    const int64_t head = i / size, at = i % size;
-    float carry = a.first_state ? a.first_state[i] : 0.0f;
-    float* const states = a.stretch_states + head * a.stretches * size + at;
+template <bool REV> __global__ __launch_bounds__(256) void scan_join_kernel(ScanWalk a, int NP, int whole) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.samples * a.heads * whole) return;
+    const int64_t head = i / whole;
+    const int at = (int)(i - head * whole), p = at / NP, n = at % NP;
+    float carry = a.first_state && p < a.dh && n < a.n ? a.first_state[(head * a.dh + p) * a.n + n] : 0.0f;
+    float* const states = a.stretch_states + head * a.stretches * whole + at;
     const double* const totals = a.stretch_totals + head * a.stretches;
+#pragma unroll 4
     for (int k = 0; k < a.stretches; ++k) {
         const int s = REV ? a.stretches - 1 - k : k;
-        const float own = states[s * size];
-        states[s * size] = carry;
-        carry = fmaf(__builtin_amdgcn_exp2f((float)totals[s]), carry, own);
+        const float own = states[(int64_t)s * whole];
+        states[(int64_t)s * whole] = carry;
+        carry = fmaf(exp2_of(totals[s]), carry, own);
     }
 }
 
-// Stretches: as many as give the chip 512 workgroups, of four chunks at least.
+// Stretches: as many as are 512 workgroups, two for each compute unit, of four chunks at least, where that is two or more.
 constexpr int kStretchGroups = 512, kStretchChunks = 4;
 inline void walk_plan(ScanWalk& w) {
     w.chunks = (int)((w.positions + kScanChunk - 1) / kScanChunk);
     w.slices = (w.dh + 63) / 64;
     const int64_t groups = w.samples * w.heads * w.slices;
-    int64_t want = std::min<int64_t>((kStretchGroups + groups - 1) / groups, w.chunks / kStretchChunks);
+    int64_t want = std::min<int64_t>(kStretchGroups / groups, w.chunks / kStretchChunks);
     if (want < 1) want = 1;
     w.each = (int)((w.chunks + want - 1) / want);
     w.stretches = (w.chunks + w.each - 1) / w.each;
@@ -295,9 +341,8 @@ inline void walk_plan(ScanWalk& w) {
 inline size_t walk_stretch_bytes(const Scan& a) {
     const int64_t chunks = (a.positions + kScanChunk - 1) / kScanChunk, slices = (a.dh + 63) / 64;
     if (chunks < 2 * kStretchChunks) return 0;
-    // samples x heads x stretches is at most the workgroups wanted / slices and as many again as there are samples and heads
-    const int64_t most = std::min<int64_t>(a.samples * a.heads * (chunks / kStretchChunks), kStretchGroups / slices + a.samples * a.heads);
-    return (size_t)most * ((size_t)a.dh * a.n * sizeof(float) + sizeof(double)) + 256;
+    const int64_t most = std::min<int64_t>(a.samples * a.heads * (chunks / kStretchChunks), kStretchGroups / slices);
+    return (size_t)most * ((size_t)padded_dh(a.dh) * padded_n(a.n) * sizeof(float) + sizeof(double)) + 256;
 }
 
 template <typename T, bool OUT, bool REV> static hipError_t walk_launch(const ScanWalk& w, hipStream_t s) {
@@ -327,9 +372,10 @@ template <typename T, bool OUT, bool REV> static hipError_t walk_stretches(ScanW
         own.chunk_states = nullptr;
         hipError_t e = walk_launch<T, false, REV>(own, s);
         if (e != hipSuccess) return e;
-        const int64_t numbers = w.samples * w.heads * w.dh * w.n;
+        const int NP = padded_n(w.n), whole = padded_dh(w.dh) * NP;
+        const int64_t numbers = w.samples * w.heads * whole;
         if ((numbers + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
-        e = launch_timed(OUT ? kcAttnFwd : kcAttnBwd, scan_join_kernel<REV>, dim3((unsigned)((numbers + 255) / 256)), dim3(256), 0, s, w);
+        e = launch_timed(OUT ? kcAttnFwd : kcAttnBwd, scan_join_kernel<REV>, dim3((unsigned)((numbers + 255) / 256)), dim3(256), 0, s, w, NP, whole);
         if (e != hipSuccess) return e;
     }
     return walk_launch<T, OUT, REV>(w, s);
