@@ -34,12 +34,16 @@ __device__ __forceinline__ float column_sum(float v) {
     return v + __shfl_xor(v, 32);
 }
 
-template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void scan_grad_kernel(ScanGrad a) {
+// Whether LDS holds what two workgroups of a compute unit need.
+template <typename T, int NP> constexpr bool kTwoGroups = sizeof(T) == 2 && NP <= 64;
+constexpr int kGradDecays = 2;   // heads whose decays are formed at a time, a wave each
+
+template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGroups<T, NP> ? 2 : 1)) void scan_grad_kernel(ScanGrad a) {
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, MP = kScanChunk + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
     constexpr int GT = kStateTerms<T>;
     constexpr int kState = PP * NP / 4 / 256;   // fours of a state of a thread
     __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[kScanChunk * MP];
-    __shared__ __attribute__((aligned(16))) ChunkDecays decays[4];
+    __shared__ __attribute__((aligned(16))) ChunkDecays decays[kGradDecays];
     __shared__ float rowq[4][kScanChunk], ya[kScanChunk], gs[kScanChunk], red[4][2];
     const ScanBackward& b = a.b;
     const Scan& f = b.f;
@@ -103,7 +107,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
                 four(a.behind + of_state + 4 * k, g4[i]);
             }
             __syncthreads();   // (what the head or slice before has left in LDS has been read)
-            if (slice == 0 && ((h - first) & 3) == 0 && h + wave < last) {
+            if (slice == 0 && (h - first) % kGradDecays == 0 && wave < kGradDecays && h + wave < last) {
                 const int mine = head + wave;
                 chunk_decays<true>(decays[wave], (const T*)f.dt + row0 * f.dt_stride + mine, f.dt_stride, rows, f.dt_bias[mine], exp((double)f.a_log[mine]) * kLog2eD, lane);
             }
@@ -138,7 +142,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
                 for (int e = 0; e < V; ++e) dskip = fmaf(vx[e], vd[e], dskip);
             }
             __syncthreads();
-            const ChunkDecays& d = decays[(h - first) & 3];
+            const ChunkDecays& d = decays[(h - first) % kGradDecays];
 
             // by columns t
             f32x4_t m[4], dz[4];
@@ -285,14 +289,14 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256) void sca
             }
         }
         // the head's steps and parameters
-        const float meet_all = wsum(meet * decays[(h - first) & 3].end + end_sum), skip_all = wsum(dskip);
+        const float meet_all = wsum(meet * decays[(h - first) % kGradDecays].end + end_sum), skip_all = wsum(dskip);
         if (lane == 0) {
             red[wave][0] = meet_all;
             red[wave][1] = skip_all;
         }
         __syncthreads();
         if (wave == 0) {
-            const ChunkDecays& d = decays[(h - first) & 3];
+            const ChunkDecays& d = decays[(h - first) % kGradDecays];
             const double rate = exp((double)f.a_log[head]);
             const float q = (rowq[0][lane] + rowq[1][lane]) + (rowq[2][lane] + rowq[3][lane]), delta = d.delta[lane], with_g = gs[lane];
             double sum = (double)ya[lane] - ((double)delta * (double)q + (double)d.to[lane] * (double)with_g);

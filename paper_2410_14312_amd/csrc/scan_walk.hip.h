@@ -7,7 +7,7 @@
 
 namespace tmps {
 
-// States in workspaces have whole tiles, PP features of a slice by NP of n, zeros behind the last.
+// States in workspaces have whole tiles, zeros behind the last feature.
 inline int padded_n(int n) { return n <= 32 ? 32 : n <= 64 ? 64 : 128; }
 inline int padded_dh(int dh) { return dh <= 32 ? 32 : (dh + 63) / 64 * 64; }
 
@@ -20,11 +20,11 @@ struct ScanWalk {
     void* y;
     int64_t y_stride;
     float* final_state;          // behind the last chunk (null: not wanted)
-    float* chunk_states;         // before each chunk of the walk: [samples, heads, chunks, PP * slices, NP] (null: not wanted)
+    float* chunk_states;         // before each chunk of the walk: [samples, heads, chunks, padded dh, NP] (null: not wanted)
     int64_t samples, positions;
     int heads, dh, groups, n;
-    int chunks, stretches, each, slices;   // chunks of a sample, stretches of them and the chunks of one, slices of a head's features
-    float* stretch_states;       // [samples, heads, stretches, PP * slices, NP]: before each stretch, or with `own` left by each
+    int chunks, stretches, each, slices, tiles;   // chunks of a sample, stretches of them and the chunks of one, slices of a head's features and their tiles of 16
+    float* stretch_states;       // [samples, heads, stretches, padded dh, NP]: before each stretch, or with `own` left by each
     double* stretch_totals;
     bool own;                    // each stretch from nothing, for its own state and exponent alone
 };
@@ -62,12 +62,13 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     const int64_t sample = unit / a.stretches;
     const int group = head / (a.heads / a.groups);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-    const int p0 = slice * 64, width = min(64, a.dh - p0);
+    const int p0 = slice * PP, width = max(min(PP, a.dh - p0), 0);   // (a slice behind the last feature reads the first one's and has zeros)
+    const int read_p0 = width ? p0 : 0, read_width = width ? width : min(PP, a.dh);
     const double rate = exp((double)a.a_log[head]) * kLog2eD;
     const float bias = a.dt_bias[head];
 
     const int64_t rows0 = sample * a.positions;
-    const T* const xg = (const T*)a.x + rows0 * a.x_stride + (int64_t)head * a.dh + p0;
+    const T* const xg = (const T*)a.x + rows0 * a.x_stride + (int64_t)head * a.dh + read_p0;
     const T* const bg = (const T*)a.b + rows0 * a.bc_stride + (int64_t)group * a.n;
     const T* const cg = (const T*)a.c + rows0 * a.bc_stride + (int64_t)group * a.n;
     const T* const dtg = (const T*)a.dt + rows0 * a.dt_stride + head;
@@ -100,7 +101,7 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     ChunkRows<T, NP, 256> br;
     constexpr int kC = (int)sizeof(T) / 2;   // pieces of eight numbers
     Requests<T, OUT ? NK * kC : 1> cr;
-    xr.places_all(a.x_stride, width);
+    xr.places_all(a.x_stride, read_width);
     br.places_all(a.bc_stride, a.n);
     const auto of_c = [&](int k, int& r, int& c) {
         r = 16 * wave + col;
@@ -110,7 +111,7 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     const auto request = [&](int chunk) {
         const int64_t t0 = (int64_t)chunk * kScanChunk;
         const int rows = rows_of(chunk);
-        xr.request_all(xg + t0 * a.x_stride, a.x_stride, rows, width);
+        xr.request_all(xg + t0 * a.x_stride, a.x_stride, rows, read_width);
         br.request_all(bg + t0 * a.bc_stride, a.bc_stride, rows, a.n);
         if constexpr (OUT) cr.request(cg + t0 * a.bc_stride, a.bc_stride, rows, a.n, of_c);
     };
@@ -329,7 +330,8 @@ template <bool REV> __global__ __launch_bounds__(256) void scan_join_kernel(Scan
 constexpr int kStretchGroups = 512, kStretchChunks = 4;
 inline void walk_plan(ScanWalk& w) {
     w.chunks = (int)((w.positions + kScanChunk - 1) / kScanChunk);
-    w.slices = (w.dh + 63) / 64;
+    w.tiles = w.dh <= 32 || w.samples * w.heads * (padded_dh(w.dh) / 64) * w.chunks < kStretchGroups ? 2 : 4;
+    w.slices = padded_dh(w.dh) / (16 * w.tiles);
     const int64_t groups = w.samples * w.heads * w.slices;
     int64_t want = std::min<int64_t>(kStretchGroups / groups, w.chunks / kStretchChunks);
     if (want < 1) want = 1;
@@ -350,7 +352,7 @@ template <typename T, bool OUT, bool REV> static hipError_t walk_launch(const Sc
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(256);
     const int kc = OUT ? kcAttnFwd : kcAttnBwd;
-    if (w.dh > 32) {
+    if (w.tiles == 4) {
         if (w.n <= 32) return launch_timed(kc, scan_walk_kernel<T, 32, 4, OUT, REV>, grid, block, 0, s, w);
         if (w.n <= 64) return launch_timed(kc, scan_walk_kernel<T, 64, 4, OUT, REV>, grid, block, 0, s, w);
         return launch_timed(kc, scan_walk_kernel<T, 128, 4, OUT, REV>, grid, block, 0, s, w);
