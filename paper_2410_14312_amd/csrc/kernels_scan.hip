@@ -106,7 +106,20 @@ template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hi
     ScanWalk w = walk_of<T>(a);
     w.y = a.y; w.y_stride = a.y_stride;
     w.final_state = a.state_out;
-    return walk_stretches<T, true, false>(w, ws, s);
+    walk_plan(w);
+    const unsigned grid = walk_grid(w);
+    if (!grid) return hipErrorInvalidValue;
+    if (w.stretches > 1) {
+        walk_room(w, static_cast<char*>(ws));
+        const ScanWalk own = own_walk(w);
+#define TMPS_OWN(NP, PT) launch_timed(kcAttnFwd, scan_walk_kernel<T, NP, PT, false, false>, dim3(grid), dim3(256), 0, s, own)
+        hipError_t e = TMPS_WALK(TMPS_OWN, own);
+        if (e != hipSuccess) return e;
+        e = launch_timed(kcAttnFwd, scan_join_kernel, dim3(join_grid(w)), dim3(256), 0, s, w, padded_n(w.n), padded_dh(w.dh) * padded_n(w.n));
+        if (e != hipSuccess) return e;
+    }
+#define TMPS_OUT(NP, PT) launch_timed(kcAttnFwd, scan_walk_kernel<T, NP, PT, true, false>, dim3(grid), dim3(256), 0, s, w)
+    return TMPS_WALK(TMPS_OUT, w);
 }
 
 hipError_t scan_forward(int dtype, const Scan& a, void* ws, hipStream_t s) { return dtype == kBF16 ? forward_type<bf16_t>(a, ws, s) : forward_type<float>(a, ws, s); }

@@ -386,7 +386,7 @@ struct GradRoom {
 static GradRoom grad_room(const Scan& f) {
     const int64_t chunks = (f.positions + kScanChunk - 1) / kScanChunk, of_chunks = f.samples * chunks;
     GradRoom r;
-    r.walk = on256(walk_stretch_bytes(f));
+    r.walk = on256(2 * walk_stretch_bytes(f));
     r.states = on256((size_t)of_chunks * f.heads * padded_dh(f.dh) * padded_n(f.n) * sizeof(float));
     r.sums = on256((size_t)of_chunks * 3 * f.heads * sizeof(float));
     // (parts x chunks is at most the workgroups wanted and as many again as there are chunks)
@@ -410,11 +410,24 @@ template <typename T> static hipError_t backward_type(const ScanBackward& b, voi
     a.shared = a.parts > 1 ? reinterpret_cast<float*>(at + room.walk + 2 * room.states + room.sums) : nullptr;
     ScanWalk w = walk_of<T>(b.f);
     w.chunk_states = before;
-    hipError_t e = walk_stretches<T, false, false>(w, ws, s);
-    if (e != hipSuccess) return e;
-    w.x = b.dy; w.x_stride = b.dy_stride; w.b = w.c;
-    w.first_state = b.dstate; w.chunk_states = behind; w.final_state = b.dstate_in;
-    e = walk_stretches<T, false, true>(w, ws, s);
+    walk_plan(w);
+    ScanWalk back = w;
+    back.x = b.dy; back.x_stride = b.dy_stride; back.b = w.c;
+    back.first_state = b.dstate; back.chunk_states = behind; back.final_state = b.dstate_in;
+    const unsigned walks = walk_grid(w);
+    if (!walks) return hipErrorInvalidValue;
+    hipError_t e = hipSuccess;
+    if (w.stretches > 1) {
+        walk_room(back, walk_room(w, at));
+        const ScanWalk own = own_walk(w), own_back = own_walk(back);
+#define TMPS_OWNS(NP, PT) launch_timed(kcAttnBwd, scan_walks_kernel<T, NP, PT>, dim3(walks, 2), dim3(256), 0, s, own, own_back)
+        e = TMPS_WALK(TMPS_OWNS, w);
+        if (e != hipSuccess) return e;
+        e = launch_timed(kcAttnBwd, scan_joins_kernel, dim3(join_grid(w), 2), dim3(256), 0, s, w, back, padded_n(w.n), padded_dh(w.dh) * padded_n(w.n));
+        if (e != hipSuccess) return e;
+    }
+#define TMPS_WALKS(NP, PT) launch_timed(kcAttnBwd, scan_walks_kernel<T, NP, PT>, dim3(walks, 2), dim3(256), 0, s, w, back)
+    e = TMPS_WALK(TMPS_WALKS, w);
     if (e != hipSuccess) return e;
     const Scan& f = b.f;
     const int64_t units = f.samples * a.chunks * f.groups * a.parts, blocks = (units + 7) / 8 * 8;

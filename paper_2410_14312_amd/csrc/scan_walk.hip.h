@@ -43,17 +43,22 @@ template <typename T> ScanWalk walk_of(const Scan& a) {
 template <typename T> constexpr int kStateTerms = sizeof(T) == 2 ? 3 : 1;    // of a state's increments: results in fp32
 template <typename T> constexpr int kResultTerms = sizeof(T) == 2 ? 2 : 1;   // of states and decayed products on their way to results of the type
 
-template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bounds__(256, 2) void scan_walk_kernel(ScanWalk a) {
+template <typename T, int NP, int PT, bool OUT> struct WalkTiles {
+    static constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V;
+    __attribute__((aligned(16))) T xs[kScanChunk * XP];
+    __attribute__((aligned(16))) T bs[kScanChunk * BP];
+    __attribute__((aligned(16))) T ss[OUT ? kResultTerms<T> * PP * BP : 8];
+    __attribute__((aligned(16))) ChunkDecays decays[4];
+    int odd[2];
+};
+
+// What one workgroup does: stretch, head, slice and sample number `unit`.
+template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinline__ void scan_walk(const ScanWalk& a, int64_t unit, WalkTiles<T, NP, PT, OUT>& tiles) {
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, NT = NP / 16, TW = NT * PT / 4, NK = NP / 32;
     constexpr int RT = kResultTerms<T>, ST = kStateTerms<T>;
-    __shared__ __attribute__((aligned(16))) T xs[kScanChunk * XP];
-    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP];
-    __shared__ __attribute__((aligned(16))) T ss[OUT ? RT * PP * BP : 8];
-    __shared__ __attribute__((aligned(16))) ChunkDecays decays[4];
-    __shared__ int odd[2];
-    const int64_t units = a.samples * a.stretches * a.heads * a.slices;
-    int64_t unit = xcd_order(blockIdx.x, gridDim.x);
-    if (unit >= units) return;
+    T *const xs = tiles.xs, *const bs = tiles.bs, *const ss = tiles.ss;
+    ChunkDecays* const decays = tiles.decays;
+    int* const odd = tiles.odd;
     const int slice = (int)(unit % a.slices);
     unit /= a.slices;
     const int head = (int)(unit % a.heads);
@@ -308,8 +313,23 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bo
     }
 }
 
+template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bounds__(256, 2) void scan_walk_kernel(ScanWalk a) {
+    __shared__ WalkTiles<T, NP, PT, OUT> tiles;
+    const int64_t unit = xcd_order(blockIdx.x, gridDim.x);
+    if (unit < a.samples * a.stretches * a.heads * a.slices) scan_walk<T, NP, PT, OUT, REV>(a, unit, tiles);
+}
+
+// The two walks of a backward pass, for the states alone, side by side: `back` goes backward.
+template <typename T, int NP, int PT> __global__ __launch_bounds__(256, 2) void scan_walks_kernel(ScanWalk ahead, ScanWalk back) {
+    __shared__ WalkTiles<T, NP, PT, false> tiles;
+    const int64_t unit = xcd_order(blockIdx.x, gridDim.x);
+    if (unit >= ahead.samples * ahead.stretches * ahead.heads * ahead.slices) return;
+    if (blockIdx.y == 0) scan_walk<T, NP, PT, false, false>(ahead, unit, tiles);
+    else scan_walk<T, NP, PT, false, true>(back, unit, tiles);
+}
+
 // The stretches' own states become those before them: a thread to a number of a state.
-template <bool REV> __global__ __launch_bounds__(256) void scan_join_kernel(ScanWalk a, int NP, int whole) {
+template <bool REV> __device__ __forceinline__ void scan_join(const ScanWalk& a, int NP, int whole) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.samples * a.heads * whole) return;
     const int64_t head = i / whole;
@@ -324,6 +344,11 @@ template <bool REV> __global__ __launch_bounds__(256) void scan_join_kernel(Scan
         states[(int64_t)s * whole] = carry;
         carry = fmaf(exp2_of(totals[s]), carry, own);
     }
+}
+static __global__ __launch_bounds__(256) void scan_join_kernel(ScanWalk a, int NP, int whole) { scan_join<false>(a, NP, whole); }
+static __global__ __launch_bounds__(256) void scan_joins_kernel(ScanWalk ahead, ScanWalk back, int NP, int whole) {
+    if (blockIdx.y == 0) scan_join<false>(ahead, NP, whole);
+    else scan_join<true>(back, NP, whole);
 }
 
 // Stretches: as many as are 512 workgroups, two for each compute unit, of four chunks at least, where that is two or more.
@@ -347,40 +372,29 @@ inline size_t walk_stretch_bytes(const Scan& a) {
     return (size_t)most * ((size_t)padded_dh(a.dh) * padded_n(a.n) * sizeof(float) + sizeof(double)) + 256;
 }
 
-template <typename T, bool OUT, bool REV> static hipError_t walk_launch(const ScanWalk& w, hipStream_t s) {
-    const int64_t units = w.samples * w.stretches * w.heads * w.slices, blocks = (units + 7) / 8 * 8;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(256);
-    const int kc = OUT ? kcAttnFwd : kcAttnBwd;
-    if (w.tiles == 4) {
-        if (w.n <= 32) return launch_timed(kc, scan_walk_kernel<T, 32, 4, OUT, REV>, grid, block, 0, s, w);
-        if (w.n <= 64) return launch_timed(kc, scan_walk_kernel<T, 64, 4, OUT, REV>, grid, block, 0, s, w);
-        return launch_timed(kc, scan_walk_kernel<T, 128, 4, OUT, REV>, grid, block, 0, s, w);
-    }
-    if (w.n <= 32) return launch_timed(kc, scan_walk_kernel<T, 32, 2, OUT, REV>, grid, block, 0, s, w);
-    if (w.n <= 64) return launch_timed(kc, scan_walk_kernel<T, 64, 2, OUT, REV>, grid, block, 0, s, w);
-    return launch_timed(kc, scan_walk_kernel<T, 128, 2, OUT, REV>, grid, block, 0, s, w);
+// Workgroups of a walk (0: more than a launch takes).
+inline unsigned walk_grid(const ScanWalk& w) {
+    const int64_t blocks = (w.samples * w.stretches * w.heads * w.slices + 7) / 8 * 8;
+    return blocks <= INT32_MAX ? (unsigned)blocks : 0u;
+}
+inline unsigned join_grid(const ScanWalk& w) { return (unsigned)((w.samples * w.heads * padded_dh(w.dh) * padded_n(w.n) + 255) / 256); }
+
+// With the memory of the stretches' states and exponents at ws; the memory behind them.
+inline char* walk_room(ScanWalk& w, char* ws) {
+    const size_t heads = (size_t)w.samples * w.heads * w.stretches, totals = (heads * sizeof(double) + 15) / 16 * 16;
+    w.stretch_totals = reinterpret_cast<double*>(ws);
+    w.stretch_states = reinterpret_cast<float*>(ws + totals);
+    return ws + totals + heads * padded_dh(w.dh) * padded_n(w.n) * sizeof(float);
+}
+// The walk of the stretches' own states.
+inline ScanWalk own_walk(ScanWalk w) {
+    w.own = true;
+    w.chunk_states = nullptr;
+    return w;
 }
 
-// A walk, in stretches where its plan has them.  ws: walk_stretch_bytes.
-template <typename T, bool OUT, bool REV> static hipError_t walk_stretches(ScanWalk w, void* ws, hipStream_t s) {
-    walk_plan(w);
-    if (w.stretches > 1) {
-        const size_t totals = (size_t)w.samples * w.heads * w.stretches * sizeof(double);
-        w.stretch_totals = static_cast<double*>(ws);
-        w.stretch_states = reinterpret_cast<float*>(static_cast<char*>(ws) + (totals + 15) / 16 * 16);
-        ScanWalk own = w;
-        own.own = true;
-        own.chunk_states = nullptr;
-        hipError_t e = walk_launch<T, false, REV>(own, s);
-        if (e != hipSuccess) return e;
-        const int NP = padded_n(w.n), whole = padded_dh(w.dh) * NP;
-        const int64_t numbers = w.samples * w.heads * whole;
-        if ((numbers + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
-        e = launch_timed(OUT ? kcAttnFwd : kcAttnBwd, scan_join_kernel<REV>, dim3((unsigned)((numbers + 255) / 256)), dim3(256), 0, s, w, NP, whole);
-        if (e != hipSuccess) return e;
-    }
-    return walk_launch<T, OUT, REV>(w, s);
-}
+#define TMPS_WALK(launch, w)                                         \
+    ((w).tiles == 4 ? ((w).n <= 32 ? launch(32, 4) : (w).n <= 64 ? launch(64, 4) : launch(128, 4)) \
+                    : ((w).n <= 32 ? launch(32, 2) : (w).n <= 64 ? launch(64, 2) : launch(128, 2)))
 
 }  // namespace tmps
