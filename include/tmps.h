@@ -354,7 +354,8 @@ int tmps_short_conv_backward(int dtype, int flags, int64_t samples, int64_t posi
  *   delta = log(1 + exp(dt + dt_bias)),   S <- exp(-delta exp(a_log)) S + delta x B',   y = S C + skip x
  * Rows of x: [x (heads * dh) | B (groups * n) | C (groups * n)]; of dt: heads; of y: heads * dh.  a_log, skip, dt_bias: [heads].  state (NULL: zeros) and state_out (NULL: not
  * wanted), float [samples, heads, dh, n]: before the first position and behind the last; state_out may be state.  A number of x, dt, B or C that is not finite reaches the results of its
- * own and later positions of its sample alone.  workspace: tmps_scan_workspace bytes (may be 0). */
+ * own and later positions of its sample alone.  For more than 8 positions a row of x has 16 bytes at least (and one of y, in the backward pass, of any number of them), and rows are at most
+ * 2^24 elements apart.  workspace: tmps_scan_workspace bytes (may be 0). */
 typedef struct {
     int32_t heads, dh, groups, n;
 } tmps_scan_desc;

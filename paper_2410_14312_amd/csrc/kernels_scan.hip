@@ -90,20 +90,18 @@ template <typename T> __global__ __launch_bounds__(256) void scan_steps_kernel(S
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-constexpr int kStepsMost = 8;   // positions that go one after the other
-
 size_t scan_workspace_bytes(const Scan& a) {
-    if (a.positions <= kStepsMost) return 0;
+    if (a.positions <= kScanSteps) return 0;
     return walk_stretch_bytes(a);
 }
 
 template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hipStream_t s) {
-    if (a.positions <= kStepsMost) {
+    if (a.positions <= kScanSteps) {
         const int64_t units = a.samples * a.heads;
         if (units > INT32_MAX) return hipErrorInvalidValue;
         return launch_timed(kcAttnFwd, scan_steps_kernel<T>, dim3((unsigned)units, (unsigned)((a.dh + 63) / 64)), dim3(256), 0, s, a);
     }
-    ScanWalk w = walk_of<T>(a);
+    ScanWalk w = walk_of(a);
     w.y = a.y; w.y_stride = a.y_stride;
     w.final_state = a.state_out;
     walk_plan(w);
@@ -111,14 +109,13 @@ template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hi
     if (!grid) return hipErrorInvalidValue;
     if (w.stretches > 1) {
         walk_room(w, static_cast<char*>(ws));
-        const ScanWalk own = own_walk(w);
-#define TMPS_OWN(NP, PT) launch_timed(kcAttnFwd, scan_walk_kernel<T, NP, PT, false, false>, dim3(grid), dim3(256), 0, s, own)
-        hipError_t e = TMPS_WALK(TMPS_OWN, own);
+#define TMPS_OWN(NP, PT) launch_timed(kcAttnFwd, scan_walk_kernel<T, NP, PT, kWalkOwn>, dim3(grid), dim3(256), 0, s, w)
+        hipError_t e = TMPS_WALK(TMPS_OWN, w);
         if (e != hipSuccess) return e;
         e = launch_timed(kcAttnFwd, scan_join_kernel, dim3(join_grid(w)), dim3(256), 0, s, w, padded_n(w.n), padded_dh(w.dh) * padded_n(w.n));
         if (e != hipSuccess) return e;
     }
-#define TMPS_OUT(NP, PT) launch_timed(kcAttnFwd, scan_walk_kernel<T, NP, PT, true, false>, dim3(grid), dim3(256), 0, s, w)
+#define TMPS_OUT(NP, PT) launch_timed(kcAttnFwd, scan_walk_kernel<T, NP, PT, kWalkResults>, dim3(grid), dim3(256), 0, s, w)
     return TMPS_WALK(TMPS_OUT, w);
 }
 

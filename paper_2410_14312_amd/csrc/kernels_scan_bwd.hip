@@ -62,15 +62,18 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
     const int in_group = f.heads / f.groups, first = part * a.each, last = min(first + a.each, in_group);   // heads of the group
     const int64_t b_at = (int64_t)f.heads * f.dh + (int64_t)group * f.n, c_at = b_at + (int64_t)f.groups * f.n;
     const int own = 16 * wave + col;   // this lane's column: a position
+    const int wide = (int)(f.heads * f.dh + 2 * f.groups * f.n), inner = f.heads * f.dh;
 
     {
         ChunkRows<T, NP, 256> r;
-        r.places_all(f.x_stride, f.n);
-        r.request_all((const T*)f.x + row0 * f.x_stride + b_at, f.x_stride, rows, f.n);
-        r.settle_all(rows, f.n);
+        const T* const base = (const T*)f.x + row0 * f.x_stride;
+        r.places_all(f.x_stride, (int)b_at, wide);
+        r.request_all(base, f.x_stride, rows, (int)b_at, wide);
+        r.settle_all(rows, f.n, (int)b_at, wide);
         r.template put<BP>(bs);
-        r.request_all((const T*)f.x + row0 * f.x_stride + c_at, f.x_stride, rows, f.n);
-        r.settle_all(rows, f.n);
+        r.places_all(f.x_stride, (int)c_at, wide);
+        r.request_all(base, f.x_stride, rows, (int)c_at, wide);
+        r.settle_all(rows, f.n, (int)c_at, wide);
         r.template put<BP>(cs);
     }
     __syncthreads();
@@ -94,10 +97,11 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
         for (int slice = 0; slice < a.slices; ++slice) {
             const int p0 = slice * 64, width = min(64, f.dh - p0);
             ChunkRows<T, PP, 256> rx, rd;
-            rx.places_all(f.x_stride, width);
-            rd.places_all(b.dy_stride, width);
-            rx.request_all((const T*)f.x + row0 * f.x_stride + (int64_t)head * f.dh + p0, f.x_stride, rows, width);
-            rd.request_all((const T*)b.dy + row0 * b.dy_stride + (int64_t)head * f.dh + p0, b.dy_stride, rows, width);
+            const int at = head * f.dh + p0;
+            rx.places_all(f.x_stride, at, wide);
+            rd.places_all(b.dy_stride, at, inner);
+            rx.request_all((const T*)f.x + row0 * f.x_stride, f.x_stride, rows, at, wide);
+            rd.request_all((const T*)b.dy + row0 * b.dy_stride, b.dy_stride, rows, at, inner);
             const int64_t of_state = (((sample * f.heads + head) * a.chunks + chunk) * a.slices + slice) * (int64_t)(PP * NP);
             float s4[kState][4], g4[kState][4];
 #pragma unroll
@@ -109,10 +113,11 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             __syncthreads();   // (what the head or slice before has left in LDS has been read)
             if (slice == 0 && (h - first) % kGradDecays == 0 && wave < kGradDecays && h + wave < last) {
                 const int mine = head + wave;
-                chunk_decays<true>(decays[wave], (const T*)f.dt + row0 * f.dt_stride + mine, f.dt_stride, rows, f.dt_bias[mine], exp((double)f.a_log[mine]) * kLog2eD, lane);
+                chunk_decays<true>(decays[wave], to_f32(((const T*)f.dt)[(row0 + min(lane, rows - 1)) * f.dt_stride + mine]), rows, f.dt_bias[mine],
+                                   exp((double)f.a_log[mine]) * kLog2eD, lane);
             }
-            rx.settle_all(rows, width);
-            rd.settle_all(rows, width);
+            rx.settle_all(rows, width, at, wide);
+            rd.settle_all(rows, width, at, inner);
             rx.template put<XP>(xs);
             rd.template put<XP>(dys);
             const auto put_state = [&](const float (&v)[kState][4]) {
@@ -318,14 +323,14 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
         }
     }
     if (own >= rows) return;
-    const int64_t wide = 2 * (int64_t)f.groups * f.n;
+    const int64_t of_shared = 2 * (int64_t)f.groups * f.n;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int n = 16 * nt + 4 * g;
         if (n >= f.n) continue;
         const float vb[4] = {db[nt][0], db[nt][1], db[nt][2], db[nt][3]}, vc[4] = {dc[nt][0], dc[nt][1], dc[nt][2], dc[nt][3]};
         if (a.shared) {
-            float* const to = a.shared + ((int64_t)part * f.samples * f.positions + row0 + own) * wide + (int64_t)group * f.n + n;
+            float* const to = a.shared + ((int64_t)part * f.samples * f.positions + row0 + own) * of_shared + (int64_t)group * f.n + n;
             put_four_any(to, vb, f.n - n);
             put_four_any(to + (int64_t)f.groups * f.n, vc, f.n - n);
         } else {
@@ -408,25 +413,24 @@ template <typename T> static hipError_t backward_type(const ScanBackward& b, voi
     a.before = before; a.behind = behind;
     a.sums = reinterpret_cast<float*>(at + room.walk + 2 * room.states);
     a.shared = a.parts > 1 ? reinterpret_cast<float*>(at + room.walk + 2 * room.states + room.sums) : nullptr;
-    ScanWalk w = walk_of<T>(b.f);
+    ScanWalk w = walk_of(b.f);
     w.chunk_states = before;
     walk_plan(w);
     ScanWalk back = w;
-    back.x = b.dy; back.x_stride = b.dy_stride; back.b = w.c;
+    back.x = b.dy; back.x_stride = b.dy_stride; back.x_wide = b.f.heads * b.f.dh; back.b_first = w.c_first;
     back.first_state = b.dstate; back.chunk_states = behind; back.final_state = b.dstate_in;
     const unsigned walks = walk_grid(w);
     if (!walks) return hipErrorInvalidValue;
     hipError_t e = hipSuccess;
     if (w.stretches > 1) {
         walk_room(back, walk_room(w, at));
-        const ScanWalk own = own_walk(w), own_back = own_walk(back);
-#define TMPS_OWNS(NP, PT) launch_timed(kcAttnBwd, scan_walks_kernel<T, NP, PT>, dim3(walks, 2), dim3(256), 0, s, own, own_back)
+#define TMPS_OWNS(NP, PT) launch_timed(kcAttnBwd, scan_walks_kernel<T, NP, PT, kWalkOwn>, dim3(walks, 2), dim3(256), 0, s, w, back)
         e = TMPS_WALK(TMPS_OWNS, w);
         if (e != hipSuccess) return e;
         e = launch_timed(kcAttnBwd, scan_joins_kernel, dim3(join_grid(w), 2), dim3(256), 0, s, w, back, padded_n(w.n), padded_dh(w.dh) * padded_n(w.n));
         if (e != hipSuccess) return e;
     }
-#define TMPS_WALKS(NP, PT) launch_timed(kcAttnBwd, scan_walks_kernel<T, NP, PT>, dim3(walks, 2), dim3(256), 0, s, w, back)
+#define TMPS_WALKS(NP, PT) launch_timed(kcAttnBwd, scan_walks_kernel<T, NP, PT, kWalkStates>, dim3(walks, 2), dim3(256), 0, s, w, back)
     e = TMPS_WALK(TMPS_WALKS, w);
     if (e != hipSuccess) return e;
     const Scan& f = b.f;

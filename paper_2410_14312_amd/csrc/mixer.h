@@ -46,6 +46,7 @@ size_t short_conv_part_elems(int64_t samples, int64_t positions, int channels, i
 //   delta = softplus(dt + dt_bias),  S_t = exp(-delta exp(a_log)) S_{t-1} + delta x_t B_t',  y_t = S_t C_t + skip x_t
 // over rows [x (heads dh) | B (groups n) | C (groups n)].  state, state_out: [samples, heads, dh, n] (null: zeros; not wanted; one may be the other).
 constexpr int kScanMaxState = 128;
+constexpr int kScanSteps = 8;   // up to so many positions go one after the other
 struct Scan {
     const void* x;
     int64_t x_stride;

@@ -130,6 +130,14 @@ static int check_scan(int dtype, const tmps_scan_desc* desc, int64_t samples, in
     return TMPS_OK;
 }
 
+// (rows are read 16 bytes at a time)
+static int check_room(int dtype, const Scan& s, bool backward) {
+    const int64_t least = 16 / (int64_t)act_bytes(dtype), inner = (int64_t)s.heads * s.dh;
+    if ((backward || s.positions > kScanSteps) && (backward ? inner : inner + 2 * (int64_t)s.groups * s.n) < least)
+        return fail(TMPS_EUNSUPPORTED, "rows of fewer than %d features", (int)least);
+    return TMPS_OK;
+}
+
 // (places in a chunk of rows are numbers of 32 bits)
 static int check_strides(int64_t rows, std::initializer_list<int64_t> strides) {
     for (int64_t s : strides)
@@ -158,7 +166,7 @@ extern "C" int tmps_scan_forward(int dtype, const tmps_scan_desc* desc, int64_t 
     Scan s = scan_of(desc, samples, positions);
     const int64_t rows = samples * positions, wide = (int64_t)s.heads * s.dh + 2 * (int64_t)s.groups * s.n, inner = (int64_t)s.heads * s.dh;
     if ((rc = check_rows("x", rows, wide, x_stride)) != TMPS_OK || (rc = check_rows("dt", rows, s.heads, dt_stride)) != TMPS_OK ||
-        (rc = check_rows("y", rows, inner, y_stride)) != TMPS_OK || (rc = check_strides(rows, {x_stride, dt_stride, y_stride})) != TMPS_OK)
+        (rc = check_rows("y", rows, inner, y_stride)) != TMPS_OK || (rc = check_strides(rows, {x_stride, dt_stride, y_stride})) != TMPS_OK || (rc = check_room(dtype, s, false)) != TMPS_OK)
         return rc;
     const size_t esz = act_bytes(dtype), heads = (size_t)s.heads * 4, states = (size_t)samples * inner * s.n * 4, need = scan_workspace_bytes(s);
     if (!whole(esz, {x, dt, y}) || !whole(4, {a_log, skip, dt_bias, state, state_out})) return fail(TMPS_ESHAPE, "a pointer is not on a whole element");
@@ -189,7 +197,7 @@ extern "C" int tmps_scan_backward(int dtype, const tmps_scan_desc* desc, int64_t
     const int64_t rows = samples * positions, wide = (int64_t)s.heads * s.dh + 2 * (int64_t)s.groups * s.n, inner = (int64_t)s.heads * s.dh;
     if ((rc = check_rows("x", rows, wide, x_stride)) != TMPS_OK || (rc = check_rows("dt", rows, s.heads, dt_stride)) != TMPS_OK ||
         (rc = check_rows("dy", rows, inner, dy_stride)) != TMPS_OK || (rc = check_rows("dx", rows, wide, dx_stride)) != TMPS_OK ||
-        (rc = check_rows("ddt", rows, s.heads, ddt_stride)) != TMPS_OK || (rc = check_strides(rows, {x_stride, dt_stride, dy_stride, dx_stride, ddt_stride})) != TMPS_OK)
+        (rc = check_rows("ddt", rows, s.heads, ddt_stride)) != TMPS_OK || (rc = check_strides(rows, {x_stride, dt_stride, dy_stride, dx_stride, ddt_stride})) != TMPS_OK || (rc = check_room(dtype, s, true)) != TMPS_OK)
         return rc;
     const size_t esz = act_bytes(dtype), heads = (size_t)s.heads * 4, states = (size_t)samples * inner * s.n * 4, need = scan_backward_workspace_bytes(dtype, s);
     if (!whole(esz, {dy, x, dt, dx, ddt}) || !whole(4, {dstate, a_log, skip, dt_bias, state, dparams, dstate_in})) return fail(TMPS_ESHAPE, "a pointer is not on a whole element");

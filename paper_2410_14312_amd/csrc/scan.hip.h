@@ -133,69 +133,54 @@ __device__ __forceinline__ void four_any(const float* p, float (&v)[4], int many
         for (int e = 0; e < 4; ++e) v[e] = e < many ? p[e] : 0.0f;
 }
 
-// N pieces of 16 bytes of a chunk's rows, at(i, row, column): piece i's row and first column.  The requests are loads without a branch (one in a branch would be waited for there), their
-// places in a whole chunk a number of 32 bits each that is formed once: where a row ends inside a piece, or before it, the piece begins as much earlier, and settle() moves what is its
-// own to its place and puts zeros behind it.
+// N pieces of 16 bytes of a chunk's rows, at(i, row, column): piece i's row and first column of those that are looked at, which begin `first` numbers into rows of `wide` (16 bytes at
+// least).  The requests are loads without a branch (one in a branch would be waited for there), their places in a whole chunk a number of 32 bits each that is formed once: where a row of
+// memory ends inside a piece, the piece begins as much earlier, and settle() moves what is its own to its place and puts zeros behind it.
 template <typename T, int N> struct Requests {
     static constexpr int V = kPiece<T>;
     uint4 u[N];
     uint32_t off[N];
-    static __device__ __forceinline__ uint32_t place(int r, int c, int64_t stride, int columns) { return (uint32_t)(r * (int)stride + (columns >= V ? min(c, columns - V) : 0)) * (uint32_t)sizeof(T); }
-    template <class At> __device__ __forceinline__ void places(int64_t stride, int columns, At&& at) {
+    static __device__ __forceinline__ uint32_t place(int r, int c, int stride, int first, int wide) { return (uint32_t)(r * stride + min(first + c, wide - V)) * (uint32_t)sizeof(T); }
+    template <class At> __device__ __forceinline__ void places(int stride, int first, int wide, At&& at) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             int r, c;
             at(i, r, c);
-            off[i] = place(r, c, stride, columns);
+            off[i] = place(r, c, stride, first, wide);
         }
     }
-    template <class At> __device__ __forceinline__ void request(const T* base, int64_t stride, int rows, int columns, At&& at) {
-        if (columns < V) {
+    // base: the chunk's first row of memory
+    template <class At> __device__ __forceinline__ void request(const T* base, int stride, int rows, int first, int wide, At&& at) {
+        uint32_t to[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = off[i];
+        if (rows < kScanChunk) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 int r, c;
                 at(i, r, c);
-                struct Values { T v[V]; } f;
-#pragma unroll
-                for (int e = 0; e < V; ++e) f.v[e] = base[min(r, rows - 1) * stride + min(e, columns - 1)];
-                u[i] = __builtin_bit_cast(uint4, f);
+                to[i] = place(min(r, rows - 1), c, stride, first, wide);
             }
-        } else if (rows < kScanChunk) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                int r, c;
-                at(i, r, c);
-                u[i] = load16_any(reinterpret_cast<const char*>(base) + place(min(r, rows - 1), c, stride, columns));
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) u[i] = load16_any(reinterpret_cast<const char*>(base) + off[i]);
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = load16_any(reinterpret_cast<const char*>(base) + to[i]);
     }
-    // rows: those from this one on are zeros.  W: columns that are looked at
-    template <class At> __device__ __forceinline__ void settle(int rows, int columns, int W, At&& at) {
-        if (rows == kScanChunk && columns == W) return;
-        if (columns % V == 0) {
+    // Zeros from row `rows` and column `columns` on.
+    template <class At> __device__ __forceinline__ void settle(int rows, int columns, int first, int wide, At&& at) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                int r, c;
-                at(i, r, c);
-                if (r >= rows || c >= columns) u[i] = make_uint4(0, 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                int r, c;
-                at(i, r, c);
+        for (int i = 0; i < N; ++i) {
+            int r, c;
+            at(i, r, c);
+            if (columns % V) {
                 uint64_t lo = u[i].x | (uint64_t)u[i].y << 32, hi = u[i].z | (uint64_t)u[i].w << 32;
-                const int early = columns >= V ? max(c + V - columns, 0) : 0, bits = early * (int)sizeof(T) * 8, keep = (columns - c) * (int)sizeof(T) * 8;
+                const int bits = max(first + c + V - wide, 0) * (int)sizeof(T) * 8, keep = (columns - c) * (int)sizeof(T) * 8;
                 if (bits >= 64) lo = hi >> (bits & 63), hi = 0;
                 else if (bits > 0) lo = lo >> bits | hi << (64 - bits), hi >>= bits;
-                if (r >= rows || keep <= 0) lo = hi = 0;
-                else if (columns < V && keep < 64) hi = 0, lo &= (uint64_t(1) << keep) - 1;
-                else if (columns < V && keep < 128) hi &= keep > 64 ? (uint64_t(1) << (keep - 64)) - 1 : 0;
+                if (keep < 64) hi = 0, lo &= keep > 0 ? (uint64_t(1) << keep) - 1 : 0;
+                else if (keep < 128) hi &= (uint64_t(1) << (keep - 64)) - 1;
                 u[i] = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
             }
+            if (r >= rows || c >= columns) u[i] = make_uint4(0, 0, 0, 0);
         }
     }
 };
@@ -210,9 +195,9 @@ template <typename T, int W, int THREADS> struct ChunkRows : Requests<T, kScanCh
         r = k / kEach;
         c = k % kEach * V;
     }
-    __device__ __forceinline__ void places_all(int64_t stride, int columns) { this->places(stride, columns, at); }
-    __device__ __forceinline__ void request_all(const T* base, int64_t stride, int rows, int columns) { this->request(base, stride, rows, columns, at); }
-    __device__ __forceinline__ void settle_all(int rows, int columns) { this->settle(rows, columns, W, at); }
+    __device__ __forceinline__ void places_all(int64_t stride, int first, int wide) { this->places((int)stride, first, wide, at); }
+    __device__ __forceinline__ void request_all(const T* base, int64_t stride, int rows, int first, int wide) { this->request(base, (int)stride, rows, first, wide, at); }
+    __device__ __forceinline__ void settle_all(int rows, int columns, int first, int wide) { this->settle(rows, columns, first, wide, at); }
     template <int PITCH> __device__ __forceinline__ void put(T* tile) const {
 #pragma unroll
         for (int i = 0; i < kMany; ++i) {
@@ -252,8 +237,9 @@ __device__ __forceinline__ float exp2_of(double e) {
     return __builtin_amdgcn_exp2f(hi) * fmaf(0.69314718f, fabsf(rest) < 1.0f ? rest : 0.0f, 1.0f);
 }
 
-template <bool SLOPE, typename T> __device__ __forceinline__ void chunk_decays(ChunkDecays& d, const T* dt, int64_t stride, int rows, float bias, double rate, int lane) {
-    const float u = to_f32(dt[min(lane, rows - 1) * stride]) + bias;
+// dt: the position's (any number behind the last row).
+template <bool SLOPE> __device__ __forceinline__ void chunk_decays(ChunkDecays& d, float dt, int rows, float bias, double rate, int lane) {
+    const float u = dt + bias;
     const float delta = lane >= rows ? 0.0f : u != u ? u : softplus(u);
     double sum = -(double)delta * rate;
 #pragma unroll

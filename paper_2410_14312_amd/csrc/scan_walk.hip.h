@@ -1,6 +1,7 @@
 // The walk over the chunks of a head's positions with its state in the accumulators: forward with the results y, forward or backward for the states of the chunks alone.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "scan.hip.h"
@@ -13,8 +14,9 @@ inline int padded_dh(int dh) { return dh <= 32 ? 32 : (dh + 63) / 64 * 64; }
 
 // The walk's operands: "x" and "b" are x and B going forward, dy and C going backward, where the state is the gradient of the state behind a chunk.
 struct ScanWalk {
-    const void *x, *b, *c, *dt;
+    const void *x, *b, *dt;         // rows of x, of B and C, of dt
     int64_t x_stride, bc_stride, dt_stride;
+    int x_wide, bc_wide, b_first, c_first;   // numbers of a row, those before B and before C
     const float *a_log, *skip, *dt_bias;
     const float* first_state;    // before the first chunk of the walk: [samples, heads, dh, n] (null: zeros)
     void* y;
@@ -24,19 +26,20 @@ struct ScanWalk {
     int64_t samples, positions;
     int heads, dh, groups, n;
     int chunks, stretches, each, slices, tiles;   // chunks of a sample, stretches of them and the chunks of one, slices of a head's features and their tiles of 16
-    float* stretch_states;       // [samples, heads, stretches, padded dh, NP]: before each stretch, or with `own` left by each
+    float* stretch_states;       // [samples, heads, stretches, padded dh, NP]: left by each, then before each
     double* stretch_totals;
-    bool own;                    // each stretch from nothing, for its own state and exponent alone
 };
 
-template <typename T> ScanWalk walk_of(const Scan& a) {
+inline ScanWalk walk_of(const Scan& a) {
     ScanWalk w;
-    w.x = a.x; w.b = (const T*)a.x + (int64_t)a.heads * a.dh; w.c = (const T*)w.b + (int64_t)a.groups * a.n;
+    w.x = w.b = a.x;
     w.dt = a.dt; w.x_stride = w.bc_stride = a.x_stride; w.dt_stride = a.dt_stride;
+    w.b_first = a.heads * a.dh; w.c_first = w.b_first + a.groups * a.n;
+    w.x_wide = w.bc_wide = w.c_first + a.groups * a.n;
     w.a_log = a.a_log; w.skip = a.skip; w.dt_bias = a.dt_bias; w.first_state = a.state;
     w.y = nullptr; w.y_stride = 0; w.final_state = nullptr; w.chunk_states = nullptr;
     w.samples = a.samples; w.positions = a.positions; w.heads = a.heads; w.dh = a.dh; w.groups = a.groups; w.n = a.n;
-    w.stretch_states = nullptr; w.stretch_totals = nullptr; w.own = false;
+    w.stretch_states = nullptr; w.stretch_totals = nullptr;
     return w;
 }
 
@@ -52,8 +55,12 @@ template <typename T, int NP, int PT, bool OUT> struct WalkTiles {
     int odd[2];
 };
 
+// What a walk leaves: results (and the state behind the last chunk), the states before its chunks, or each stretch's own state and exponent, from nothing.
+enum { kWalkResults, kWalkStates, kWalkOwn };
+
 // What one workgroup does: stretch, head, slice and sample number `unit`.
-template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinline__ void scan_walk(const ScanWalk& a, int64_t unit, WalkTiles<T, NP, PT, OUT>& tiles) {
+template <typename T, int NP, int PT, int LEAVES, bool REV> __device__ __forceinline__ void scan_walk(const ScanWalk& a, int64_t unit, WalkTiles<T, NP, PT, LEAVES == kWalkResults>& tiles) {
+    constexpr bool OUT = LEAVES == kWalkResults;
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, NT = NP / 16, TW = NT * PT / 4, NK = NP / 32;
     constexpr int RT = kResultTerms<T>, ST = kStateTerms<T>;
     T *const xs = tiles.xs, *const bs = tiles.bs, *const ss = tiles.ss;
@@ -67,16 +74,15 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
     const int64_t sample = unit / a.stretches;
     const int group = head / (a.heads / a.groups);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-    const int p0 = slice * PP, width = max(min(PP, a.dh - p0), 0);   // (a slice behind the last feature reads the first one's and has zeros)
-    const int read_p0 = width ? p0 : 0, read_width = width ? width : min(PP, a.dh);
+    const int p0 = slice * PP, width = max(min(PP, a.dh - p0), 0);   // (a slice behind the last feature has zeros)
     const double rate = exp((double)a.a_log[head]) * kLog2eD;
     const float bias = a.dt_bias[head];
 
     const int64_t rows0 = sample * a.positions;
-    const T* const xg = (const T*)a.x + rows0 * a.x_stride + (int64_t)head * a.dh + read_p0;
-    const T* const bg = (const T*)a.b + rows0 * a.bc_stride + (int64_t)group * a.n;
-    const T* const cg = (const T*)a.c + rows0 * a.bc_stride + (int64_t)group * a.n;
+    const T* const xg = (const T*)a.x + rows0 * a.x_stride;
+    const T* const bg = (const T*)a.b + rows0 * a.bc_stride;
     const T* const dtg = (const T*)a.dt + rows0 * a.dt_stride + head;
+    const int x_first = head * a.dh + min(p0, a.dh - 1), b_first = a.b_first + group * a.n, c_first = a.c_first + group * a.n;
 
     // this wave's tiles of the state: 16 features p, n tiles a few apart; rows n, columns p
     const int pt = wave % PT, nt0 = wave / PT;
@@ -90,7 +96,7 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
 #pragma unroll
     for (int k = 0; k < TW; ++k) {
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.own) {
+        if (LEAVES == kWalkOwn) {
         } else if (a.stretches > 1) {
             four(a.stretch_states + of_stretch + n_of(k), v);
         } else if (a.first_state && p < width && n_of(k) < a.n) {
@@ -102,44 +108,53 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
     const int first = stretch * a.each, many = min(a.each, a.chunks - first);
     const auto chunk_of = [&](int i) { return REV ? first + many - 1 - i : first + i; };
     const auto rows_of = [&](int chunk) { return (int)min<int64_t>(kScanChunk, a.positions - (int64_t)chunk * kScanChunk); };
+    constexpr int kC = (int)sizeof(T) / 2;   // pieces of eight numbers
     ChunkRows<T, PP, 256> xr;
     ChunkRows<T, NP, 256> br;
-    constexpr int kC = (int)sizeof(T) / 2;   // pieces of eight numbers
     Requests<T, OUT ? NK * kC : 1> cr;
-    xr.places_all(a.x_stride, read_width);
-    br.places_all(a.bc_stride, a.n);
+    float dt = 0.0f;
     const auto of_c = [&](int k, int& r, int& c) {
         r = 16 * wave + col;
         c = 32 * (k / kC) + 8 * g + k % kC * V;
     };
-    if constexpr (OUT) cr.places(a.bc_stride, a.n, of_c);
-    const auto request = [&](int chunk) {
-        const int64_t t0 = (int64_t)chunk * kScanChunk;
-        const int rows = rows_of(chunk);
-        xr.request_all(xg + t0 * a.x_stride, a.x_stride, rows, read_width);
-        br.request_all(bg + t0 * a.bc_stride, a.bc_stride, rows, a.n);
-        if constexpr (OUT) cr.request(cg + t0 * a.bc_stride, a.bc_stride, rows, a.n, of_c);
-    };
-    double total = 0.0;
-    if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-    request(chunk_of(0));
-    for (int i = 0; i < many; ++i) {
-        const int chunk = chunk_of(i), rows = rows_of(chunk);
-        const int64_t t0 = (int64_t)chunk * kScanChunk;
-        __syncthreads();   // (the chunk before has been read)
-        if ((i & 3) == 0 && i + wave < many) {
-            const int mine = chunk_of(i + wave);
-            chunk_decays<false>(decays[wave], dtg + (int64_t)mine * kScanChunk * a.dt_stride, a.dt_stride, rows_of(mine), bias, rate, lane);
+    xr.places_all(a.x_stride, x_first, a.x_wide);
+    br.places_all(a.bc_stride, b_first, a.bc_wide);
+    if constexpr (OUT) cr.places((int)a.bc_stride, c_first, a.bc_wide, of_c);
+    // a chunk's numbers on their way; with every fourth chunk the steps of the next four, one of which a wave has
+    const auto request = [&](int i) {
+        if ((i & 3) == 0) {
+            const int mine = chunk_of(min(i + wave, many - 1));
+            dt = to_f32(dtg[((int64_t)mine * kScanChunk + min(lane, rows_of(mine) - 1)) * a.dt_stride]);
         }
-        xr.settle_all(rows, width);
-        br.settle_all(rows, a.n);
+        const int chunk = chunk_of(min(i, many - 1)), rows = rows_of(chunk);
+        const int64_t t0 = (int64_t)chunk * kScanChunk;
+        xr.request_all(xg + t0 * a.x_stride, a.x_stride, rows, x_first, a.x_wide);
+        br.request_all(bg + t0 * a.bc_stride, a.bc_stride, rows, b_first, a.bc_wide);
+        if constexpr (OUT) cr.request(bg + t0 * a.bc_stride, (int)a.bc_stride, rows, c_first, a.bc_wide, of_c);
+    };
+    const bool plain = width == PP && a.n == NP;   // (whole chunks then have no zeros to be put in)
+    const auto put = [&](int i) {
+        const int rows = rows_of(chunk_of(min(i, many - 1)));
+        if (!plain || rows < kScanChunk) {
+            xr.settle_all(rows, width, x_first, a.x_wide);
+            br.settle_all(rows, a.n, b_first, a.bc_wide);
+            if constexpr (OUT) cr.settle(rows, a.n, c_first, a.bc_wide, of_c);
+        }
         xr.template put<XP>(xs);
         br.template put<BP>(bs);
-        Oct<T> cf[OUT ? NK : 1];
         if constexpr (OUT) {
             if (xr.odd()) odd[i & 1] = 1;
-            if (threadIdx.x == 0) odd[(i + 1) & 1] = 0;   // (last read before the barrier above)
-            cr.settle(rows, a.n, NP, of_c);
+        }
+        if ((i & 3) == 0) chunk_decays<false>(decays[wave], dt, i + wave < many ? rows_of(chunk_of(i + wave)) : 0, bias, rate, lane);
+    };
+    double total = 0.0;
+
+    const auto step = [&](auto whole_chunk, int i) {
+        constexpr bool FULL = decltype(whole_chunk)::value;
+        const int chunk = chunk_of(i), rows = FULL ? kScanChunk : rows_of(chunk);
+        const int64_t t0 = (int64_t)chunk * kScanChunk;
+        Oct<T> cf[OUT ? NK : 1];
+        if constexpr (OUT) {
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
                 struct Eight { uint4 u[kC]; } e;
@@ -162,9 +177,8 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
             }
         }
         __syncthreads();
-        if (i + 1 < many) request(chunk_of(i + 1));
-        const ChunkDecays& d = decays[i & 3];
-        if (!OUT && a.chunk_states) {
+        if (OUT && threadIdx.x == 0) odd[(i + 1) & 1] = 0;   // (last read before the barrier that ended the step before)
+        if constexpr (LEAVES == kWalkStates) {
             float* const to = a.chunk_states + ((sample * a.heads + head) * a.chunks + chunk) * whole + in_whole;
 #pragma unroll
             for (int k = 0; k < TW; ++k) {
@@ -172,6 +186,9 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
                 put_four(to + n_of(k), v);
             }
         }
+        request(i + 1);
+        __builtin_amdgcn_sched_barrier(0);   // (they are under way before what the step computes, or there would be nothing to hide them behind)
+        const ChunkDecays& d = decays[i & 3];
         if constexpr (OUT) {
             const int t = 16 * wave + col;
             const float sum_t = d.sum[t], rest_t = d.rest[t];
@@ -204,33 +221,36 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
             // rows p, column t: what the state before the chunk gives, then the chunk's own
             f32x4_t y[PT];
 #pragma unroll
-            for (int j = 0; j < PT; ++j) {
-                y[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < PT; ++j) y[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int h = RT - 1; h >= 0; --h)
+            for (int h = RT - 1; h >= 0; --h)
 #pragma unroll
-                    for (int k = 0; k < NK; ++k) y[j] = mma(along<false>(ss + h * PP * BP + (16 * j + col) * BP, 32 * k, lane), cf[k], y[j]);
-                y[j] *= d.from[t];
-            }
+                for (int k = 0; k < NK; ++k)
+#pragma unroll
+                    for (int j = 0; j < PT; ++j) y[j] = mma(along<false>(ss + h * PP * BP + (16 * j + col) * BP, 32 * k, lane), cf[k], y[j]);
+#pragma unroll
+            for (int j = 0; j < PT; ++j) y[j] *= d.from[t];
             // (numbers of x that are not finite would reach every position in products with 0: they are taken out, and put in by themselves where they belong)
-            const bool some_odd = odd[i & 1];
+            const bool some_odd = __builtin_amdgcn_readfirstlane(odd[i & 1]);
 #pragma unroll
             for (int pair = 0; pair < 2; ++pair) {
                 if (2 * pair > wave) continue;
-                Oct<T> mf[RT];
+                Oct<T> mf[RT], xf[PT];
+#pragma unroll
+                for (int j = 0; j < PT; ++j) xf[j] = across<true>(xs, XP, 32 * pair, 16 * j, lane);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) terms_of(m[2 * pair + e / 4][e % 4], e, mf);
+                if (some_odd) {
 #pragma unroll
-                for (int j = 0; j < PT; ++j) {
-                    Oct<T> xf = across<true>(xs, XP, 32 * pair, 16 * j, lane);
-                    if (some_odd) {
+                    for (int j = 0; j < PT; ++j)
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            if (!(fabsf(xf.get(e)) < __builtin_inff())) xf.set(e, 0.0f);
-                    }
-#pragma unroll
-                    for (int h = RT - 1; h >= 0; --h) y[j] = mma(xf, mf[h], y[j]);
+                            if (!(fabsf(xf[j].get(e)) < __builtin_inff())) xf[j].set(e, 0.0f);
                 }
+#pragma unroll
+                for (int h = RT - 1; h >= 0; --h)
+#pragma unroll
+                    for (int j = 0; j < PT; ++j) y[j] = mma(xf[j], mf[h], y[j]);
             }
             if (some_odd) {
 #pragma clang loop unroll(disable)
@@ -262,17 +282,16 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
                             if (!(fabsf(x[j][e]) < __builtin_inff())) y[j][e] = fmaf(by, x[j][e], y[j][e]);
                 }
             }
-            if (t < rows) {
-                T* const row = (T*)a.y + (rows0 + t0 + t) * a.y_stride + (int64_t)head * a.dh + p0;
-                const float skip = a.skip[head];
+            T* const row = (T*)a.y + (rows0 + t0 + t) * a.y_stride + (int64_t)head * a.dh + p0;
+            const float skip = a.skip[head];
 #pragma unroll
-                for (int j = 0; j < PT; ++j) {
-                    float x[4], v[4];
-                    four(xs + t * XP + 16 * j + 4 * g, x);
+            for (int j = 0; j < PT; ++j) {
+                float x[4], v[4];
+                four(xs + t * XP + 16 * j + 4 * g, x);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = fmaf(skip, x[e], y[j][e]);
-                    put_four_of(row + 16 * j + 4 * g, v, width - 16 * j - 4 * g, width % 4 == 0);
-                }
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(skip, x[e], y[j][e]);
+                if constexpr (FULL) put_four_any(row + 16 * j + 4 * g, v, 4);
+                else if (t < rows) put_four_any(row + 16 * j + 4 * g, v, width - 16 * j - 4 * g);
             }
         }
         // the state behind the chunk
@@ -285,20 +304,34 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
             for (int e = 0; e < 8; ++e) terms_of(x.get(e) * weights[e], e, xw[k]);
         }
 #pragma unroll
-        for (int k = 0; k < TW; ++k) {
-            state[k] *= d.end;
-            const int nt = nt0 + k * NSTEP;
+        for (int k = 0; k < TW; ++k) state[k] *= d.end;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const Oct<T> b = across<false>(bs, BP, 32 * h, 16 * nt, lane);
+        for (int h = 0; h < 2; ++h) {
+            Oct<T> b[TW];
 #pragma unroll
-                for (int e = ST - 1; e >= 0; --e) state[k] = mma(b, xw[h][e], state[k]);
-            }
+            for (int k = 0; k < TW; ++k) b[k] = across<false>(bs, BP, 32 * h, 16 * (nt0 + k * NSTEP), lane);
+#pragma unroll
+            for (int e = ST - 1; e >= 0; --e)
+#pragma unroll
+                for (int k = 0; k < TW; ++k) state[k] = mma(b[k], xw[h][e], state[k]);
         }
         total += d.total;
-    }
-    if (a.own && threadIdx.x == 0 && slice == 0) a.stretch_totals[(sample * a.heads + head) * a.stretches + stretch] = total;
-    if (a.own) {
+        __syncthreads();   // (the chunk has been read)
+        put(i + 1);
+    };
+    if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+    request(0);
+    __syncthreads();
+    put(0);
+    // (whole chunks in a loop of their own, where the number of memory's operations between a request and its use is known: the results' writing is not waited for)
+    int i = 0;
+    const auto whole_chunk = [&](int k) { return plain && rows_of(chunk_of(k)) == kScanChunk; };
+    if (REV && !whole_chunk(0)) step(std::false_type{}, i++);
+    while (i < many && whole_chunk(i)) step(std::true_type{}, i++);
+    while (i < many) step(std::false_type{}, i++);
+
+    if (LEAVES == kWalkOwn) {
+        if (threadIdx.x == 0 && slice == 0) a.stretch_totals[(sample * a.heads + head) * a.stretches + stretch] = total;
 #pragma unroll
         for (int k = 0; k < TW; ++k) {
             const float v[4] = {state[k][0], state[k][1], state[k][2], state[k][3]};
@@ -313,19 +346,19 @@ template <typename T, int NP, int PT, bool OUT, bool REV> __device__ __forceinli
     }
 }
 
-template <typename T, int NP, int PT, bool OUT, bool REV> __global__ __launch_bounds__(256, 2) void scan_walk_kernel(ScanWalk a) {
-    __shared__ WalkTiles<T, NP, PT, OUT> tiles;
+template <typename T, int NP, int PT, int LEAVES> __global__ __launch_bounds__(256, 2) void scan_walk_kernel(ScanWalk a) {
+    __shared__ WalkTiles<T, NP, PT, LEAVES == kWalkResults> tiles;
     const int64_t unit = xcd_order(blockIdx.x, gridDim.x);
-    if (unit < a.samples * a.stretches * a.heads * a.slices) scan_walk<T, NP, PT, OUT, REV>(a, unit, tiles);
+    if (unit < a.samples * a.stretches * a.heads * a.slices) scan_walk<T, NP, PT, LEAVES, false>(a, unit, tiles);
 }
 
 // The two walks of a backward pass, for the states alone, side by side: `back` goes backward.
-template <typename T, int NP, int PT> __global__ __launch_bounds__(256, 2) void scan_walks_kernel(ScanWalk ahead, ScanWalk back) {
+template <typename T, int NP, int PT, int LEAVES> __global__ __launch_bounds__(256, 2) void scan_walks_kernel(ScanWalk ahead, ScanWalk back) {
     __shared__ WalkTiles<T, NP, PT, false> tiles;
     const int64_t unit = xcd_order(blockIdx.x, gridDim.x);
     if (unit >= ahead.samples * ahead.stretches * ahead.heads * ahead.slices) return;
-    if (blockIdx.y == 0) scan_walk<T, NP, PT, false, false>(ahead, unit, tiles);
-    else scan_walk<T, NP, PT, false, true>(back, unit, tiles);
+    if (blockIdx.y == 0) scan_walk<T, NP, PT, LEAVES, false>(ahead, unit, tiles);
+    else scan_walk<T, NP, PT, LEAVES, true>(back, unit, tiles);
 }
 
 // The stretches' own states become those before them: a thread to a number of a state.
@@ -386,13 +419,6 @@ inline char* walk_room(ScanWalk& w, char* ws) {
     w.stretch_states = reinterpret_cast<float*>(ws + totals);
     return ws + totals + heads * padded_dh(w.dh) * padded_n(w.n) * sizeof(float);
 }
-// The walk of the stretches' own states.
-inline ScanWalk own_walk(ScanWalk w) {
-    w.own = true;
-    w.chunk_states = nullptr;
-    return w;
-}
-
 #define TMPS_WALK(launch, w)                                         \
     ((w).tiles == 4 ? ((w).n <= 32 ? launch(32, 4) : (w).n <= 64 ? launch(64, 4) : launch(128, 4)) \
                     : ((w).n <= 32 ? launch(32, 2) : (w).n <= 64 ? launch(64, 2) : launch(128, 2)))
