@@ -50,6 +50,9 @@ class Array(C.Structure):
     _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
+_ARRAY = np.dtype({"names": ["data", "out", "n", "dtype"], "formats": ["u8", "u8", "i8", "i4"], "itemsize": C.sizeof(Array)})   # the same for numpy
+
+
 EXPORTS = {
     "tmps_stage_bytes": (C.c_int, [C.POINTER(LayerDesc), C.c_int, C.POINTER(StageCfg), C.POINTER(C.c_size_t),
                                    C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
@@ -708,11 +711,28 @@ def clip_gradients(grads, limit, out=None, stream=None):
     to = grads if out is None else list(out)
     if len(to) != len(grads):
         raise ValueError("out: %d tensors are wanted, not %d" % (len(grads), len(to)))
-    norm_alone = out is None and limit == float("inf")
-    arrays = (Array * len(grads))()
-    for a, g, o in zip(arrays, grads, to):
-        a.data, a.n, a.dtype = _operand("grads", g, g.shape, g.dtype, dev), g.numel(), _dtype_code(g)
-        a.out = None if norm_alone else a.data if o is g else _operand("out", o, g.shape, g.dtype, dev)
+    if dev.type != "cuda":
+        raise ValueError("tensors on a GPU are wanted, not on %s" % dev)
+    # (a few attributes of each of hundreds of tensors: they are what such a call costs the host)
+    codes, index = {torch.float32: TMPS_F32, torch.bfloat16: TMPS_BF16_F32MASTER}, dev.index
+    record = np.empty(len(grads), dtype=_ARRAY)
+    kinds = [codes.get(g.dtype, -1) for g in grads]
+    if -1 in kinds:
+        _dtype_code(grads[kinds.index(-1)])
+    for g in grads:
+        if g.get_device() != index or not g.is_contiguous() or g.requires_grad:
+            _operand("grads", g, g.shape, g.dtype, dev)
+    record["data"] = at = [g.data_ptr() for g in grads]
+    record["n"] = [g.numel() for g in grads]
+    record["dtype"] = kinds
+    if out is None:
+        record["out"] = 0 if limit == float("inf") else at
+    else:
+        for g, o in zip(grads, to):
+            if o.dtype is not g.dtype or o.get_device() != index or not o.is_contiguous() or o.requires_grad or o.shape != g.shape:
+                _operand("out", o, g.shape, g.dtype, dev)
+        record["out"] = [o.data_ptr() for o in to]
+    arrays = C.cast(record.ctypes.data, C.POINTER(Array))
     norm = torch.empty((), dtype=torch.float32, device=dev)
     need = load_library().tmps_clip_workspace(arrays, len(grads))
     ws = _workspace(need, dev)

@@ -1,5 +1,6 @@
 // The norm of many arrays together, and the arrays scaled to at most a given norm.  Squares are added in 64 bits (no square of a float overflows there, and the sum of any number of
-// them keeps 2^-50 of itself), in a fixed order: of a thread, a workgroup, all workgroups.
+// them keeps 2^-50 of itself), in a fixed order: of a thread, a workgroup, all workgroups.  Bound by memory: all arrays are read for the norm and again for the scaling, which begins with
+// what was read last, and is still in the last cache.
 #include "launch.h"
 #include "mixer.h"
 #include "pieces.hip.h"
@@ -8,17 +9,26 @@ namespace tmps {
 
 // Arrays of a launch: as many as fit the 4 KiB that a kernel takes for arguments.
 constexpr int kClipArrays = 120;
-constexpr int kClipBlock = 16384;   // elements of a workgroup
+// Elements of a workgroup: so many that some three thousand workgroups have them all, each of which then adds up all workgroups' sums for itself (a launch less: 5 us), and no fewer than
+// gives a thread four pieces.
+constexpr int kClipLeast = 8192, kClipMost = 1 << 20, kClipWanted = 3072, kClipOwnSum = 6144;
 struct ClipTable {
     const void* in[kClipArrays];
     void* out[kClipArrays];
     int64_t n[kClipArrays];
     uint32_t first[kClipArrays + 1];   // the first workgroup of each, bit 31: bf16
-    int count;
+    int count, block;                  // arrays, elements of a workgroup
 };
-static_assert(sizeof(ClipTable) + 32 <= 4096, "a kernel's arguments");
+static_assert(sizeof(ClipTable) + 64 <= 4096, "a kernel's arguments");
 
-int64_t clip_blocks(int64_t n) { return (n + kClipBlock - 1) / kClipBlock; }
+static int64_t blocks_of(int64_t n, int block) { return (n + block - 1) / block; }
+static int clip_block(const ClipArray* list, int n) {
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i) all += list[i].n;
+    int block = kClipLeast;
+    while (block < kClipMost && all > (int64_t)block * kClipWanted) block *= 2;
+    return block;
+}
 
 __device__ __forceinline__ int clip_find(const ClipTable& t, uint32_t block) {
     int lo = 0, hi = t.count;   // first[lo] <= block < first[hi]
@@ -30,41 +40,53 @@ __device__ __forceinline__ int clip_find(const ClipTable& t, uint32_t block) {
     return lo;
 }
 
-// f(values, how many) over a workgroup's elements in pieces of 16 bytes from `from` on
+// f(values, the first one's place, how many) over a workgroup's elements in pieces of 16 bytes from `from` on, eight of a thread's under way at a time
 template <typename T, class F> __device__ __forceinline__ void clip_pieces(const T* from, int n, F&& f) {
-    constexpr int V = kPiece<T>;
-    constexpr int N = kClipBlock / (256 * V);
-#pragma unroll 4
-    for (int i = 0; i < N; ++i) {
-        const int at = (i * 256 + (int)threadIdx.x) * V;
-        if (at + V <= n) {
-            float v[V];
-            unpack(load16_any(from + at), v);
-            f(v, at, V);
-        } else if (at < n) {
-            float v[V];
+    constexpr int V = kPiece<T>, U = 8;
+    int at = (int)threadIdx.x * V;
+    for (; at + (U - 1) * 256 * V + V <= n; at += U * 256 * V) {
+        uint4 u[U];
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = at + e < n ? to_f32(from[at + e]) : 0.0f;
-            f(v, at, n - at);
+        for (int k = 0; k < U; ++k) u[k] = load16_any(from + at + k * 256 * V);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            float v[V];
+            unpack(u[k], v);
+            f(v, at + k * 256 * V, V);
         }
+    }
+    for (; at < n; at += 256 * V) {
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = at + e < n ? to_f32(from[at + e]) : 0.0f;
+        f(v, at, min(V, n - at));
     }
 }
 
+// The same in every thread.
 __device__ __forceinline__ double clip_block_sum(double v) {
-    __shared__ double red[256];
-    red[threadIdx.x] = v;
+    __shared__ double red[4];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int d = 128; d > 0; d >>= 1) {
-        if ((int)threadIdx.x < d) red[threadIdx.x] += red[threadIdx.x + d];
-        __syncthreads();
-    }
-    return red[0];
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// The norm and the factor of all workgroups' sums.
+__device__ __forceinline__ double clip_norm(const double* part, int64_t n, float limit, float& scale) {
+    double sum = 0.0;
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[i];
+    const double r = sqrt(clip_block_sum(sum));
+    scale = r > (double)limit && r < __builtin_inf() ? (float)((double)limit / r) : 1.0f;
+    return r;
 }
 
 __global__ __launch_bounds__(256) void clip_squares_kernel(ClipTable t, double* part) {
     const int a = clip_find(t, blockIdx.x);
-    const int64_t begin = (int64_t)(blockIdx.x - (t.first[a] & 0x7fffffffu)) * kClipBlock;
-    const int n = (int)min<int64_t>(kClipBlock, t.n[a] - begin);
+    const int64_t begin = (int64_t)(blockIdx.x - (t.first[a] & 0x7fffffffu)) * t.block;
+    const int n = (int)min<int64_t>(t.block, t.n[a] - begin);
     double sum = 0.0;
     auto add = [&](const auto& v, int, int) {
 #pragma unroll
@@ -77,22 +99,28 @@ __global__ __launch_bounds__(256) void clip_squares_kernel(ClipTable t, double* 
 }
 
 __global__ __launch_bounds__(256) void clip_norm_kernel(const double* part, int64_t n, float limit, float* norm, float* scale) {
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[i];
-    sum = clip_block_sum(sum);
+    float by;
+    const double r = clip_norm(part, n, limit, by);
     if (threadIdx.x == 0) {
-        const double r = sqrt(sum);
         *norm = (float)r;
-        *scale = r > (double)limit && r < __builtin_inf() ? (float)((double)limit / r) : 1.0f;
+        *scale = by;
     }
 }
 
-__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const float* scale) {
-    const int a = clip_find(t, blockIdx.x);
-    const float by = *scale;
+// scale: the factor, or null where each workgroup forms it from the `sums` of all.  Workgroups come in the opposite order of the first pass's.
+__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const float* scale, const double* part, int64_t sums, float limit, float* norm) {
+    const uint32_t block = gridDim.x - 1 - blockIdx.x;
+    const int a = clip_find(t, block);
+    float by;
+    if (scale) {
+        by = *scale;
+    } else {
+        const double r = clip_norm(part, sums, limit, by);
+        if (norm && block == 0 && threadIdx.x == 0) *norm = (float)r;
+    }
     if (by == 1.0f && t.in[a] == t.out[a]) return;
-    const int64_t begin = (int64_t)(blockIdx.x - (t.first[a] & 0x7fffffffu)) * kClipBlock;
-    const int n = (int)min<int64_t>(kClipBlock, t.n[a] - begin);
+    const int64_t begin = (int64_t)(block - (t.first[a] & 0x7fffffffu)) * t.block;
+    const int n = (int)min<int64_t>(t.block, t.n[a] - begin);
     auto scaled = [&](auto* to) {
         return [=](auto& v, int at, int m) {
             constexpr int V = sizeof(v) / sizeof(v[0]);
@@ -111,45 +139,57 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const floa
     else clip_pieces((const float*)t.in[a] + begin, n, scaled((float*)t.out[a] + begin));
 }
 
-// f(table, its workgroups, the workgroups before it) for the arrays in launches
-template <class F> static hipError_t clip_tables(const ClipArray* list, int n, F&& f) {
-    int64_t before = 0;
-    for (int i = 0; i < n;) {
-        ClipTable t;
-        t.count = 0;
-        int64_t blocks = 0;
-        for (; i < n && t.count < kClipArrays && (t.count == 0 || blocks + clip_blocks(list[i].n) < (1 << 30)); ++i) {
-            if (list[i].n <= 0) continue;
-            t.in[t.count] = list[i].in; t.out[t.count] = list[i].out; t.n[t.count] = list[i].n;
-            t.first[t.count] = (uint32_t)blocks | (list[i].dtype == kBF16 ? 0x80000000u : 0u);
-            blocks += clip_blocks(list[i].n);
-            ++t.count;
-        }
-        if (!t.count) break;
-        t.first[t.count] = (uint32_t)blocks;
-        const hipError_t e = f(t, blocks, before);
-        if (e != hipSuccess) return e;
-        before += blocks;
+// The arrays from `i` on that one launch takes; returns its workgroups.
+static int64_t clip_table(ClipTable& t, const ClipArray* list, int n, int block, int& i) {
+    int64_t blocks = 0;
+    t.count = 0;
+    t.block = block;
+    for (; i < n && t.count < kClipArrays && (t.count == 0 || blocks + blocks_of(list[i].n, block) < (1 << 30)); ++i) {
+        if (list[i].n <= 0) continue;
+        t.in[t.count] = list[i].in; t.out[t.count] = list[i].out; t.n[t.count] = list[i].n;
+        t.first[t.count] = (uint32_t)blocks | (list[i].dtype == kBF16 ? 0x80000000u : 0u);
+        blocks += blocks_of(list[i].n, block);
+        ++t.count;
     }
-    return hipSuccess;
+    t.first[t.count] = (uint32_t)blocks;
+    return blocks;
 }
 
-size_t clip_workspace_bytes(int64_t blocks) { return (size_t)(blocks + 1) * sizeof(double); }
+size_t clip_workspace_bytes(const ClipArray* list, int n) {
+    const int block = clip_block(list, n);
+    int64_t blocks = 0;
+    for (int i = 0; i < n; ++i) blocks += list[i].n > 0 ? blocks_of(list[i].n, block) : 0;
+    return (size_t)(blocks + 1) * sizeof(double);
+}
 
 hipError_t clip_gradients(const ClipArray* list, int n, float limit, float* norm, void* ws, hipStream_t s) {
     double* const part = static_cast<double*>(ws);
+    const int block = clip_block(list, n);
+    std::vector<ClipTable> tables;
+    std::vector<int64_t> blocks;
     int64_t total = 0;
-    hipError_t e = clip_tables(list, n, [&](const ClipTable& t, int64_t blocks, int64_t before) {
-        total = before + blocks;
-        return launch_timed(kcReduce, clip_squares_kernel, dim3((unsigned)blocks), dim3(256), 0, s, t, part + before);
-    });
-    if (e != hipSuccess) return e;
+    for (int i = 0; i < n;) {
+        tables.emplace_back();
+        blocks.push_back(clip_table(tables.back(), list, n, block, i));
+        if (!blocks.back()) break;
+        const hipError_t e = launch_timed(kcReduce, clip_squares_kernel, dim3((unsigned)blocks.back()), dim3(256), 0, s, tables.back(), part + total);
+        if (e != hipSuccess) return e;
+        total += blocks.back();
+    }
+    const bool scaled = n > 0 && list[0].out;
     float* const scale = reinterpret_cast<float*>(part + total);
-    e = launch_timed(kcReduce, clip_norm_kernel, dim3(1), dim3(256), 0, s, (const double*)part, total, limit, norm, scale);
-    if (e != hipSuccess || !list || n < 1 || !list[0].out) return e;
-    return clip_tables(list, n, [&](const ClipTable& t, int64_t blocks, int64_t) {
-        return launch_timed(kcUpdate, clip_scale_kernel, dim3((unsigned)blocks), dim3(256), 0, s, t, (const float*)scale);
-    });
+    const bool own = scaled && total > 0 && total <= kClipOwnSum;
+    if (!own) {
+        const hipError_t e = launch_timed(kcReduce, clip_norm_kernel, dim3(1), dim3(256), 0, s, (const double*)part, total, limit, norm, scale);
+        if (e != hipSuccess || !scaled) return e;
+    }
+    for (size_t k = tables.size(); k-- > 0;) {
+        if (!blocks[k]) continue;
+        const hipError_t e = launch_timed(kcUpdate, clip_scale_kernel, dim3((unsigned)blocks[k]), dim3(256), 0, s, tables[k], own ? nullptr : (const float*)scale, (const double*)part, total,
+                                          limit, k == 0 ? norm : nullptr);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace tmps

@@ -112,8 +112,7 @@ struct ClipArray {
     int64_t n;
     int dtype;
 };
-int64_t clip_blocks(int64_t n);               // workgroups of an array of n elements
-size_t clip_workspace_bytes(int64_t blocks);   // of all arrays' workgroups
+size_t clip_workspace_bytes(const ClipArray* list, int n);
 hipError_t clip_gradients(const ClipArray* list, int n, float limit, float* norm, void* ws, hipStream_t s);
 
 }  // namespace tmps

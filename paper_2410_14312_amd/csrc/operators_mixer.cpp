@@ -296,11 +296,23 @@ static int check_clip(const tmps_array* arrays, int n) {
     return TMPS_OK;
 }
 
+// The arrays that have elements.
+static std::vector<ClipArray> clip_list(const tmps_array* arrays, int n) {
+    std::vector<ClipArray> list;
+    list.reserve(n);
+    for (int i = 0; i < n; ++i)
+        if (arrays[i].n) list.push_back(ClipArray{arrays[i].data, arrays[i].out, arrays[i].n, arrays[i].dtype});
+    return list;
+}
+
 extern "C" size_t tmps_clip_workspace(const tmps_array* arrays, int n) {
     if (check_clip(arrays, n) != TMPS_OK) return 0;
-    int64_t blocks = 0;
-    for (int i = 0; i < n; ++i) blocks += clip_blocks(arrays[i].n);
-    return clip_workspace_bytes(blocks);
+    try {
+        const std::vector<ClipArray> list = clip_list(arrays, n);
+        return clip_workspace_bytes(list.data(), (int)list.size());
+    } catch (const std::bad_alloc&) {
+        return 0;
+    }
 }
 
 // Whether no result lies over another array or its result.
@@ -329,25 +341,21 @@ extern "C" int tmps_clip_gradients(const tmps_array* arrays, int n, float limit,
     if (!(limit >= 0.0f)) return fail(TMPS_EINVAL, "limit must not be negative");
     if (!norm) return fail(TMPS_EINVAL, "norm is null");
     if (!aligned(norm, 4)) return fail(TMPS_ESHAPE, "norm is not on a whole element");
-    const size_t need = tmps_clip_workspace(arrays, n);
-    if ((rc = room(workspace, workspace_bytes, need)) != TMPS_OK) return rc;
     try {
-        std::vector<ClipArray> list;
-        list.reserve(n);
+        const std::vector<ClipArray> list = clip_list(arrays, n);
+        const size_t need = clip_workspace_bytes(list.data(), (int)list.size());
+        if ((rc = room(workspace, workspace_bytes, need)) != TMPS_OK) return rc;
         const Range of_norm{norm, 4}, of_ws{workspace, need};
-        bool with = false, without = false;
         if (of_norm.meets(of_ws)) return fail(TMPS_EINVAL, "norm lies in the workspace");
-        for (int i = 0; i < n; ++i) {
-            const tmps_array& a = arrays[i];
+        bool with = false, without = false;
+        for (const ClipArray& a : list) {
             const size_t bytes = (size_t)a.n * act_bytes(a.dtype);
-            if (!a.n) continue;
-            const Range in{a.data, bytes}, out{a.out, a.out ? bytes : 0};
-            if (in.meets(of_norm) || in.meets(of_ws) || out.meets(of_norm) || out.meets(of_ws)) return fail(TMPS_EINVAL, "array %d overlaps the norm or the workspace", i);
+            const Range in{a.in, bytes}, out{a.out, bytes};
+            if (in.meets(of_norm) || in.meets(of_ws) || out.meets(of_norm) || out.meets(of_ws)) return fail(TMPS_EINVAL, "an array or its result overlaps the norm or the workspace");
             (a.out ? with : without) = true;
-            list.push_back(ClipArray{a.data, a.out, a.n, a.dtype});
         }
         if (with && without) return fail(TMPS_EINVAL, "some arrays have a result and others none");
-        if (!clip_apart(list)) return fail(TMPS_EINVAL, "a result overlaps another array or its result");
+        if (with && !clip_apart(list)) return fail(TMPS_EINVAL, "a result overlaps another array or its result");
         TMPS_HIP(clip_gradients(list.data(), (int)list.size(), limit, norm, workspace, (hipStream_t)hip_stream));
     } catch (const std::bad_alloc&) {
         return fail(TMPS_EINVAL, "out of host memory");
