@@ -12,7 +12,7 @@ namespace tmps {
 // also those of the piece before, and come out the same there.  NARROW: rows of fewer channels than a piece.
 constexpr int kConvRuns = 4;
 constexpr int kConvRun = 16;     // positions of a run
-constexpr int kConvAhead = 4;    // positions at a time, as many more under way
+constexpr int kConvAhead = 2;    // positions at a time, as many more under way
 
 // Forward 16 bytes; backward four channels, whose inputs, gradients and sums fit the registers of four waves of a SIMD.
 template <typename T> constexpr int kConvForward = kPiece<T>;
@@ -22,10 +22,12 @@ template <typename T, int V, bool NARROW> struct ConvPiece {
     struct Values { T v[V]; };
     typedef std::conditional_t<V * sizeof(T) == 16, any_u32x4_t, any_u32x2_t> words_t;   // (at any address)
     int C, at;   // channels, the first of this piece
+    uint32_t off;   // its place in a row
     bool any;
-    __device__ __forceinline__ ConvPiece(int piece, int channels) : C(channels), at(NARROW ? 0 : min(piece * V, channels - V)), any(piece * V < channels) {}
+    __device__ __forceinline__ ConvPiece(int piece, int channels)
+        : C(channels), at(NARROW ? 0 : min(piece * V, channels - V)), off((uint32_t)at * (uint32_t)sizeof(T)), any(piece * V < channels) {}
     __device__ __forceinline__ words_t request(const T* row) const {
-        if constexpr (!NARROW) return *reinterpret_cast<const words_t*>(row + at);
+        if constexpr (!NARROW) return *reinterpret_cast<const words_t*>(reinterpret_cast<const char*>(row) + off);
         Values f;
 #pragma unroll
         for (int e = 0; e < V; ++e) f.v[e] = row[min(e, C - 1)];
@@ -48,18 +50,23 @@ template <typename T, int V, bool NARROW> struct ConvPiece {
         }
     }
     __device__ __forceinline__ void load(float (&v)[V], const T* row) const { open(request(row), v); }
-    // (first: the first channel to store)
-    __device__ __forceinline__ void store(T* row, const float (&v)[V], int first = 0) const {
+    __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
         Values f;
 #pragma unroll
         for (int e = 0; e < V; ++e) f.v[e] = from_f32<T>(v[e]);
-        if (!NARROW && first <= at) {
-            *reinterpret_cast<words_t*>(row + at) = __builtin_bit_cast(words_t, f);
+        if constexpr (!NARROW) {
+            *reinterpret_cast<words_t*>(reinterpret_cast<char*>(row) + off) = __builtin_bit_cast(words_t, f);
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                if (at + e < C && at + e >= first) row[at + e] = f.v[e];
+                if (e < C) row[e] = f.v[e];
         }
+    }
+    // The channels from `first` on.
+    __device__ __forceinline__ void store_from(T* row, const float (&v)[V], int first) const {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (at + e < C && at + e >= first) row[at + e] = from_f32<T>(v[e]);
     }
 };
 
@@ -72,7 +79,7 @@ struct ConvPlace {
         group = blockIdx.x / blocks;
         first = (int)(blockIdx.x % blocks) * 64;
         piece = first + (int)(threadIdx.x & 63);
-        const int64_t unit = group * kConvRuns + (threadIdx.x >> 6);
+        const int64_t unit = group * kConvRuns + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // (known to be the same for a wave: rows' addresses are scalars then)
         sample = unit / runs;
         t0 = (unit - sample * runs) * kConvRun;
     }
@@ -145,7 +152,10 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
                 z[e] = taps.bias[e];
 #pragma unroll
                 for (int j = 0; j < K; ++j) z[e] = fmaf(taps.w[j][e], u[k + j][e], z[e]);
-                if (a.silu) z[e] *= conv_sigmoid<T>(z[e]);
+            }
+            if (a.silu) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) z[e] *= conv_sigmoid<T>(z[e]);
             }
             if (k < many) p.store(y + (from + k) * a.y_stride, z);
         }
@@ -155,7 +165,7 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
             for (int j = 0; j < K - 1; ++j)
 #pragma unroll
                 for (int k = 1; k <= A; ++k)
-                    if (k == many) p.store(out + (int64_t)j * a.channels, u[k + j], at.piece * V);
+                    if (k == many) p.store_from(out + (int64_t)j * a.channels, u[k + j], at.piece * V);
         }
 #pragma unroll
         for (int j = 0; j < K - 1; ++j)
@@ -171,7 +181,7 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
     const ConvPlace at(a.positions, a.channels, V);
     const ConvPiece<T, V, NARROW> p(at.piece, a.channels);
     const int64_t sample = at.sample, t0 = at.t0;
-    const int run = threadIdx.x >> 6;
+    const int run = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float dw[K + 1][V];
 #pragma unroll
     for (int j = 0; j <= K; ++j)
@@ -208,26 +218,27 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
                 p.open(ny[k], dz[K - 1 + k]);
             }
             if (from + A < end) request(from + A);
+            if (a.silu) {
+#pragma unroll
+                for (int k = 0; k < A; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        float z = taps.bias[e];
+#pragma unroll
+                        for (int j = 0; j < K; ++j) z = fmaf(taps.w[j][e], u[k + j][e], z);
+                        const float s = conv_sigmoid<T>(z);
+                        dz[K - 1 + k][e] *= s * fmaf(z, 1.0f - s, 1.0f);
+                    }
+            }
 #pragma unroll
             for (int k = 0; k < A; ++k) {
                 const bool here = from + k < a.positions, mine = from + k < t1;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    float g = dz[K - 1 + k][e];
-                    if (a.silu) {
-                        float z = taps.bias[e];
+                    const float g = dz[K - 1 + k][e] = here ? dz[K - 1 + k][e] : 0.0f, of_run = mine ? g : 0.0f;
 #pragma unroll
-                        for (int j = 0; j < K; ++j) z = fmaf(taps.w[j][e], u[k + j][e], z);
-                        const float s = conv_sigmoid<T>(z);
-                        g *= s * fmaf(z, 1.0f - s, 1.0f);
-                    }
-                    dz[K - 1 + k][e] = here ? g : 0.0f;
-                    const float of_run = mine ? g : 0.0f;
-                    if (mine) {
-#pragma unroll
-                        for (int j = 0; j < K; ++j) dw[j][e] = fmaf(of_run, u[k + j][e], dw[j][e]);
-                        dw[K][e] += of_run;
-                    }
+                    for (int j = 0; j < K; ++j) dw[j][e] = fmaf(of_run, u[k + j][e], dw[j][e]);
+                    dw[K][e] += of_run;
                 }
             }
             // (the gradient of the input K - 1 positions back is complete with a position's dz; the first run also has those of the tail)
