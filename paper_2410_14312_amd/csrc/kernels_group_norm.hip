@@ -1,6 +1,7 @@
-// Group norm with its activation, and its gradients.  Two forms, both bound by memory:
+// Group norm with its activation, and its gradients.  Three forms, all bound by memory:
 //   rows  one position a sample: each group of a sample is a row of its own, held in the registers of a team of threads, one pass;
-//   maps  more positions: sums of slices of positions, the samples' sums, and a second pass over the map.
+//   held  a sample's map fits the registers of a workgroup: one pass;
+//   maps  larger ones: sums of slices of positions, the samples' sums, and a second pass over the map.
 // Of a group's values the mean is taken first and the differences from it squared; what several threads or slices have is joined as (number, mean, sum of squared differences).
 #include <algorithm>
 
@@ -225,7 +226,38 @@ template <typename T> struct MapPlace {
     }
 };
 
-constexpr int kMapBlock = 8;   // positions whose values a thread has at a time
+constexpr int kMapBlock = 8, kMapPairs = 4;   // positions whose values, or values and gradients, a thread has at a time
+
+// Mean and sum of squared differences, by channel, of up to B positions' values; the first `many` count.  With rms the mean is 0.
+template <typename T, int B> __device__ __forceinline__ void block_moments(const uint4 (&u)[B], int many, bool rms, float (&mean)[kPiece<T>], float (&m2)[kPiece<T>]) {
+    constexpr int V = kPiece<T>;
+#pragma unroll
+    for (int e = 0; e < V; ++e) mean[e] = m2[e] = 0.0f;
+    if (!rms) {
+#pragma unroll
+        for (int k = 0; k < B; ++k)
+            if (k < many) {
+                float v[V];
+                unpack(u[k], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) mean[e] += v[e];
+            }
+        const float by = 1.0f / (float)max(many, 1);
+#pragma unroll
+        for (int e = 0; e < V; ++e) mean[e] *= by;
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k)
+        if (k < many) {
+            float v[V];
+            unpack(u[k], v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = v[e] - mean[e];
+                m2[e] = fmaf(d, d, m2[e]);
+            }
+        }
+}
 
 // Mean and sum of squared differences of every channel over a slice: part [sample][slice][channels][2].
 template <typename T> __global__ __launch_bounds__(256) void group_map_moments_kernel(const T* x, int64_t positions, int channels, int64_t slice, int slices, bool rms, float* part) {
@@ -243,30 +275,9 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_moments_k
             uint4 u[kMapBlock];
             const int many = (int)min<int64_t>(kMapBlock, (t1 - t + p.lanes - 1) / p.lanes);
 #pragma unroll
-            for (int k = 0; k < kMapBlock; ++k)
-                if (k < many) u[k] = p.request(rows + (t + (int64_t)k * p.lanes) * channels);
-            float v[kMapBlock][V], bm[V], b2[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) bm[e] = b2[e] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kMapBlock; ++k)
-                if (k < many) {
-                    unpack(u[k], v[k]);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) bm[e] += v[k][e];
-                }
-            const float by = rms ? 0.0f : 1.0f / (float)many;
-#pragma unroll
-            for (int e = 0; e < V; ++e) bm[e] *= by;
-#pragma unroll
-            for (int k = 0; k < kMapBlock; ++k)
-                if (k < many) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float d = v[k][e] - bm[e];
-                        b2[e] = fmaf(d, d, b2[e]);
-                    }
-                }
+            for (int k = 0; k < kMapBlock; ++k) u[k] = p.request(rows + min(t + (int64_t)k * p.lanes, t1 - 1) * channels);
+            float bm[V], b2[V];
+            block_moments<T>(u, many, rms, bm, b2);
             const float all = n + (float)many, share = (float)many / all, between = n * share;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -300,26 +311,47 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_moments_k
     }
 }
 
-// The groups' means and 1/std from those of the slices' channels: 16 lanes to a group.
+// Moments of a group from those of the 2^STEPS lanes that share it.
+template <int LANES> __device__ __forceinline__ void join_lanes(float& n, float& mean, float& m2) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) {
+        const float n2 = __shfl_xor(n, d), mean2 = __shfl_xor(mean, d), m22 = __shfl_xor(m2, d);
+        // (the same in both lanes: the lower one's first)
+        const bool low = (threadIdx.x & d) == 0;
+        float an = low ? n : n2, am = low ? mean : mean2, as = low ? m2 : m22;
+        const float bn = low ? n2 : n, bm = low ? mean2 : mean, bs = low ? m22 : m2;
+        if (an == 0.0f) an = bn, am = bm, as = bs;
+        else join_moments(an, am, as, bn, bm, bs);
+        n = an; mean = am; m2 = as;
+    }
+}
+
+// The groups' means and 1/std from those of the slices' channels: a wave to a group, eight of a lane's under way at a time.
 __global__ __launch_bounds__(256) void group_map_stats_kernel(const float* part, int64_t samples, int64_t positions, int channels, int groups, int64_t slice, int slices, bool rms, float* stats) {
-    const int64_t g = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int64_t g = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
     if (g >= samples * groups) return;
     const int64_t sample = g / groups;
-    const int size = channels / groups, first = (int)(g % groups) * size;
+    const int size = channels / groups, first = (int)(g % groups) * size, lane = threadIdx.x & 63;
+    const int64_t all = (int64_t)size * slices;
+    const float2* const from = reinterpret_cast<const float2*>(part) + sample * slices * channels + first;
     float n = 0.0f, mean = 0.0f, m2 = 0.0f;
-    for (int i = threadIdx.x % 16; i < size * slices; i += 16) {
-        const int cut = i / size;
-        const float many = (float)min<int64_t>(slice, positions - cut * slice);
-        const float* const f = part + ((sample * slices + cut) * channels + first + i % size) * 2;
-        join_moments(n, mean, m2, many, f[0], f[1]);
-    }
+    for (int64_t i0 = lane; i0 < all; i0 += 64 * 8) {
+        float2 f[8];
+        float many[8];
 #pragma unroll
-    for (int d = 8; d > 0; d >>= 1) {
-        const float n2 = __shfl_xor(n, d), mean2 = __shfl_xor(mean, d), m22 = __shfl_xor(m2, d);
-        if (n == 0.0f) n = n2, mean = mean2, m2 = m22;
-        else join_moments(n, mean, m2, n2, mean2, m22);
+        for (int k = 0; k < 8; ++k) {
+            const int64_t i = min(i0 + 64 * k, all - 1), cut = i / size;
+            f[k] = from[cut * channels + i % size];
+            many[k] = i0 + 64 * k < all ? (float)min<int64_t>(slice, positions - cut * slice) : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (n == 0.0f) n = many[k], mean = f[k].x, m2 = f[k].y;
+            else join_moments(n, mean, m2, many[k], f[k].x, f[k].y);
+        }
     }
-    if (threadIdx.x % 16 == 0) {
+    join_lanes<64>(n, mean, m2);
+    if (lane == 0) {
         stats[2 * g] = rms ? 0.0f : mean;
         stats[2 * g + 1] = 1.0f / sqrtf(m2 / ((float)size * (float)positions) + 1e-5f);
     }
@@ -340,16 +372,23 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_apply_ker
     p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
     const T* const x = (const T*)a.x + sample * a.positions * a.channels;
     T* const y = (T*)a.y + sample * a.positions * a.channels;
-#pragma unroll 4
-    for (int64_t t = t0 + p.lane; t < t1; t += p.lanes) {
-        float v[V];
-        unpack(p.request(x + t * a.channels), v);
+    for (int64_t t = t0 + p.lane; t < t1; t += (int64_t)p.lanes * kMapPairs) {
+        uint4 u[kMapPairs];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float xhat;
-            v[e] = norm_act<T>(a.act, norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat));
+        for (int k = 0; k < kMapPairs; ++k) u[k] = p.request(x + min(t + (int64_t)k * p.lanes, t1 - 1) * a.channels);
+#pragma unroll
+        for (int k = 0; k < kMapPairs; ++k) {
+            const int64_t at = t + (int64_t)k * p.lanes;
+            if (at >= t1) continue;
+            float v[V];
+            unpack(u[k], v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float xhat;
+                v[e] = norm_act<T>(a.act, norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat));
+            }
+            p.store(y + at * a.channels, v);
         }
-        p.store(y + t * a.channels, v);
     }
 }
 
@@ -373,18 +412,28 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_sums_kern
         p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
         const T* const x = (const T*)a.x + sample * a.positions * a.channels;
         const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
-#pragma unroll 4
-        for (int64_t t = t0 + p.lane; t < t1; t += p.lanes) {
-            float v[V], g[V];
-            unpack(p.request(x + t * a.channels), v);
-            unpack(p.request(dy + t * a.channels), g);
+        for (int64_t t = t0 + p.lane; t < t1; t += (int64_t)p.lanes * kMapPairs) {
+            uint4 ux[kMapPairs], ug[kMapPairs];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                float xhat;
-                const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
-                const float dz = norm_act_grad<T>(a.act, z, g[e]);
-                with_xhat[e] = fmaf(dz, xhat, with_xhat[e]);
-                alone[e] += dz;
+            for (int k = 0; k < kMapPairs; ++k) {
+                const int64_t row = min(t + (int64_t)k * p.lanes, t1 - 1) * a.channels;
+                ux[k] = p.request(x + row);
+                ug[k] = p.request(dy + row);
+            }
+#pragma unroll
+            for (int k = 0; k < kMapPairs; ++k) {
+                if (t + (int64_t)k * p.lanes >= t1) continue;
+                float v[V], g[V];
+                unpack(ux[k], v);
+                unpack(ug[k], g);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float xhat;
+                    const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
+                    const float dz = norm_act_grad<T>(a.act, z, g[e]);
+                    with_xhat[e] = fmaf(dz, xhat, with_xhat[e]);
+                    alone[e] += dz;
+                }
             }
         }
     }
@@ -404,28 +453,60 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_sums_kern
     }
 }
 
-// Each group's sums of gain dz and of gain dz xhat over its values, divided by their number: means [samples][groups][2].
-__global__ __launch_bounds__(256) void group_map_means_kernel(const float* part, const float* gain, int64_t samples, int64_t positions, int channels, int groups, int slices, bool rms, float* means) {
-    const int64_t g = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    if (g >= samples * groups) return;
-    const int64_t sample = g / groups;
-    const int size = channels / groups, first = (int)(g % groups) * size;
-    float with_xhat = 0.0f, alone = 0.0f;
-    for (int i = threadIdx.x % 16; i < size * slices; i += 16) {
-        const int c = first + i % size;
-        const float* const f = part + (sample * slices + i / size) * 2 * channels + c;
-        with_xhat = fmaf(gain[c], f[0], with_xhat);
-        alone = fmaf(gain[c], f[channels], alone);
-    }
+// The slices' sums of a sample's channels added up, and of them each group's means of gain dz and of gain dz xhat over its values.  A workgroup has whole groups, `columns` channels of a
+// sample: sums [sample][2][channels], means [samples][groups][2].
+__global__ __launch_bounds__(512) void group_map_fold_kernel(const float* part, const float* gain, int64_t positions, int channels, int groups, int columns, int slices, bool rms, float* sums,
+                                                             float* means) {
+    __shared__ float fold[512];
+    const int blocks = (channels + columns - 1) / columns;
+    const int64_t sample = blockIdx.x / blocks;
+    const int c0 = (int)(blockIdx.x % blocks) * columns, width = min(columns, channels - c0), size = channels / groups;
+    const float* const from = part + sample * slices * 2 * channels;
+    float* const to = sums + sample * 2 * channels;
+    // (lanes of slices to a sum: as many as fill the workgroup)
+    const int lanes = max(1, 512 / (2 * width)), lane = (int)threadIdx.x / (2 * width);
+    for (int i0 = 0; i0 < 2 * width; i0 += 512) {
+        const int i = lanes > 1 ? (int)threadIdx.x % (2 * width) : i0 + (int)threadIdx.x;
+        const bool any = i < 2 * width && lane < lanes;
+        const int64_t column = (int64_t)(i / width) * channels + c0 + i % width;
+        float s = 0.0f;
+        if (any)
+            for (int z = lanes > 1 ? lane : 0; z < slices; z += lanes * 8) {
+                float v[8];
 #pragma unroll
-    for (int d = 8; d > 0; d >>= 1) {
-        with_xhat += __shfl_xor(with_xhat, d);
-        alone += __shfl_xor(alone, d);
+                for (int k = 0; k < 8; ++k) v[k] = from[(int64_t)min(z + k * lanes, slices - 1) * 2 * channels + column];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += z + k * lanes < slices ? v[k] : 0.0f;
+            }
+        if (lanes > 1) {
+            fold[threadIdx.x] = s;
+            __syncthreads();
+            if (lane == 0)
+                for (int l = 1; l < lanes; ++l) s += fold[l * 2 * width + i];
+        }
+        if (any && (lanes == 1 || lane == 0)) to[column] = s;
     }
-    if (threadIdx.x % 16 == 0) {
-        const float n = (float)size * (float)positions;
-        means[2 * g] = rms ? 0.0f : alone / n;
-        means[2 * g + 1] = with_xhat / n;
+    __threadfence_block();
+    __syncthreads();
+    // eight lanes to a group
+    const float n = (float)size * (float)positions;
+    for (int g = (int)threadIdx.x / 8; g < width / size; g += 64) {
+        float with_xhat = 0.0f, alone = 0.0f;
+        for (int i = threadIdx.x % 8; i < size; i += 8) {
+            const int c = c0 + g * size + i;
+            with_xhat = fmaf(gain[c], to[c], with_xhat);
+            alone = fmaf(gain[c], to[channels + c], alone);
+        }
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) {
+            with_xhat += __shfl_xor(with_xhat, d);
+            alone += __shfl_xor(alone, d);
+        }
+        if (threadIdx.x % 8 == 0) {
+            float* const mean = means + (sample * groups + c0 / size + g) * 2;
+            mean[0] = rms ? 0.0f : alone / n;
+            mean[1] = with_xhat / n;
+        }
     }
 }
 
@@ -447,25 +528,37 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_apply_bwd
     const T* const x = (const T*)a.x + sample * a.positions * a.channels;
     const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
     T* const dx = (T*)a.dx + sample * a.positions * a.channels;
-#pragma unroll 2
-    for (int64_t t = t0 + p.lane; t < t1; t += p.lanes) {
-        float v[V], g[V];
-        unpack(p.request(x + t * a.channels), v);
-        unpack(p.request(dy + t * a.channels), g);
+    for (int64_t t = t0 + p.lane; t < t1; t += (int64_t)p.lanes * kMapPairs) {
+        uint4 ux[kMapPairs], ug[kMapPairs];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float xhat;
-            const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
-            const float dz = norm_act_grad<T>(a.act, z, g[e]) * gain[e];
-            v[e] = (fmaf(-xhat, with_xhat[e], dz) - alone[e]) * rstd[e];
+        for (int k = 0; k < kMapPairs; ++k) {
+            const int64_t row = min(t + (int64_t)k * p.lanes, t1 - 1) * a.channels;
+            ux[k] = p.request(x + row);
+            ug[k] = p.request(dy + row);
         }
-        p.store(dx + t * a.channels, v);
+#pragma unroll
+        for (int k = 0; k < kMapPairs; ++k) {
+            const int64_t at = t + (int64_t)k * p.lanes;
+            if (at >= t1) continue;
+            float v[V], g[V];
+            unpack(ux[k], v);
+            unpack(ug[k], g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float xhat;
+                const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
+                const float dz = norm_act_grad<T>(a.act, z, g[e]) * gain[e];
+                v[e] = (fmaf(-xhat, with_xhat[e], dz) - alone[e]) * rstd[e];
+            }
+            p.store(dx + at * a.channels, v);
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------------------ launches
 // Slices of a sample's positions: as many as give the chip 2048 workgroups, of 32 positions at least.
 constexpr int kMapGroups = 2048, kMapPositions = 32;
+constexpr int kFoldColumns = 64;   // channels whose slices' sums a workgroup adds up, in whole groups
 struct MapPlan {
     int64_t slice;
     int slices, blocks;   // blocks: of 256 pieces of channels
@@ -499,7 +592,7 @@ size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions,
     if (by_rows(positions, channels, groups)) return backward ? (size_t)row_teams(samples, groups, 16, kRowsEachBack) / groups * 2 * channels * sizeof(float) : 0;
     const int64_t blocks = map_plan(samples, positions, channels, dtype == kBF16 ? 8 : 4).blocks;
     const int64_t most = std::min(samples * ((positions + kMapPositions - 1) / kMapPositions), samples + kMapGroups / blocks + 1);
-    return ((size_t)most * 2 * channels + (backward ? (size_t)samples * groups * 2 : 0)) * sizeof(float);
+    return ((size_t)most * 2 * channels + (backward ? (size_t)samples * 2 * (groups + channels) : 0)) * sizeof(float);
 }
 
 template <typename T, int TEAM, int N, bool WHOLE> static hipError_t rows_fwd(const GroupNorm& a, hipStream_t s) {
@@ -540,7 +633,7 @@ template <typename T> static hipError_t forward_type(const GroupNorm& a, float* 
     const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
     hipError_t e = launch_timed(kcLayerNorm, group_map_moments_kernel<T>, grid, dim3(256), 0, s, (const T*)a.x, a.positions, a.channels, m.slice, m.slices, a.rms, ws);
     if (e != hipSuccess) return e;
-    e = launch_timed(kcLayerNorm, group_map_stats_kernel, dim3((unsigned)((a.samples * a.groups + 15) / 16)), dim3(256), 0, s, (const float*)ws, a.samples, a.positions, a.channels,
+    e = launch_timed(kcLayerNorm, group_map_stats_kernel, dim3((unsigned)((a.samples * a.groups + 3) / 4)), dim3(256), 0, s, (const float*)ws, a.samples, a.positions, a.channels,
                      a.groups, m.slice, m.slices, a.rms, a.stats);
     if (e != hipSuccess) return e;
     return launch_timed(kcLayerNorm, group_map_apply_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices);
@@ -551,16 +644,18 @@ template <typename T> static hipError_t backward_type(const GroupNormBackward& a
     const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
     if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
     float* const means = ws + a.samples * m.slices * 2 * (int64_t)a.channels;
+    float* const sums = means + a.samples * a.groups * 2;
     const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
     hipError_t e = launch_timed(kcLayerNorm, group_map_sums_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices, ws);
     if (e != hipSuccess) return e;
-    e = launch_timed(kcLayerNorm, group_map_means_kernel, dim3((unsigned)((a.samples * a.groups + 15) / 16)), dim3(256), 0, s, (const float*)ws, a.gain, a.samples, a.positions,
-                     a.channels, a.groups, m.slices, a.rms, means);
+    const int size = a.channels / a.groups, columns = (kFoldColumns + size - 1) / size * size;
+    const int64_t folds = a.samples * ((a.channels + columns - 1) / columns);
+    e = launch_timed(kcLayerNorm, group_map_fold_kernel, dim3((unsigned)folds), dim3(512), 0, s, (const float*)ws, a.gain, a.positions, a.channels, a.groups, columns, m.slices, a.rms, sums,
+                     means);
     if (e != hipSuccess) return e;
     e = launch_timed(kcLayerNorm, group_map_apply_bwd_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices, (const float*)means);
     if (e != hipSuccess) return e;
-    Reductions sums(1, Reduction{ws, a.dparams, 2 * (int64_t)a.channels, (int)(a.samples * m.slices), true});
-    return reduce_all(sums, s);
+    return reduce_all(Reductions(1, Reduction{sums, a.dparams, 2 * (int64_t)a.channels, (int)a.samples, true}), s);
 }
 
 hipError_t group_norm_forward(int dtype, const GroupNorm& a, void* ws, hipStream_t s) {
