@@ -197,8 +197,8 @@ template <typename T> struct MapPlace {
     static constexpr int V = kPiece<T>;
     int C, pieces, width, lanes, lane, at;   // pieces of a row; of this workgroup; positions side by side; this thread's; its first channel
     bool any;
-    __device__ __forceinline__ MapPlace(int channels, int block, int threads) : C(channels), pieces((channels + V - 1) / V) {
-        width = min(pieces - block * 256, 256);
+    __device__ __forceinline__ MapPlace(int channels, int block, int threads, int most = 256) : C(channels), pieces((channels + V - 1) / V) {
+        width = min(pieces - block * 256, most);
         lanes = threads / width;
         lane = (int)threadIdx.x / width;
         any = lane < lanes;
@@ -555,6 +555,218 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_apply_bwd
     }
 }
 
+// ------------------------------------------------------------------------------------------------ held
+// A workgroup has a sample, its threads every `lanes`-th position of a piece of channels each.
+constexpr int kHeldPieces = 8, kHeldPairs = 4;   // of a thread: values, values and gradients
+constexpr int kHeldGroups = 512;
+
+// Lanes that share an item of `items` of a workgroup's.
+__device__ __forceinline__ int lanes_each(int threads, int items) {
+    int n = 1;
+    while (n < 16 && 2 * n * items <= threads) n *= 2;
+    return n;
+}
+
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void group_held_fwd_kernel(GroupNorm a) {
+    constexpr int V = kPiece<T>;
+    __shared__ float fold[THREADS][2 * V + 1];
+    __shared__ float group_stats[kHeldGroups][2];
+    const MapPlace<T> p(a.channels, 0, THREADS, THREADS);
+    const int64_t sample = blockIdx.x;
+    const int positions = (int)a.positions, size = a.channels / a.groups;
+    const T* const x = (const T*)a.x + sample * a.positions * a.channels;
+    uint4 u[kHeldPieces];
+    const int many = p.any && p.lane < positions ? (positions - p.lane + p.lanes - 1) / p.lanes : 0;
+#pragma unroll
+    for (int k = 0; k < kHeldPieces; ++k)
+        if (k * p.lanes < positions) u[k] = p.request(x + (int64_t)min(p.lane + k * p.lanes, positions - 1) * a.channels);
+    float mean[V], m2[V], gain[V], shift[V];
+    p.params(gain, [&](int c) { return a.gain[c]; });
+    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    block_moments<T>(u, many, a.rms, mean, m2);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        fold[threadIdx.x][e] = mean[e];
+        fold[threadIdx.x][V + e] = m2[e];
+    }
+    fold[threadIdx.x][2 * V] = (float)many;
+    __syncthreads();
+    // the channels' moments, to the rows of the first lane
+    {
+        const int items = p.width * V, sub = lanes_each(THREADS, items), h = threadIdx.x % sub;
+        for (int i0 = 0; i0 < items; i0 += THREADS / sub) {
+            const int i = i0 + (int)threadIdx.x / sub, k = min(i, items - 1) / V, e = i % V;
+            float n = 0.0f, m = 0.0f, s = 0.0f;
+            for (int l = h; l < p.lanes; l += sub) {
+                const float* const f = fold[l * p.width + k];
+                if (n == 0.0f) n = f[2 * V], m = f[e], s = f[V + e];
+                else join_moments(n, m, s, f[2 * V], f[e], f[V + e]);
+            }
+            for (int d = 1; d < sub; d <<= 1) {
+                const float n2 = __shfl_xor(n, d), mean2 = __shfl_xor(m, d), m22 = __shfl_xor(s, d);
+                if (n == 0.0f) n = n2, m = mean2, s = m22;
+                else join_moments(n, m, s, n2, mean2, m22);
+            }
+            __syncthreads();
+            if (i < items && h == 0) {
+                fold[k][e] = m;
+                fold[k][V + e] = s;
+            }
+        }
+    }
+    __syncthreads();
+    {
+        const int sub = lanes_each(THREADS, a.groups), h = threadIdx.x % sub;
+        for (int g0 = 0; g0 < a.groups; g0 += THREADS / sub) {
+            const int g = min(g0 + (int)threadIdx.x / sub, a.groups - 1);
+            float n = 0.0f, m = 0.0f, s = 0.0f;
+            for (int i = h; i < size; i += sub) {
+                const int c = g * size + i, k = c / V, e = c - min(k * V, max(a.channels - V, 0));
+                if (n == 0.0f) n = (float)positions, m = fold[k][e], s = fold[k][V + e];
+                else join_moments(n, m, s, (float)positions, fold[k][e], fold[k][V + e]);
+            }
+            for (int d = 1; d < sub; d <<= 1) {
+                const float n2 = __shfl_xor(n, d), mean2 = __shfl_xor(m, d), m22 = __shfl_xor(s, d);
+                if (n == 0.0f) n = n2, m = mean2, s = m22;
+                else join_moments(n, m, s, n2, mean2, m22);
+            }
+            if (h == 0 && g0 + (int)threadIdx.x / sub < a.groups) {
+                const float rstd = 1.0f / sqrtf(s / ((float)size * (float)positions) + 1e-5f), to = a.rms ? 0.0f : m;
+                group_stats[g][0] = to;
+                group_stats[g][1] = rstd;
+                a.stats[(sample * a.groups + g) * 2] = to;
+                a.stats[(sample * a.groups + g) * 2 + 1] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    float rstd[V];
+    p.params(mean, [&](int c) { return group_stats[c / size][0]; });
+    p.params(rstd, [&](int c) { return group_stats[c / size][1]; });
+    T* const y = (T*)a.y + sample * a.positions * a.channels;
+#pragma unroll
+    for (int k = 0; k < kHeldPieces; ++k) {
+        if (k >= many) continue;
+        float v[V];
+        unpack(u[k], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float xhat;
+            v[e] = norm_act<T>(a.act, norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat));
+        }
+        p.store(y + (int64_t)(p.lane + k * p.lanes) * a.channels, v);
+    }
+}
+
+// sums: [sample][2][channels]
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void group_held_bwd_kernel(GroupNormBackward a, float* sums) {
+    constexpr int V = kPiece<T>;
+    __shared__ float fold[THREADS][2 * V];
+    __shared__ float group_means[kHeldGroups][2];
+    const MapPlace<T> p(a.channels, 0, THREADS, THREADS);
+    const int64_t sample = blockIdx.x;
+    const int positions = (int)a.positions, size = a.channels / a.groups;
+    const T* const x = (const T*)a.x + sample * a.positions * a.channels;
+    const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
+    const float* const stats = a.stats + sample * a.groups * 2;
+    uint4 ux[kHeldPairs], ug[kHeldPairs];
+    const int many = p.any && p.lane < positions ? (positions - p.lane + p.lanes - 1) / p.lanes : 0;
+#pragma unroll
+    for (int k = 0; k < kHeldPairs; ++k)
+        if (k * p.lanes < positions) {
+            const int64_t row = (int64_t)min(p.lane + k * p.lanes, positions - 1) * a.channels;
+            ux[k] = p.request(x + row);
+            ug[k] = p.request(dy + row);
+        }
+    float mean[V], rstd[V], gain[V], shift[V], with_xhat[V], alone[V];
+    p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
+    p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
+    p.params(gain, [&](int c) { return a.gain[c]; });
+    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+#pragma unroll
+    for (int e = 0; e < V; ++e) with_xhat[e] = alone[e] = 0.0f;
+    // xhat and dz of piece k
+    const auto parts = [&](int k, float (&v)[V], float (&g)[V]) {
+        unpack(ux[k], v);
+        unpack(ug[k], g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float xhat;
+            const float z = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
+            g[e] = norm_act_grad<T>(a.act, z, g[e]);
+            v[e] = xhat;
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < kHeldPairs; ++k) {
+        if (k >= many) continue;
+        float v[V], g[V];
+        parts(k, v, g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            with_xhat[e] = fmaf(g[e], v[e], with_xhat[e]);
+            alone[e] += g[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        fold[threadIdx.x][e] = with_xhat[e];
+        fold[threadIdx.x][V + e] = alone[e];
+    }
+    __syncthreads();
+    float* const mine = sums + sample * 2 * a.channels;
+    {
+        const int items = 2 * p.width * V, sub = lanes_each(THREADS, items), h = threadIdx.x % sub;
+        for (int i0 = 0; i0 < items; i0 += THREADS / sub) {
+            const int i = i0 + (int)threadIdx.x / sub, at = min(i, items - 1), which = at / (p.width * V), k = at / V % p.width, e = at % V;
+            float s = 0.0f;
+            for (int l = h; l < p.lanes; l += sub) s += fold[l * p.width + k][which * V + e];
+            for (int d = 1; d < sub; d <<= 1) s += __shfl_xor(s, d);
+            __syncthreads();
+            if (i < items && h == 0) {
+                fold[k][which * V + e] = s;
+                const int ch = min(k * V, max(a.channels - V, 0)) + e;
+                if (ch >= k * V && ch < a.channels) mine[which * (int64_t)a.channels + ch] = s;
+            }
+        }
+    }
+    __syncthreads();
+    {
+        const int sub = lanes_each(THREADS, a.groups), h = threadIdx.x % sub;
+        const float n = (float)size * (float)positions;
+        for (int g0 = 0; g0 < a.groups; g0 += THREADS / sub) {
+            const int g = min(g0 + (int)threadIdx.x / sub, a.groups - 1);
+            float with = 0.0f, without = 0.0f;
+            for (int i = h; i < size; i += sub) {
+                const int c = g * size + i, k = c / V, e = c - min(k * V, max(a.channels - V, 0));
+                with = fmaf(a.gain[c], fold[k][e], with);
+                without = fmaf(a.gain[c], fold[k][V + e], without);
+            }
+            for (int d = 1; d < sub; d <<= 1) {
+                with += __shfl_xor(with, d);
+                without += __shfl_xor(without, d);
+            }
+            if (h == 0) {
+                group_means[g][0] = a.rms ? 0.0f : without / n;
+                group_means[g][1] = with / n;
+            }
+        }
+    }
+    __syncthreads();
+    p.params(alone, [&](int c) { return group_means[c / size][0]; });
+    p.params(with_xhat, [&](int c) { return group_means[c / size][1]; });
+    T* const dx = (T*)a.dx + sample * a.positions * a.channels;
+#pragma unroll
+    for (int k = 0; k < kHeldPairs; ++k) {
+        if (k >= many) continue;
+        float v[V], g[V];
+        parts(k, v, g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = (fmaf(-v[e], with_xhat[e], g[e] * gain[e]) - alone[e]) * rstd[e];
+        p.store(dx + (int64_t)(p.lane + k * p.lanes) * a.channels, v);
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ launches
 // Slices of a sample's positions: as many as give the chip 2048 workgroups, of 32 positions at least.
 constexpr int kMapGroups = 2048, kMapPositions = 32;
@@ -586,6 +798,15 @@ constexpr int kRowsEachBack = 8;
 
 constexpr int kRowFeatures = 16384;   // of a group in the form by rows
 static bool by_rows(int64_t positions, int channels, int groups) { return positions == 1 && channels / groups <= kRowFeatures; }
+
+// Threads that hold a sample's map, `pieces` of a thread's (0: more than a workgroup has).
+static int held_threads(int64_t positions, int channels, int groups, int V, int pieces) {
+    const int width = (channels + V - 1) / V;
+    if (groups > kHeldGroups) return 0;
+    for (int threads : {256, 1024})
+        if (width <= threads && positions <= (int64_t)(threads / width) * pieces) return threads;
+    return 0;
+}
 
 // (as much as any call of no more samples and positions takes)
 size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions, int channels, int groups, bool backward) {
@@ -628,6 +849,9 @@ template <typename T> static hipError_t rows_bwd_type(const GroupNormBackward& a
 
 template <typename T> static hipError_t forward_type(const GroupNorm& a, float* ws, hipStream_t s) {
     if (by_rows(a.positions, a.channels, a.groups)) return rows_fwd_type<T>(a, s);
+    if (const int threads = held_threads(a.positions, a.channels, a.groups, kPiece<T>, kHeldPieces))
+        return threads == 256 ? launch_timed(kcLayerNorm, group_held_fwd_kernel<T, 256>, dim3((unsigned)a.samples), dim3(256), 0, s, a)
+                              : launch_timed(kcLayerNorm, group_held_fwd_kernel<T, 1024>, dim3((unsigned)a.samples), dim3(1024), 0, s, a);
     const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
     if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
@@ -641,6 +865,12 @@ template <typename T> static hipError_t forward_type(const GroupNorm& a, float* 
 
 template <typename T> static hipError_t backward_type(const GroupNormBackward& a, float* ws, hipStream_t s) {
     if (by_rows(a.positions, a.channels, a.groups)) return rows_bwd_type<T>(a, ws, s);
+    if (const int threads = held_threads(a.positions, a.channels, a.groups, kPiece<T>, kHeldPairs)) {
+        const hipError_t e = threads == 256 ? launch_timed(kcLayerNorm, group_held_bwd_kernel<T, 256>, dim3((unsigned)a.samples), dim3(256), 0, s, a, ws)
+                                            : launch_timed(kcLayerNorm, group_held_bwd_kernel<T, 1024>, dim3((unsigned)a.samples), dim3(1024), 0, s, a, ws);
+        if (e != hipSuccess) return e;
+        return reduce_all(Reductions(1, Reduction{ws, a.dparams, 2 * (int64_t)a.channels, (int)a.samples, true}), s);
+    }
     const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
     if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
     float* const means = ws + a.samples * m.slices * 2 * (int64_t)a.channels;

@@ -10,7 +10,7 @@ from tests.mixers import DEV, TYPES, near
 
 pytestmark = pytest.mark.gpu
 SIZES = [(1, 1, 16, 1), (3, 1, 64, 4), (5, 1, 1536, 24), (2, 1, 99, 3), (2, 1, 20000, 1), (4, 16, 32, 8), (2, 49, 24, 3), (3, 33, 10, 2), (2, 300, 256, 32), (1, 1000, 7, 1), (2, 64, 2060, 5),
-         (1, 4, 4200, 2), (70, 5, 40, 4), (1, 4000, 64, 64)]
+         (1, 4, 4200, 2), (70, 5, 40, 4), (1, 4000, 64, 64), (2, 2000, 8, 2), (3, 31, 1024, 16), (2, 8, 4096, 512), (2, 8, 1040, 520), (1, 5000, 16, 1), (2, 61, 513, 9)]
 
 
 @pytest.fixture(autouse=True)
