@@ -13,10 +13,10 @@
 
 namespace tmps {
 
-// z = gain xhat + shift in single steps, so that both passes have the same bits and a ReLU the same border.
+// xhat = (x - mean) rstd and z = gain xhat + shift, the same bits in both passes (and so a ReLU's border).  The mean is taken off first: of values that are all the same nothing is left.
 __device__ __forceinline__ float norm_z(float x, float mean, float rstd, float gain, float shift, float& xhat) {
     xhat = (x - mean) * rstd;
-    return gain * xhat + shift;
+    return fmaf(gain, xhat, shift);
 }
 
 // The hardware's exponential and reciprocal are off by some 2^-23, enough for results of 8 bits, not for fp32.
@@ -29,6 +29,19 @@ template <typename T> __device__ __forceinline__ float norm_act(int act, float z
     if (act == kNormActGelu) return sizeof(T) == 2 ? gelu_f(z) : z * (0.5f + 0.5f * erff(z * 0.70710678118654752f));
     if (act == kNormActSilu) return z * norm_sigmoid<T>(z);
     return z;
+}
+// (the activation is asked for once)
+template <typename T, int V> __device__ __forceinline__ void norm_act_all(int act, float (&z)[V]) {
+    if (act == kNormActSilu) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = norm_act<T>(kNormActSilu, z[e]);
+    } else if (act == kNormActRelu) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = norm_act<T>(kNormActRelu, z[e]);
+    } else if (act == kNormActGelu) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = norm_act<T>(kNormActGelu, z[e]);
+    }
 }
 template <typename T> __device__ __forceinline__ float norm_act_grad(int act, float z, float dy) {
     if (act == kNormActRelu) return z > 0.0f ? dy : 0.0f;
@@ -64,6 +77,7 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
     if (row >= step) return;   // (teams of a workgroup with barriers are the whole of it)
     int place = 0;
     const int group = (int)(row % a.groups);
+    const float part = 1.0f / (float)D;   // (a quotient and a root of every row, by the library, would be a fifth of its instructions; the hardware's root is off by a step)
     float gain[N][V], shift[N][V];
     uint4 next[N];
     request_row(next, (const T*)a.x + row * D, p);
@@ -78,7 +92,7 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             unpack(next[i], v[i]);
-            if (p.any(i)) {
+            if (!a.rms && p.any(i)) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) s[0] += p.own(i, e) ? v[i][e] : 0.0f;
             }
@@ -86,28 +100,33 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
         if (row + step < rows) request_row(next, (const T*)a.x + (row + step) * D, p);
         if (!a.rms) {
             Team<TEAM>::sums(s, red, place);
-            mean = s[0] / (float)D;
+            mean = s[0] * part;
         }
         s[0] = 0.0f;
+        const auto squares = [&](float of) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (p.any(i)) {
+            for (int i = 0; i < N; ++i)
+                if (p.any(i)) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float d = p.own(i, e) ? v[i][e] - mean : 0.0f;
-                    s[0] = fmaf(d, d, s[0]);
+                    for (int e = 0; e < V; ++e) {
+                        const float d = p.own(i, e) ? v[i][e] - of : 0.0f;
+                        s[0] = fmaf(d, d, s[0]);
+                    }
                 }
-            }
+        };
+        if (a.rms) squares(0.0f);
+        else squares(mean);
         Team<TEAM>::sums(s, red, place);
-        const float rstd = 1.0f / sqrtf(s[0] / (float)D + 1e-5f);
+        const float rstd = __builtin_amdgcn_rsqf(fmaf(s[0], part, 1e-5f));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (!p.any(i)) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float xhat;
-                v[i][e] = norm_act<T>(a.act, norm_z(v[i][e], mean, rstd, gain[i][e], shift[i][e], xhat));
+                v[i][e] = norm_z(v[i][e], mean, rstd, gain[i][e], shift[i][e], xhat);
             }
+            norm_act_all<T>(a.act, v[i]);
             store_piece((T*)a.y + row * D, p, i, v[i]);
         }
         if (threadIdx.x % TEAM == 0) {
@@ -128,6 +147,7 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
     if (row >= step) return;
     int place = 0;
     const int group = (int)(row % a.groups);
+    const float share = 1.0f / (float)D;
     float* const mine = part + (row / a.groups) * 2 * (int64_t)a.channels + (int64_t)group * D;
     float gain[N][V], shift[N][V], dgain[N][V], dshift[N][V];
 #pragma unroll
@@ -169,7 +189,7 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
             }
         }
         Team<TEAM>::sums(s, red, place);
-        const float of_mean = a.rms ? 0.0f : s[0] / (float)D, of_xhat = s[1] / (float)D;
+        const float of_mean = a.rms ? 0.0f : s[0] * share, of_xhat = s[1] * share;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (!p.any(i)) continue;
@@ -385,8 +405,9 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_apply_ker
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float xhat;
-                v[e] = norm_act<T>(a.act, norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat));
+                v[e] = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
             }
+            norm_act_all<T>(a.act, v);
             p.store(y + at * a.channels, v);
         }
     }
@@ -652,8 +673,9 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             float xhat;
-            v[e] = norm_act<T>(a.act, norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat));
+            v[e] = norm_z(v[e], mean[e], rstd[e], gain[e], shift[e], xhat);
         }
+        norm_act_all<T>(a.act, v);
         p.store(y + (int64_t)(p.lane + k * p.lanes) * a.channels, v);
     }
 }
