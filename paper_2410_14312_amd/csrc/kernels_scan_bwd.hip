@@ -3,8 +3,8 @@
 // Two walks leave, for every chunk of 64 positions, the state S before it and the gradient G of the state behind it (the recurrence's adjoint: G <- d_end G + sum_t d_t dy_t C_t').  Chunks
 // are independent then.  With Z[t][s] = C_t . B_s, R[t][s] = dy_t . x_s, D the decays, w_s = D[end][s] delta_s, sums over s <= t:
 //   dx_s = sum_t Z D delta_s dy_t + w_s G B_s + skip dy_s      dB_s = sum_t R D delta_s C_t + w_s G' x_s      dC_t = sum_s R D delta_s B_s + d_t S' dy_t
-// The exponent up to t is in the row t of Z R D delta and in d_t with a plus, in the column t and in w_t with a minus: the gradient of position t's own exponent is the sum of those
-// differences over the chunk's positions from t on, and <S behind the chunk, G>.  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
+// With q = Z R D, the gradient of position t's own exponent is what passes through it: sum_{t' >= t > s} q[t'][s] delta_s, and of the states sum_{t' >= t} d_t' C_t' S' dy_t' +
+// sum_{s < t} w_s x_s G B_s + d_end <S, G>.  The first is had from sums over the rows and columns of tiles of 16 positions, without differences but inside a tile.  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
 // once and whose gradients of B and C stay in its accumulators.
 #include "launch.h"
 #include "scan_walk.hip.h"
@@ -20,13 +20,20 @@ struct ScanGrad {
     int chunks, parts, each, slices;
 };
 
-// over the 16 lanes of a row
-__device__ __forceinline__ float lane_sum16(float v) {
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false));   // row_ror:8
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xF, 0xF, false));   // row_ror:4
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xF, 0xF, false));   // row_ror:2
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xF, 0xF, false));   // row_ror:1
-    return v;
+// Sums of 16 values over the 16 lanes of a row: lane i of them has that of value i.  Each step halves the values: 45 instructions, where a sum of each in all lanes takes 64.
+template <int CTRL, int N> __device__ __forceinline__ void halve(float (&v)[16], bool upper) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float keep = upper ? v[i + N] : v[i], give = upper ? v[i] : v[i + N];
+        v[i] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), CTRL, 0xF, 0xF, false));
+    }
+}
+__device__ __forceinline__ float sixteen_sums(float (&v)[16], int lane) {
+    halve<0x128, 8>(v, lane & 8);   // row_ror:8: lane ^ 8
+    halve<0x141, 4>(v, lane & 4);   // row_half_mirror: lane ^ 7
+    halve<0x1B, 2>(v, lane & 2);    // quad_perm 3, 2, 1, 0: lane ^ 3
+    halve<0xB1, 1>(v, lane & 1);    // quad_perm 1, 0, 3, 2: lane ^ 1
+    return v[0];
 }
 // over the four lanes of a column
 __device__ __forceinline__ float column_sum(float v) {
@@ -40,11 +47,11 @@ constexpr int kGradDecays = 2;   // heads whose decays are formed at a time, a w
 
 template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGroups<T, NP> ? 2 : 1)) void scan_grad_kernel(ScanGrad a) {
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, MP = kScanChunk + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
-    constexpr int GT = kStateTerms<T>;
+    constexpr int GT = kResultTerms<T>;   // of S and G
     constexpr int kState = PP * NP / 4 / 256;   // fours of a state of a thread
     __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[kScanChunk * MP];
     __shared__ __attribute__((aligned(16))) ChunkDecays decays[kGradDecays];
-    __shared__ float rowq[4][kScanChunk], ya[kScanChunk], gs[kScanChunk], red[4][2];
+    __shared__ float colq[4][kScanChunk], rowq[kScanChunk], diagq[kScanChunk], of_c[kScanChunk], of_b[kScanChunk], red[4][2];
     const ScanBackward& b = a.b;
     const Scan& f = b.f;
     const int64_t units = f.samples * a.chunks * f.groups * a.parts;
@@ -93,7 +100,6 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
         const int head = group * in_group + h;
         const float skip = f.skip[head];
         float dskip = 0.0f, meet = 0.0f;   // sums of dy x and of S G
-        float end_sum = 0.0f;              // of w_s x_s G B_s (a lane's column)
         for (int slice = 0; slice < a.slices; ++slice) {
             const int p0 = slice * 64, width = min(64, f.dh - p0);
             ChunkRows<T, PP, 256> rx, rd;
@@ -138,20 +144,14 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             for (int i = 0; i < kState; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) meet = fmaf(s4[i][e], g4[i][e], meet);
-#pragma unroll
-            for (int i = 0; i < ChunkRows<T, PP, 256>::kMany; ++i) {
-                float vx[V], vd[V];
-                unpack(rx.u[i], vx);
-                unpack(rd.u[i], vd);
-#pragma unroll
-                for (int e = 0; e < V; ++e) dskip = fmaf(vx[e], vd[e], dskip);
-            }
             __syncthreads();
             const ChunkDecays& d = decays[(h - first) % kGradDecays];
 
             // by columns t
             f32x4_t m[4], dz[4];
-            float from_row = 0.0f;
+            float from_row = 0.0f, q16[16];
+            // (accumulated over a head's slices)
+            const auto put_sum = [&](float& to, float v) { to = slice == 0 ? v : to + v; };
             Oct<T> dyf[PK];
 #pragma unroll
             for (int k = 0; k < PK; ++k) dyf[k] = along<false>(dys + own * XP, 32 * k, lane);
@@ -181,24 +181,24 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float zd = z[st][e] * decay[e];
-                        const float q = r[e] * zd;
+                        float q = r[e] * zd;
                         m[st][e] = zd * delta_s[e];
                         dz[st][e] = r[e] * (decay[e] * delta_s[e]);
+                        if (st == wave && 4 * g + e == col) {   // (a position's own: nothing passes through)
+                            put_sum(diagq[own], q);
+                            dskip += r[e];
+                            q = 0.0f;
+                        }
                         from_row = fmaf(q, delta_s[e], from_row);
                         r[e] = q;
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float q = lane_sum16(r[e]);
-                    if (col == 0) {
-                        if (slice == 0) rowq[wave][16 * st + 4 * g + e] = q;
-                        else rowq[wave][16 * st + 4 * g + e] += q;
-                    }
-                }
+                for (int e = 0; e < 4; ++e) q16[4 * st + e] = r[e];
                 const float v[4] = {m[st][0], m[st][1], m[st][2], m[st][3]};
                 put_four(mm + own * MP + 16 * st + 4 * g, v);
             }
+            put_sum(colq[wave][16 * (col >> 2) + 4 * g + (col & 3)], sixteen_sums(q16, lane));
             float with_c = 0.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -221,10 +221,11 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 for (int e = 0; e < 4; ++e) with_c = fmaf(v[e], c[e], with_c);
                 dc[nt] += v * d.from[own];
             }
-            from_row = column_sum(fmaf(d.from[own], with_c, from_row));
+            from_row = column_sum(from_row);
+            with_c = column_sum(with_c);
             if (g == 0) {
-                if (slice == 0) ya[own] = from_row;
-                else ya[own] += from_row;
+                put_sum(rowq[own], from_row);
+                put_sum(of_c[own], with_c);
             }
             __syncthreads();   // (S has been read, the decayed products are there)
 
@@ -287,14 +288,10 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 db[nt] += v * to;
             }
             with_b = column_sum(with_b);
-            if (g == 0) {
-                if (slice == 0) gs[own] = with_b;
-                else gs[own] += with_b;
-                end_sum = fmaf(to, with_b, end_sum);
-            }
+            if (g == 0) put_sum(of_b[own], with_b);
         }
         // the head's steps and parameters
-        const float meet_all = wsum(meet * decays[(h - first) % kGradDecays].end + end_sum), skip_all = wsum(dskip);
+        const float meet_all = wsum(meet), skip_all = wsum(dskip);
         if (lane == 0) {
             red[wave][0] = meet_all;
             red[wave][1] = skip_all;
@@ -302,18 +299,46 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
         __syncthreads();
         if (wave == 0) {
             const ChunkDecays& d = decays[(h - first) % kGradDecays];
-            const double rate = exp((double)f.a_log[head]);
-            const float q = (rowq[0][lane] + rowq[1][lane]) + (rowq[2][lane] + rowq[3][lane]), delta = d.delta[lane], with_g = gs[lane];
-            double sum = (double)ya[lane] - ((double)delta * (double)q + (double)d.to[lane] * (double)with_g);
+            const float rate = (float)exp((double)f.a_log[head]), delta = d.delta[lane], slope = d.slope[lane];
+            // sums of q over the positions of each tile of 16, from the tile of position s (its own, below) on
+            const int tile = lane >> 4;
+            float later[4], in_tile = 0.0f, behind = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                later[w] = w > tile ? colq[w][lane] : 0.0f;
+                in_tile = w == tile ? colq[w][lane] : in_tile;
+                behind += later[w];
+            }
+            // tiles before t's to tiles behind it
+            float over1 = tile == 0 ? delta * (later[2] + later[3]) : 0.0f, over2 = tile <= 1 ? delta * later[3] : 0.0f;
+            over1 = wsum(over1);
+            over2 = wsum(over2);
+            // in tile order: from t on of rows (less what lies inside the tile from t on), before t of columns
+            float rows_on = rowq[lane] - delta * in_tile, columns_before = delta * behind;
+#pragma unroll
+            for (int k = 1; k < 16; k <<= 1) {
+                const float on = __shfl_down(rows_on, k, 16), before = __shfl_up(columns_before, k, 16);
+                if ((lane & 15) + k < 16) rows_on += on;
+                if ((lane & 15) >= k) columns_before += before;
+            }
+            columns_before = __shfl_up(columns_before, 1, 16);
+            columns_before = (lane & 15) ? columns_before : 0.0f;
+            // of the states: from t on, and before t
+            const float with_g = of_b[lane];
+            float states_on = d.from[lane] * of_c[lane], states_before = d.to[lane] * with_g;
 #pragma unroll
             for (int k = 1; k < 64; k <<= 1) {
-                const double behind = __shfl_down(sum, k);
-                if (lane + k < 64) sum += behind;
+                const float on = __shfl_down(states_on, k), before = __shfl_up(states_before, k);
+                if (lane + k < 64) states_on += on;
+                if (lane >= k) states_before += before;
             }
-            const double of_exponent = sum + (((double)red[0][0] + (double)red[1][0]) + ((double)red[2][0] + (double)red[3][0]));
-            const float ddelta = (float)((double)q + (double)d.back[lane] * (double)with_g - rate * of_exponent), du = lane < rows ? ddelta * d.slope[lane] : 0.0f;
+            states_before = __shfl_up(states_before, 1);
+            states_before = lane ? states_before : 0.0f;
+            const float whole = d.end * ((red[0][0] + red[1][0]) + (red[2][0] + red[3][0]));
+            const float of_exponent = ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
+            const float ddelta = fmaf(-rate, of_exponent, (diagq[lane] + (in_tile + behind)) + d.back[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;
             if (lane < rows) ((T*)b.ddt)[(row0 + lane) * b.ddt_stride + head] = from_f32<T>(du);
-            const float drate = wsum(lane < rows ? (float)(-rate * (double)delta * of_exponent) : 0.0f), dbias = wsum(du);
+            const float drate = wsum(lane < rows ? -rate * delta * of_exponent : 0.0f), dbias = wsum(du);
             if (lane == 0) {
                 float* const to = a.sums + (sample * a.chunks + chunk) * 3 * f.heads + head;
                 to[0] = drate;
