@@ -49,7 +49,8 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, MP = kScanChunk + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
     constexpr int GT = kResultTerms<T>;   // of S and G
     constexpr int kState = PP * NP / 4 / 256;   // fours of a state of a thread
-    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[kScanChunk * MP];
+    constexpr bool kApart = sizeof(T) == 2;     // the decayed products and their gradients in memory of their own (fp32: one after the other)
+    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[(kApart ? 2 : 1) * kScanChunk * MP];
     __shared__ __attribute__((aligned(16))) ChunkDecays decays[kGradDecays];
     __shared__ float colq[4][kScanChunk], rowq[kScanChunk], diagq[kScanChunk], of_c[kScanChunk], of_b[kScanChunk], red[4][2];
     const ScanBackward& b = a.b;
@@ -197,6 +198,10 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 for (int e = 0; e < 4; ++e) q16[4 * st + e] = r[e];
                 const float v[4] = {m[st][0], m[st][1], m[st][2], m[st][3]};
                 put_four(mm + own * MP + 16 * st + 4 * g, v);
+                if constexpr (kApart) {
+                    const float u[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
+                    put_four(mm + kScanChunk * MP + own * MP + 16 * st + 4 * g, u);
+                }
             }
             put_sum(colq[wave][16 * (col >> 2) + 4 * g + (col & 3)], sixteen_sums(q16, lane));
             float with_c = 0.0f;
@@ -241,13 +246,23 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                     dx[j] = mma(across<false>(dys, XP, 32 * pair, 16 * j, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), dx[j]);
                 }
             }
-            __syncthreads();
+            if constexpr (!kApart) {
+                __syncthreads();
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                const float v[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
-                put_four(mm + own * MP + 16 * st + 4 * g, v);
+                for (int st = 0; st < 4; ++st) {
+                    const float v[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
+                    put_four(mm + own * MP + 16 * st + 4 * g, v);
+                }
+                __syncthreads();
             }
-            __syncthreads();
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    if (2 * pair + 1 < wave) continue;
+                    db[nt] = mma(across<false>(cs, BP, 32 * pair, 16 * nt, lane), across<false>(mm + (kApart ? kScanChunk * MP : 0), MP, 32 * pair, 16 * wave, lane), db[nt]);
+                }
+            if constexpr (kApart) __syncthreads();   // (G is there)
             Oct<T> xf[PK], bf[NK];
 #pragma unroll
             for (int k = 0; k < PK; ++k) xf[k] = along<false>(xs + own * XP, 32 * k, lane);
@@ -271,11 +286,6 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             float with_b = 0.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int pair = 0; pair < 2; ++pair) {
-                    if (2 * pair + 1 < wave) continue;
-                    db[nt] = mma(across<false>(cs, BP, 32 * pair, 16 * nt, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), db[nt]);
-                }
                 f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int term = GT - 1; term >= 0; --term)
