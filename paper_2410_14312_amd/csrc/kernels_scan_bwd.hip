@@ -43,16 +43,23 @@ __device__ __forceinline__ float column_sum(float v) {
 
 // Whether LDS holds what two workgroups of a compute unit need.
 template <typename T, int NP> constexpr bool kTwoGroups = sizeof(T) == 2 && NP <= 64;
-constexpr int kGradDecays = 2;   // heads whose decays are formed at a time, a wave each
+// Heads whose decays are formed before, and whose steps' gradients behind the others, at a time, a wave each: four, or what LDS holds.
+template <typename T, int NP> constexpr int kHeadsAtOnce = sizeof(T) == 4 && NP == 128 ? 2 : 4;
+
+// Of a head's chunk: sums of q over the rows of each tile of 16 positions by column, over a row's earlier columns, q of each position itself, C S' dy and x G B, and of each wave its parts of
+// <S, G> and of dy x.
+struct HeadSums {
+    float columns[4][kScanChunk], row[kScanChunk], self[kScanChunk], of_c[kScanChunk], of_b[kScanChunk], parts[4][2];
+};
 
 template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGroups<T, NP> ? 2 : 1)) void scan_grad_kernel(ScanGrad a) {
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, MP = kScanChunk + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
     constexpr int GT = kResultTerms<T>;   // of S and G
+    constexpr int kHeads = kHeadsAtOnce<T, NP>;
     constexpr int kState = PP * NP / 4 / 256;   // fours of a state of a thread
-    constexpr bool kApart = sizeof(T) == 2;     // the decayed products and their gradients in memory of their own (fp32: one after the other)
-    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[(kApart ? 2 : 1) * kScanChunk * MP];
-    __shared__ __attribute__((aligned(16))) ChunkDecays decays[kGradDecays];
-    __shared__ float colq[4][kScanChunk], rowq[kScanChunk], diagq[kScanChunk], of_c[kScanChunk], of_b[kScanChunk], red[4][2];
+    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[kScanChunk * MP];
+    __shared__ __attribute__((aligned(16))) ChunkDecays<true> decays[kHeads];
+    __shared__ HeadSums sums[kHeads];
     const ScanBackward& b = a.b;
     const Scan& f = b.f;
     const int64_t units = f.samples * a.chunks * f.groups * a.parts;
@@ -97,34 +104,45 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) db[nt] = dc[nt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
+    const bool plain = rows == kScanChunk && f.dh % PP == 0;   // (no zeros to be put in)
+    ChunkRows<T, PP, 256> rx, rd;
+    rx.places_all(f.x_stride, 0, wide);
+    rd.places_all(b.dy_stride, 0, inner);
     for (int h = first; h < last; ++h) {
         const int head = group * in_group + h;
         const float skip = f.skip[head];
         float dskip = 0.0f, meet = 0.0f;   // sums of dy x and of S G
         for (int slice = 0; slice < a.slices; ++slice) {
             const int p0 = slice * 64, width = min(64, f.dh - p0);
-            ChunkRows<T, PP, 256> rx, rd;
             const int at = head * f.dh + p0;
-            rx.places_all(f.x_stride, at, wide);
-            rd.places_all(b.dy_stride, at, inner);
-            rx.request_all((const T*)f.x + row0 * f.x_stride, f.x_stride, rows, at, wide);
-            rd.request_all((const T*)b.dy + row0 * b.dy_stride, b.dy_stride, rows, at, inner);
-            const int64_t of_state = (((sample * f.heads + head) * a.chunks + chunk) * a.slices + slice) * (int64_t)(PP * NP);
+            const T *xg = (const T*)f.x + row0 * f.x_stride, *dyg = (const T*)b.dy + row0 * b.dy_stride;
+            if (plain) {   // (the same places in each head's columns)
+                xg += at;
+                dyg += at;
+            } else {
+                rx.places_all(f.x_stride, at, wide);
+                rd.places_all(b.dy_stride, at, inner);
+            }
+            rx.request_all(xg, f.x_stride, rows, at, wide);
+            rd.request_all(dyg, b.dy_stride, rows, at, inner);
             float s4[kState][4], g4[kState][4];
+            const int64_t of_state = (((sample * f.heads + head) * a.chunks + chunk) * a.slices + slice) * (int64_t)(PP * NP);
+            const float *const before = a.before + of_state, *const behind = a.behind + of_state;
 #pragma unroll
             for (int i = 0; i < kState; ++i) {
-                const int k = (int)threadIdx.x + 256 * i;
-                four(a.before + of_state + 4 * k, s4[i]);
-                four(a.behind + of_state + 4 * k, g4[i]);
+                four(before + 4 * threadIdx.x + 1024 * i, s4[i]);
+                four(behind + 4 * threadIdx.x + 1024 * i, g4[i]);
             }
             __syncthreads();   // (what the head or slice before has left in LDS has been read)
-            if (slice == 0 && (h - first) % kGradDecays == 0 && wave < kGradDecays && h + wave < last) {
+            if (slice == 0 && (h - first) % kHeads == 0 && wave < kHeads && h + wave < last) {
                 const int mine = head + wave;
-                chunk_decays<true>(decays[wave], to_f32(((const T*)f.dt)[(row0 + min(lane, rows - 1)) * f.dt_stride + mine]), rows, f.dt_bias[mine],
+                chunk_decays(decays[wave], to_f32(((const T*)f.dt)[(row0 + min(lane, rows - 1)) * f.dt_stride + mine]), rows, f.dt_bias[mine],
                                    exp((double)f.a_log[mine]) * kLog2eD, lane);
             }
-            rx.settle_all(rows, width, at, wide);
-            rd.settle_all(rows, width, at, inner);
+            if (!plain) {
+                rx.settle_all(rows, width, at, wide);
+                rd.settle_all(rows, width, at, inner);
+            }
             rx.template put<XP>(xs);
             rd.template put<XP>(dys);
             const auto put_state = [&](const float (&v)[kState][4]) {
@@ -146,11 +164,12 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
 #pragma unroll
                 for (int e = 0; e < 4; ++e) meet = fmaf(s4[i][e], g4[i][e], meet);
             __syncthreads();
-            const ChunkDecays& d = decays[(h - first) % kGradDecays];
+            const ChunkDecays<true>& d = decays[(h - first) % kHeads];
+            HeadSums& sum = sums[(h - first) % kHeads];
 
             // by columns t
             f32x4_t m[4], dz[4];
-            float from_row = 0.0f, q16[16];
+            float from_row = 0.0f, of_self = 0.0f, q16[16];
             // (accumulated over a head's slices)
             const auto put_sum = [&](float& to, float v) { to = slice == 0 ? v : to + v; };
             Oct<T> dyf[PK];
@@ -185,10 +204,11 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                         float q = r[e] * zd;
                         m[st][e] = zd * delta_s[e];
                         dz[st][e] = r[e] * (decay[e] * delta_s[e]);
-                        if (st == wave && 4 * g + e == col) {   // (a position's own: nothing passes through)
-                            put_sum(diagq[own], q);
-                            dskip += r[e];
-                            q = 0.0f;
+                        if (st == wave) {   // (of a position itself nothing passes through)
+                            const bool self = 4 * g + e == col;
+                            of_self = self ? q : of_self;
+                            dskip += self ? r[e] : 0.0f;
+                            q = self ? 0.0f : q;
                         }
                         from_row = fmaf(q, delta_s[e], from_row);
                         r[e] = q;
@@ -198,12 +218,9 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 for (int e = 0; e < 4; ++e) q16[4 * st + e] = r[e];
                 const float v[4] = {m[st][0], m[st][1], m[st][2], m[st][3]};
                 put_four(mm + own * MP + 16 * st + 4 * g, v);
-                if constexpr (kApart) {
-                    const float u[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
-                    put_four(mm + kScanChunk * MP + own * MP + 16 * st + 4 * g, u);
-                }
             }
-            put_sum(colq[wave][16 * (col >> 2) + 4 * g + (col & 3)], sixteen_sums(q16, lane));
+            put_sum(sum.columns[wave][16 * (col >> 2) + 4 * g + (col & 3)], sixteen_sums(q16, lane));
+            if (col >> 2 == g) put_sum(sum.self[own], of_self);
             float with_c = 0.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -229,8 +246,8 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             from_row = column_sum(from_row);
             with_c = column_sum(with_c);
             if (g == 0) {
-                put_sum(rowq[own], from_row);
-                put_sum(of_c[own], with_c);
+                put_sum(sum.row[own], from_row);
+                put_sum(sum.of_c[own], with_c);
             }
             __syncthreads();   // (S has been read, the decayed products are there)
 
@@ -246,29 +263,26 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                     dx[j] = mma(across<false>(dys, XP, 32 * pair, 16 * j, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), dx[j]);
                 }
             }
-            if constexpr (!kApart) {
-                __syncthreads();
+            __syncthreads();
 #pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const float v[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
-                    put_four(mm + own * MP + 16 * st + 4 * g, v);
-                }
-                __syncthreads();
+            for (int st = 0; st < 4; ++st) {
+                const float v[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
+                put_four(mm + own * MP + 16 * st + 4 * g, v);
             }
+            __syncthreads();
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int pair = 0; pair < 2; ++pair) {
                     if (2 * pair + 1 < wave) continue;
-                    db[nt] = mma(across<false>(cs, BP, 32 * pair, 16 * nt, lane), across<false>(mm + (kApart ? kScanChunk * MP : 0), MP, 32 * pair, 16 * wave, lane), db[nt]);
+                    db[nt] = mma(across<false>(cs, BP, 32 * pair, 16 * nt, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), db[nt]);
                 }
-            if constexpr (kApart) __syncthreads();   // (G is there)
             Oct<T> xf[PK], bf[NK];
 #pragma unroll
             for (int k = 0; k < PK; ++k) xf[k] = along<false>(xs + own * XP, 32 * k, lane);
 #pragma unroll
             for (int k = 0; k < NK; ++k) bf[k] = along<false>(bs + own * BP, 32 * k, lane);
-            const float to = d.to[own];
+            const float to = d.delta[own] * d.to[own];
 #pragma unroll
             for (int j = 0; j < PT; ++j) {
                 f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -298,25 +312,29 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 db[nt] += v * to;
             }
             with_b = column_sum(with_b);
-            if (g == 0) put_sum(of_b[own], with_b);
+            if (g == 0) put_sum(sum.of_b[own], with_b);
         }
-        // the head's steps and parameters
         const float meet_all = wsum(meet), skip_all = wsum(dskip);
         if (lane == 0) {
-            red[wave][0] = meet_all;
-            red[wave][1] = skip_all;
+            sums[(h - first) % kHeads].parts[wave][0] = meet_all;
+            sums[(h - first) % kHeads].parts[wave][1] = skip_all;
         }
+        if ((h - first) % kHeads != kHeads - 1 && h + 1 < last) continue;
+        // the heads' steps and parameters, a head to a wave
         __syncthreads();
-        if (wave == 0) {
-            const ChunkDecays& d = decays[(h - first) % kGradDecays];
+        const int mine = h - (h - first) % kHeads + wave;
+        if (wave < kHeads && mine <= h) {
+            const int head = group * in_group + mine;
+            const ChunkDecays<true>& d = decays[wave];
+            const HeadSums& sum = sums[wave];
             const float rate = (float)exp((double)f.a_log[head]), delta = d.delta[lane], slope = d.slope[lane];
             // sums of q over the positions of each tile of 16, from the tile of position s (its own, below) on
             const int tile = lane >> 4;
             float later[4], in_tile = 0.0f, behind = 0.0f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                later[w] = w > tile ? colq[w][lane] : 0.0f;
-                in_tile = w == tile ? colq[w][lane] : in_tile;
+                later[w] = w > tile ? sum.columns[w][lane] : 0.0f;
+                in_tile = w == tile ? sum.columns[w][lane] : in_tile;
                 behind += later[w];
             }
             // tiles before t's to tiles behind it
@@ -324,7 +342,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             over1 = wsum(over1);
             over2 = wsum(over2);
             // in tile order: from t on of rows (less what lies inside the tile from t on), before t of columns
-            float rows_on = rowq[lane] - delta * in_tile, columns_before = delta * behind;
+            float rows_on = sum.row[lane] - delta * in_tile, columns_before = delta * behind;
 #pragma unroll
             for (int k = 1; k < 16; k <<= 1) {
                 const float on = __shfl_down(rows_on, k, 16), before = __shfl_up(columns_before, k, 16);
@@ -334,8 +352,8 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             columns_before = __shfl_up(columns_before, 1, 16);
             columns_before = (lane & 15) ? columns_before : 0.0f;
             // of the states: from t on, and before t
-            const float with_g = of_b[lane];
-            float states_on = d.from[lane] * of_c[lane], states_before = d.to[lane] * with_g;
+            const float with_g = sum.of_b[lane];
+            float states_on = d.from[lane] * sum.of_c[lane], states_before = delta * d.to[lane] * with_g;
 #pragma unroll
             for (int k = 1; k < 64; k <<= 1) {
                 const float on = __shfl_down(states_on, k), before = __shfl_up(states_before, k);
@@ -344,15 +362,15 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             }
             states_before = __shfl_up(states_before, 1);
             states_before = lane ? states_before : 0.0f;
-            const float whole = d.end * ((red[0][0] + red[1][0]) + (red[2][0] + red[3][0]));
+            const float whole = d.end * ((sum.parts[0][0] + sum.parts[1][0]) + (sum.parts[2][0] + sum.parts[3][0]));
             const float of_exponent = ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
-            const float ddelta = fmaf(-rate, of_exponent, (diagq[lane] + (in_tile + behind)) + d.back[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;
+            const float ddelta = fmaf(-rate, of_exponent, (sum.self[lane] + (in_tile + behind)) + d.to[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;
             if (lane < rows) ((T*)b.ddt)[(row0 + lane) * b.ddt_stride + head] = from_f32<T>(du);
             const float drate = wsum(lane < rows ? -rate * delta * of_exponent : 0.0f), dbias = wsum(du);
             if (lane == 0) {
                 float* const to = a.sums + (sample * a.chunks + chunk) * 3 * f.heads + head;
                 to[0] = drate;
-                to[f.heads] = (red[0][1] + red[1][1]) + (red[2][1] + red[3][1]);
+                to[f.heads] = (sum.parts[0][1] + sum.parts[1][1]) + (sum.parts[2][1] + sum.parts[3][1]);
                 to[2 * f.heads] = dbias;
             }
         }

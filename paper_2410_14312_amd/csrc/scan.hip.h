@@ -220,10 +220,10 @@ template <typename T, int W, int THREADS> struct ChunkRows : Requests<T, kScanCh
 };
 
 // The steps and decays of a chunk, a position to a lane: delta, the sum of the exponents up to the position in units of log 2 (in two floats: of sums of hundreds their differences keep
-// their last places), the decay from before the chunk, that to its end and delta times it, that to the end of the position's sixteen, and the slope of softplus.  Positions behind the last
-// have delta 0: they change nothing.
-struct ChunkDecays {
-    float delta[kScanChunk], sum[kScanChunk], rest[kScanChunk], from[kScanChunk], back[kScanChunk], to[kScanChunk], tile[kScanChunk], slope[kScanChunk];
+// their last places), the decay from before the chunk, that to the end of the position's sixteen and that to the chunk's end, for the walks times delta, for the gradients alone; and for
+// those the slope of softplus.  Positions behind the last have delta 0: they change nothing.
+template <bool GRADIENTS> struct ChunkDecays {
+    float delta[kScanChunk], sum[kScanChunk], rest[kScanChunk], from[kScanChunk], tile[kScanChunk], to[kScanChunk], slope[GRADIENTS ? kScanChunk : 4];
     float end;       // the decay over the whole chunk
     double total;    // its exponent
 };
@@ -238,7 +238,7 @@ __device__ __forceinline__ float exp2_of(double e) {
 }
 
 // dt: the position's (any number behind the last row).
-template <bool SLOPE> __device__ __forceinline__ void chunk_decays(ChunkDecays& d, float dt, int rows, float bias, double rate, int lane) {
+template <bool GRADIENTS> __device__ __forceinline__ void chunk_decays(ChunkDecays<GRADIENTS>& d, float dt, int rows, float bias, double rate, int lane) {
     const float u = dt + bias;
     const float delta = lane >= rows ? 0.0f : u != u ? u : softplus(u);
     double sum = -(double)delta * rate;
@@ -253,11 +253,9 @@ template <bool SLOPE> __device__ __forceinline__ void chunk_decays(ChunkDecays& 
     d.sum[lane] = hi;
     d.rest[lane] = hi - hi == 0.0f ? (float)(sum - (double)hi) : 0.0f;
     d.from[lane] = exp2_of(sum);
-    const float back = exp2_of(total - sum);
-    d.back[lane] = back;
-    d.to[lane] = delta * back;
+    d.to[lane] = exp2_of(total - sum) * (GRADIENTS ? 1.0f : delta);
     d.tile[lane] = exp2_of(of_tile - sum);
-    if constexpr (SLOPE) d.slope[lane] = lane < rows ? 1.0f / (1.0f + expf(-u)) : 0.0f;
+    if constexpr (GRADIENTS) d.slope[lane] = lane < rows ? 1.0f / (1.0f + expf(-u)) : 0.0f;
     if (lane == 63) {
         d.end = exp2_of(total);
         d.total = total;

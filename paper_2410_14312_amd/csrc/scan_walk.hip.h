@@ -51,7 +51,7 @@ template <typename T, int NP, int PT, bool OUT> struct WalkTiles {
     __attribute__((aligned(16))) T xs[kScanChunk * XP];
     __attribute__((aligned(16))) T bs[kScanChunk * BP];
     __attribute__((aligned(16))) T ss[OUT ? kResultTerms<T> * PP * BP : 8];
-    __attribute__((aligned(16))) ChunkDecays decays[4];
+    __attribute__((aligned(16))) ChunkDecays<false> decays[4];
     int odd[2];
 };
 
@@ -64,7 +64,7 @@ template <typename T, int NP, int PT, int LEAVES, bool REV> __device__ __forcein
     constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, NT = NP / 16, TW = NT * PT / 4, NK = NP / 32;
     constexpr int RT = kResultTerms<T>, ST = kStateTerms<T>;
     T *const xs = tiles.xs, *const bs = tiles.bs, *const ss = tiles.ss;
-    ChunkDecays* const decays = tiles.decays;
+    ChunkDecays<false>* const decays = tiles.decays;
     int* const odd = tiles.odd;
     const int slice = (int)(unit % a.slices);
     unit /= a.slices;
@@ -145,7 +145,7 @@ template <typename T, int NP, int PT, int LEAVES, bool REV> __device__ __forcein
         if constexpr (OUT) {
             if (xr.odd()) odd[i & 1] = 1;
         }
-        if ((i & 3) == 0) chunk_decays<false>(decays[wave], dt, i + wave < many ? rows_of(chunk_of(i + wave)) : 0, bias, rate, lane);
+        if ((i & 3) == 0) chunk_decays(decays[wave], dt, i + wave < many ? rows_of(chunk_of(i + wave)) : 0, bias, rate, lane);
     };
     double total = 0.0;
 
@@ -188,7 +188,7 @@ template <typename T, int NP, int PT, int LEAVES, bool REV> __device__ __forcein
         }
         request(i + 1);
         __builtin_amdgcn_sched_barrier(0);   // (they are under way before what the step computes, or there would be nothing to hide them behind)
-        const ChunkDecays& d = decays[i & 3];
+        const ChunkDecays<false>& d = decays[i & 3];
         if constexpr (OUT) {
             const int t = 16 * wave + col;
             const float sum_t = d.sum[t], rest_t = d.rest[t];
