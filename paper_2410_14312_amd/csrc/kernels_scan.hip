@@ -14,77 +14,90 @@
 namespace tmps {
 
 // ------------------------------------------------------------------------------------------------ single positions
-// 16 lanes to a feature, which share its state's n; four features at a time to each of 16 teams.
-template <typename T> __global__ __launch_bounds__(256) void scan_steps_kernel(Scan a) {
+// 16 lanes to a feature, which share its state's n, four neighbours to each (and as many 64 further, HALVES == 2); four features to each of 16 teams.  PLAIN: n is 64 HALVES and a head's
+// features whole 64s: every access is whole and none is in a branch, so that all of a thread's states are under way together.  64 sequences of 24 heads of 64 x 64: 25 MB read and 25
+// written.
+template <typename T, int HALVES, bool PLAIN> __global__ __launch_bounds__(256) void scan_steps_kernel(Scan a) {
     constexpr int kPasses = 4;
     const int64_t unit = blockIdx.x;
     const int head = (int)(unit % a.heads), group = head / (a.heads / a.groups);
     const int64_t sample = unit / a.heads;
-    const int lane = threadIdx.x & 15, team = threadIdx.x >> 4;
-    const double rate = exp((double)a.a_log[head]) * kLog2eD;
-    const float skip = a.skip[head], bias = a.dt_bias[head];
+    const int lane = threadIdx.x & 15, team = threadIdx.x >> 4, p0 = blockIdx.y * (16 * kPasses);
     const int64_t of_head = unit * a.dh * a.n;
     const T* const xr = (const T*)a.x + sample * a.positions * a.x_stride;
     const T* const dtr = (const T*)a.dt + sample * a.positions * a.dt_stride + head;
     T* const yr = (T*)a.y + sample * a.positions * a.y_stride + (int64_t)head * a.dh;
     const int64_t b_at = (int64_t)a.heads * a.dh + (int64_t)group * a.n, c_at = b_at + (int64_t)a.groups * a.n;
-    for (int p0 = blockIdx.y * (16 * kPasses); p0 < min(a.dh, (int)(blockIdx.y + 1) * (16 * kPasses)); p0 += 16 * kPasses) {
-        float s[kPasses][2][4];
+    float s[kPasses][HALVES][4];
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+        const int p = p0 + team + 16 * k;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+            const int n = 4 * lane + 64 * h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[k][h][e] = 0.0f;
+            if (a.state) {
+                if constexpr (PLAIN) unpack(load16_any(a.state + of_head + (int64_t)p * a.n + n), s[k][h]);
+                else if (p < a.dh && n < a.n) four_any(a.state + of_head + (int64_t)p * a.n + n, s[k][h], a.n - n);
+            }
+        }
+    }
+    const double rate = exp((double)a.a_log[head]) * kLog2eD;
+    const float skip = a.skip[head], bias = a.dt_bias[head];
+    for (int64_t t = 0; t < a.positions; ++t) {
+        const T* const row = xr + t * a.x_stride;
+        float b[HALVES][4], c[HALVES][4], x[kPasses];
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+            const int n = 4 * lane + 64 * h;
+            if constexpr (PLAIN) {
+                four_anywhere(row + b_at + n, b[h]);
+                four_anywhere(row + c_at + n, c[h]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool any = n + e < a.n;
+                    b[h][e] = any ? to_f32(row[b_at + (any ? n + e : 0)]) : 0.0f;
+                    c[h][e] = any ? to_f32(row[c_at + (any ? n + e : 0)]) : 0.0f;
+                }
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kPasses; ++k) {
             const int p = p0 + team + 16 * k;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int n = 4 * lane + 64 * h;
-                if (a.state && p < a.dh && n < a.n) four_any(a.state + of_head + (int64_t)p * a.n + n, s[k][h], a.n - n);
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[k][h][e] = 0.0f;
-            }
+            x[k] = PLAIN || p < a.dh ? to_f32(row[(int64_t)head * a.dh + p]) : 0.0f;
         }
-        for (int64_t t = 0; t < a.positions; ++t) {
-            const T* const row = xr + t * a.x_stride;
-            const float u = to_f32(dtr[t * a.dt_stride]) + bias, delta = u != u ? u : softplus(u);
-            const float decay = __builtin_amdgcn_exp2f((float)(-(double)delta * rate));
-            float b[2][4], c[2][4];
+        const float u = to_f32(dtr[t * a.dt_stride]) + bias, delta = u != u ? u : softplus(u);
+        const float decay = exp2_of(-(double)delta * rate);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int k = 0; k < kPasses; ++k) {
+            const int p = p0 + team + 16 * k;
+            const float add = delta * x[k];
+            float y = 0.0f;
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int n = 4 * lane + 64 * h + e;
-                    b[h][e] = n < a.n ? to_f32(row[b_at + n]) : 0.0f;
-                    c[h][e] = n < a.n ? to_f32(row[c_at + n]) : 0.0f;
+                    s[k][h][e] = fmaf(decay, s[k][h][e], add * b[h][e]);
+                    y = fmaf(s[k][h][e], c[h][e], y);
                 }
-#pragma unroll
-            for (int k = 0; k < kPasses; ++k) {
-                const int p = p0 + team + 16 * k;
-                const float x = p < a.dh ? to_f32(row[(int64_t)head * a.dh + p]) : 0.0f;
-                const float add = delta * x;
-                float y = 0.0f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[k][h][e] = fmaf(decay, s[k][h][e], add * b[h][e]);
-                        y = fmaf(s[k][h][e], c[h][e], y);
-                    }
-                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xF, 0xF, false));   // row_ror:8
-                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x124, 0xF, 0xF, false));   // row_ror:4
-                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x122, 0xF, 0xF, false));   // row_ror:2
-                y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x121, 0xF, 0xF, false));   // row_ror:1
-                if (lane == 0 && p < a.dh) yr[t * a.y_stride + p] = from_f32<T>(fmaf(skip, x, y));
-            }
+            y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x128, 0xF, 0xF, false));   // row_ror:8
+            y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x124, 0xF, 0xF, false));   // row_ror:4
+            y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x122, 0xF, 0xF, false));   // row_ror:2
+            y += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0x121, 0xF, 0xF, false));   // row_ror:1
+            if (lane == 0 && (PLAIN || p < a.dh)) yr[t * a.y_stride + p] = from_f32<T>(fmaf(skip, x[k], y));
         }
-        if (a.state_out) {
+    }
+    if (!a.state_out) return;
 #pragma unroll
-            for (int k = 0; k < kPasses; ++k) {
-                const int p = p0 + team + 16 * k;
+    for (int k = 0; k < kPasses; ++k) {
+        const int p = p0 + team + 16 * k;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int n = 4 * lane + 64 * h;
-                    if (p < a.dh && n < a.n) put_four_any(a.state_out + of_head + (int64_t)p * a.n + n, s[k][h], a.n - n);
-                }
-            }
+        for (int h = 0; h < HALVES; ++h) {
+            const int n = 4 * lane + 64 * h;
+            if constexpr (PLAIN) store16_any(a.state_out + of_head + (int64_t)p * a.n + n, pack(s[k][h]));
+            else if (p < a.dh && n < a.n) put_four_any(a.state_out + of_head + (int64_t)p * a.n + n, s[k][h], a.n - n);
         }
     }
 }
@@ -99,7 +112,10 @@ template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hi
     if (a.positions <= kScanSteps) {
         const int64_t units = a.samples * a.heads;
         if (units > INT32_MAX) return hipErrorInvalidValue;
-        return launch_timed(kcAttnFwd, scan_steps_kernel<T>, dim3((unsigned)units, (unsigned)((a.dh + 63) / 64)), dim3(256), 0, s, a);
+        const bool whole = a.dh % 64 == 0;
+        auto kern = a.n > 64 ? (whole && a.n == 128 ? scan_steps_kernel<T, 2, true> : scan_steps_kernel<T, 2, false>)
+                             : (whole && a.n == 64 ? scan_steps_kernel<T, 1, true> : scan_steps_kernel<T, 1, false>);
+        return launch_timed(kcAttnFwd, kern, dim3((unsigned)units, (unsigned)((a.dh + 63) / 64)), dim3(256), 0, s, a);
     }
     ScanWalk w = walk_of(a);
     w.y = a.y; w.y_stride = a.y_stride;

@@ -93,6 +93,13 @@ __device__ __forceinline__ void four(const float* p, float (&v)[4]) {
     const float4 f = *reinterpret_cast<const float4*>(p);
     v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
 }
+__device__ __forceinline__ void four_anywhere(const bf16_t* p, float (&v)[4]) {   // (at any address)
+    const any_u32x2_t u = *reinterpret_cast<const any_u32x2_t*>(p);
+    const uint32_t a = u[0], b = u[1];
+    v[0] = __builtin_bit_cast(float, a << 16); v[1] = __builtin_bit_cast(float, a & 0xffff0000u);
+    v[2] = __builtin_bit_cast(float, b << 16); v[3] = __builtin_bit_cast(float, b & 0xffff0000u);
+}
+__device__ __forceinline__ void four_anywhere(const float* p, float (&v)[4]) { unpack(load16_any(p), v); }
 __device__ __forceinline__ void put_four(bf16_t* p, const float (&v)[4]) {   // (on 8 bytes)
     union { bf16_t h[4]; uint2 u; } k;
 #pragma unroll

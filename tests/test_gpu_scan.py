@@ -16,7 +16,7 @@ FP32, BF16, ROUNDED = 2.0 ** -16, 2.0 ** -15, 2.0 ** -8
 SIZES = [  # samples, positions, heads, dh, groups, n, from a given state
     (1, 1, 1, 1, 1, 1, False), (2, 1, 3, 64, 1, 64, True), (3, 8, 2, 20, 2, 128, True), (2, 9, 2, 16, 1, 16, True), (1, 63, 3, 32, 3, 32, False), (2, 64, 2, 64, 1, 64, True),
     (1, 65, 4, 40, 2, 24, True), (2, 130, 5, 7, 1, 5, True), (1, 200, 2, 64, 1, 128, True), (1, 100, 2, 128, 1, 33, True), (1, 70, 2, 65, 1, 127, False), (1, 1100, 2, 33, 1, 16, True),
-    (9, 33, 1, 200, 1, 100, True)]
+    (9, 33, 1, 200, 1, 100, True), (3, 2, 2, 128, 1, 128, True), (2, 5, 4, 64, 2, 64, False), (2, 3, 1, 96, 1, 128, True)]
 
 
 @pytest.fixture(autouse=True)
