@@ -331,7 +331,7 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_moments_k
     }
 }
 
-// Moments of a group from those of the 2^STEPS lanes that share it.
+// Moments of a group from those of the LANES lanes that share it.
 template <int LANES> __device__ __forceinline__ void join_lanes(float& n, float& mean, float& m2) {
 #pragma unroll
     for (int d = LANES / 2; d > 0; d >>= 1) {
@@ -793,6 +793,7 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
 // Slices of a sample's positions: as many as give the chip 2048 workgroups, of 32 positions at least.
 constexpr int kMapGroups = 2048, kMapPositions = 32;
 constexpr int kFoldColumns = 64;   // channels whose slices' sums a workgroup adds up, in whole groups
+static int fold_columns(int size) { return (kFoldColumns + size - 1) / size * size; }
 struct MapPlan {
     int64_t slice;
     int slices, blocks;   // blocks: of 256 pieces of channels
@@ -828,6 +829,17 @@ static int held_threads(int64_t positions, int channels, int groups, int V, int 
     for (int threads : {256, 1024})
         if (width <= threads && positions <= (int64_t)(threads / width) * pieces) return threads;
     return 0;
+}
+
+// Whether every launch of a forward and a backward pass can be had.
+bool group_norm_fits(int dtype, int64_t samples, int64_t positions, int channels, int groups) {
+    if (samples > INT32_MAX) return false;
+    // (below, products of samples with groups or slices are under 2^58)
+    if (samples == 0 || by_rows(positions, channels, groups)) return true;   // (teams are counted by the chip)
+    const int V = dtype == kBF16 ? 8 : 4, size = channels / groups, columns = fold_columns(size);
+    const MapPlan m = map_plan(samples, positions, channels, V);
+    return launchable(samples * m.slices, 256) && launchable((samples * groups + 3) / 4, 256) && launchable(samples * ((channels + columns - 1) / columns), 512) &&
+           launchable(samples, std::max(256, std::max(held_threads(positions, channels, groups, V, kHeldPieces), held_threads(positions, channels, groups, V, kHeldPairs))));
 }
 
 // (as much as any call of no more samples and positions takes)
@@ -875,7 +887,6 @@ template <typename T> static hipError_t forward_type(const GroupNorm& a, float* 
         return threads == 256 ? launch_timed(kcLayerNorm, group_held_fwd_kernel<T, 256>, dim3((unsigned)a.samples), dim3(256), 0, s, a)
                               : launch_timed(kcLayerNorm, group_held_fwd_kernel<T, 1024>, dim3((unsigned)a.samples), dim3(1024), 0, s, a);
     const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
-    if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
     hipError_t e = launch_timed(kcLayerNorm, group_map_moments_kernel<T>, grid, dim3(256), 0, s, (const T*)a.x, a.positions, a.channels, m.slice, m.slices, a.rms, ws);
     if (e != hipSuccess) return e;
@@ -894,13 +905,12 @@ template <typename T> static hipError_t backward_type(const GroupNormBackward& a
         return reduce_all(Reductions(1, Reduction{ws, a.dparams, 2 * (int64_t)a.channels, (int)a.samples, true}), s);
     }
     const MapPlan m = map_plan(a.samples, a.positions, a.channels, kPiece<T>);
-    if (a.samples > INT32_MAX / m.slices) return hipErrorInvalidValue;
     float* const means = ws + a.samples * m.slices * 2 * (int64_t)a.channels;
     float* const sums = means + a.samples * a.groups * 2;
     const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
     hipError_t e = launch_timed(kcLayerNorm, group_map_sums_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices, ws);
     if (e != hipSuccess) return e;
-    const int size = a.channels / a.groups, columns = (kFoldColumns + size - 1) / size * size;
+    const int columns = fold_columns(a.channels / a.groups);
     const int64_t folds = a.samples * ((a.channels + columns - 1) / columns);
     e = launch_timed(kcLayerNorm, group_map_fold_kernel, dim3((unsigned)folds), dim3(512), 0, s, (const float*)ws, a.gain, a.positions, a.channels, a.groups, columns, m.slices, a.rms, sums,
                      means);

@@ -110,12 +110,12 @@ size_t scan_workspace_bytes(const Scan& a) {
 
 template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hipStream_t s) {
     if (a.positions <= kScanSteps) {
-        const int64_t units = a.samples * a.heads;
-        if (units > INT32_MAX) return hipErrorInvalidValue;
+        const int64_t units = a.samples * a.heads, cuts = (a.dh + 63) / 64;
+        if (!launchable(units, 256) || cuts > 65535) return hipErrorInvalidValue;
         const bool whole = a.dh % 64 == 0;
         auto kern = a.n > 64 ? (whole && a.n == 128 ? scan_steps_kernel<T, 2, true> : scan_steps_kernel<T, 2, false>)
                              : (whole && a.n == 64 ? scan_steps_kernel<T, 1, true> : scan_steps_kernel<T, 1, false>);
-        return launch_timed(kcAttnFwd, kern, dim3((unsigned)units, (unsigned)((a.dh + 63) / 64)), dim3(256), 0, s, a);
+        return launch_timed(kcAttnFwd, kern, dim3((unsigned)units, (unsigned)cuts), dim3(256), 0, s, a);
     }
     ScanWalk w = walk_of(a);
     w.y = a.y; w.y_stride = a.y_stride;

@@ -473,7 +473,9 @@ template <typename T> static hipError_t backward_type(const ScanBackward& b, voi
     back.x = b.dy; back.x_stride = b.dy_stride; back.x_wide = b.f.heads * b.f.dh; back.b_first = w.c_first;
     back.first_state = b.dstate; back.chunk_states = behind; back.final_state = b.dstate_in;
     const unsigned walks = walk_grid(w);
-    if (!walks) return hipErrorInvalidValue;
+    const int64_t units = b.f.samples * a.chunks * b.f.groups * a.parts, blocks = (units + 7) / 8 * 8;
+    const int64_t shared_blocks = ((b.f.samples * b.f.positions * 2 * b.f.groups * b.f.n + 3) / 4 + 255) / 256;
+    if (!walks || !launchable(blocks, 256) || !launchable(shared_blocks, 256)) return hipErrorInvalidValue;
     hipError_t e = hipSuccess;
     if (w.stretches > 1) {
         walk_room(back, walk_room(w, at));
@@ -487,8 +489,6 @@ template <typename T> static hipError_t backward_type(const ScanBackward& b, voi
     e = TMPS_WALK(TMPS_WALKS, w);
     if (e != hipSuccess) return e;
     const Scan& f = b.f;
-    const int64_t units = f.samples * a.chunks * f.groups * a.parts, blocks = (units + 7) / 8 * 8;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(256);
     if (f.dh > 32) {
         if (f.n <= 32) e = launch_timed(kcAttnBwd, scan_grad_kernel<T, 32, 4>, grid, block, 0, s, a);
@@ -501,9 +501,7 @@ template <typename T> static hipError_t backward_type(const ScanBackward& b, voi
     }
     if (e != hipSuccess) return e;
     if (a.shared) {
-        const int64_t fours = (f.samples * f.positions * 2 * f.groups * f.n + 3) / 4;
-        if ((fours + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
-        e = launch_timed(kcAttnBwd, scan_shared_kernel<T>, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, s, a);
+        e = launch_timed(kcAttnBwd, scan_shared_kernel<T>, dim3((unsigned)shared_blocks), dim3(256), 0, s, a);
         if (e != hipSuccess) return e;
     }
     return reduce_all(Reductions(1, Reduction{a.sums, b.dparams, 3 * (int64_t)f.heads, (int)(f.samples * a.chunks), true}), s);

@@ -294,7 +294,7 @@ size_t short_conv_part_elems(int64_t samples, int64_t positions, int channels, i
 // Workgroups of a launch (0: more than a launch takes).
 static unsigned conv_grid(int64_t samples, int64_t positions, int channels, int V) {
     const int64_t blocks = conv_groups(samples, positions), pieces = ((channels + V - 1) / V + 63) / 64;
-    return blocks <= INT32_MAX / pieces ? (unsigned)(blocks * pieces) : 0u;
+    return launchable(blocks * pieces, 256) ? (unsigned)(blocks * pieces) : 0u;
 }
 
 template <typename T, int K> static hipError_t conv_fwd(const ShortConv& a, hipStream_t s) {

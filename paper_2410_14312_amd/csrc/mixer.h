@@ -6,6 +6,9 @@
 
 namespace tmps {
 
+// Whether a launch takes so many workgroups (its threads are counted in 32 bits).
+inline bool launchable(int64_t workgroups, int threads) { return workgroups < (int64_t(1) << 32) / threads; }
+
 // Causal convolution of `taps` taps along the positions of each sample, channels apart, z = bias + sum_j weight[c][j] u[t - taps + 1 + j][c], and with silu
 // y = z / (1 + exp(-z)).  u: x's rows (x_stride elements apart), before them those of tail ([samples, taps - 1, channels]; null: zeros).  tail_out (may be null, or tail for one
 // position): the last taps - 1 inputs.
@@ -91,6 +94,7 @@ struct GroupNorm {
     int channels, groups, act;
     bool rms;
 };
+bool group_norm_fits(int dtype, int64_t samples, int64_t positions, int channels, int groups);
 size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions, int channels, int groups, bool backward);
 hipError_t group_norm_forward(int dtype, const GroupNorm& a, void* ws, hipStream_t s);
 // Its gradients: dx and dparams: [channels] of gain, then, with a shift, [channels] of it.

@@ -55,7 +55,8 @@ int check_conv(int dtype, int flags, int64_t samples, int64_t positions, int cha
     if (taps > kConvMaxTaps) return fail(TMPS_EUNSUPPORTED, "more than %d taps", kConvMaxTaps);
     if (channels > (1 << 24)) return fail(TMPS_EUNSUPPORTED, "more than 2^24 channels");
     // (a launch has a workgroup for every 64 positions of 256 channels)
-    if ((samples * ((positions + 15) / 16) + 3) / 4 > INT32_MAX / ((channels + 255) / 256)) return fail(TMPS_EUNSUPPORTED, "too many positions");
+    const int64_t groups = (samples * ((positions + 15) / 16) + 3) / 4;
+    if (!launchable(groups, 256) || !launchable(groups * ((channels + 255) / 256), 256)) return fail(TMPS_EUNSUPPORTED, "too many positions");
     return TMPS_OK;
 }
 
@@ -127,6 +128,8 @@ static int check_scan(int dtype, const tmps_scan_desc* desc, int64_t samples, in
     if ((int64_t)desc->heads * desc->dh + 2 * (int64_t)desc->groups * desc->n > (1 << 24)) return fail(TMPS_EUNSUPPORTED, "rows of more than 2^24 features");
     const int64_t head_numbers = (int64_t)desc->heads * desc->dh * desc->n;   // (of a sample's states)
     if (samples > ((int64_t)INT32_MAX - 1) * 256 / head_numbers) return fail(TMPS_EUNSUPPORTED, "too many samples");
+    // (numbers of the chunks' states, whole tiles of them: their places are 64-bit numbers)
+    if ((double)samples * (double)((positions + 63) / 64) * desc->heads * (desc->dh + 63.0) * 128.0 > 0x1p50) return fail(TMPS_EUNSUPPORTED, "too many positions");
     return TMPS_OK;
 }
 
@@ -230,7 +233,7 @@ static int check_group_norm(int dtype, int flags, int64_t samples, int64_t posit
     if (channels < 1 || groups < 1) return fail(TMPS_EINVAL, "channels and groups must be positive");
     if (channels % groups) return fail(TMPS_ESHAPE, "%d channels in %d groups", channels, groups);
     if (channels > kGroupNormMaxChannels) return fail(TMPS_EUNSUPPORTED, "more than %d channels", kGroupNormMaxChannels);
-    if (samples * positions > kMaxElems / channels || samples > INT32_MAX / 64 || samples > ((int64_t)INT32_MAX - 1) * 16 / groups) return fail(TMPS_EUNSUPPORTED, "too many rows");
+    if (samples * positions > kMaxElems / channels || !group_norm_fits(dtype, samples, positions, channels, groups)) return fail(TMPS_EUNSUPPORTED, "too many rows");
     return TMPS_OK;
 }
 

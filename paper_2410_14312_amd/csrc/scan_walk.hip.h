@@ -346,7 +346,8 @@ template <typename T, int NP, int PT, int LEAVES, bool REV> __device__ __forcein
     }
 }
 
-template <typename T, int NP, int PT, int LEAVES> __global__ __launch_bounds__(256, 2) void scan_walk_kernel(ScanWalk a) {
+// (two workgroups to a compute unit where its LDS has room for them)
+template <typename T, int NP, int PT, int LEAVES> __global__ __launch_bounds__(256, (sizeof(WalkTiles<T, NP, PT, LEAVES == kWalkResults>) <= 81920 ? 2 : 1)) void scan_walk_kernel(ScanWalk a) {
     __shared__ WalkTiles<T, NP, PT, LEAVES == kWalkResults> tiles;
     const int64_t unit = xcd_order(blockIdx.x, gridDim.x);
     if (unit < a.samples * a.stretches * a.heads * a.slices) scan_walk<T, NP, PT, LEAVES, false>(a, unit, tiles);
@@ -408,7 +409,7 @@ inline size_t walk_stretch_bytes(const Scan& a) {
 // Workgroups of a walk (0: more than a launch takes).
 inline unsigned walk_grid(const ScanWalk& w) {
     const int64_t blocks = (w.samples * w.stretches * w.heads * w.slices + 7) / 8 * 8;
-    return blocks <= INT32_MAX ? (unsigned)blocks : 0u;
+    return launchable(blocks, 256) ? (unsigned)blocks : 0u;
 }
 inline unsigned join_grid(const ScanWalk& w) { return (unsigned)((w.samples * w.heads * padded_dh(w.dh) * padded_n(w.n) + 255) / 256); }
 
