@@ -935,6 +935,10 @@ class Stage:
     def update(self, stream=None):
         _check(lib().tmps_update(self.handle, C.c_void_p(self._stream(stream))))
 
+    def clip_gradients(self, limit, stream=None):
+        """Between a backward pass and its update, on their stream: the norm of all of this stage's gradients, and the gradients clipped to it (see clip_gradients)."""
+        return clip_gradients([self._flat(1, 1)], limit, stream=stream)
+
     def use_graphs(self, on=True):
         """Forward and backward passes replay captured HIP graphs (see tmps_stage_use_graphs)."""
         _check(lib().tmps_stage_use_graphs(self.handle, 1 if on else 0))
