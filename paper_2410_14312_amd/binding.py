@@ -1,5 +1,6 @@
 """ctypes binding of libtmps.so: same names as the C ABI, argument marshalling only."""
 import ctypes as C
+import operator
 import os
 
 import numpy as np
@@ -697,9 +698,13 @@ def group_norm_backward(dy, x, stats, gain, shift=None, groups=1, positions=1, a
     return dx, dgain, dshift if shift is not None else None
 
 
+_DTYPE_OF, _REQUIRES_GRAD_OF = operator.attrgetter("dtype"), operator.attrgetter("requires_grad")
+
+
 def clip_gradients(grads, limit, out=None, stream=None):
-    """The norm of all tensors of `grads` together, fp32 of no dimension, and each of them times limit / norm where that is less than one, in place or in the tensors `out`
-    (tmps_clip_gradients).  limit = inf: the norm alone.  A norm that is not finite leaves the values as they are.  Tensors are contiguous, fp32 or bf16.  `stream` as for rotary."""
+    """The norm of all tensors of `grads` together, fp32 of no dimension, and each of them times limit / norm where that is less than one, in place or in the tensors `out`,
+    of the same types and numbers of elements (tmps_clip_gradients).  limit = inf: the norm alone.  A norm that is not finite leaves the values as they are.  Tensors are
+    contiguous, fp32 or bf16.  `stream` as for rotary."""
     grads = list(grads)
     if not grads:
         raise ValueError("grads: one tensor at least is wanted")
@@ -714,24 +719,20 @@ def clip_gradients(grads, limit, out=None, stream=None):
     if dev.type != "cuda":
         raise ValueError("tensors on a GPU are wanted, not on %s" % dev)
     # (a few attributes of each of hundreds of tensors: they are what such a call costs the host)
-    codes, index = {torch.float32: TMPS_F32, torch.bfloat16: TMPS_BF16_F32MASTER}, dev.index
-    record = np.empty(len(grads), dtype=_ARRAY)
-    kinds = [codes.get(g.dtype, -1) for g in grads]
-    if -1 in kinds:
-        _dtype_code(grads[kinds.index(-1)])
-    for g in grads:
-        if g.get_device() != index or not g.is_contiguous() or g.requires_grad:
-            _operand("grads", g, g.shape, g.dtype, dev)
-    record["data"] = at = [g.data_ptr() for g in grads]
-    record["n"] = [g.numel() for g in grads]
-    record["dtype"] = kinds
-    if out is None:
-        record["out"] = 0 if limit == float("inf") else at
-    else:
-        for g, o in zip(grads, to):
-            if o.dtype is not g.dtype or o.get_device() != index or not o.is_contiguous() or o.requires_grad or o.shape != g.shape:
-                _operand("out", o, g.shape, g.dtype, dev)
-        record["out"] = [o.data_ptr() for o in to]
+    many, n, T = grads if out is None else grads + to, len(grads), torch.Tensor
+    types, sizes = list(map(_DTYPE_OF, many)), list(map(T.numel, many))
+    kinds = list(map({torch.float32: TMPS_F32, torch.bfloat16: TMPS_BF16_F32MASTER}.get, types[:n]))
+    if None in kinds:
+        _dtype_code(grads[kinds.index(None)])
+    if set(map(T.get_device, many)) != {dev.index} or not all(map(T.is_contiguous, many)) or any(map(_REQUIRES_GRAD_OF, many)):
+        for k, g in enumerate(many):
+            _operand("grads" if k < n else "out", g, g.shape, g.dtype, dev)
+    if out is not None and (types[n:] != types[:n] or sizes[n:] != sizes[:n]):
+        raise ValueError("out: tensors of the types and sizes of grads are wanted")
+    record = np.empty(n, dtype=_ARRAY)
+    at = list(map(T.data_ptr, many))
+    record["data"], record["n"], record["dtype"] = at[:n], sizes[:n], kinds
+    record["out"] = at[n:] if out is not None else 0 if limit == float("inf") else at
     arrays = C.cast(record.ctypes.data, C.POINTER(Array))
     norm = torch.empty((), dtype=torch.float32, device=dev)
     need = load_library().tmps_clip_workspace(arrays, len(grads))

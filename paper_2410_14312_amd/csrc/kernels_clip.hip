@@ -144,7 +144,7 @@ static int64_t clip_table(ClipTable& t, const ClipArray* list, int n, int block,
     int64_t blocks = 0;
     t.count = 0;
     t.block = block;
-    for (; i < n && t.count < kClipArrays && (t.count == 0 || blocks + blocks_of(list[i].n, block) < (1 << 30)); ++i) {
+    for (; i < n && t.count < kClipArrays && (t.count == 0 || launchable(blocks + blocks_of(list[i].n, block), 256)); ++i) {
         if (list[i].n <= 0) continue;
         t.in[t.count] = list[i].in; t.out[t.count] = list[i].out; t.n[t.count] = list[i].n;
         t.first[t.count] = (uint32_t)blocks | (list[i].dtype == kBF16 ? 0x80000000u : 0u);
@@ -172,6 +172,7 @@ hipError_t clip_gradients(const ClipArray* list, int n, float limit, float* norm
         tables.emplace_back();
         blocks.push_back(clip_table(tables.back(), list, n, block, i));
         if (!blocks.back()) break;
+        if (!launchable(blocks.back(), 256)) return hipErrorInvalidValue;
         const hipError_t e = launch_timed(kcReduce, clip_squares_kernel, dim3((unsigned)blocks.back()), dim3(256), 0, s, tables.back(), part + total);
         if (e != hipSuccess) return e;
         total += blocks.back();
