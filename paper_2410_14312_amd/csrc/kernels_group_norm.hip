@@ -57,10 +57,10 @@ template <typename T> __device__ __forceinline__ float norm_act_grad(int act, fl
 // (count, mean, sum of squared differences) of two sets as one
 __device__ __forceinline__ void join_moments(float& n, float& mean, float& m2, float n2, float mean2, float m22) {
     if (n2 == 0.0f) return;
-    const float all = n + n2, d = mean2 - mean;
-    mean += d * (n2 / all);
-    m2 += m22 + d * d * (n * n2 / all);
-    n = all;
+    const float d = mean2 - mean, share = n2 * __builtin_amdgcn_rcpf(n + n2);   // (off by a step, of the means' difference)
+    mean = fmaf(d, share, mean);
+    m2 += fmaf(d * d, n * share, m22);
+    n += n2;
 }
 
 // ------------------------------------------------------------------------------------------------ rows
@@ -240,9 +240,41 @@ template <typename T> struct MapPlace {
                 if (e < C) row[e] = from_f32<T>(v[e]);
         }
     }
-    template <class F> __device__ __forceinline__ void params(float (&v)[V], F&& f) const {
+    // its channels' numbers of a vector (null: zeros)
+    __device__ __forceinline__ void params(float (&v)[V], const float* p) const {
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = f(min(at + e, C - 1));
+        for (int e = 0; e < V; ++e) v[e] = 0.0f;
+        if (!p) return;
+        if (C >= V) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+                float f[4];
+                unpack(load16_any(p + at + e), f);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[e + k] = f[k];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = p[min(e, C - 1)];
+        }
+    }
+    // f(e, group) of each
+    template <class F> __device__ __forceinline__ void groups(int size, F&& f) const {
+        int g = at / size, end = (g + 1) * size;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (min(at + e, C - 1) >= end) ++g, end += size;
+            f(e, g);
+        }
+    }
+    // the two numbers of their groups
+    __device__ __forceinline__ void pairs(float (&first)[V], float (&second)[V], const float* p, int size) const {
+        groups(size, [&](int e, int g) {
+            const any_u32x2_t u = *reinterpret_cast<const any_u32x2_t*>(p + 2 * g);
+            const uint32_t a = u[0], b = u[1];
+            first[e] = __builtin_bit_cast(float, a);
+            second[e] = __builtin_bit_cast(float, b);
+        });
     }
 };
 
@@ -346,23 +378,26 @@ template <int LANES> __device__ __forceinline__ void join_lanes(float& n, float&
     }
 }
 
-// The groups' means and 1/std from those of the slices' channels: a wave to a group, eight of a lane's under way at a time.
-__global__ __launch_bounds__(256) void group_map_stats_kernel(const float* part, int64_t samples, int64_t positions, int channels, int groups, int64_t slice, int slices, bool rms, float* stats) {
-    const int64_t g = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (g >= samples * groups) return;
+// The groups' means and 1/std from those of the slices' channels: WAVES waves to a group, eight of a lane's under way at a time.
+template <int WAVES> __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void group_map_stats_kernel(const float* part, int64_t samples, int64_t positions, int channels, int groups,
+                                                                                                              int64_t slice, int slices, bool rms, float* stats) {
+    __shared__ float waves[WAVES][3];
+    constexpr int kThreads = 64 * WAVES;
+    const int64_t g = WAVES == 1 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
+    if (g >= samples * groups) return;   // (of workgroups with a barrier none)
     const int64_t sample = g / groups;
-    const int size = channels / groups, first = (int)(g % groups) * size, lane = threadIdx.x & 63;
-    const int64_t all = (int64_t)size * slices;
+    const int size = channels / groups, first = (int)(g % groups) * size, lane = (int)threadIdx.x % kThreads;
+    const int all = size * slices, last = (int)(positions - (slices - 1) * slice);   // (slices are as many as there are workgroups at most: 2^11, channels 2^16)
     const float2* const from = reinterpret_cast<const float2*>(part) + sample * slices * channels + first;
     float n = 0.0f, mean = 0.0f, m2 = 0.0f;
-    for (int64_t i0 = lane; i0 < all; i0 += 64 * 8) {
+    for (int i0 = lane; i0 < all; i0 += kThreads * 8) {
         float2 f[8];
         float many[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int64_t i = min(i0 + 64 * k, all - 1), cut = i / size;
-            f[k] = from[cut * channels + i % size];
-            many[k] = i0 + 64 * k < all ? (float)min<int64_t>(slice, positions - cut * slice) : 0.0f;
+            const uint32_t i = (uint32_t)min(i0 + kThreads * k, all - 1), cut = i / (uint32_t)size;
+            f[k] = from[(int64_t)cut * channels + (i - cut * (uint32_t)size)];
+            many[k] = i0 + kThreads * k >= all ? 0.0f : (int)cut == slices - 1 ? (float)last : (float)slice;
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -371,6 +406,16 @@ __global__ __launch_bounds__(256) void group_map_stats_kernel(const float* part,
         }
     }
     join_lanes<64>(n, mean, m2);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+            waves[threadIdx.x / 64][0] = n;
+            waves[threadIdx.x / 64][1] = mean;
+            waves[threadIdx.x / 64][2] = m2;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) join_moments(n, mean, m2, waves[w][0], waves[w][1], waves[w][2]);
+    }
     if (lane == 0) {
         stats[2 * g] = rms ? 0.0f : mean;
         stats[2 * g + 1] = 1.0f / sqrtf(m2 / ((float)size * (float)positions) + 1e-5f);
@@ -386,10 +431,9 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_apply_ker
     const int size = a.channels / a.groups;
     const float* const stats = a.stats + sample * a.groups * 2;
     float mean[V], rstd[V], gain[V], shift[V];
-    p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
-    p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
-    p.params(gain, [&](int c) { return a.gain[c]; });
-    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    p.pairs(mean, rstd, stats, size);
+    p.params(gain, a.gain);
+    p.params(shift, a.shift);
     const T* const x = (const T*)a.x + sample * a.positions * a.channels;
     T* const y = (T*)a.y + sample * a.positions * a.channels;
     for (int64_t t = t0 + p.lane; t < t1; t += (int64_t)p.lanes * kMapPairs) {
@@ -427,10 +471,9 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_sums_kern
         const int size = a.channels / a.groups;
         const float* const stats = a.stats + sample * a.groups * 2;
         float mean[V], rstd[V], gain[V], shift[V];
-        p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
-        p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
-        p.params(gain, [&](int c) { return a.gain[c]; });
-        p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+        p.pairs(mean, rstd, stats, size);
+        p.params(gain, a.gain);
+        p.params(shift, a.shift);
         const T* const x = (const T*)a.x + sample * a.positions * a.channels;
         const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
         for (int64_t t = t0 + p.lane; t < t1; t += (int64_t)p.lanes * kMapPairs) {
@@ -540,12 +583,10 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_apply_bwd
     const int size = a.channels / a.groups;
     const float *const stats = a.stats + sample * a.groups * 2, *const of = means + sample * a.groups * 2;
     float mean[V], rstd[V], gain[V], shift[V], alone[V], with_xhat[V];
-    p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
-    p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
-    p.params(alone, [&](int c) { return of[2 * (c / size)]; });
-    p.params(with_xhat, [&](int c) { return of[2 * (c / size) + 1]; });
-    p.params(gain, [&](int c) { return a.gain[c]; });
-    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    p.pairs(mean, rstd, stats, size);
+    p.pairs(alone, with_xhat, of, size);
+    p.params(gain, a.gain);
+    p.params(shift, a.shift);
     const T* const x = (const T*)a.x + sample * a.positions * a.channels;
     const T* const dy = (const T*)a.dy + sample * a.positions * a.channels;
     T* const dx = (T*)a.dx + sample * a.positions * a.channels;
@@ -584,7 +625,7 @@ constexpr int kHeldGroups = 512;
 // Lanes that share an item of `items` of a workgroup's.
 __device__ __forceinline__ int lanes_each(int threads, int items) {
     int n = 1;
-    while (n < 16 && 2 * n * items <= threads) n *= 2;
+    while (n < 64 && 2 * n * items <= threads) n *= 2;
     return n;
 }
 
@@ -602,8 +643,8 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
     for (int k = 0; k < kHeldPieces; ++k)
         if (k * p.lanes < positions) u[k] = p.request(x + (int64_t)min(p.lane + k * p.lanes, positions - 1) * a.channels);
     float mean[V], m2[V], gain[V], shift[V];
-    p.params(gain, [&](int c) { return a.gain[c]; });
-    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    p.params(gain, a.gain);
+    p.params(shift, a.shift);
     block_moments<T>(u, many, a.rms, mean, m2);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -662,8 +703,7 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
     }
     __syncthreads();
     float rstd[V];
-    p.params(mean, [&](int c) { return group_stats[c / size][0]; });
-    p.params(rstd, [&](int c) { return group_stats[c / size][1]; });
+    p.pairs(mean, rstd, &group_stats[0][0], size);
     T* const y = (T*)a.y + sample * a.positions * a.channels;
 #pragma unroll
     for (int k = 0; k < kHeldPieces; ++k) {
@@ -701,10 +741,9 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
             ug[k] = p.request(dy + row);
         }
     float mean[V], rstd[V], gain[V], shift[V], with_xhat[V], alone[V];
-    p.params(mean, [&](int c) { return stats[2 * (c / size)]; });
-    p.params(rstd, [&](int c) { return stats[2 * (c / size) + 1]; });
-    p.params(gain, [&](int c) { return a.gain[c]; });
-    p.params(shift, [&](int c) { return a.shift ? a.shift[c] : 0.0f; });
+    p.pairs(mean, rstd, stats, size);
+    p.params(gain, a.gain);
+    p.params(shift, a.shift);
 #pragma unroll
     for (int e = 0; e < V; ++e) with_xhat[e] = alone[e] = 0.0f;
     // xhat and dz of piece k
@@ -775,8 +814,7 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
         }
     }
     __syncthreads();
-    p.params(alone, [&](int c) { return group_means[c / size][0]; });
-    p.params(with_xhat, [&](int c) { return group_means[c / size][1]; });
+    p.pairs(alone, with_xhat, &group_means[0][0], size);
     T* const dx = (T*)a.dx + sample * a.positions * a.channels;
 #pragma unroll
     for (int k = 0; k < kHeldPairs; ++k) {
@@ -790,20 +828,24 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void gr
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-// Slices of a sample's positions: as many as give the chip 2048 workgroups, of 32 positions at least.
+// Slices of a sample's positions: as many as give the chip 2048 workgroups, of at least 32 positions, or four, and no fewer than eight, of a thread's where there are few side by side.
 constexpr int kMapGroups = 2048, kMapPositions = 32;
+constexpr int kStatGroups = 1024;   // groups of all samples from which a wave to each is enough
 constexpr int kFoldColumns = 64;   // channels whose slices' sums a workgroup adds up, in whole groups
 static int fold_columns(int size) { return (kFoldColumns + size - 1) / size * size; }
 struct MapPlan {
     int64_t slice;
     int slices, blocks;   // blocks: of 256 pieces of channels
 };
+static int64_t map_slices(int64_t positions, int channels, int V) {
+    const int lanes = 256 / std::min((channels + V - 1) / V, 256), least = std::max(8, std::min(kMapPositions, 4 * lanes));
+    return (positions + least - 1) / least;
+}
 static MapPlan map_plan(int64_t samples, int64_t positions, int channels, int V) {
     MapPlan m;
     m.blocks = ((channels + V - 1) / V + 255) / 256;
     int64_t want = (kMapGroups + samples * m.blocks - 1) / (samples * m.blocks);
-    if (want > (positions + kMapPositions - 1) / kMapPositions) want = (positions + kMapPositions - 1) / kMapPositions;
-    if (want < 1) want = 1;
+    want = std::max<int64_t>(1, std::min(want, map_slices(positions, channels, V)));
     m.slice = (positions + want - 1) / want;
     m.slices = (int)((positions + m.slice - 1) / m.slice);
     return m;
@@ -845,8 +887,8 @@ bool group_norm_fits(int dtype, int64_t samples, int64_t positions, int channels
 // (as much as any call of no more samples and positions takes)
 size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions, int channels, int groups, bool backward) {
     if (by_rows(positions, channels, groups)) return backward ? (size_t)row_teams(samples, groups, 16, kRowsEachBack) / groups * 2 * channels * sizeof(float) : 0;
-    const int64_t blocks = map_plan(samples, positions, channels, dtype == kBF16 ? 8 : 4).blocks;
-    const int64_t most = std::min(samples * ((positions + kMapPositions - 1) / kMapPositions), samples + kMapGroups / blocks + 1);
+    const int V = dtype == kBF16 ? 8 : 4;
+    const int64_t blocks = map_plan(samples, positions, channels, V).blocks, most = std::min(samples * map_slices(positions, channels, V), samples + kMapGroups / blocks + 1);
     return ((size_t)most * 2 * channels + (backward ? (size_t)samples * 2 * (groups + channels) : 0)) * sizeof(float);
 }
 
@@ -890,8 +932,11 @@ template <typename T> static hipError_t forward_type(const GroupNorm& a, float* 
     const dim3 grid((unsigned)(a.samples * m.slices), (unsigned)m.blocks);
     hipError_t e = launch_timed(kcLayerNorm, group_map_moments_kernel<T>, grid, dim3(256), 0, s, (const T*)a.x, a.positions, a.channels, m.slice, m.slices, a.rms, ws);
     if (e != hipSuccess) return e;
-    e = launch_timed(kcLayerNorm, group_map_stats_kernel, dim3((unsigned)((a.samples * a.groups + 3) / 4)), dim3(256), 0, s, (const float*)ws, a.samples, a.positions, a.channels,
-                     a.groups, m.slice, m.slices, a.rms, a.stats);
+    const int64_t stats = a.samples * a.groups;
+    e = stats >= kStatGroups ? launch_timed(kcLayerNorm, group_map_stats_kernel<1>, dim3((unsigned)((stats + 3) / 4)), dim3(256), 0, s, (const float*)ws, a.samples, a.positions,
+                                            a.channels, a.groups, m.slice, m.slices, a.rms, a.stats)
+                             : launch_timed(kcLayerNorm, group_map_stats_kernel<16>, dim3((unsigned)stats), dim3(1024), 0, s, (const float*)ws, a.samples, a.positions, a.channels,
+                                            a.groups, m.slice, m.slices, a.rms, a.stats);
     if (e != hipSuccess) return e;
     return launch_timed(kcLayerNorm, group_map_apply_kernel<T>, grid, dim3(256), 0, s, a, m.slice, m.slices);
 }
