@@ -137,6 +137,8 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
     };
     request(t0);
     const ConvTaps<K, V> taps(p.at, a.channels, a.weight, a.bias);
+    // (where tail_out is the tail, what a piece that begins earlier has read of the piece before may be that one's outcome already)
+    const bool own_only = p.at < at.piece * V && a.tail && a.tail_out == a.tail;
     float u[K - 1 + A][V];   // the inputs from position `from` - K + 1 on
     conv_before<T, K>(u, p, x, a.x_stride, tail, t0);
     for (int64_t from = t0; from < t1; from += A) {
@@ -157,7 +159,9 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
 #pragma unroll
                 for (int e = 0; e < V; ++e) z[e] *= conv_sigmoid<T>(z[e]);
             }
-            if (k < many) p.store(y + (from + k) * a.y_stride, z);
+            if (k >= many) continue;
+            if (own_only) p.store_from(y + (from + k) * a.y_stride, z, at.piece * V);
+            else p.store(y + (from + k) * a.y_stride, z);
         }
         if (a.tail_out && from + A >= a.positions) {   // (the last positions': the inputs up to the last one)
             T* const out = (T*)a.tail_out + sample * (K - 1) * a.channels;

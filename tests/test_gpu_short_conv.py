@@ -78,6 +78,17 @@ def test_token_by_token_in_place(channels):
         tmps.short_conv(i["x"], i["weight"], i["bias"], positions=20, tail=tail, tail_out=tail)
 
 
+@pytest.mark.parametrize("dtype,channels", [("bf16", 513), ("bf16", 1025 + 6), ("f32", 257), ("f32", 259), ("bf16", 9)])
+def test_in_place_where_a_last_piece_is_another_workgroups(dtype, channels):
+    """Channels of the piece before are read again by the last, which starts within it: its results must not come from a tail that has moved on."""
+    i = inputs(5, 300, 1, channels, 4, mixers.TYPES[dtype])
+    want, after = tmps.short_conv(i["x"], i["weight"], i["bias"], tail=i["tail"], want_tail=True)
+    for _ in range(5):
+        tail = i["tail"].clone()
+        y, out = tmps.short_conv(i["x"], i["weight"], i["bias"], tail=tail, tail_out=tail)
+        assert out is tail and torch.equal(y, want) and torch.equal(tail, after)
+
+
 def test_a_number_that_is_not_finite_stays_within_its_taps():
     i = inputs(4, 1, 60, 16, 4, torch.float32, carried=False)
     want, _ = tmps.short_conv(i["x"], i["weight"], i["bias"], positions=60)
