@@ -327,7 +327,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             const int head = group * in_group + mine;
             const ChunkDecays<true>& d = decays[wave];
             const HeadSums& sum = sums[wave];
-            const float rate = (float)exp((double)f.a_log[head]), delta = d.delta[lane], slope = d.slope[lane];
+            const float rate = fminf((float)exp((double)f.a_log[head]), 3.4e38f), delta = d.delta[lane], slope = d.slope[lane];
             // sums of q over the positions of each tile of 16, from the tile of position s (its own, below) on
             const int tile = lane >> 4;
             float later[4], in_tile = 0.0f, behind = 0.0f;
@@ -363,7 +363,9 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             states_before = __shfl_up(states_before, 1);
             states_before = lane ? states_before : 0.0f;
             const float whole = d.end * ((sum.parts[0][0] + sum.parts[1][0]) + (sum.parts[2][0] + sum.parts[3][0]));
-            const float of_exponent = ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
+            // (a step that leaves nothing of what was before: of its exponent's gradient there are only roundings, which such a rate would make large)
+            const float of_exponent = delta * rate > 1024.0f ? 0.0f
+                                                             : ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
             const float ddelta = fmaf(-rate, of_exponent, (sum.self[lane] + (in_tile + behind)) + d.to[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;
             if (lane < rows) ((T*)b.ddt)[(row0 + lane) * b.ddt_stride + head] = from_f32<T>(du);
             const float drate = wsum(lane < rows ? -rate * delta * of_exponent : 0.0f), dbias = wsum(du);

@@ -248,7 +248,9 @@ __device__ __forceinline__ float exp2_of(double e) {
 template <bool GRADIENTS> __device__ __forceinline__ void chunk_decays(ChunkDecays<GRADIENTS>& d, float dt, int rows, float bias, double rate, int lane) {
     const float u = dt + bias;
     const float delta = lane >= rows ? 0.0f : u != u ? u : softplus(u);
-    double sum = -(double)delta * rate;
+    // (a step's exponent below -1024 leaves nothing of what was before, and no sum of such is infinite)
+    const double own = delta == 0.0f ? 0.0 : -(double)delta * rate;
+    double sum = own < -1024.0 ? -1024.0 : own;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
         const double before = __shfl_up(sum, k);

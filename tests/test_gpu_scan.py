@@ -203,3 +203,23 @@ def test_no_samples():
     i = mixers.scan_inputs(1, *size[:6], torch.float32, True)
     y, state = forward(i, size, want_state=True)
     assert y.shape == (0, 32) and state.shape == (0, 2, 16, 16)
+
+
+@pytest.mark.parametrize("a_log", [90.0, 200.0, 720.0])
+@pytest.mark.parametrize("positions", [5, 200])
+def test_rates_beyond_single_precision(positions, a_log):
+    """Nothing of a state is left after a step: y = delta (C . B) x + skip x, and no gradient of the rate."""
+    sizes = (2, positions, 2, 16, 1, 8, True)
+    i = mixers.scan_inputs(19, *sizes[:6], torch.float32, True, True)
+    i["a_log"] = torch.full_like(i["a_log"], a_log)
+    y, state = forward(i, sizes, want_state=True)
+    x = i["x"].double()
+    xs, bs, cs = x[:, :32].view(-1, 2, 16), x[:, 32:40], x[:, 40:]
+    delta = torch.nn.functional.softplus(i["dt"].double() + i["dt_bias"].double())
+    terms = delta[..., None] * (cs * bs).sum(1)[:, None, None] * xs
+    size = delta[..., None] * (cs * bs).abs().sum(1)[:, None, None] * xs.abs() + (i["skip"].double()[:, None] * xs).abs()
+    mixers.near(y, (terms + i["skip"].double()[:, None] * xs).reshape(-1, 32), size.reshape(-1, 32), 32 * mixers.F32)
+    last = (delta[..., None] * xs)[..., None] * bs[:, None, None]
+    mixers.near(state, last.view(2, positions, 2, 16, 8)[:, -1], last.abs().view(2, positions, 2, 16, 8)[:, -1], 16 * mixers.F32)
+    back = backward(i, sizes)
+    assert all(bool(torch.isfinite(v).all()) for v in back.values()) and not bool(back["da_log"].any()) and not bool(back["dstate"].any())
