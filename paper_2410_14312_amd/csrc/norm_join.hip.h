@@ -11,13 +11,19 @@
 
 namespace tmps {
 
-// A team is 16, 32 or 64 lanes of a wave, in workgroups of four waves, or a whole workgroup.
+// A team is 4, 8, 16, 32 or 64 lanes of a wave, in workgroups of four waves, or a whole workgroup.
 template <int TEAM> struct Team {
     static constexpr int kThreads = TEAM <= 64 ? 256 : TEAM;
     static constexpr int kRows = kThreads / TEAM;   // teams of a workgroup
     static constexpr int kWaves = TEAM <= 64 ? 1 : TEAM / 64;
     static __device__ __forceinline__ float lanes_sum(float v) {
         if constexpr (TEAM >= 64) return wsum(v);
+        if constexpr (TEAM <= 8) {
+            v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, false));    // quad_perm:[1,0,3,2]
+            v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, false));    // quad_perm:[2,3,0,1]
+            if constexpr (TEAM == 8) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, false));   // row_half_mirror
+            return v;
+        }
         if constexpr (TEAM == 32) {
             const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
             v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
