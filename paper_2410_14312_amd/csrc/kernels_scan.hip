@@ -43,7 +43,7 @@ template <typename T, int HALVES, bool PLAIN> __global__ __launch_bounds__(256) 
             }
         }
     }
-    const double rate = exp((double)a.a_log[head]) * kLog2eD;
+    const double rate = rate_of(a.a_log[head]) * kLog2eD;
     const float skip = a.skip[head], bias = a.dt_bias[head];
     for (int64_t t = 0; t < a.positions; ++t) {
         const T* const row = xr + t * a.x_stride;

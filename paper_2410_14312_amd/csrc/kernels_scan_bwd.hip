@@ -137,7 +137,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             if (slice == 0 && (h - first) % kHeads == 0 && wave < kHeads && h + wave < last) {
                 const int mine = head + wave;
                 chunk_decays(decays[wave], to_f32(((const T*)f.dt)[(row0 + min(lane, rows - 1)) * f.dt_stride + mine]), rows, f.dt_bias[mine],
-                                   exp((double)f.a_log[mine]) * kLog2eD, lane);
+                                   rate_of(f.a_log[mine]) * kLog2eD, lane);
             }
             if (!plain) {
                 rx.settle_all(rows, width, at, wide);
@@ -327,7 +327,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             const int head = group * in_group + mine;
             const ChunkDecays<true>& d = decays[wave];
             const HeadSums& sum = sums[wave];
-            const float rate = fminf((float)exp((double)f.a_log[head]), 3.4e38f), delta = d.delta[lane], slope = d.slope[lane];
+            const float rate = (float)rate_of(f.a_log[head]), delta = d.delta[lane], slope = d.slope[lane];
             // sums of q over the positions of each tile of 16, from the tile of position s (its own, below) on
             const int tile = lane >> 4;
             float later[4], in_tile = 0.0f, behind = 0.0f;
@@ -363,12 +363,12 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             states_before = __shfl_up(states_before, 1);
             states_before = lane ? states_before : 0.0f;
             const float whole = d.end * ((sum.parts[0][0] + sum.parts[1][0]) + (sum.parts[2][0] + sum.parts[3][0]));
+            const float of_exponent = ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
             // (a step that leaves nothing of what was before: of its exponent's gradient there are only roundings, which such a rate would make large)
-            const float of_exponent = delta * rate > 1024.0f ? 0.0f
-                                                             : ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
-            const float ddelta = fmaf(-rate, of_exponent, (sum.self[lane] + (in_tile + behind)) + d.to[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;
+            const float by = delta * rate > 1024.0f ? 0.0f : -rate;
+            const float ddelta = fmaf(by, of_exponent, (sum.self[lane] + (in_tile + behind)) + d.to[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;
             if (lane < rows) ((T*)b.ddt)[(row0 + lane) * b.ddt_stride + head] = from_f32<T>(du);
-            const float drate = wsum(lane < rows ? -rate * delta * of_exponent : 0.0f), dbias = wsum(du);
+            const float drate = wsum(lane < rows ? by * delta * of_exponent : 0.0f), dbias = wsum(du);
             if (lane == 0) {
                 float* const to = a.sums + (sample * a.chunks + chunk) * 3 * f.heads + head;
                 to[0] = drate;

@@ -235,6 +235,11 @@ template <bool GRADIENTS> struct ChunkDecays {
     double total;    // its exponent
 };
 constexpr double kLog2eD = 1.4426950408889634074;
+// A head's rate, e^a: from 2^100 on nothing is left of a state after any step.
+__device__ __forceinline__ double rate_of(float a_log) {
+    const double rate = exp((double)a_log);
+    return rate > 0x1p100 ? 0x1p100 : rate;
+}
 
 __device__ __forceinline__ float softplus(float u) { return fmaxf(u, 0.0f) + log1pf(expf(-fabsf(u))); }
 
@@ -248,9 +253,9 @@ __device__ __forceinline__ float exp2_of(double e) {
 template <bool GRADIENTS> __device__ __forceinline__ void chunk_decays(ChunkDecays<GRADIENTS>& d, float dt, int rows, float bias, double rate, int lane) {
     const float u = dt + bias;
     const float delta = lane >= rows ? 0.0f : u != u ? u : softplus(u);
-    // (a step's exponent below -1024 leaves nothing of what was before, and no sum of such is infinite)
-    const double own = delta == 0.0f ? 0.0 : -(double)delta * rate;
-    double sum = own < -1024.0 ? -1024.0 : own;
+    // (an exponent of -1024 leaves nothing of what was before; of larger ones the sums' roundings would matter)
+    const float most = 1024.0f * __builtin_amdgcn_rcpf((float)rate);
+    double sum = -(double)(delta > most ? most : delta) * rate;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) {
         const double before = __shfl_up(sum, k);

@@ -75,7 +75,7 @@ template <typename T, int NP, int PT, int LEAVES, bool REV> __device__ __forcein
     const int group = head / (a.heads / a.groups);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
     const int p0 = slice * PP, width = max(min(PP, a.dh - p0), 0);   // (a slice behind the last feature has zeros)
-    const double rate = exp((double)a.a_log[head]) * kLog2eD;
+    const double rate = rate_of(a.a_log[head]) * kLog2eD;
     const float bias = a.dt_bias[head];
 
     const int64_t rows0 = sample * a.positions;
