@@ -6,6 +6,8 @@
 // With q = Z R D, the gradient of position t's own exponent is what passes through it: sum_{t' >= t > s} q[t'][s] delta_s, and of the states sum_{t' >= t} d_t' C_t' S' dy_t' +
 // sum_{s < t} w_s x_s G B_s + d_end <S, G>.  The first is had from sums over the rows and columns of tiles of 16 positions, without differences but inside a tile.  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
 // once and whose gradients of B and C stay in its accumulators.
+// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 41 us the walks (100 MB of states written, most of it read again from the last cache), 64 the chunks (vector instructions and latency, two
+// waves to a SIMD; with another head's operands on their way 212 bytes of registers spill: 115), 5 the parts' gradients of B and C, 5 the sums.
 #include "launch.h"
 #include "scan_walk.hip.h"
 #include "wave.hip.h"

@@ -1,4 +1,5 @@
-// A causal convolution of few taps along the positions, channels apart, with SiLU behind it, and its gradients.  Bound by memory: every number is read and written once.
+// A causal convolution of few taps along the positions, channels apart, with SiLU behind it, and its gradients.  Bound by memory: every number is read and written once.  8192 rows of 1664
+// channels in bf16, four taps: 17.5 us (3.1 TB/s; 10.8 at a copy's rate), back 28.0 with the sums of the partial results (16.2 at a copy's rate).
 #include "launch.h"
 #include "mixer.h"
 #include "pieces.hip.h"
