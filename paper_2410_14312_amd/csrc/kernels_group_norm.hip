@@ -64,7 +64,8 @@ __device__ __forceinline__ void join_moments(float& n, float& mean, float& m2, f
 }
 
 // ------------------------------------------------------------------------------------------------ rows
-constexpr int kGroupRowThreads = 524288;   // threads of a launch at most
+constexpr int kGroupRowThreads = 524288;   // threads of a launch at most; backward, where teams leave partial results, kBackRowThreads
+constexpr int kBackRowThreads = 262144;     // (4000 rows of 4096 in bf16: 43 us, with 524288 51, with 131072 68)
 
 // The rows are the samples' groups; a team's rows are a whole number of samples apart, so that its group's parameters stay in registers.
 template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(Team<TEAM>::kThreads) void group_rows_fwd_kernel(GroupNorm a, int64_t step) {
@@ -852,8 +853,8 @@ static MapPlan map_plan(int64_t samples, int64_t positions, int channels, int V)
 }
 
 // Teams of a launch of rows: a whole number of samples' groups.
-static int64_t row_teams(int64_t samples, int groups, int team, int rows_each) {
-    const int64_t rows = samples * groups, most = kGroupRowThreads / team;
+static int64_t row_teams(int64_t samples, int groups, int team, int rows_each, int threads) {
+    const int64_t rows = samples * groups, most = threads / team;
     int64_t n = (samples + rows_each - 1) / rows_each;
     if (n * groups > most) n = most / groups;
     if (n < 1) n = 1;
@@ -886,19 +887,19 @@ bool group_norm_fits(int dtype, int64_t samples, int64_t positions, int channels
 
 // (as much as any call of no more samples and positions takes)
 size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions, int channels, int groups, bool backward) {
-    if (by_rows(positions, channels, groups)) return backward ? (size_t)row_teams(samples, groups, 4, kRowsEachBack) / groups * 2 * channels * sizeof(float) : 0;
+    if (by_rows(positions, channels, groups)) return backward ? (size_t)row_teams(samples, groups, 4, kRowsEachBack, kBackRowThreads) / groups * 2 * channels * sizeof(float) : 0;
     const int V = dtype == kBF16 ? 8 : 4;
     const int64_t blocks = map_plan(samples, positions, channels, V).blocks, most = std::min(samples * map_slices(positions, channels, V), samples + kMapGroups / blocks + 1);
     return ((size_t)most * 2 * channels + (backward ? (size_t)samples * 2 * (groups + channels) : 0)) * sizeof(float);
 }
 
 template <typename T, int TEAM, int N, bool WHOLE> static hipError_t rows_fwd(const GroupNorm& a, hipStream_t s) {
-    const int64_t teams = row_teams(a.samples, a.groups, TEAM, 1);
+    const int64_t teams = row_teams(a.samples, a.groups, TEAM, 1, kGroupRowThreads);
     const dim3 grid((unsigned)((teams + Team<TEAM>::kRows - 1) / Team<TEAM>::kRows));
     return launch_timed(kcLayerNorm, group_rows_fwd_kernel<T, TEAM, N, WHOLE>, grid, dim3(Team<TEAM>::kThreads), 0, s, a, teams);
 }
 template <typename T, int TEAM, int N, bool WHOLE> static hipError_t rows_bwd(const GroupNormBackward& a, float* part, hipStream_t s) {
-    const int64_t teams = row_teams(a.samples, a.groups, TEAM, kRowsEachBack);
+    const int64_t teams = row_teams(a.samples, a.groups, TEAM, kRowsEachBack, kBackRowThreads);
     const dim3 grid((unsigned)((teams + Team<TEAM>::kRows - 1) / Team<TEAM>::kRows));
     const hipError_t e = launch_timed(kcLayerNorm, group_rows_bwd_kernel<T, TEAM, N, WHOLE>, grid, dim3(Team<TEAM>::kThreads), 0, s, a, teams, part);
     if (e != hipSuccess) return e;
