@@ -5,9 +5,11 @@
 //   dx_s = sum_t Z D delta_s dy_t + w_s G B_s + skip dy_s      dB_s = sum_t R D delta_s C_t + w_s G' x_s      dC_t = sum_s R D delta_s B_s + d_t S' dy_t
 // With q = Z R D, the gradient of position t's own exponent is what passes through it: sum_{t' >= t > s} q[t'][s] delta_s, and of the states sum_{t' >= t} d_t' C_t' S' dy_t' +
 // sum_{s < t} w_s x_s G B_s + d_end <S, G>.  The first is had from sums over the rows and columns of tiles of 16 positions, without differences but inside a tile.  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
-// once and whose gradients of B and C stay in its accumulators.
-// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 41 us the walks (100 MB of states written, most of it read again from the last cache), 64 the chunks (vector instructions and latency, two
-// waves to a SIMD; with another head's operands on their way 212 bytes of registers spill: 115), 5 the parts' gradients of B and C, 5 the sums.
+// once and whose gradients of B and C stay in its accumulators.  Products are formed by columns t and again by columns s: decayed, they are then operands as they lie in the accumulators.
+// In bf16 calls these are the sum of two bf16 terms (2^-17 of themselves), S and G of three (2^-25), since gradients of exponents are fp32 sums over them: with one and two terms dx was off by
+// 1.1e-3 beside the 1.7e-3 of its rounding, and the fp32 results by 1.2e-6 instead of 0.7e-6 (the matrix unit's sums).
+// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 41 us the walks (100 MB of states written, most of it read again from the last cache), 73 the chunks (63 with one and two terms; vector
+// instructions and latency, two waves to a SIMD), 5 the parts' gradients of B and C, 5 the sums.
 #include "launch.h"
 #include "scan_walk.hip.h"
 #include "wave.hip.h"
@@ -55,11 +57,11 @@ struct HeadSums {
 };
 
 template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGroups<T, NP> ? 2 : 1)) void scan_grad_kernel(ScanGrad a) {
-    constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, MP = kScanChunk + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
-    constexpr int GT = kResultTerms<T>;   // of S and G
+    constexpr int V = kPiece<T>, PP = PT * 16, XP = PP + V, BP = NP + V, NT = NP / 16, NK = NP / 32, PK = PP / 32;
+    constexpr int GT = kStateTerms<T>, RT = kResultTerms<T>;   // of S and G on their way to exponents' gradients, fp32; of those and decayed products to gradients of the type
     constexpr int kHeads = kHeadsAtOnce<T, NP>;
     constexpr int kState = PP * NP / 4 / 256;   // fours of a state of a thread
-    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP], mm[kScanChunk * MP];
+    __shared__ __attribute__((aligned(16))) T bs[kScanChunk * BP], cs[kScanChunk * BP], xs[kScanChunk * XP], dys[kScanChunk * XP], sg[GT * PP * BP];
     __shared__ __attribute__((aligned(16))) ChunkDecays<true> decays[kHeads];
     __shared__ HeadSums sums[kHeads];
     const ScanBackward& b = a.b;
@@ -94,13 +96,15 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
         r.template put<BP>(cs);
     }
     __syncthreads();
-    f32x4_t z[4];   // rows s, column t
+    f32x4_t z[4], zs[4];   // rows s, column t; rows t, column s
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
-        z[st] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        if (st > wave) continue;
+        z[st] = zs[st] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < NK; ++k) z[st] = mma(along<false>(bs + (16 * st + col) * BP, 32 * k, lane), along<false>(cs + own * BP, 32 * k, lane), z[st]);
+        for (int k = 0; k < NK; ++k) {
+            if (st <= wave) z[st] = mma(along<false>(bs + (16 * st + col) * BP, 32 * k, lane), along<false>(cs + own * BP, 32 * k, lane), z[st]);
+            if (st >= wave) zs[st] = mma(along<false>(cs + (16 * st + col) * BP, 32 * k, lane), along<false>(bs + own * BP, 32 * k, lane), zs[st]);
+        }
     }
     f32x4_t db[NT], dc[NT];   // rows n, columns s and t
 #pragma unroll
@@ -170,7 +174,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             HeadSums& sum = sums[(h - first) % kHeads];
 
             // by columns t
-            f32x4_t m[4], dz[4];
+            f32x4_t dz[4];
             float from_row = 0.0f, of_self = 0.0f, q16[16];
             // (accumulated over a head's slices)
             const auto put_sum = [&](float& to, float v) { to = slice == 0 ? v : to + v; };
@@ -181,7 +185,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
 #pragma unroll
             for (int st = 0; st < 4; ++st) {
                 f32x4_t r = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-                m[st] = dz[st] = r;
+                dz[st] = r;
                 if (st <= wave) {
 #pragma unroll
                     for (int k = 0; k < PK; ++k) r = mma(along<false>(xs + (16 * st + col) * XP, 32 * k, lane), dyf[k], r);
@@ -202,9 +206,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float zd = z[st][e] * decay[e];
-                        float q = r[e] * zd;
-                        m[st][e] = zd * delta_s[e];
+                        float q = r[e] * (z[st][e] * decay[e]);
                         dz[st][e] = r[e] * (decay[e] * delta_s[e]);
                         if (st == wave) {   // (of a position itself nothing passes through)
                             const bool self = 4 * g + e == col;
@@ -218,22 +220,25 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) q16[4 * st + e] = r[e];
-                const float v[4] = {m[st][0], m[st][1], m[st][2], m[st][3]};
-                put_four(mm + own * MP + 16 * st + 4 * g, v);
             }
             put_sum(sum.columns[wave][16 * (col >> 2) + 4 * g + (col & 3)], sixteen_sums(q16, lane));
             if (col >> 2 == g) put_sum(sum.self[own], of_self);
+#pragma unroll
+            for (int pair = 0; pair < 2; ++pair) {
+                if (2 * pair > wave) continue;
+                Oct<T> zf[RT];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) terms_of(dz[2 * pair + e / 4][e % 4], e, zf);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const Oct<T> b = across<true>(bs, BP, 32 * pair, 16 * nt, lane);
+#pragma unroll
+                    for (int term = RT - 1; term >= 0; --term) dc[nt] = mma(b, zf[term], dc[nt]);
+                }
+            }
             float with_c = 0.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int pair = 0; pair < 2; ++pair) {
-                    if (2 * pair > wave) continue;
-                    Oct<T> zf[1];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) terms_of(dz[2 * pair + e / 4][e % 4], e, zf);
-                    dc[nt] = mma(across<true>(bs, BP, 32 * pair, 16 * nt, lane), zf[0], dc[nt]);
-                }
                 f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int term = GT - 1; term >= 0; --term)
@@ -251,45 +256,73 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                 put_sum(sum.row[own], from_row);
                 put_sum(sum.of_c[own], with_c);
             }
-            __syncthreads();   // (S has been read, the decayed products are there)
 
-            // by columns s
-            put_state(g4);
-            f32x4_t dx[PT];
-#pragma unroll
-            for (int j = 0; j < PT; ++j) {
-                dx[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int pair = 0; pair < 2; ++pair) {
-                    if (2 * pair + 1 < wave) continue;
-                    dx[j] = mma(across<false>(dys, XP, 32 * pair, 16 * j, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), dx[j]);
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                const float v[4] = {dz[st][0], dz[st][1], dz[st][2], dz[st][3]};
-                put_four(mm + own * MP + 16 * st + 4 * g, v);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int pair = 0; pair < 2; ++pair) {
-                    if (2 * pair + 1 < wave) continue;
-                    db[nt] = mma(across<false>(cs, BP, 32 * pair, 16 * nt, lane), across<false>(mm, MP, 32 * pair, 16 * wave, lane), db[nt]);
-                }
-            Oct<T> xf[PK], bf[NK];
+            // by columns s: the same products anew, whose rows t are then operands as they lie
+            Oct<T> xf[PK];
 #pragma unroll
             for (int k = 0; k < PK; ++k) xf[k] = along<false>(xs + own * XP, 32 * k, lane);
+            const float delta_own = d.delta[own];
+            f32x4_t m[4];
+            {
+                const float sum_end = d.sum[16 * wave + 15], rest_end = d.rest[16 * wave + 15], tile_own = d.tile[own];
+#pragma unroll
+                for (int tt = 0; tt < 4; ++tt) {
+                    f32x4_t r = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                    m[tt] = dz[tt] = r;
+                    if (tt < wave) continue;
+#pragma unroll
+                    for (int k = 0; k < PK; ++k) r = mma(along<false>(dys + (16 * tt + col) * XP, 32 * k, lane), xf[k], r);
+                    float sum_r[4], rest_r[4];
+                    four(d.sum + 16 * tt + 4 * g, sum_r);
+                    four(d.rest + 16 * tt + 4 * g, rest_r);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float decay;
+                        if (tt > wave) decay = tile_own * decay_between(sum_r[e], rest_r[e], sum_end, rest_end);
+                        else decay = 4 * g + e >= col ? decay_between(sum_r[e], rest_r[e], sum_t, rest_t) : 0.0f;
+                        decay *= delta_own;
+                        m[tt][e] = zs[tt][e] * decay;
+                        dz[tt][e] = r[e] * decay;
+                    }
+                }
+            }
+            f32x4_t dx[PT];
+#pragma unroll
+            for (int j = 0; j < PT; ++j) dx[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int pair = 0; pair < 2; ++pair) {
+                if (2 * pair + 1 < wave) continue;
+                Oct<T> mf[RT], zf[RT];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    terms_of(m[2 * pair + e / 4][e % 4], e, mf);
+                    terms_of(dz[2 * pair + e / 4][e % 4], e, zf);
+                }
+#pragma unroll
+                for (int j = 0; j < PT; ++j) {
+                    const Oct<T> dy = across<true>(dys, XP, 32 * pair, 16 * j, lane);
+#pragma unroll
+                    for (int term = RT - 1; term >= 0; --term) dx[j] = mma(dy, mf[term], dx[j]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const Oct<T> c = across<true>(cs, BP, 32 * pair, 16 * nt, lane);
+#pragma unroll
+                    for (int term = RT - 1; term >= 0; --term) db[nt] = mma(c, zf[term], db[nt]);
+                }
+            }
+            __syncthreads();   // (S has been read)
+            put_state(g4);
+            __syncthreads();
+            Oct<T> bf[NK];
 #pragma unroll
             for (int k = 0; k < NK; ++k) bf[k] = along<false>(bs + own * BP, 32 * k, lane);
-            const float to = d.delta[own] * d.to[own];
+            const float to = delta_own * d.to[own];
 #pragma unroll
             for (int j = 0; j < PT; ++j) {
                 f32x4_t v = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int term = GT - 1; term >= 0; --term)
+                for (int term = RT - 1; term >= 0; --term)
 #pragma unroll
                     for (int k = 0; k < NK; ++k) v = mma(along<false>(sg + (term * PP + 16 * j + col) * BP, 32 * k, lane), bf[k], v);
                 float dyv[4], out[4];

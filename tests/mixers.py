@@ -67,8 +67,8 @@ def scan_inputs(seed, samples, positions, heads, dh, groups, n, t, carried, back
     return {k: v.to(DEV) if v is not None else None for k, v in out.items()}
 
 
-def scan(i, samples, positions, heads, dh, groups, n, backward=False, size=False):
-    """Position by position.  size: every product and sum of absolute values in its place."""
+def scan(i, samples, positions, heads, dh, groups, n, backward=False, size=False, across=False):
+    """Position by position.  size: every product and sum of absolute values in its place.  across: of the gradient of an exponent those terms alone that pass through its position."""
     b, s, h, p, g = samples, positions, heads, dh, groups
     mag = (lambda v: v.abs()) if size else (lambda v: v)
     x = mag(i["x"].double())
@@ -108,7 +108,7 @@ def scan(i, samples, positions, heads, dh, groups, n, backward=False, size=False
             running = running + (dy[:, t] * y[:, t]).sum(2) + delta[:, t] * of_x
             lost = running
         state = kept[t]
-        if not size:
+        if not size or across:
             lost = (gs * state).sum((2, 3)) * decay[:, t]
         ddelta[:, t] = of_x + sign * rate * lost
         drate += sign * (delta[:, t] * lost).sum(0)

@@ -223,3 +223,36 @@ def test_rates_beyond_single_precision(positions, a_log):
     mixers.near(state, last.view(2, positions, 2, 16, 8)[:, -1], last.abs().view(2, positions, 2, 16, 8)[:, -1], 16 * mixers.F32)
     back = backward(i, sizes)
     assert all(bool(torch.isfinite(v).all()) for v in back.values()) and not bool(back["da_log"].any()) and not bool(back["dstate"].any())
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_backward_of_bf16_as_exact_as_forward(size):
+    """Decayed products go into dx (of x, B and C) in two terms, as they do into y: the bound is the forward pass's."""
+    i = mixers.scan_inputs(2, *size[:6], torch.bfloat16, size[6], backward=True)
+    if size[2] * size[3] < 8:
+        return   # (refused)
+    want, sizes = mixers.scan(i, *size[:6], backward=True), mixers.scan(i, *size[:6], backward=True, size=True)
+    near(backward(i, size)["dx"], want["dx"], sizes["dx"], BF16, "dx")
+
+
+@pytest.mark.parametrize("of", ["state", "dstate"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_exponents_gradients_keep_the_states_bits(dtype, of):
+    """A state, or gradient of one, of 1 + 2^-9 + 2^-17 - 2^-23 everywhere, of which two bf16 terms leave out 2^-17, and of which the sums with ones below are exact but for some 32
+    roundings of 2^-24 (16 and 2 additions of a column, 6 of positions, and products) and what decays and steps are off by, 2^-22 each: 2^-18 of both terms, what a step adds and what
+    it leaves of the state."""
+    size = (1, 64, 1, 64, 1, 64, True)
+    i = mixers.scan_inputs(30, *size[:6], TYPES[dtype], True, backward=True)
+    for name in ("x", "dy", "state", "dstate"):
+        i[name].zero_()
+    i[of].fill_(1.0 + 2.0 ** -9 + 2.0 ** -17 - 2.0 ** -23)
+    if of == "state":
+        i["x"][:, 128:] = 1.0
+        i["dy"].fill_(1.0)
+    else:
+        i["x"][:, :128] = 1.0
+    i["a_log"].zero_()
+    got = backward(i, size)
+    want, sizes = mixers.scan(i, *size[:6], backward=True), mixers.scan(i, *size[:6], backward=True, size=True, across=True)
+    for name in ("ddt", "da_log", "ddt_bias"):
+        near(got[name], want[name], sizes[name], 2.0 ** -18, name)
