@@ -4,11 +4,13 @@
 // are independent then.  With Z[t][s] = C_t . B_s, R[t][s] = dy_t . x_s, D the decays, w_s = D[end][s] delta_s, sums over s <= t:
 //   dx_s = sum_t Z D delta_s dy_t + w_s G B_s + skip dy_s      dB_s = sum_t R D delta_s C_t + w_s G' x_s      dC_t = sum_s R D delta_s B_s + d_t S' dy_t
 // With q = Z R D, the gradient of position t's own exponent is what passes through it: sum_{t' >= t > s} q[t'][s] delta_s, and of the states sum_{t' >= t} d_t' C_t' S' dy_t' +
-// sum_{s < t} w_s x_s G B_s + d_end <S, G>.  The first is had from sums over the rows and columns of tiles of 16 positions, without differences but inside a tile.  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
+// sum_{s < t} w_s x_s G B_s + d_end <S, G>.  The first is had from sums over the rows and columns of tiles of 16 positions, and over the pairs around a position inside its own: nothing is
+// added that would have to be taken off again (what does not pass through it can be thousands of times larger, and a rate multiplies its roundings).  A workgroup has a chunk and, one after the other, a part of the heads that share its B and C, whose Z it forms
 // once and whose gradients of B and C stay in its accumulators.  Products are formed by columns t and again by columns s: decayed, they are then operands as they lie in the accumulators.
 // In bf16 calls these are the sum of two bf16 terms (2^-17 of themselves), S and G of three (2^-25), since gradients of exponents are fp32 sums over them: with one and two terms dx was off by
-// 1.1e-3 beside the 1.7e-3 of its rounding, and the fp32 results by 1.2e-6 instead of 0.7e-6 (the matrix unit's sums).
-// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 41 us the walks (100 MB of states written, most of it read again from the last cache), 73 the chunks (63 with one and two terms; vector
+// 1.1e-3 beside the 1.7e-3 of its rounding, and da_log and ddt_bias by 1.1e-6 instead of 7.5e-7 and 3.5e-7.  (Sums of 32 bf16 products come out of the matrix unit 1.5e-10 of the products'
+// sizes too low on average: over thousands of pairs of positions that is what is left of da_log's error, fp32 calls have 1.5e-7.)
+// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 41 us the walks (100 MB of states written, most of it read again from the last cache), 76 the chunks (63 with one and two terms; vector
 // instructions and latency, two waves to a SIMD), 5 the parts' gradients of B and C, 5 the sums.
 #include "launch.h"
 #include "scan_walk.hip.h"
@@ -25,7 +27,7 @@ struct ScanGrad {
 };
 
 // Sums of 16 values over the 16 lanes of a row: lane i of them has that of value i.  Each step halves the values: 45 instructions, where a sum of each in all lanes takes 64.
-template <int CTRL, int N> __device__ __forceinline__ void halve(float (&v)[16], bool upper) {
+template <int CTRL, int N, int M> __device__ __forceinline__ void halve(float (&v)[M], bool upper) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float keep = upper ? v[i + N] : v[i], give = upper ? v[i] : v[i + N];
@@ -39,6 +41,13 @@ __device__ __forceinline__ float sixteen_sums(float (&v)[16], int lane) {
     halve<0xB1, 1>(v, lane & 1);    // quad_perm 1, 0, 3, 2: lane ^ 1
     return v[0];
 }
+// The same of four values: lanes 4 i .. 4 i + 3 of them have that of value i.
+__device__ __forceinline__ float four_sums(float (&v)[4], int lane) {
+    halve<0x128, 2>(v, lane & 8);
+    halve<0x141, 1>(v, lane & 4);
+    v[0] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[0]), 0xB1, 0xF, 0xF, false));          // quad_perm 1, 0, 3, 2
+    return v[0] + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[0]), 0x4E, 0xF, 0xF, false));   // quad_perm 2, 3, 0, 1
+}
 // over the four lanes of a column
 __device__ __forceinline__ float column_sum(float v) {
     v += __shfl_xor(v, 16);
@@ -50,10 +59,10 @@ template <typename T, int NP> constexpr bool kTwoGroups = sizeof(T) == 2 && NP <
 // Heads whose decays are formed before, and whose steps' gradients behind the others, at a time, a wave each: four, or what LDS holds.
 template <typename T, int NP> constexpr int kHeadsAtOnce = sizeof(T) == 4 && NP == 128 ? 2 : 4;
 
-// Of a head's chunk: sums of q over the rows of each tile of 16 positions by column, over a row's earlier columns, q of each position itself, C S' dy and x G B, and of each wave its parts of
-// <S, G> and of dy x.
+// Of a head's chunk: sums of q over the rows of each tile of 16 positions by column, over a row's columns of earlier tiles, over what passes through a position inside its tile, q of each
+// position itself, C S' dy and x G B, and of each wave its parts of <S, G> and of dy x.
 struct HeadSums {
-    float columns[4][kScanChunk], row[kScanChunk], self[kScanChunk], of_c[kScanChunk], of_b[kScanChunk], parts[4][2];
+    float columns[4][kScanChunk], row[kScanChunk], tile[kScanChunk], self[kScanChunk], of_c[kScanChunk], of_b[kScanChunk], parts[4][2];
 };
 
 template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGroups<T, NP> ? 2 : 1)) void scan_grad_kernel(ScanGrad a) {
@@ -175,7 +184,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
 
             // by columns t
             f32x4_t dz[4];
-            float from_row = 0.0f, of_self = 0.0f, q16[16];
+            float from_row = 0.0f, of_self = 0.0f, q16[16], through[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             // (accumulated over a head's slices)
             const auto put_sum = [&](float& to, float v) { to = slice == 0 ? v : to + v; };
             Oct<T> dyf[PK];
@@ -213,8 +222,10 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
                             of_self = self ? q : of_self;
                             dskip += self ? r[e] : 0.0f;
                             q = self ? 0.0f : q;
+                            through[e] = q * delta_s[e];
+                        } else {
+                            from_row = fmaf(q, delta_s[e], from_row);
                         }
-                        from_row = fmaf(q, delta_s[e], from_row);
                         r[e] = q;
                     }
                 }
@@ -223,6 +234,19 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             }
             put_sum(sum.columns[wave][16 * (col >> 2) + 4 * g + (col & 3)], sixteen_sums(q16, lane));
             if (col >> 2 == g) put_sum(sum.self[own], of_self);
+            {
+                // inside the tile: of each t' what comes from the positions up to s, and of that, for the position behind s, the sum over t' from it on
+#pragma unroll
+                for (int e = 1; e < 4; ++e) through[e] += through[e - 1];
+                const float below1 = __shfl_up(through[3], 16), below2 = __shfl_up(through[3], 32), below3 = __shfl_up(through[3], 48);
+                const float below = ((g > 2 ? below3 : 0.0f) + (g > 1 ? below2 : 0.0f)) + (g > 0 ? below1 : 0.0f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) through[e] = col > 4 * g + e ? below + through[e] : 0.0f;
+                const float over = four_sums(through, lane);
+                const int t = 4 * g + (col >> 2) + 1;
+                if ((col & 3) == 0 && t < 16) put_sum(sum.tile[16 * wave + t], over);
+                if (lane == 1) sum.tile[16 * wave] = 0.0f;
+            }
 #pragma unroll
             for (int pair = 0; pair < 2; ++pair) {
                 if (2 * pair > wave) continue;
@@ -376,8 +400,8 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             float over1 = tile == 0 ? delta * (later[2] + later[3]) : 0.0f, over2 = tile <= 1 ? delta * later[3] : 0.0f;
             over1 = wsum(over1);
             over2 = wsum(over2);
-            // in tile order: from t on of rows (less what lies inside the tile from t on), before t of columns
-            float rows_on = sum.row[lane] - delta * in_tile, columns_before = delta * behind;
+            // in tile order: from t on of rows, before t of columns
+            float rows_on = sum.row[lane], columns_before = delta * behind;
 #pragma unroll
             for (int k = 1; k < 16; k <<= 1) {
                 const float on = __shfl_down(rows_on, k, 16), before = __shfl_up(columns_before, k, 16);
@@ -398,7 +422,7 @@ template <typename T, int NP, int PT> __global__ __launch_bounds__(256, (kTwoGro
             states_before = __shfl_up(states_before, 1);
             states_before = lane ? states_before : 0.0f;
             const float whole = d.end * ((sum.parts[0][0] + sum.parts[1][0]) + (sum.parts[2][0] + sum.parts[3][0]));
-            const float of_exponent = ((rows_on + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
+            const float of_exponent = (((sum.tile[lane] + rows_on) + columns_before) + (tile == 1 ? over1 : tile == 2 ? over2 : 0.0f)) + ((states_on + states_before) + whole);
             // (a step that leaves nothing of what was before: of its exponent's gradient there are only roundings, which such a rate would make large)
             const float by = delta * rate > 1024.0f ? 0.0f : -rate;
             const float ddelta = fmaf(by, of_exponent, (sum.self[lane] + (in_tile + behind)) + d.to[lane] * with_g), du = lane < rows ? ddelta * slope : 0.0f;

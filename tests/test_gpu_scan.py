@@ -256,3 +256,33 @@ def test_exponents_gradients_keep_the_states_bits(dtype, of):
     want, sizes = mixers.scan(i, *size[:6], backward=True), mixers.scan(i, *size[:6], backward=True, size=True, across=True)
     for name in ("ddt", "da_log", "ddt_bias"):
         near(got[name], want[name], sizes[name], 2.0 ** -18, name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_exponents_gradients_of_what_passes_through_alone(dtype):
+    """Steps that forget nearly all between steps that forget next to nothing, at a large rate: what ends before a position, or begins behind it, leaves nothing in the gradient of its
+    exponent.  At the first position, from no state, that is all of it."""
+    size = (2, 150, 2, 32, 1, 32, False)
+    i = mixers.scan_inputs(31, *size[:6], TYPES[dtype], False, backward=True)
+    i["a_log"] = torch.tensor([8.0, 10.0], device=DEV)
+    i["dt_bias"].zero_()
+    steps = torch.where(torch.arange(150) % 5 == 1, 300.0, 0.02)[None, :, None] * torch.exp(-i["a_log"].cpu())   # times the rate
+    i["dt"] = torch.log(torch.expm1(steps.double())).expand(2, 150, 2).reshape(300, 2).to(TYPES[dtype]).to(DEV)
+    x = i["x"].view(2, 150, -1)
+    x[:, 0, :64] *= 2.0 ** -10
+    got = backward(i, size)
+    want, sizes = mixers.scan(i, *size[:6], backward=True), mixers.scan(i, *size[:6], backward=True, size=True, across=True)
+    for name in ("ddt", "da_log", "ddt_bias"):
+        near(got[name], want[name], sizes[name], FP32, name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES)
+def test_exponents_gradients_of_any_size_of_what_passes_through(size, dtype):
+    i = mixers.scan_inputs(32, *size[:6], TYPES[dtype], size[6], backward=True)
+    if size[2] * size[3] * i["x"].element_size() < 16:
+        return   # (refused)
+    got = backward(i, size)
+    want, sizes = mixers.scan(i, *size[:6], backward=True), mixers.scan(i, *size[:6], backward=True, size=True, across=True)
+    for name in ("ddt", "da_log", "ddt_bias"):
+        near(got[name], want[name], sizes[name], FP32, name)
