@@ -59,7 +59,7 @@ __device__ __forceinline__ void join_moments(float& n, float& mean, float& m2, f
     if (n2 == 0.0f) return;
     const float d = mean2 - mean, share = n2 * __builtin_amdgcn_rcpf(n + n2);   // (off by a step, of the means' difference)
     mean = fmaf(d, share, mean);
-    m2 += fmaf(d * d, n * share, m22);
+    m2 += fmaf(d * (n * share), d, m22);
     n += n2;
 }
 
@@ -336,7 +336,7 @@ template <typename T> __global__ __launch_bounds__(256) void group_map_moments_k
             for (int e = 0; e < V; ++e) {
                 const float d = bm[e] - mean[e];
                 mean[e] = fmaf(d, share, mean[e]);
-                m2[e] += fmaf(d * d, between, b2[e]);
+                m2[e] += fmaf(d * between, d, b2[e]);   // (of the first positions' 0: no square of d, which may be infinite)
             }
             n = all;
         }

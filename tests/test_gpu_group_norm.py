@@ -134,3 +134,12 @@ def test_a_workspace_for_more_is_enough_for_fewer():
             assert sizes == sorted(sizes)
             sizes = [lib.tmps_group_norm_workspace(0, positions, p, 96, 6, backward) for p in range(2, 300)]
             assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("positions,size", [(1, 300), (175, 5), (3001, 5), (5003, 24)])
+def test_values_whose_squares_are_beyond_single_precision(positions, size):
+    """Every sum is finite, and what is left of values that are all the same at most their roundings' squares: infinite or not, they leave the shift, and no NaN."""
+    x = torch.full((2 * positions, 3 * size), -1e30, device=DEV)
+    i = inputs(6, 2, positions, 3 * size, torch.float32)
+    y, _ = tmps.group_norm(x, i["gain"], i["shift"], groups=3, positions=positions)
+    assert torch.equal(y, i["shift"].expand_as(y))
