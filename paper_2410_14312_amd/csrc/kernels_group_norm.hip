@@ -103,8 +103,8 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
             Team<TEAM>::sums(s, red, place);
             mean = s[0] * part;
         }
-        s[0] = 0.0f;
         const auto squares = [&](float of) {
+            s[0] = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (p.any(i)) {
@@ -114,10 +114,24 @@ template <typename T, int TEAM, int N, bool WHOLE> __global__ __launch_bounds__(
                         s[0] = fmaf(d, d, s[0]);
                     }
                 }
+            Team<TEAM>::sums(s, red, place);
         };
         if (a.rms) squares(0.0f);
         else squares(mean);
-        Team<TEAM>::sums(s, red, place);
+        // Where the values lie far from 0 for what they differ by (or their squares are beyond a float), what the sum and the share have rounded is added to the mean, and the differences are
+        // taken anew: of values that are all the same the mean is then the value in every bit.  (For every row it is one more sum of the team: 4096 rows of 4096 in bf16 21 us instead of 17.)
+        if (!a.rms && mean != 0.0f && s[0] * part <= 0x1p-16f * (mean * mean)) {
+            s[0] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (p.any(i)) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s[0] += p.own(i, e) ? v[i][e] - mean : 0.0f;
+                }
+            Team<TEAM>::sums(s, red, place);
+            mean = fmaf(s[0], part, mean);
+            squares(mean);
+        }
         const float rstd = __builtin_amdgcn_rsqf(fmaf(s[0], part, 1e-5f));
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -286,18 +300,21 @@ template <typename T, int B> __device__ __forceinline__ void block_moments(const
     constexpr int V = kPiece<T>;
 #pragma unroll
     for (int e = 0; e < V; ++e) mean[e] = m2[e] = 0.0f;
-    if (!rms) {
+    if (!rms && many > 0) {
+        // (that of the differences from the first one, so that of values that are all the same it is the value in every bit)
+        float first[V];
+        unpack(u[0], first);
 #pragma unroll
-        for (int k = 0; k < B; ++k)
+        for (int k = 1; k < B; ++k)
             if (k < many) {
                 float v[V];
                 unpack(u[k], v);
 #pragma unroll
-                for (int e = 0; e < V; ++e) mean[e] += v[e];
+                for (int e = 0; e < V; ++e) mean[e] += v[e] - first[e];
             }
-        const float by = 1.0f / (float)max(many, 1);
+        const float by = 1.0f / (float)many;
 #pragma unroll
-        for (int e = 0; e < V; ++e) mean[e] *= by;
+        for (int e = 0; e < V; ++e) mean[e] = fmaf(mean[e], by, first[e]);
     }
 #pragma unroll
     for (int k = 0; k < B; ++k)

@@ -136,6 +136,30 @@ def test_a_workspace_for_more_is_enough_for_fewer():
             assert sizes == sorted(sizes)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [0.1, 100.0, 1000.0, 12345.678, 1e5, -1e30])
+@pytest.mark.parametrize("positions,size", [(1, 41), (1, 60), (1, 61), (1, 83), (1, 100), (1, 249), (1, 500), (1, 1003), (1, 5001), (1, 12001), (7, 5), (61, 3), (175, 4), (175, 5),
+                                            (357, 5), (357, 8), (3001, 5), (5003, 24)])
+def test_any_value_that_is_all_there_is_leaves_nothing(positions, size, value, dtype):
+    """Whatever the number of values: their mean is the value itself, in every bit."""
+    x = torch.full((2 * positions, 3 * size), value, dtype=TYPES[dtype], device=DEV)
+    i = inputs(6, 2, positions, 3 * size, TYPES[dtype])
+    kw = dict(groups=3, positions=positions)
+    y, stats = tmps.group_norm(x, i["gain"], i["shift"], **kw)
+    assert torch.equal(y, i["shift"].to(x.dtype).expand_as(y)) and torch.equal(stats[..., 0], x[:1, :1].float().expand(2, 3))
+    assert bool(((stats[..., 1].double() * 1e-5 ** 0.5 - 1).abs() <= 2.0 ** -21).all())   # (the hardware's root and 1e-5's rounding)
+    dx, dgain, dshift = tmps.group_norm_backward(i["dy"], x, stats, i["gain"], i["shift"], **kw)
+    assert not bool(dgain.any()) and bool(torch.isfinite(dx).all())
+
+
+@pytest.mark.parametrize("size", [64, 600, 5000])
+def test_a_mean_that_is_infinite_is_said_to_be(size):
+    x = torch.randn(3, size, generator=mixers.generator(7)).to(DEV)
+    x[1, size // 2] = float("inf")
+    y, stats = tmps.group_norm(x, torch.ones(size, device=DEV), groups=1)
+    assert float(stats[1, 0, 0]) == float("inf") and bool(torch.isnan(y[1]).all()) and bool(torch.isfinite(y[[0, 2]]).all()) and bool(torch.isfinite(stats[[0, 2]]).all())
+
+
 @pytest.mark.parametrize("positions,size", [(1, 300), (175, 5), (3001, 5), (5003, 24)])
 def test_values_whose_squares_are_beyond_single_precision(positions, size):
     """Every sum is finite, and what is left of values that are all the same at most their roundings' squares: infinite or not, they leave the shift, and no NaN."""
