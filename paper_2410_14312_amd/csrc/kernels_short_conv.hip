@@ -240,10 +240,11 @@ template <typename T, int K, bool NARROW> __global__ __launch_bounds__(256) void
                 const bool here = from + k < a.positions, mine = from + k < t1;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float g = dz[K - 1 + k][e] = here ? dz[K - 1 + k][e] : 0.0f, of_run = mine ? g : 0.0f;
+                    const float g = dz[K - 1 + k][e] = here ? dz[K - 1 + k][e] : 0.0f;
+                    if (!mine) continue;   // (no product with 0: an input may be infinite)
 #pragma unroll
-                    for (int j = 0; j < K; ++j) dw[j][e] = fmaf(of_run, u[k + j][e], dw[j][e]);
-                    dw[K][e] += of_run;
+                    for (int j = 0; j < K; ++j) dw[j][e] = fmaf(g, u[k + j][e], dw[j][e]);
+                    dw[K][e] += g;
                 }
             }
             // (the gradient of the input K - 1 positions back is complete with a position's dz; the first run also has those of the tail)

@@ -120,3 +120,40 @@ def test_replays_of_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, work()))
+
+
+def alike(got, want, size, relative, name):
+    """near() where both are finite; infinities and NaN in the same places."""
+    got, want = got.double().cpu(), want.double().cpu()
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isfinite(got), fine) and torch.equal(got[torch.isinf(want)], want[torch.isinf(want)]), name
+    assert bool(((got - want).abs() <= relative * size.double().cpu() + 1e-37)[fine].all()), name
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("at", [0, 12, 13, 15, 16, 30, 31, 32, 35, 36, 37, 38])
+@pytest.mark.parametrize("of", ["x", "dy", "tail"])
+def test_gradients_of_numbers_that_are_not_finite(of, at, bad):
+    """Without SiLU a weight's gradient is a sum of products dy x: one infinity leaves an infinity, and taps that no position of the sample reads it by are as they are without it."""
+    i = inputs(6, 2, 39, 24, 4, torch.float32)
+    clean = {k: v.clone() for k, v in i.items()}
+    if of == "tail":
+        if at > 2:
+            return
+        i["tail"][0, at, 5] = bad
+    else:
+        i[of][at, 5] = bad
+    names, kw = ("dx", "dweight", "dbias", "dtail"), dict(positions=39, silu=False)
+    got = dict(zip(names, tmps.short_conv_backward(i["dy"], i["x"], i["weight"], i["bias"], tail=i["tail"], dtail=i["dtail"], **kw)))
+    # (from the formula: autograd's sums take zeros times what lies beside a slice)
+    u = torch.cat([i["tail"], i["x"].view(2, 39, 24)], 1).double()
+    dz = i["dy"].view(2, 39, 24).double()
+    want = {"dweight": torch.stack([(dz * u[:, j:j + 39]).sum((0, 1)) for j in range(4)], 1), "dbias": dz.sum((0, 1))}
+    du = torch.zeros_like(u)
+    du[:, 39:] = i["dtail"].double()
+    for j in range(4):
+        du[:, j:j + 39] += dz * i["weight"][:, j].double()
+    want["dx"], want["dtail"] = du[:, 3:].reshape(78, 24), du[:, :3]
+    _, size = mixers.conv(clean["x"], clean["weight"], clean["bias"], 39, clean["tail"], False, clean["dy"], clean["dtail"])
+    for name in names:
+        alike(got[name], want[name], size[name] + want[name].abs().nan_to_num(0.0, 0.0, 0.0).cpu(), SUMS, name)
