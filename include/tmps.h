@@ -384,7 +384,7 @@ int tmps_group_norm_backward(int dtype, int flags, int64_t samples, int64_t posi
                              const float* gain, const float* shift, void* dx, float* dparams, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The norm of all arrays together, *norm = sqrt(sum of all squares) (formed in 64 bits, in a fixed order), and each array times limit / norm in its `out` where the norm is over the
- * limit (limit >= 0; infinity: never).  out may be data; it is NULL in all arrays where the norm alone is wanted.  A norm that is not finite leaves the arrays' values as they are.
+ * limit (limit >= 0; infinity: never).  out may be data; it is NULL in all arrays where the norm alone is wanted.  A norm that is not finite, as it is returned, leaves the values as they are.
  * Results lie over no other array.  workspace: tmps_clip_workspace bytes. */
 typedef struct {
     const void* data;

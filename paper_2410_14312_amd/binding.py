@@ -703,7 +703,7 @@ _DTYPE_OF, _REQUIRES_GRAD_OF = operator.attrgetter("dtype"), operator.attrgetter
 
 def clip_gradients(grads, limit, out=None, stream=None):
     """The norm of all tensors of `grads` together, fp32 of no dimension, and each of them times limit / norm where that is less than one, in place or in the tensors `out`,
-    of the same types and numbers of elements (tmps_clip_gradients).  limit = inf: the norm alone.  A norm that is not finite leaves the values as they are.  Tensors are
+    of the same types and numbers of elements (tmps_clip_gradients).  limit = inf: the norm alone.  A norm that is not finite (in fp32) leaves the values as they are.  Tensors are
     contiguous, fp32 or bf16.  `stream` as for rotary."""
     grads = list(grads)
     if not grads:

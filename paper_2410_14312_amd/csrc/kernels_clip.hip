@@ -73,13 +73,13 @@ __device__ __forceinline__ double clip_block_sum(double v) {
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// The norm and the factor of all workgroups' sums.
+// The norm and the factor of all workgroups' sums.  (Whether the norm is finite is asked of what is returned of it, which may not be where its 64 bits are.)
 __device__ __forceinline__ double clip_norm(const double* part, int64_t n, float limit, float& scale) {
     double sum = 0.0;
 #pragma unroll 8
     for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[i];
     const double r = sqrt(clip_block_sum(sum));
-    scale = r > (double)limit && r < __builtin_inf() ? (float)((double)limit / r) : 1.0f;
+    scale = r > (double)limit && (float)r < __builtin_inff() ? (float)((double)limit / r) : 1.0f;
     return r;
 }
 

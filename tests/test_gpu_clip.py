@@ -120,3 +120,13 @@ def test_the_norm_alone_takes_an_array_twice():
     with pytest.raises(tmps.TmpsError):
         tmps.clip_gradients([g[:30]], 1.0, out=[g[10:40]])
     assert bool((g == 1).all())
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_norm_beyond_single_precision_leaves_the_values(dtype, in_place):
+    """Every square and their sum are finite in 64 bits, the norm is not in 32: what is returned says that nothing was scaled."""
+    g = torch.full((1000,), 1e38, dtype=mixers.TYPES[dtype], device=DEV)
+    before, out = g.clone(), None if in_place else torch.zeros_like(g)
+    assert bool(torch.isinf(tmps.clip_gradients([g], 1.0, out=None if in_place else [out])))
+    assert torch.equal(g, before) and (in_place or torch.equal(out, before))
