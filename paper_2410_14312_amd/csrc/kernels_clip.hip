@@ -74,12 +74,12 @@ __device__ __forceinline__ double clip_block_sum(double v) {
 }
 
 // The norm and the factor of all workgroups' sums.  (Whether the norm is finite is asked of what is returned of it, which may not be where its 64 bits are.)
-__device__ __forceinline__ double clip_norm(const double* part, int64_t n, float limit, float& scale) {
+__device__ __forceinline__ double clip_norm(const double* part, int64_t n, float limit, double& scale) {
     double sum = 0.0;
 #pragma unroll 8
     for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[i];
     const double r = sqrt(clip_block_sum(sum));
-    scale = r > (double)limit && (float)r < __builtin_inff() ? (float)((double)limit / r) : 1.0f;
+    scale = r > (double)limit && (float)r < __builtin_inff() ? (double)limit / r : 1.0;
     return r;
 }
 
@@ -98,8 +98,8 @@ __global__ __launch_bounds__(256) void clip_squares_kernel(ClipTable t, double* 
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(256) void clip_norm_kernel(const double* part, int64_t n, float limit, float* norm, float* scale) {
-    float by;
+__global__ __launch_bounds__(256) void clip_norm_kernel(const double* part, int64_t n, float limit, float* norm, double* scale) {
+    double by;
     const double r = clip_norm(part, n, limit, by);
     if (threadIdx.x == 0) {
         *norm = (float)r;
@@ -108,16 +108,20 @@ __global__ __launch_bounds__(256) void clip_norm_kernel(const double* part, int6
 }
 
 // scale: the factor, or null where each workgroup forms it from the `sums` of all.  Workgroups come in the opposite order of the first pass's.
-__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const float* scale, const double* part, int64_t sums, float limit, float* norm) {
+__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const double* scale, const double* part, int64_t sums, float limit, float* norm) {
     const uint32_t block = gridDim.x - 1 - blockIdx.x;
     const int a = clip_find(t, block);
-    float by;
+    double all;
     if (scale) {
-        by = *scale;
+        all = *scale;
     } else {
-        const double r = clip_norm(part, sums, limit, by);
+        const double r = clip_norm(part, sums, limit, all);
         if (norm && block == 0 && threadIdx.x == 0) *norm = (float)r;
     }
+    // (a factor below the normal range has few bits in a float, if any, where products have all: its power of two is apart)
+    int power = 0;
+    if (all < 0x1p-126) all = frexp(all, &power);
+    const float by = (float)all;
     if (by == 1.0f && t.in[a] == t.out[a]) return;
     const int64_t begin = (int64_t)(block - (t.first[a] & 0x7fffffffu)) * t.block;
     const int n = (int)min<int64_t>(t.block, t.n[a] - begin);
@@ -125,7 +129,7 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const floa
         return [=](auto& v, int at, int m) {
             constexpr int V = sizeof(v) / sizeof(v[0]);
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] *= by;
+            for (int e = 0; e < V; ++e) v[e] = __builtin_ldexpf(v[e] * by, power);
             if (m == V) {
                 store16_any(to + at, pack(v));
             } else {
@@ -178,7 +182,7 @@ hipError_t clip_gradients(const ClipArray* list, int n, float limit, float* norm
         total += blocks.back();
     }
     const bool scaled = n > 0 && list[0].out;
-    float* const scale = reinterpret_cast<float*>(part + total);
+    double* const scale = part + total;
     const bool own = scaled && total > 0 && total <= kClipOwnSum;
     if (!own) {
         const hipError_t e = launch_timed(kcSliceSum, clip_norm_kernel, dim3(1), dim3(256), 0, s, (const double*)part, total, limit, norm, scale);
@@ -186,7 +190,7 @@ hipError_t clip_gradients(const ClipArray* list, int n, float limit, float* norm
     }
     for (size_t k = tables.size(); k-- > 0;) {
         if (!blocks[k]) continue;
-        const hipError_t e = launch_timed(kcAffine, clip_scale_kernel, dim3((unsigned)blocks[k]), dim3(256), 0, s, tables[k], own ? nullptr : (const float*)scale, (const double*)part, total,
+        const hipError_t e = launch_timed(kcAffine, clip_scale_kernel, dim3((unsigned)blocks[k]), dim3(256), 0, s, tables[k], own ? nullptr : (const double*)scale, (const double*)part, total,
                                           limit, k == 0 ? norm : nullptr);
         if (e != hipSuccess) return e;
     }

@@ -130,3 +130,14 @@ def test_a_norm_beyond_single_precision_leaves_the_values(dtype, in_place):
     before, out = g.clone(), None if in_place else torch.zeros_like(g)
     assert bool(torch.isinf(tmps.clip_gradients([g], 1.0, out=None if in_place else [out])))
     assert torch.equal(g, before) and (in_place or torch.equal(out, before))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("limit", [1.0, 1e-3, 1e-6, 1e-8])
+@pytest.mark.parametrize("many", [1, 6200])   # (so many arrays that workgroups read the factor, instead of forming it)
+def test_factors_below_the_normal_range(limit, dtype, many):
+    whole = (torch.randn(many * 7, generator=mixers.generator(9)) * 1e36).to(mixers.TYPES[dtype]).to(DEV)
+    a = whole.double()
+    norm, limit = float(a.square().sum().sqrt()), float(torch.tensor(limit, dtype=torch.float32))
+    tmps.clip_gradients(whole.split(7), limit)
+    near(whole, a * (limit / norm), a.abs() * (limit / norm), 2.0 ** -22, "scaled")
