@@ -141,3 +141,20 @@ def test_factors_below_the_normal_range(limit, dtype, many):
     norm, limit = float(a.square().sum().sqrt()), float(torch.tensor(limit, dtype=torch.float32))
     tmps.clip_gradients(whole.split(7), limit)
     near(whole, a * (limit / norm), a.abs() * (limit / norm), 2.0 ** -22, "scaled")
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_more_arrays_than_workgroups_that_add_up_for_themselves(in_place):
+    """The norm is formed once, by a launch of its own, and over fifty launches read the factor."""
+    count = 6200
+    g = mixers.generator(10)
+    whole, kept = torch.randn(count * 9, generator=g).to(DEV), torch.full((count * 9,), 5.0, device=DEV)
+    grads, out = [v[:7] for v in whole.split(9)], [v[:7] for v in kept.split(9)]   # (two numbers between neighbours)
+    before = whole.clone()
+    norm = float(before.view(count, 9)[:, :7].double().square().sum().sqrt())
+    got = tmps.clip_gradients(grads, 2.0, out=None if in_place else out)
+    near(got, torch.tensor(norm), torch.tensor(norm), 2.0 ** -40, "norm")
+    into = whole if in_place else kept
+    near(into.view(count, 9)[:, :7], before.view(count, 9)[:, :7].double() * (2.0 / norm), before.view(count, 9)[:, :7].double().abs() * (2.0 / norm), 2.0 ** -22, "scaled")
+    assert torch.equal(into.view(count, 9)[:, 7:], before.view(count, 9)[:, 7:] if in_place else torch.full((count, 2), 5.0, device=DEV))
+    assert in_place or torch.equal(whole, before)
