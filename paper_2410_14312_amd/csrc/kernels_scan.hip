@@ -26,7 +26,8 @@ template <typename T, int HALVES, bool PLAIN> __global__ __launch_bounds__(256) 
     const int64_t unit = blockIdx.x;
     const int head = (int)(unit % a.heads), group = head / (a.heads / a.groups);
     const int64_t sample = unit / a.heads;
-    const int lane = threadIdx.x & 15, team = threadIdx.x >> 4, p0 = blockIdx.y * (16 * kPasses);
+    const int lane = threadIdx.x & 15, team = threadIdx.x >> 4, p0 = (int)(blockIdx.z * gridDim.y + blockIdx.y) * (16 * kPasses);
+    if (p0 >= a.dh) return;
     const int64_t of_head = unit * a.dh * a.n;
     const T* const xr = (const T*)a.x + sample * a.positions * a.x_stride;
     const T* const dtr = (const T*)a.dt + sample * a.positions * a.dt_stride + head;
@@ -114,12 +115,13 @@ size_t scan_workspace_bytes(const Scan& a) {
 
 template <typename T> static hipError_t forward_type(const Scan& a, void* ws, hipStream_t s) {
     if (a.positions <= kScanSteps) {
-        const int64_t units = a.samples * a.heads, cuts = (a.dh + 63) / 64;
-        if (!launchable(units, 256) || cuts > 65535) return hipErrorInvalidValue;
+        const int64_t units = a.samples * a.heads;
+        const unsigned cuts = (unsigned)(a.dh + 63) / 64, in_y = std::min(cuts, 32768u);   // (a launch has 65535 workgroups in its second direction)
+        if (!launchable(units, 256)) return hipErrorInvalidValue;
         const bool whole = a.dh % 64 == 0;
         auto kern = a.n > 64 ? (whole && a.n == 128 ? scan_steps_kernel<T, 2, true> : scan_steps_kernel<T, 2, false>)
                              : (whole && a.n == 64 ? scan_steps_kernel<T, 1, true> : scan_steps_kernel<T, 1, false>);
-        return launch_timed(kcAttnFwd, kern, dim3((unsigned)units, (unsigned)cuts), dim3(256), 0, s, a);
+        return launch_timed(kcAttnFwd, kern, dim3((unsigned)units, in_y, (cuts + in_y - 1) / in_y), dim3(256), 0, s, a);
     }
     ScanWalk w = walk_of(a);
     w.y = a.y; w.y_stride = a.y_stride;

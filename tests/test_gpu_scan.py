@@ -286,3 +286,14 @@ def test_exponents_gradients_of_any_size_of_what_passes_through(size, dtype):
     want, sizes = mixers.scan(i, *size[:6], backward=True), mixers.scan(i, *size[:6], backward=True, size=True, across=True)
     for name in ("ddt", "da_log", "ddt_bias"):
         near(got[name], want[name], sizes[name], FP32, name)
+
+
+@pytest.mark.parametrize("positions", [1, 3])
+def test_heads_of_millions_of_features(positions):
+    """More slices of 64 features than a launch has in its second direction."""
+    size = (1, positions, 1, 4194304 + 65, 1, 2, True)
+    i = mixers.scan_inputs(33, *size[:6], torch.bfloat16, True)
+    y, state = forward(i, size, want_state=True)
+    want, sizes = mixers.scan(i, *size[:6]), mixers.scan(i, *size[:6], size=True)
+    near(y, want["y"], sizes["y"], BF16, "y")
+    near(state, want["state"], sizes["state"], FP32, "state")
