@@ -461,8 +461,8 @@ int tmps_streams_destroy(void** streams, int n);
  * milliseconds and launch counts per class into total_ms[] / launches[] (host arrays of n_classes >=
  * TMPS_KERNEL_CLASSES entries), clears the record and returns TMPS_KERNEL_CLASSES.  Rotary positions count
  * under TMPS_KC_EMBEDDING, norm joins and group norm under TMPS_KC_LAYERNORM, distillation under TMPS_KC_SOFTMAX_CE, short
- * convolutions under TMPS_KC_CONV_FWD and TMPS_KC_CONV_DGRAD, state spaces under TMPS_KC_ATTN_FWD and TMPS_KC_ATTN_BWD, the
- * norm of gradients under TMPS_KC_REDUCE and their scaling under TMPS_KC_UPDATE.
+ * convolutions under TMPS_KC_CONV_FWD and TMPS_KC_CONV_DGRAD, state spaces under TMPS_KC_ATTN_FWD and TMPS_KC_ATTN_BWD, sums of
+ * their partial results and the norm of gradients under TMPS_KC_SLICE_SUM, the scaling of gradients under TMPS_KC_AFFINE.
  * Timing adds host overhead: measure throughput with profiling off. */
 enum {
     TMPS_KC_DENSE_FWD = 0, TMPS_KC_DENSE_DGRAD, TMPS_KC_DENSE_WGRAD, TMPS_KC_CONV_FWD,

@@ -65,7 +65,7 @@ struct Scan {
 };
 size_t scan_workspace_bytes(const Scan& a);
 hipError_t scan_forward(int dtype, const Scan& a, void* ws, hipStream_t s);
-// Its gradients from dy and, of state_out, dstate (may be null): dx (rows as x's), ddt, dparams: [3][heads] of a_log, skip, dt_bias; dstate_in (may be null, or dstate).
+// Its gradients from dy and, of state_out, dstate (may be null): dx (rows as x's), ddt, dparams: [3][heads] of a_log, skip, dt_bias; dstate_in (may be null).
 struct ScanBackward {
     Scan f;   // y and state_out are not looked at
     const void* dy;
@@ -97,7 +97,7 @@ struct GroupNorm {
 bool group_norm_fits(int dtype, int64_t samples, int64_t positions, int channels, int groups);
 size_t group_norm_workspace_bytes(int dtype, int64_t samples, int64_t positions, int channels, int groups, bool backward);
 hipError_t group_norm_forward(int dtype, const GroupNorm& a, void* ws, hipStream_t s);
-// Its gradients: dx and dparams: [channels] of gain, then, with a shift, [channels] of it.
+// Its gradients: dx and dparams: [channels] of gain, then [channels] of shift (also where there is none).
 struct GroupNormBackward {
     const void *dy, *x;
     const float *stats, *gain, *shift;

@@ -158,3 +158,13 @@ def test_more_arrays_than_workgroups_that_add_up_for_themselves(in_place):
     near(into.view(count, 9)[:, :7], before.view(count, 9)[:, :7].double() * (2.0 / norm), before.view(count, 9)[:, :7].double().abs() * (2.0 / norm), 2.0 ** -22, "scaled")
     assert torch.equal(into.view(count, 9)[:, 7:], before.view(count, 9)[:, 7:] if in_place else torch.full((count, 2), 5.0, device=DEV))
     assert in_place or torch.equal(whole, before)
+
+
+def test_a_profile_has_the_launches_under_the_classes_that_the_header_names():
+    grads = arrays(11, SHAPES)
+    tmps.profile_enable(True)
+    tmps.profile_read()
+    tmps.clip_gradients(grads, 1.0)
+    counts = {k: v[1] for k, v in tmps.profile_read().items() if v[1]}
+    tmps.profile_enable(False)
+    assert counts == {"slice_sum": 1, "affine": 1}
