@@ -10,8 +10,8 @@
 // In bf16 calls these are the sum of two bf16 terms (2^-17 of themselves), S and G of three (2^-25), since gradients of exponents are fp32 sums over them: with one and two terms dx was off by
 // 1.1e-3 beside the 1.7e-3 of its rounding, and da_log and ddt_bias by 1.1e-6 instead of 7.5e-7 and 3.5e-7.  (Sums of 32 bf16 products come out of the matrix unit 1.5e-10 of the products'
 // sizes too low on average: over thousands of pairs of positions that is what is left of da_log's error, fp32 calls have 1.5e-7.)
-// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 41 us the walks (100 MB of states written, most of it read again from the last cache), 76 the chunks (63 with one and two terms; vector
-// instructions and latency, two waves to a SIMD), 5 the parts' gradients of B and C, 5 the sums.
+// 16 x 512 positions of 24 heads of 64 x 64 in bf16: 43 us the walks (100 MB of states written, most of it read again from the last cache), 81 the chunks (64 with one and two terms; vector
+// instructions and latency, two waves to a SIMD; 56 bytes of registers spill, addresses that are asked for once a head), 5 the parts' gradients of B and C, 5 the sums.
 #include "launch.h"
 #include "scan_walk.hip.h"
 #include "wave.hip.h"

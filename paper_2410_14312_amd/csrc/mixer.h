@@ -109,7 +109,7 @@ struct GroupNormBackward {
 };
 hipError_t group_norm_backward(int dtype, const GroupNormBackward& a, void* ws, hipStream_t s);
 
-// norm = the 2-norm of all arrays together, in 64 bits; out = in times limit / norm where that is less than one and the norm is finite.  out may be in, or null in all: the norm alone.
+// norm = the 2-norm of all arrays together, in 64 bits; out = in times limit / norm where that is less than one and the norm finite as a float.  out may be in, or null in all: the norm alone.
 struct ClipArray {
     const void* in;
     void* out;
